@@ -294,12 +294,159 @@ rlda_status rl_decode_attn_run_multi(rl_decode_attn_t handle, int32_t batch, int
                                      const int32_t* seq_lens, const int32_t* q_start, void* out, void* workspace,
                                      size_t workspace_bytes, void* stream, void* event_begin, void* event_end);
 
+/* Rows [rows][heads][head_dim] with head_dim contiguous; strides in elements, not negative. */
+typedef struct {
+  const void* data;      /* 16-byte aligned, as every row and head of it has to be */
+  int64_t row_stride;
+  int64_t head_stride;
+} rl_decode_attn_rows;
+
+/*
+ * Rotary positions: pair j of a row at position n is turned by the angle t = n * freqs[j]
+ * and scaled by the amplitude A,
+ *     a' = A (a cos t - b sin t),   b' = A (b cos t + a sin t)      (inverse: by -t)
+ * on pairs (j, j + rot_dim / 2), or (2j, 2j + 1) where `interleaved`, of a head's first
+ * rot_dim elements; the others pass.  The angle is computed in 64 bits, the products in
+ * fp32, and the result is rounded once.
+ */
+typedef struct {
+  const double* freqs;   /* DEVICE [rot_dim / 2], radians a position (any scaling for long contexts is in them) */
+  int32_t rot_dim;       /* a multiple of 16, at most head_dim */
+  int32_t interleaved;
+  float amplitude;       /* finite; 1: a rotation */
+  int32_t inverse;       /* the transpose: takes a gradient back, and (amplitude 1) a rotation */
+} rl_decode_attn_rotary;
+
+/*
+ * Turn rows by their positions: out[r][h] = x[r][h] turned by positions[r] (int32, device,
+ * any sign).  dtype RLDA_F32 or RLDA_BF16 for x and out; heads <= 256, head_dim a multiple
+ * of 8 in [32, 256] (else RLDA_ERR_UNSUPPORTED).  x may be read through any strides (a
+ * slice of a fused projection; 0: one row for all); out's rows must not overlap each
+ * other, and out is x itself (same strides) or apart from it.  No handle, no workspace,
+ * one kernel, asynchronous.
+ */
+rlda_status rl_decode_attn_rotate(rlda_dtype dtype, int32_t rows, int32_t heads, int32_t head_dim,
+                                  const rl_decode_attn_rows* x, const int32_t* positions,
+                                  const rl_decode_attn_rotary* rotary, const rl_decode_attn_rows* out, void* stream);
+
+/*
+ * rl_decode_attn_append with rotary positions, for one token or several of each sequence:
+ * q and k_new are turned by their rows' positions, k_new (turned) and v_new are written
+ * into the caches, q to q_out.
+ *   q, q_out       [total_q][Hq][d]   q_dtype; q_out is q itself (same strides) or apart from it
+ *   k_new, v_new   [total_q][Hkv][d]  q_dtype
+ *   q_start        [batch + 1] int32 device as for rl_decode_attn_run_multi, or NULL: one row a
+ *                  sequence (total_q = batch).  Row q_start[b] + i of sequence b, one of its
+ *                  last n_b tokens, is token seq_lens[b] - n_b + i.
+ *   positions      [total_q] int32 device, or NULL: the rows' tokens
+ *   k_cache, v_cache (two different pools), k_scale, v_scale, block_table, seq_lens: as for
+ *                  rl_decode_attn_append
+ * bf16 and f32 caches store the rows rounded once to their type.  fp8 caches keep the rule
+ * of rl_decode_attn_append with the call's rows of one page taken together (amax over all
+ * of them, the turned K rows in fp32): a page whose slot 0 is among them starts with scale
+ * amax / 448; in another the scale is raised, and its earlier rows are re-encoded, once.
+ * Rows that no sequence names, rows of sequences with inconsistent q_start entries or a
+ * length outside [0, capacity], and rows before token 0 (n_b > seq_lens[b]) are not
+ * written, q_out included (flag bit 1, but for rows of no sequence and for an empty
+ * sequence without q_start); of a token whose page id is outside the pool only q_out is
+ * (flag bit 0).  The pages one call writes must each belong to one sequence.
+ * workspace: as for rl_decode_attn_run (only its flag word is used).  One kernel, asynchronous.
+ */
+rlda_status rl_decode_attn_append_rotary(rl_decode_attn_t handle, int32_t batch, int32_t num_pages, int32_t total_q,
+                                         const rl_decode_attn_rotary* rotary, const rl_decode_attn_rows* q,
+                                         const rl_decode_attn_rows* k_new, const rl_decode_attn_rows* v_new,
+                                         const int32_t* q_start, const int32_t* positions, void* k_cache, void* v_cache,
+                                         float* k_scale, float* v_scale, const int32_t* block_table,
+                                         const int32_t* seq_lens, const rl_decode_attn_rows* q_out, void* workspace,
+                                         size_t workspace_bytes, void* stream);
+
+/*
+ * The pages of a pool.  Its state is one reference count per page, refs[num_pages] int32
+ * (device; 0: free; a page that k rows of the block table use has k), with the block
+ * table and the lengths as for rl_decode_attn_run.  Every layer's cache shares that state
+ * (page id p means page p of each of them), so taking, sharing and returning pages is one
+ * call for all layers, and what moves contents takes a list of caches:
+ */
+typedef struct {
+  void* k_cache;
+  void* v_cache;
+  float* k_scale;        /* fp8 caches only */
+  float* v_scale;
+} rl_decode_attn_cache;
+
+/* Bytes of device workspace the page operations need for a pool of `num_pages` (host-only).
+ * 256-byte aligned; its first word accumulates the flags (zero it before the first use;
+ * rl_decode_attn_read_flags reads it).  Calls that may overlap in time need separate ones. */
+rlda_status rl_decode_attn_page_workspace_size(rl_decode_attn_t handle, int32_t num_pages, size_t* bytes);
+
+/*
+ * Room for new tokens: seq_lens[b] grows by add[b] (int32 device; NULL: by one each), and
+ * the pages this needs are taken (refs 0 -> 1) and written to the block-table row.  The
+ * requests take the lowest-numbered free pages, in sequence order; from the first that
+ * finds too few left on, requests for pages are not served and their rows stay as they were
+ * (flag bit 4).  A length or growth out of range leaves its row alone (flag bit 1).
+ * One kernel (two for pools above 131072 pages), asynchronous.
+ */
+rlda_status rl_decode_attn_page_grow(rl_decode_attn_t handle, int32_t batch, int32_t num_pages, int32_t* refs,
+                                     int32_t* block_table, int32_t* seq_lens, const int32_t* add, void* workspace,
+                                     size_t workspace_bytes, void* stream);
+
+/*
+ * rows[0 .. count) give up their pages: each of a row's pages loses a reference, and the
+ * row's length becomes 0 (its table entries stay as they were).  A row named twice is
+ * released once.  Row ids outside [0, batch) and lengths out of range: flag bit 1; page
+ * ids outside the pool, and pages that nobody holds: flag bit 0.  One kernel, asynchronous.
+ */
+rlda_status rl_decode_attn_page_release(rl_decode_attn_t handle, int32_t batch, int32_t num_pages, int32_t* refs,
+                                        int32_t* block_table, int32_t* seq_lens, int32_t count, const int32_t* rows,
+                                        void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * children[f] becomes a copy of parents[f], f < count <= max_batch (int32 device; a
+ * response of a GRPO prompt, a branch of a search): it shares the parent's full pages
+ * (one more reference each), and the parent's partial last page, which both will write to,
+ * is copied to a page of its own in every cache (whole, as it is).  Those pages are taken
+ * as in rl_decode_attn_page_grow, in fork order.  Parents are read as they were before the
+ * call; a parent may have any number of children.  Not done, and the child stays empty: a
+ * row id out of range, parent = child, a child whose length is not 0 or that an earlier
+ * fork of the call names, a parent's length out of range (flag bit 1); no page left (flag
+ * bit 4).  Two kernels (three for pools above 131072 pages, one more for every 64 caches
+ * beyond 64), asynchronous.
+ */
+rlda_status rl_decode_attn_page_fork(rl_decode_attn_t handle, int32_t batch, int32_t num_pages, int32_t* refs,
+                                     int32_t* block_table, int32_t* seq_lens, int32_t count, const int32_t* parents,
+                                     const int32_t* children, int32_t num_caches, const rl_decode_attn_cache* caches,
+                                     void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * The live pages (refs > 0), *live of them (int32 device), move to ids [0, *live): those at
+ * or above it to the free ids below, both in ascending order.  Contents move in every
+ * cache, the table entries of rows [0, batch) and the counts follow.  Every row that uses
+ * the pool has to be in the table; an entry whose page nothing counts, or outside the
+ * pool, stays (flag bit 0), a row with a length out of range too (flag bit 1).  Pages at
+ * or above *live are free afterwards, their contents stale.  Two kernels, more as above.
+ */
+rlda_status rl_decode_attn_page_compact(rl_decode_attn_t handle, int32_t batch, int32_t num_pages, int32_t* refs,
+                                        int32_t* block_table, int32_t* seq_lens, int32_t num_caches,
+                                        const rl_decode_attn_cache* caches, int32_t* live, void* workspace,
+                                        size_t workspace_bytes, void* stream);
+
+/*
+ * Page src[i] is copied over page dst[i] in every cache, i < count (int32 device).  No dst
+ * may be another pair's src or dst.  Ids outside the pool: skipped, flag bit 0.  One kernel
+ * (one more for every 64 caches beyond 64), asynchronous.
+ */
+rlda_status rl_decode_attn_page_copy(rl_decode_attn_t handle, int32_t num_pages, int32_t count, const int32_t* src,
+                                     const int32_t* dst, int32_t num_caches, const rl_decode_attn_cache* caches,
+                                     void* workspace, size_t workspace_bytes, void* stream);
+
 /* Flags raised by device-side contract checks since the workspace was zeroed
  * (bit 0: page id outside [0, num_pages); bit 1: seq_len beyond capacity;
  * bit 2: a group's shared prompt clamped to its shortest member; bit 3: a
  * segment counter was not zero when the run began, so the run counted more pieces
  * than a segment has or merged a partial it had not written: the workspace was not
- * zero-filled, or runs overlapped on it).
+ * zero-filled, or runs overlapped on it; bit 4: fewer free pages than a page operation
+ * asked for).
  * SYNCHRONISES `stream` (waits for queued work, copies 4 bytes to the host). */
 rlda_status rl_decode_attn_read_flags(rl_decode_attn_t handle, const void* workspace, void* stream,
                                       uint32_t* flags);

@@ -13,8 +13,10 @@ import ctypes
 from typing import Optional
 
 from . import _abi
+from .cache_ops import CacheOps
+from .rotary import rotary_frequencies, rotate
 
-__all__ = ["DecodeAttention", "decode_attention", "RldaError", "library_path"]
+__all__ = ["DecodeAttention", "decode_attention", "rotate", "rotary_frequencies", "RldaError", "library_path"]
 
 RldaError = _abi.RldaError
 library_path = _abi.LIB_PATH
@@ -25,10 +27,7 @@ def _torch():
     return torch
 
 
-def _torch_dtype(code: int):
-    torch = _torch()
-    return {_abi.RLDA_F32: torch.float32, _abi.RLDA_BF16: torch.bfloat16,
-            _abi.RLDA_FP8_E4M3FN: torch.float8_e4m3fn}[code]
+_torch_dtype = _abi.torch_dtype
 
 
 def _dtype_code(t) -> int:
@@ -42,7 +41,7 @@ def _dtype_code(t) -> int:
     raise TypeError(f"unsupported dtype {t}")
 
 
-class DecodeAttention:
+class DecodeAttention(CacheOps):
     """A configured decode-attention layer (a library handle).
 
     k_cache / v_cache passed to __call__ are 4-D tensors of shape
@@ -81,6 +80,7 @@ class DecodeAttention:
                    "rl_decode_attn_grouped_workspace_size")
         self.grouped_workspace_bytes = int(n.value)
         self._ws = {}
+        self._page_ws = {}
         # The native call path (csrc/fastcall.cpp); it shares the workspaces by device.
         native = _abi.fastcall()
         self._fast = _abi.LEFT_TO_PYTHON if native is None else native.Layer(

@@ -14,6 +14,9 @@ STATUS = {0: "RLDA_OK", -1: "RLDA_ERR_INVALID_ARG", -2: "RLDA_ERR_UNSUPPORTED", 
 EXPORTS = ["rl_decode_attn_create", "rl_decode_attn_workspace_size", "rl_decode_attn_run",
            "rl_decode_attn_run_profiled", "rl_decode_attn_run_grouped", "rl_decode_attn_grouped_workspace_size",
            "rl_decode_attn_append", "rl_decode_attn_run_multi", "rl_decode_attn_run_noalloc",
+           "rl_decode_attn_rotate", "rl_decode_attn_append_rotary", "rl_decode_attn_page_workspace_size",
+           "rl_decode_attn_page_grow", "rl_decode_attn_page_release", "rl_decode_attn_page_fork",
+           "rl_decode_attn_page_compact", "rl_decode_attn_page_copy",
            "rl_decode_attn_read_flags", "rl_decode_attn_destroy", "rl_decode_attn_strerror"]
 
 
@@ -35,6 +38,25 @@ class Config(ctypes.Structure):
         ("kv_stride_slot", ctypes.c_int64),
         ("num_work_ranges", ctypes.c_int32),
     ]
+
+
+class Rows(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("row_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64)]
+
+
+class Rotary(ctypes.Structure):
+    _fields_ = [("freqs", ctypes.c_void_p), ("rot_dim", ctypes.c_int32), ("interleaved", ctypes.c_int32),
+                ("amplitude", ctypes.c_float), ("inverse", ctypes.c_int32)]
+
+
+class Cache(ctypes.Structure):
+    _fields_ = [("k_cache", ctypes.c_void_p), ("v_cache", ctypes.c_void_p), ("k_scale", ctypes.c_void_p),
+                ("v_scale", ctypes.c_void_p)]
+
+
+def torch_dtype(code: int):
+    import torch
+    return {RLDA_F32: torch.float32, RLDA_BF16: torch.bfloat16, RLDA_FP8_E4M3FN: torch.float8_e4m3fn}[code]
 
 
 class RldaError(RuntimeError):
@@ -73,6 +95,19 @@ def load() -> ctypes.CDLL:
         lib.rl_decode_attn_run_multi.restype = ctypes.c_int
         lib.rl_decode_attn_run_noalloc.argtypes = [vp, i32, i32] + [vp] * 8 + [vp, vp]
         lib.rl_decode_attn_run_noalloc.restype = ctypes.c_int
+        rows, rot = ctypes.POINTER(Rows), ctypes.POINTER(Rotary)
+        lib.rl_decode_attn_rotate.argtypes = [ctypes.c_int, i32, i32, i32, rows, vp, rot, rows, vp]
+        lib.rl_decode_attn_append_rotary.argtypes = [vp, i32, i32, i32, rot, rows, rows, rows] + [vp] * 8 + [rows, vp, sz, vp]
+        lib.rl_decode_attn_page_workspace_size.argtypes = [vp, i32, ctypes.POINTER(sz)]
+        state, caches = [vp, i32, i32, vp, vp, vp], [i32, ctypes.POINTER(Cache)]
+        lib.rl_decode_attn_page_grow.argtypes = state + [vp, vp, sz, vp]
+        lib.rl_decode_attn_page_release.argtypes = state + [i32, vp, vp, sz, vp]
+        lib.rl_decode_attn_page_fork.argtypes = state + [i32, vp, vp] + caches + [vp, sz, vp]
+        lib.rl_decode_attn_page_compact.argtypes = state + caches + [vp, vp, sz, vp]
+        lib.rl_decode_attn_page_copy.argtypes = [vp, i32, i32, vp, vp] + caches + [vp, sz, vp]
+        for name in ("rotate", "append_rotary", "page_workspace_size", "page_grow", "page_release", "page_fork",
+                     "page_compact", "page_copy"):
+            getattr(lib, "rl_decode_attn_" + name).restype = ctypes.c_int
         lib.rl_decode_attn_read_flags.argtypes = [vp, vp, vp, ctypes.POINTER(ctypes.c_uint32)]
         lib.rl_decode_attn_read_flags.restype = ctypes.c_int
         lib.rl_decode_attn_destroy.argtypes = [vp]

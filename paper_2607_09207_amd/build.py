@@ -11,7 +11,8 @@ CSRC = os.path.join(HERE, "csrc")
 INCLUDE = os.path.join(ROOT, "include")
 LIB = os.path.join(HERE, "librl_decode_attn.so")
 SOURCES = [os.path.join(CSRC, "rlda_kernels.hip"), os.path.join(CSRC, "rlda_multi.hip"),
-           os.path.join(CSRC, "rlda_host.cpp")]
+           os.path.join(CSRC, "rlda_host.cpp"), os.path.join(CSRC, "rlda_rotary.hip"),
+           os.path.join(CSRC, "rlda_pages.hip"), os.path.join(CSRC, "rlda_ops.cpp")]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 # Read-bandwidth reference kernels (bench support, not the attention path).
 PROBE_SOURCES = [os.path.join(CSRC, "hbm_probe.hip")]

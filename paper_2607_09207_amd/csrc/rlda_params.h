@@ -29,6 +29,7 @@ constexpr uint32_t kFlagBadPage = 1u;
 constexpr uint32_t kFlagBadLen = 2u;
 constexpr uint32_t kFlagPrefixClamped = 4u;
 constexpr uint32_t kFlagStaleState = 8u;   // a counter or a partial this call did not write (workspace not zeroed)
+constexpr uint32_t kFlagNoPages = 16u;     // fewer free pages than a page operation asked for
 
 // Static scratch of rl_decode_attn_run_noalloc (one copy per GPU, in the kernel
 // source): the flag word, then segment counters for batch * Hkv <= kScratchMaxSegments,
@@ -93,6 +94,77 @@ struct Params {
   int16_t q_head[kMaxQHeads];  // q_head[g * G + i] = i-th query head of KV head g
 };
 
+constexpr int kRotaryWindow = 16;   // rows of a workgroup's window (rlda_rotary.hip)
+
+// Rotary positions: rows turned alone (hq heads of q to q_out), or q, k_in and v_in on
+// their way into the cache.  Strides of rows and heads in elements.
+struct RotaryParams {
+  const void* q;
+  const void* k_in;
+  const void* v_in;
+  void* q_out;
+  int64_t q_rs, q_hs, k_rs, k_hs, v_rs, v_hs, o_rs, o_hs;
+  void* k;                     // the pools, as in Params
+  void* v;
+  float* k_scale;
+  float* v_scale;
+  const int32_t* block_table;
+  const int32_t* seq_lens;
+  const int32_t* q_start;      // [batch + 1], or null: one row a sequence
+  const int32_t* positions;    // [rows], or null: the rows' tokens
+  const double* freqs;         // [half] radians a position
+  uint32_t* flags;
+  int64_t stride_page, stride_head;   // bytes
+  int32_t stride_slot;                // bytes
+  int32_t rows, batch, hq, hkv;
+  int32_t half;                // pairs of a head
+  int32_t units;               // units of a head (rlda_rotary.hip)
+  int32_t interleaved, inverse;
+  int32_t num_pages, max_pages;
+  int32_t parts;               // workgroups of a window
+  float amplitude;
+  uint32_t magic_u, magic_qu, magic_ku, magic_half;   // ceil(2^32 / x) of units, hq units, hkv units, half
+};
+
+constexpr int kPageGroups = 2048;    // groups of mask words the page manager searches (rlda_pages.hip)
+constexpr int kPageMaxCaches = 64;   // caches (layers) of one launch
+
+struct PageCache {
+  char* k;
+  char* v;
+  float* k_scale;
+  float* v_scale;
+};
+
+struct PageParams {
+  int32_t* refs;               // [num_pages]
+  int32_t* block_table;        // [batch][max_pages]
+  int32_t* seq_lens;           // [batch]
+  const int32_t* add;          // grow: [batch] tokens, or null: one each
+  const int32_t* list_a;       // release: rows; fork: parents
+  const int32_t* list_b;       // fork: children
+  int32_t* list_src;           // pages to copy
+  int32_t* list_dst;
+  int32_t* fork_full;          // [count] full pages of each fork, -1: refused
+  int32_t* map;                // compaction: [num_pages] the moved pages' new numbers
+  int32_t* count_out;          // compaction: moves
+  int32_t* live_out;           // compaction: live pages
+  uint64_t* mask;              // [words] free pages
+  int32_t* group_free;         // [kPageGroups] free pages of each group of words
+  uint32_t* flags;
+  int64_t stride_page, stride_head;   // bytes
+  int32_t stride_slot;                // bytes
+  int32_t page_bytes, row_bytes;      // of one page of one cache (all KV heads), of one row of it
+  int32_t linear;              // ... and it lies in one piece
+  int32_t num_pages, num_kv_heads, batch, max_pages;
+  int32_t count;               // rows, forks or pairs
+  int32_t words, group_words;  // mask words of the pool, of a group
+  int32_t in_lds;              // the manager reads the pool itself
+  int32_t share;               // the launch that changes tables and references
+  int32_t num_caches, block_layers, layer_blocks;   // caches; of a workgroup; workgroups of a page
+  PageCache caches[kPageMaxCaches];
+};
+
 enum class KvKind { F32, BF16, FP8 };
 
 // Kernel launchers (rlda_kernels.hip).  Return hipSuccess or the launch error.
@@ -145,5 +217,18 @@ constexpr int kPackMaxPages = 32767;   // ... pages per sequence (16-bit LDS ent
 constexpr int kTwoWgMaxBatch = 512;      // two workgroups per CU (fp8, bf16 d = 64 decode): per-sequence LDS tables of this size
 constexpr int kTwoTileMaxBatch = 2048;   // two-tile multi-token rows: per-sequence LDS tables of this size
                                          // leave room for 32-row merge slots
+
+// Rotary positions (rlda_rotary.hip).
+int launch_rotate(bool f32, const RotaryParams& p, void* stream);
+int launch_append_rotary(KvKind kind, int head_dim, const RotaryParams& p, void* stream);
+
+// Pages of the cache (rlda_pages.hip).
+int launch_page_grow(const PageParams& p, void* stream);
+int launch_page_release(const PageParams& p, void* stream);
+int launch_page_fork(const PageParams& p, void* stream);        // which forks stand, their new pages
+int launch_page_fork_rows(const PageParams& p, void* stream);   // their table rows, references and copies
+int launch_page_compact(const PageParams& p, void* stream);     // the moves
+int launch_page_move(const PageParams& p, int grid, void* stream);   // tables and copies
+int launch_page_copy(const PageParams& p, void* stream);
 
 }  // namespace rlda

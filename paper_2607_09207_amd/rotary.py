@@ -1,0 +1,154 @@
+"""Rotary positions: turning rows by their positions, and the frequencies for it.
+
+The arithmetic runs in the library's kernels (csrc/rlda_rotary.hip); the frequencies are a
+small table of float64 values, laid out once.
+"""
+from __future__ import annotations
+
+import ctypes
+import math
+
+from . import _abi
+
+__all__ = ["rotate", "rotary_frequencies"]
+
+
+def rotary_frequencies(rot_dim: int, base: float = 10000.0, scaling=None, device="cuda"):
+    """(freqs, amplitude): radians a position of the rot_dim / 2 pairs (float64, on `device`),
+    f_j = base ** (-2 j / rot_dim), and the factor of the turned values.
+
+    scaling, for contexts longer than the one trained on:
+      None
+      {"type": "linear", "factor": s}                     positions divided by s
+      {"type": "base", "factor": s}                       the base raised so that the slowest pair turns 1 / s as far
+      {"type": "ramp", "factor": s, "context": n, "fast": 32, "slow": 1}
+            a pair that turns `fast` times or more over the trained context n keeps its
+            frequency, one that turns `slow` times or less has it divided by s, with a
+            linear ramp in the pair's index between them; the amplitude is
+            0.1 ln(s) + 1 ("amplitude" overrides it)
+    """
+    import torch
+    rot_dim = int(rot_dim)
+    if rot_dim < 2 or rot_dim % 2:
+        raise ValueError(f"rot_dim must be even and positive, got {rot_dim}")
+    if not base > 1.0:
+        raise ValueError(f"base must exceed 1, got {base}")
+    kind = None if scaling is None else scaling.get("type")
+    if kind not in (None, "linear", "base", "ramp"):
+        raise ValueError(f"unknown scaling {kind!r}")
+    s = 1.0 if scaling is None else float(scaling["factor"])
+    if not s > 0.0:
+        raise ValueError(f"factor must be positive, got {s}")
+    base, amplitude = float(base), 1.0
+    if kind == "base" and rot_dim > 2:
+        base *= s ** (rot_dim / (rot_dim - 2))
+    j = torch.arange(rot_dim // 2, dtype=torch.float64)
+    freqs = base ** (-2.0 * j / rot_dim)
+    if kind == "linear":
+        freqs = freqs / s
+    elif kind == "ramp":
+        fast, slow, n = float(scaling.get("fast", 32)), float(scaling.get("slow", 1)), float(scaling["context"])
+        if not (fast > slow > 0 and n > 0):
+            raise ValueError("ramp needs fast > slow > 0 and a positive context")
+        # The pair that turns r times over the context: n base^(-2j/rot) = 2 pi r.
+        pair = lambda r: rot_dim * math.log(n / (2 * math.pi * r)) / (2 * math.log(base))   # noqa: E731
+        lo = max(math.floor(pair(fast)), 0)
+        hi = min(math.ceil(pair(slow)), rot_dim - 1)
+        keep = 1.0 - ((j - lo) / max(hi - lo, 1e-3)).clamp(0.0, 1.0)
+        freqs = freqs * keep + freqs / s * (1.0 - keep)
+        amplitude = float(scaling.get("amplitude", 0.1 * math.log(s) + 1.0 if s > 1.0 else 1.0))
+    return freqs.to(device), amplitude
+
+
+def rows_of(t):
+    """Rows [n][heads][d] as the C ABI takes them (d contiguous, or of one element)."""
+    return _abi.Rows(t.data_ptr(), t.stride(0), t.stride(1))
+
+
+def rotary_of(freqs, interleaved, amplitude, inverse=False):
+    return _abi.Rotary(freqs.data_ptr(), 2 * freqs.shape[0], int(bool(interleaved)), float(amplitude), int(bool(inverse)))
+
+
+def check_rows(fail, name, t, dtype, shape, device):
+    if t is None:
+        fail(f"{name} is required")
+    if not t.is_cuda or t.device != device:
+        fail(f"{name} must be on {device}, got {t.device}")
+    if t.dtype != dtype:
+        fail(f"{name} must be {dtype}, got {t.dtype}")
+    if t.dim() != 3 or tuple(t.shape) != tuple(shape):
+        fail(f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
+    if t.shape[2] > 1 and t.stride(2) != 1:
+        fail(f"{name} needs its last dimension contiguous")
+    per = 16 // t.element_size()
+    if t.numel() and (t.data_ptr() % 16 or any(t.stride(i) % per for i in (0, 1) if t.shape[i] > 1)):
+        fail(f"{name} needs 16-byte aligned rows (strides {tuple(t.stride())})")
+
+
+def check_freqs(fail, freqs, d, device):
+    import torch
+    if freqs is None or not freqs.is_cuda or freqs.device != device:
+        fail(f"freqs must be on {device}")
+    if freqs.dtype != torch.float64 or freqs.dim() != 1 or not freqs.is_contiguous():
+        fail("freqs must be a contiguous float64 vector")
+    if not 16 <= 2 * freqs.shape[0] <= d or freqs.shape[0] % 8:
+        fail(f"freqs turns {2 * freqs.shape[0]} elements: a multiple of 16 up to head_dim {d} is supported")
+
+
+def on_device(device):
+    """A context in which `device` is the current one (nothing where it is already)."""
+    import contextlib
+
+    import torch
+    return contextlib.nullcontext() if torch.cuda.current_device() == device.index else torch.cuda.device(device)
+
+
+def raw_stream(device, stream):
+    import torch
+    if stream is None:
+        return torch.cuda.current_stream(device).cuda_stream
+    return getattr(stream, "cuda_stream", stream)
+
+
+def used_on(t, device, stream):
+    """A tensor made here and used on the caller's stream: its memory waits for it."""
+    import torch
+    if stream is not None:
+        t.record_stream(stream if hasattr(stream, "cuda_stream") else torch.cuda.ExternalStream(stream, device=device))
+
+
+def rotate(x, positions, freqs, *, interleaved: bool = False, amplitude: float = 1.0, inverse: bool = False, out=None,
+           stream=None):
+    """Rows x [n][heads][head_dim] (bf16 or fp32; any row and head strides that keep rows
+    16-byte aligned, e.g. a slice of a fused projection) turned by positions [n] (int32), pair j
+    by positions * freqs[j] radians (rl_decode_attn_rotate).  freqs: float64 [rot_dim / 2]
+    (rotary_frequencies); elements past rot_dim pass.  inverse=True takes the gradient of
+    the result back to x.  Returns `out` (x itself for in place), or a new tensor."""
+    import torch
+    what = "rl_decode_attn_rotate"
+
+    def fail(msg):
+        raise _abi.RldaError(-1, f"{what}: {msg}")
+
+    if not x.is_cuda:
+        fail(f"x must be on a GPU, got {x.device}")
+    if x.dtype not in (torch.bfloat16, torch.float32):
+        fail(f"x must be bfloat16 or float32, got {x.dtype}")
+    dev = x.device
+    shape = tuple(x.shape)
+    check_rows(fail, "x", x, x.dtype, shape, dev)
+    check_freqs(fail, freqs, shape[2], dev)
+    if positions is None or positions.device != dev or positions.dtype != torch.int32 or \
+            tuple(positions.shape) != (shape[0],) or not positions.is_contiguous():
+        fail(f"positions must be a contiguous int32 tensor of {shape[0]} on {dev}")
+    with on_device(dev):
+        if out is None:
+            out = torch.empty(shape, dtype=x.dtype, device=dev)
+            used_on(out, dev, stream)
+        else:
+            check_rows(fail, "out", out, x.dtype, shape, dev)
+        xr, outr, rot = rows_of(x), rows_of(out), rotary_of(freqs, interleaved, amplitude, inverse)
+        _abi.check(_abi.load().rl_decode_attn_rotate(
+            _abi.RLDA_F32 if x.dtype == torch.float32 else _abi.RLDA_BF16, shape[0], shape[1], shape[2], ctypes.byref(xr),
+            positions.data_ptr(), ctypes.byref(rot), ctypes.byref(outr), raw_stream(dev, stream)), what)
+    return out
