@@ -294,6 +294,40 @@ rlda_status rl_decode_attn_run_multi(rl_decode_attn_t handle, int32_t batch, int
                                      const int32_t* seq_lens, const int32_t* q_start, void* out, void* workspace,
                                      size_t workspace_bytes, void* stream, void* event_begin, void* event_end);
 
+/*
+ * Attention with modified scores.  With s = scale q . k for a query row at position `pos`
+ * (its token; seq_lens[b] - 1, or as for rl_decode_attn_run_multi) and the key of token t:
+ *   score_cap c > 0:   s <- c tanh(s / c)
+ *   slopes:            s <- s - slopes[h] |pos - t|         (query head h; any finite value)
+ * and the row sees the keys t of one interval only,
+ *   max(key_start[row], pos - window + 1, 0) <= t < max(pos + 1, min(prefix_lens[b], seq_lens[b])):
+ * a sliding window, documents packed in one sequence, a prefix that every row sees whole.
+ * A row that sees no key gives zeros.  A key that a row does not see has no part in it,
+ * whatever its values (infinities and NaN too).  Fields that are 0 or NULL change nothing.
+ */
+typedef struct {
+  float score_cap;              /* 0, or in [2^-10, 2^30] */
+  int32_t window;               /* keys a row sees up to its own; 0: all */
+  const float* slopes;          /* DEVICE [Hq] fp32 */
+  const int32_t* key_start;     /* DEVICE [total_q] */
+  const int32_t* prefix_lens;   /* DEVICE [batch] */
+} rl_decode_attn_scores;
+
+/*
+ * rl_decode_attn_run (q_start NULL, total_q = batch: one row a sequence) or
+ * rl_decode_attn_run_multi (q_start given) with modified scores; arguments, limits, checks
+ * and workspace as for these.  Pages below every row's interval are not read, their
+ * block-table entries neither.  Supported for bf16 and fp8 caches (RLDA_ERR_UNSUPPORTED
+ * for f32).  Rows at negative positions (n_b > seq_lens[b]) give zeros.  One kernel,
+ * asynchronous; events: both NULL, or both recorded around it.
+ */
+rlda_status rl_decode_attn_run_scored(rl_decode_attn_t handle, const rl_decode_attn_scores* scores, int32_t batch,
+                                      int32_t num_pages, int32_t total_q, int32_t max_q_len, const void* q,
+                                      const void* k_cache, const void* v_cache, const float* k_scale,
+                                      const float* v_scale, const int32_t* block_table, const int32_t* seq_lens,
+                                      const int32_t* q_start, void* out, void* workspace, size_t workspace_bytes,
+                                      void* stream, void* event_begin, void* event_end);
+
 /* Rows [rows][heads][head_dim] with head_dim contiguous; strides in elements, not negative. */
 typedef struct {
   const void* data;      /* 16-byte aligned, as every row and head of it has to be */

@@ -14,7 +14,7 @@ from typing import Optional
 
 from . import _abi
 from .cache_ops import CacheOps
-from .rotary import rotary_frequencies, rotate
+from .rotary import on_device, raw_stream, rotary_frequencies, rotate, used_on
 
 __all__ = ["DecodeAttention", "decode_attention", "rotate", "rotary_frequencies", "RldaError", "library_path"]
 
@@ -332,6 +332,53 @@ class DecodeAttention(CacheOps):
                                                       ptr(q_start), ptr(out), wp, ws.numel() - (wp - ws.data_ptr()),
                                                       stream, e0, e1),
                    "rl_decode_attn_run_multi")
+        return out
+
+    def scored(self, q, k_cache, v_cache, block_table, seq_lens, *, q_start=None, max_q_len: int = 0,
+               score_cap: float = 0.0, slopes=None, window: int = 0, key_start=None, prefix_lens=None, k_scale=None,
+               v_scale=None, out=None, workspace=None, stream=None, num_pages: Optional[int] = None, events=None):
+        """Attention with modified scores (rl_decode_attn_run_scored), one row a sequence or,
+        with q_start, as multi(): scores capped at score_cap by a tanh, less slopes[h] (fp32
+        [Hq]) times the distance, and every row seeing the keys from max(key_start[row],
+        pos - window + 1) to its own position, or to prefix_lens[b] where that is further
+        (int32 device tensors [rows] and [batch]).  Rows that see no key give zeros."""
+        torch = _torch()
+        what = "rl_decode_attn_run_scored"
+        cfg = self.config
+        if not q.is_cuda:
+            self._fail(what, f"q must be on a GPU, got {q.device}")
+        dev, total = q.device, int(q.shape[0])
+        B = total
+        if q_start is not None:
+            B = int(q_start.shape[0]) - 1 if q_start.dim() == 1 else -1
+            self._tensor(what, "q_start", q_start, torch.int32, (B + 1,), dev)
+        if B < 0:
+            self._fail(what, "q_start must hold batch + 1 offsets")
+        if out is not None:
+            self._check_rows(what, q, out, total, dev)
+        else:
+            self._tensor(what, "q", q, _torch_dtype(cfg.q_dtype), (total, cfg.num_q_heads, cfg.head_dim), dev)
+        npages = int(k_cache.shape[0]) if num_pages is None else int(num_pages)
+        self._check_table(what, block_table, seq_lens, B, dev)
+        self._check_cache(what, k_cache, v_cache, k_scale, v_scale, npages, dev)
+        for name, t, dt, n in (("slopes", slopes, torch.float32, cfg.num_q_heads), ("key_start", key_start, torch.int32, total),
+                               ("prefix_lens", prefix_lens, torch.int32, B)):
+            if t is not None:
+                self._tensor(what, name, t, dt, (n,), dev)
+        with on_device(dev):
+            if out is None:
+                out = torch.empty((total, cfg.num_q_heads, cfg.head_dim), dtype=_torch_dtype(cfg.out_dtype), device=dev)
+                used_on(out, dev, stream)
+            ws = workspace if workspace is not None else self._own_workspace(dev, stream)
+            self._check_workspace(what, ws, dev)
+            ptr = lambda t: None if t is None else t.data_ptr()   # noqa: E731
+            sc = _abi.Scores(float(score_cap), int(window), ptr(slopes), ptr(key_start), ptr(prefix_lens))
+            wp = self._aligned_ptr(ws)
+            e0, e1 = (None, None) if events is None else tuple(self._event_handle(e) for e in events)
+            _abi.check(self._lib.rl_decode_attn_run_scored(
+                self._h, ctypes.byref(sc), B, npages, total, int(max_q_len), ptr(q), ptr(k_cache), ptr(v_cache), ptr(k_scale),
+                ptr(v_scale), ptr(block_table), ptr(seq_lens), ptr(q_start), ptr(out), wp,
+                ws.numel() - (wp - ws.data_ptr()), raw_stream(dev, stream), e0, e1), what)
         return out
 
     def append(self, k_new, v_new, k_cache, v_cache, block_table, seq_lens, k_scale=None, v_scale=None,

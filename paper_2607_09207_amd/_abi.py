@@ -14,7 +14,7 @@ STATUS = {0: "RLDA_OK", -1: "RLDA_ERR_INVALID_ARG", -2: "RLDA_ERR_UNSUPPORTED", 
 EXPORTS = ["rl_decode_attn_create", "rl_decode_attn_workspace_size", "rl_decode_attn_run",
            "rl_decode_attn_run_profiled", "rl_decode_attn_run_grouped", "rl_decode_attn_grouped_workspace_size",
            "rl_decode_attn_append", "rl_decode_attn_run_multi", "rl_decode_attn_run_noalloc",
-           "rl_decode_attn_rotate", "rl_decode_attn_append_rotary", "rl_decode_attn_page_workspace_size",
+           "rl_decode_attn_run_scored", "rl_decode_attn_rotate", "rl_decode_attn_append_rotary", "rl_decode_attn_page_workspace_size",
            "rl_decode_attn_page_grow", "rl_decode_attn_page_release", "rl_decode_attn_page_fork",
            "rl_decode_attn_page_compact", "rl_decode_attn_page_copy",
            "rl_decode_attn_read_flags", "rl_decode_attn_destroy", "rl_decode_attn_strerror"]
@@ -38,6 +38,11 @@ class Config(ctypes.Structure):
         ("kv_stride_slot", ctypes.c_int64),
         ("num_work_ranges", ctypes.c_int32),
     ]
+
+
+class Scores(ctypes.Structure):
+    _fields_ = [("score_cap", ctypes.c_float), ("window", ctypes.c_int32), ("slopes", ctypes.c_void_p),
+                ("key_start", ctypes.c_void_p), ("prefix_lens", ctypes.c_void_p)]
 
 
 class Rows(ctypes.Structure):
@@ -95,6 +100,8 @@ def load() -> ctypes.CDLL:
         lib.rl_decode_attn_run_multi.restype = ctypes.c_int
         lib.rl_decode_attn_run_noalloc.argtypes = [vp, i32, i32] + [vp] * 8 + [vp, vp]
         lib.rl_decode_attn_run_noalloc.restype = ctypes.c_int
+        lib.rl_decode_attn_run_scored.argtypes = [vp, ctypes.POINTER(Scores), i32, i32, i32, i32] + [vp] * 9 + [vp, sz, vp, vp, vp]
+        lib.rl_decode_attn_run_scored.restype = ctypes.c_int
         rows, rot = ctypes.POINTER(Rows), ctypes.POINTER(Rotary)
         lib.rl_decode_attn_rotate.argtypes = [ctypes.c_int, i32, i32, i32, rows, vp, rot, rows, vp]
         lib.rl_decode_attn_append_rotary.argtypes = [vp, i32, i32, i32, rot, rows, rows, rows] + [vp] * 8 + [rows, vp, sz, vp]

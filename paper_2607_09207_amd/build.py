@@ -12,7 +12,8 @@ INCLUDE = os.path.join(ROOT, "include")
 LIB = os.path.join(HERE, "librl_decode_attn.so")
 SOURCES = [os.path.join(CSRC, "rlda_kernels.hip"), os.path.join(CSRC, "rlda_multi.hip"),
            os.path.join(CSRC, "rlda_host.cpp"), os.path.join(CSRC, "rlda_rotary.hip"),
-           os.path.join(CSRC, "rlda_pages.hip"), os.path.join(CSRC, "rlda_ops.cpp")]
+           os.path.join(CSRC, "rlda_pages.hip"), os.path.join(CSRC, "rlda_ops.cpp"),
+           os.path.join(CSRC, "rlda_scored.hip")]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 # Read-bandwidth reference kernels (bench support, not the attention path).
 PROBE_SOURCES = [os.path.join(CSRC, "hbm_probe.hip")]
@@ -33,17 +34,31 @@ FLAGS = [
 
 
 def build(verbose: bool = False, out: str = LIB, defines=(), sources=None) -> str:
+    """Compile the sources (each by a process of its own, four at a time: two of them take
+    over a minute) and link them."""
+    import tempfile
+    from concurrent.futures import ThreadPoolExecutor
     tmp = out + ".tmp%d" % os.getpid()
-    cmd = [HIPCC] + FLAGS + ["-D" + d for d in defines] + (sources or SOURCES) + ["-o", tmp]
-    if verbose:
-        print(" ".join(cmd), flush=True)
-    r = subprocess.run(cmd, capture_output=True, text=True)
     noise = "is not a recognized feature for this target"
-    msgs = [ln for ln in (r.stdout + r.stderr).splitlines() if noise not in ln]
-    if r.returncode != 0:
-        raise RuntimeError("hipcc failed:\n" + "\n".join(msgs))
-    if verbose and msgs:
-        print("\n".join(msgs), flush=True)
+
+    def hipcc(args):
+        cmd = [HIPCC] + args
+        if verbose:
+            print(" ".join(cmd), flush=True)
+        r = subprocess.run(cmd, capture_output=True, text=True)
+        msgs = [ln for ln in (r.stdout + r.stderr).splitlines() if noise not in ln]
+        if r.returncode != 0:
+            raise RuntimeError("hipcc failed:\n" + "\n".join(msgs))
+        if verbose and msgs:
+            print("\n".join(msgs), flush=True)
+
+    flags = [f for f in FLAGS if f != "-shared"] + ["-D" + d for d in defines]
+    with tempfile.TemporaryDirectory() as d:
+        srcs = list(sources or SOURCES)
+        objs = [os.path.join(d, "%d.o" % i) for i in range(len(srcs))]
+        with ThreadPoolExecutor(4) as pool:
+            list(pool.map(lambda so: hipcc(flags + ["-c", so[0], "-o", so[1]]), zip(srcs, objs)))
+        hipcc(["--offload-arch=gfx950", "-shared", "-fPIC"] + objs + ["-o", tmp])
     os.replace(tmp, out)
     return out
 

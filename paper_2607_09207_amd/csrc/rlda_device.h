@@ -100,5 +100,20 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
   return __builtin_bit_cast(uint32_t, v);
 }
 
+// tanh of a score, y -> cap tanh(y / cap) in log2 units (cap_log2 = cap log2(e), cap_arg =
+// 2 / cap): 1 - 2 / (e^(2 y / cap) + 1), exact at both ends.  Its error is 2^-23 of the cap,
+// 8e-6 in a score at a cap of 64.  Wider caps take the odd series where |y| is below a
+// sixteenth of the cap (the next term is 2e-9 of the result): their error stays 2^-20 of the score.
+__device__ __forceinline__ float cap_score(float y, float cap_log2, float cap_arg) {
+  const float t = 1.f - 2.f * __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(y * cap_arg) + 1.f);
+  float r = cap_log2 * t;
+  if (cap_log2 > 64.f * 1.4426950408889634f) {
+    const float x = y * cap_arg * 0.34657359027997264f, x2 = x * x;   // y / cap_log2
+    const float small = y * __builtin_fmaf(x2, __builtin_fmaf(x2, __builtin_fmaf(x2, -17.f / 315.f, 2.f / 15.f), -1.f / 3.f), 1.f);
+    r = __builtin_fabsf(x) < 0.0625f ? small : r;
+  }
+  return r;
+}
+
 }  // namespace
 }  // namespace rlda

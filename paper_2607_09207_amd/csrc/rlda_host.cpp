@@ -157,13 +157,32 @@ struct RunMem {
   int ranges_cap;   // work ranges the partial slots are sized for
 };
 
+// Modified scores a call may have; the host values are checked, the arrays are the device's.
+bool scores_ok(const rl_decode_attn_scores* s) {
+  if (!s) return false;
+  const float c = s->score_cap;
+  if (c != 0.f && !(c >= 0x1p-10f && c <= 0x1p30f)) return false;
+  return s->window >= 0 && !((uintptr_t)s->slopes & 3u) && !((uintptr_t)s->key_start & 3u) &&
+         !((uintptr_t)s->prefix_lens & 3u);
+}
+
+void set_scores(rlda::Params& p, const rl_decode_attn_scores& s) {
+  p.cap_log2 = s.score_cap * 1.4426950408889634f;
+  p.cap_arg = s.score_cap > 0.f ? 2.f / s.score_cap : 0.f;
+  p.slopes = s.slopes;
+  p.window = s.window;
+  p.key_start = s.key_start;
+  p.prefix_lens = s.prefix_lens;
+}
+
 // group_size == 0: plain run; > 0: grouped run with prefix_pages.  With `mem` the
-// run uses it instead of a workspace (plain runs only).
+// run uses it instead of a workspace, with `scores` they are modified (plain runs only).
 rlda_status run_impl(rl_decode_attn_t h, int32_t batch, int32_t num_pages, int32_t group_size,
                      const int32_t* prefix_pages, int32_t prompt_pages_hint, const void* q, const void* k_cache, const void* v_cache,
                      const float* k_scale, const float* v_scale, const int32_t* block_table,
                      const int32_t* seq_lens, void* out, void* workspace, size_t workspace_bytes, void* stream,
-                     void* ev_begin, void* ev_end, const RunMem* mem = nullptr) {
+                     void* ev_begin, void* ev_end, const RunMem* mem = nullptr,
+                     const rl_decode_attn_scores* scores = nullptr) {
   if (!h) return RLDA_ERR_INVALID_ARG;
   const rl_decode_attn_config& c = h->cfg;
   const bool grouped = group_size > 0;
@@ -242,6 +261,11 @@ rlda_status run_impl(rl_decode_attn_t h, int32_t batch, int32_t num_pages, int32
   p.scale_log2 = h->scale * 1.4426950408889634f;
   p.out_bf16 = c.out_dtype == RLDA_BF16;
   memcpy(p.q_head, h->q_head, sizeof p.q_head);
+  if (scores) {
+    set_scores(p, *scores);
+    if (rlda::launch_scored(h->kind, c.head_dim, two, p, stream, ev_begin, ev_end) != hipSuccess) return RLDA_ERR_HIP;
+    return RLDA_OK;
+  }
   if (!grouped) {
     const int e = two ? rlda::launch_decode_two(h->kind, c.head_dim, p, stream, ev_begin, ev_end)
                       : rlda::launch_decode(h->kind, c.head_dim, h->group, p, stream, ev_begin, ev_end);
@@ -297,6 +321,124 @@ rlda_status run_impl(rl_decode_attn_t h, int32_t batch, int32_t num_pages, int32
   p.pfx_splits = split < 1 ? 1 : (int)split;
   p.pfx_slots = (int)(slots < INT32_MAX ? slots : INT32_MAX);
   if (rlda::launch_grouped(h->kind, c.head_dim, h->group, p, ngroups, stream, ev_begin, ev_end) != hipSuccess)
+    return RLDA_ERR_HIP;
+  return RLDA_OK;
+}
+
+// Multi-token queries, with modified scores where `scores`.
+rlda_status multi_impl(rl_decode_attn_t h, const rl_decode_attn_scores* scores, int32_t batch, int32_t num_pages,
+                       int32_t total_q, int32_t max_q_len, const void* q, const void* k_cache, const void* v_cache,
+                       const float* k_scale, const float* v_scale, const int32_t* block_table, const int32_t* seq_lens,
+                       const int32_t* q_start, void* out, void* workspace, size_t workspace_bytes, void* stream,
+                       void* event_begin, void* event_end) {
+  if (!h) return RLDA_ERR_INVALID_ARG;
+  const rl_decode_attn_config& c = h->cfg;
+  if (batch < 0 || batch > c.max_batch || num_pages < 0 || total_q < 0 || max_q_len < 0) return RLDA_ERR_INVALID_ARG;
+  if ((!event_begin) != (!event_end)) return RLDA_ERR_INVALID_ARG;
+  if (h->kind == rlda::KvKind::F32) return RLDA_ERR_UNSUPPORTED;
+  // Few rows per sequence: the decode kernel's page stream, which splits long
+  // sequences across workgroups.  The rows of a (sequence, KV head), at most 64,
+  // are held by a wave as one or two 16-row tiles against each page; more than 32
+  // take two segments.  Otherwise the 128-row MFMA kernel.
+  const int64_t rows = (int64_t)max_q_len * h->group;
+  const int two_tiles = scores ? rlda::kScoredTwoTileMaxBatch : rlda::kTwoTileMaxBatch;
+  int tiles = rows > rlda::kMaxGroup && batch <= two_tiles ? rlda::kMaxRowTiles : 1;
+  int64_t row_chunks = (rows + rlda::kMaxGroup * tiles - 1) / (rlda::kMaxGroup * tiles);
+  const bool rows_path = max_q_len >= 1 && max_q_len <= rlda::kMaxRowsQLen &&
+                         rows <= (int64_t)rlda::kMaxGroup * rlda::kMaxRowChunks &&
+                         (!scores || batch <= rlda::kScoredMaxBatch) &&
+                         (int64_t)batch * (c.max_pages_per_seq + rlda::kStartCost) * c.num_kv_heads * row_chunks <= INT32_MAX;
+  if (!rows_path && batch > rlda::kMultiMaxBatch) return RLDA_ERR_UNSUPPORTED;
+  // The kernels address q with 32-bit byte offsets.
+  if ((int64_t)total_q * c.num_q_heads * c.head_dim * 2 > INT32_MAX) return RLDA_ERR_UNSUPPORTED;
+  if (batch == 0 || total_q == 0) return RLDA_OK;
+  if (!q || !block_table || !seq_lens || !q_start || !out) return RLDA_ERR_INVALID_ARG;
+  if (num_pages > 0 && (!k_cache || !v_cache)) return RLDA_ERR_INVALID_ARG;
+  if (!aligned16(q) || !aligned16(k_cache) || !aligned16(v_cache) || !aligned16(out)) return RLDA_ERR_INVALID_ARG;
+  if (((uintptr_t)block_table & 3u) || ((uintptr_t)seq_lens & 3u) || ((uintptr_t)q_start & 3u))
+    return RLDA_ERR_INVALID_ARG;
+  if (h->kind == rlda::KvKind::FP8 && num_pages > 0 &&
+      (!k_scale || !v_scale || ((uintptr_t)k_scale & 3u) || ((uintptr_t)v_scale & 3u)))
+    return RLDA_ERR_INVALID_ARG;
+  const WsLayout wl = layout_of(h);
+  if (!workspace || ((uintptr_t)workspace % kAlign)) return RLDA_ERR_WORKSPACE;
+  if (workspace_bytes < wl.total) return RLDA_ERR_WORKSPACE;
+  char* ws = (char*)workspace;
+  rlda::Params p;
+  memset(&p, 0, sizeof p);
+  p.q = q;
+  p.k = k_cache;
+  p.v = v_cache;
+  p.k_scale = k_scale;
+  p.v_scale = v_scale;
+  p.block_table = block_table;
+  p.seq_lens = seq_lens;
+  p.q_start = q_start;
+  p.total_q = total_q;
+  p.max_q_len = max_q_len;
+  p.out = out;
+  p.flags = (uint32_t*)(ws + wl.flags);
+  const int eb = elem_bytes(c.kv_dtype);
+  p.stride_page = h->stride_page * eb;
+  p.stride_head = h->stride_head * eb;
+  p.stride_slot = (int32_t)(h->stride_slot * eb);
+  p.batch = batch;
+  p.num_pages = num_pages;
+  p.num_q_heads = c.num_q_heads;
+  p.num_kv_heads = c.num_kv_heads;
+  p.group = h->group;
+  p.max_pages = c.max_pages_per_seq;
+  p.scale_log2 = h->scale * 1.4426950408889634f;
+  p.out_bf16 = c.out_dtype == RLDA_BF16;
+  memcpy(p.q_head, h->q_head, sizeof p.q_head);
+  if (scores) set_scores(p, *scores);
+  if (rows_path) {
+    int dev = 0;
+    if (hipGetDevice(&dev) != hipSuccess) return RLDA_ERR_HIP;
+    int ranges = c.num_work_ranges > 0 ? c.num_work_ranges : cu_count(dev);
+    if (ranges <= 0) return RLDA_ERR_HIP;
+    // Partial slots hold one segment's rows each; the workspace has room for
+    // 2 * ws_ranges * 16 rows.  A workspace sized for fewer ranges than two-tile
+    // slots need falls back to one tile per segment.
+    if (tiles == 2 && (int64_t)h->ws_ranges * rlda::kMaxGroup / std::min<int64_t>(rows, 32) < 1) {
+      tiles = 1;
+      row_chunks = (rows + rlda::kMaxGroup - 1) / rlda::kMaxGroup;
+    }
+    p.row_chunks = (int)row_chunks;
+    p.part_rows = (int)std::min<int64_t>(rows, (int64_t)rlda::kMaxGroup * tiles);
+    const int64_t cap_ranges = (int64_t)h->ws_ranges * rlda::kMaxGroup / p.part_rows;
+    if (ranges > cap_ranges) ranges = (int)cap_ranges;
+    if (ranges > rlda::kMaxRanges) ranges = rlda::kMaxRanges;
+    const int64_t max_units = (int64_t)batch * c.num_kv_heads * row_chunks * c.max_pages_per_seq;
+    if (ranges > max_units) ranges = (int)max_units;
+    if (ranges < 1) ranges = 1;
+    p.nranges = ranges;
+    p.inv_ranges = c.num_work_ranges > 0 ? 0.f : 1.0f / (float)ranges;
+    p.counters = (uint32_t*)(ws + wl.counters);
+    p.call_tag = next_call_tag();
+    p.part_ml = (float*)(ws + wl.part_ml);
+    p.part_acc = (float*)(ws + wl.part_acc);
+    auto* const launch_rows = scores ? rlda::launch_scored_rows : rlda::launch_decode_rows;
+    if (launch_rows(h->kind, c.head_dim, tiles, p, stream, event_begin, event_end) != hipSuccess)
+      return RLDA_ERR_HIP;
+    return RLDA_OK;
+  }
+  // One workgroup per (row block, KV head): a sequence's n_b * G rows take at most
+  // n_b * G / rows_per_block + 1 blocks, so this grid covers every consistent q_start.
+  const auto blocks_of = [&](int per) { return ((int64_t)total_q * h->group + per - 1) / per + batch; };
+  // At most one 128-row workgroup a CU: the grid has room for 32-row ones too, and the
+  // kernel chooses from the lengths (use_split in rlda_multi.hip).
+  int dev = 0;
+  if (hipGetDevice(&dev) != hipSuccess) return RLDA_ERR_HIP;
+  p.nranges = cu_count(dev);
+  const bool small = rlda::kMultiSplits && blocks_of(rlda::kMultiRows) * c.num_kv_heads <= p.nranges;
+  const int64_t blocks = blocks_of(small ? rlda::kMultiSmallRows : rlda::kMultiRows);
+  // Four KV heads: each XCD takes one KV head of one of two sequence classes, and
+  // the grid holds 8 blocks per row block so that either class fits (see the kernel).
+  const int64_t grid = blocks * (c.num_kv_heads == 4 ? 8 : c.num_kv_heads);
+  if (grid > INT32_MAX) return RLDA_ERR_UNSUPPORTED;
+  auto* const launch = scores ? rlda::launch_scored_multi : rlda::launch_multi;
+  if (launch(h->kind, c.head_dim, small, p, (int)grid, stream, event_begin, event_end) != hipSuccess)
     return RLDA_ERR_HIP;
   return RLDA_OK;
 }
@@ -407,111 +549,24 @@ rlda_status rl_decode_attn_run_multi(rl_decode_attn_t h, int32_t batch, int32_t 
                                      const float* k_scale, const float* v_scale, const int32_t* block_table,
                                      const int32_t* seq_lens, const int32_t* q_start, void* out, void* workspace,
                                      size_t workspace_bytes, void* stream, void* event_begin, void* event_end) {
-  if (!h) return RLDA_ERR_INVALID_ARG;
-  const rl_decode_attn_config& c = h->cfg;
-  if (batch < 0 || batch > c.max_batch || num_pages < 0 || total_q < 0 || max_q_len < 0) return RLDA_ERR_INVALID_ARG;
-  if ((!event_begin) != (!event_end)) return RLDA_ERR_INVALID_ARG;
+  return multi_impl(h, nullptr, batch, num_pages, total_q, max_q_len, q, k_cache, v_cache, k_scale, v_scale, block_table,
+                    seq_lens, q_start, out, workspace, workspace_bytes, stream, event_begin, event_end);
+}
+
+rlda_status rl_decode_attn_run_scored(rl_decode_attn_t h, const rl_decode_attn_scores* scores, int32_t batch,
+                                      int32_t num_pages, int32_t total_q, int32_t max_q_len, const void* q,
+                                      const void* k_cache, const void* v_cache, const float* k_scale,
+                                      const float* v_scale, const int32_t* block_table, const int32_t* seq_lens,
+                                      const int32_t* q_start, void* out, void* workspace, size_t workspace_bytes,
+                                      void* stream, void* event_begin, void* event_end) {
+  if (!h || !scores_ok(scores) || (!event_begin) != (!event_end)) return RLDA_ERR_INVALID_ARG;
   if (h->kind == rlda::KvKind::F32) return RLDA_ERR_UNSUPPORTED;
-  // Few rows per sequence: the decode kernel's page stream, which splits long
-  // sequences across workgroups.  The rows of a (sequence, KV head), at most 64,
-  // are held by a wave as one or two 16-row tiles against each page; more than 32
-  // take two segments.  Otherwise the 128-row MFMA kernel.
-  const int64_t rows = (int64_t)max_q_len * h->group;
-  int tiles = rows > rlda::kMaxGroup && batch <= rlda::kTwoTileMaxBatch ? rlda::kMaxRowTiles : 1;
-  int64_t row_chunks = (rows + rlda::kMaxGroup * tiles - 1) / (rlda::kMaxGroup * tiles);
-  const bool rows_path = max_q_len >= 1 && max_q_len <= rlda::kMaxRowsQLen &&
-                         rows <= (int64_t)rlda::kMaxGroup * rlda::kMaxRowChunks &&
-                         (int64_t)batch * (c.max_pages_per_seq + rlda::kStartCost) * c.num_kv_heads * row_chunks <= INT32_MAX;
-  if (!rows_path && batch > rlda::kMultiMaxBatch) return RLDA_ERR_UNSUPPORTED;
-  // The kernels address q with 32-bit byte offsets.
-  if ((int64_t)total_q * c.num_q_heads * c.head_dim * 2 > INT32_MAX) return RLDA_ERR_UNSUPPORTED;
-  if (batch == 0 || total_q == 0) return RLDA_OK;
-  if (!q || !block_table || !seq_lens || !q_start || !out) return RLDA_ERR_INVALID_ARG;
-  if (num_pages > 0 && (!k_cache || !v_cache)) return RLDA_ERR_INVALID_ARG;
-  if (!aligned16(q) || !aligned16(k_cache) || !aligned16(v_cache) || !aligned16(out)) return RLDA_ERR_INVALID_ARG;
-  if (((uintptr_t)block_table & 3u) || ((uintptr_t)seq_lens & 3u) || ((uintptr_t)q_start & 3u))
-    return RLDA_ERR_INVALID_ARG;
-  if (h->kind == rlda::KvKind::FP8 && num_pages > 0 &&
-      (!k_scale || !v_scale || ((uintptr_t)k_scale & 3u) || ((uintptr_t)v_scale & 3u)))
-    return RLDA_ERR_INVALID_ARG;
-  const WsLayout wl = layout_of(h);
-  if (!workspace || ((uintptr_t)workspace % kAlign)) return RLDA_ERR_WORKSPACE;
-  if (workspace_bytes < wl.total) return RLDA_ERR_WORKSPACE;
-  char* ws = (char*)workspace;
-  rlda::Params p;
-  memset(&p, 0, sizeof p);
-  p.q = q;
-  p.k = k_cache;
-  p.v = v_cache;
-  p.k_scale = k_scale;
-  p.v_scale = v_scale;
-  p.block_table = block_table;
-  p.seq_lens = seq_lens;
-  p.q_start = q_start;
-  p.total_q = total_q;
-  p.max_q_len = max_q_len;
-  p.out = out;
-  p.flags = (uint32_t*)(ws + wl.flags);
-  const int eb = elem_bytes(c.kv_dtype);
-  p.stride_page = h->stride_page * eb;
-  p.stride_head = h->stride_head * eb;
-  p.stride_slot = (int32_t)(h->stride_slot * eb);
-  p.batch = batch;
-  p.num_pages = num_pages;
-  p.num_q_heads = c.num_q_heads;
-  p.num_kv_heads = c.num_kv_heads;
-  p.group = h->group;
-  p.max_pages = c.max_pages_per_seq;
-  p.scale_log2 = h->scale * 1.4426950408889634f;
-  p.out_bf16 = c.out_dtype == RLDA_BF16;
-  memcpy(p.q_head, h->q_head, sizeof p.q_head);
-  if (rows_path) {
-    int dev = 0;
-    if (hipGetDevice(&dev) != hipSuccess) return RLDA_ERR_HIP;
-    int ranges = c.num_work_ranges > 0 ? c.num_work_ranges : cu_count(dev);
-    if (ranges <= 0) return RLDA_ERR_HIP;
-    // Partial slots hold one segment's rows each; the workspace has room for
-    // 2 * ws_ranges * 16 rows.  A workspace sized for fewer ranges than two-tile
-    // slots need falls back to one tile per segment.
-    if (tiles == 2 && (int64_t)h->ws_ranges * rlda::kMaxGroup / std::min<int64_t>(rows, 32) < 1) {
-      tiles = 1;
-      row_chunks = (rows + rlda::kMaxGroup - 1) / rlda::kMaxGroup;
-    }
-    p.row_chunks = (int)row_chunks;
-    p.part_rows = (int)std::min<int64_t>(rows, (int64_t)rlda::kMaxGroup * tiles);
-    const int64_t cap_ranges = (int64_t)h->ws_ranges * rlda::kMaxGroup / p.part_rows;
-    if (ranges > cap_ranges) ranges = (int)cap_ranges;
-    if (ranges > rlda::kMaxRanges) ranges = rlda::kMaxRanges;
-    const int64_t max_units = (int64_t)batch * c.num_kv_heads * row_chunks * c.max_pages_per_seq;
-    if (ranges > max_units) ranges = (int)max_units;
-    if (ranges < 1) ranges = 1;
-    p.nranges = ranges;
-    p.inv_ranges = c.num_work_ranges > 0 ? 0.f : 1.0f / (float)ranges;
-    p.counters = (uint32_t*)(ws + wl.counters);
-    p.call_tag = next_call_tag();
-    p.part_ml = (float*)(ws + wl.part_ml);
-    p.part_acc = (float*)(ws + wl.part_acc);
-    if (rlda::launch_decode_rows(h->kind, c.head_dim, tiles, p, stream, event_begin, event_end) != hipSuccess)
-      return RLDA_ERR_HIP;
-    return RLDA_OK;
-  }
-  // One workgroup per (row block, KV head): a sequence's n_b * G rows take at most
-  // n_b * G / rows_per_block + 1 blocks, so this grid covers every consistent q_start.
-  const auto blocks_of = [&](int per) { return ((int64_t)total_q * h->group + per - 1) / per + batch; };
-  // At most one 128-row workgroup a CU: the grid has room for 32-row ones too, and the
-  // kernel chooses from the lengths (use_split in rlda_multi.hip).
-  int dev = 0;
-  if (hipGetDevice(&dev) != hipSuccess) return RLDA_ERR_HIP;
-  p.nranges = cu_count(dev);
-  const bool small = rlda::kMultiSplits && blocks_of(rlda::kMultiRows) * c.num_kv_heads <= p.nranges;
-  const int64_t blocks = blocks_of(small ? rlda::kMultiSmallRows : rlda::kMultiRows);
-  // Four KV heads: each XCD takes one KV head of one of two sequence classes, and
-  // the grid holds 8 blocks per row block so that either class fits (see the kernel).
-  const int64_t grid = blocks * (c.num_kv_heads == 4 ? 8 : c.num_kv_heads);
-  if (grid > INT32_MAX) return RLDA_ERR_UNSUPPORTED;
-  if (rlda::launch_multi(h->kind, c.head_dim, small, p, (int)grid, stream, event_begin, event_end) != hipSuccess)
-    return RLDA_ERR_HIP;
-  return RLDA_OK;
+  if (q_start)
+    return multi_impl(h, scores, batch, num_pages, total_q, max_q_len, q, k_cache, v_cache, k_scale, v_scale, block_table,
+                      seq_lens, q_start, out, workspace, workspace_bytes, stream, event_begin, event_end);
+  if (total_q != batch) return RLDA_ERR_INVALID_ARG;
+  return run_impl(h, batch, num_pages, 0, nullptr, -1, q, k_cache, v_cache, k_scale, v_scale, block_table, seq_lens, out,
+                  workspace, workspace_bytes, stream, event_begin, event_end, nullptr, scores);
 }
 
 rlda_status rl_decode_attn_read_flags(rl_decode_attn_t h, const void* workspace, void* stream, uint32_t* flags) {

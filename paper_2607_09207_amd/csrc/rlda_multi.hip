@@ -78,7 +78,7 @@ static_assert(kTile * kNT * kWaves == kMultiRows, "a workgroup's rows are its wa
 
 // SMALL: calls of few row blocks, which may take 32 rows to a workgroup and deal the keys
 // to its waves (chosen on the device, see "How few row blocks are cut").
-template <int D, bool FP8, bool SMALL>
+template <int D, bool FP8, bool SMALL, bool MOD = false>
 struct MqShape {
   static constexpr int KS = D / 16;           // 32x32x16 k-steps of K Q^T
   static constexpr int DT = D / 32;           // 32-wide output tiles of O^T
@@ -96,7 +96,8 @@ struct MqShape {
 #ifdef RLDA_MQ_WAVES
   static constexpr int WAVES = SMALL ? 2 : RLDA_MQ_WAVES;
 #else
-  static constexpr int WAVES = SMALL ? 2 : kNT == 1 ? (D == 64 ? RLDA_MQ_WAVES_D64 : 3) : 1;
+  // (MOD: the intervals, the bias and the noted infinities are 15 registers more.)
+  static constexpr int WAVES = SMALL ? 2 : kNT == 1 ? (D == 64 ? RLDA_MQ_WAVES_D64 : MOD ? 2 : 3) : 1;
 #endif
   static constexpr int krs(bool dma) { return dma ? 2 * D : 2 * D + RLDA_MQ_KPAD; }   // LDS row stride of the K block (bytes)
   static constexpr int vrs(bool dma) { return dma ? 2 * D : 2 * D + RLDA_MQ_VPAD; }   // ... of the V block
@@ -141,11 +142,38 @@ __device__ __forceinline__ bf16x4 lds_tr_read(const char* p) {
   return __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4*)(__attribute__((address_space(3))) char*)p);
 }
 
-template <int D, bool FP8, bool SMALL>
+// Non-zero where one of eight bf16 values is an infinity or NaN (their exponent bits are all set).
+__device__ __forceinline__ uint32_t not_finite(u32x4 w) {
+  uint32_t r = 0;
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    r |= (uint32_t)((w[i] & 0x7F80u) == 0x7F80u) | (uint32_t)((w[i] & 0x7F800000u) == 0x7F800000u);
+  return r;
+}
+
+// Infinities and NaN turned into zeros.
+__device__ __forceinline__ bf16x8 without_odd(bf16x8 v) {
+  typedef uint16_t u16x8_t __attribute__((ext_vector_type(8)));
+  u16x8_t x = __builtin_bit_cast(u16x8_t, v);
+#pragma unroll
+  for (int e = 0; e < 8; ++e) x[e] = (x[e] & 0x7F80u) == 0x7F80u ? (uint16_t)0 : x[e];
+  return __builtin_bit_cast(bf16x8, x);
+}
+
+// The largest and the smallest of non-negative values over the wave.
+__device__ __forceinline__ int wave_max(int x) { return __builtin_amdgcn_readlane(wave_scan_max(x), 63); }
+__device__ __forceinline__ int wave_min(int x) { return 0x7fffffff - wave_max(0x7fffffff - x); }
+
+// MOD: modified scores (rl_decode_attn_run_scored): the cap and the bias are applied to the
+// score registers, and a row sees the keys of an interval.  The workgroup walks the blocks
+// from the first key that one of its rows sees to the last; a wave skips those that none of
+// its own sees, and masks only the ones that some of its rows sees in part.
+template <int D, bool FP8, bool SMALL, bool MOD = false>
 __global__ __attribute__((amdgpu_flat_work_group_size(kThreads, kThreads),
-                          amdgpu_waves_per_eu(MqShape<D, FP8, SMALL>::WAVES, MqShape<D, FP8, SMALL>::WAVES)))
+                          amdgpu_waves_per_eu(MqShape<D, FP8, SMALL, MOD>::WAVES,
+                                              MqShape<D, FP8, SMALL, MOD>::WAVES)))
 void multi_query_kernel(const Params p) {
-  using S = MqShape<D, FP8, SMALL>;
+  using S = MqShape<D, FP8, SMALL, MOD>;
   // Block buffers: block kb is computed from one while the next blocks are written to
   // the others; waves that split the keys have one each.
   __shared__ __align__(16) char s_k[S::NBUF][kKeys * S::KRS];
@@ -228,7 +256,8 @@ void multi_query_kernel(const Params p) {
       key0 = s_key[lane];
     }
     if constexpr (SMALL) {
-      split = use_split(sum32 * Hkv, emax, p.nranges);
+      // (A window bounds the keys of a row block.)
+      split = use_split(sum32 * Hkv, MOD && p.window > 0 ? min(emax, p.window) : emax, p.nranges);
       if (split) {
         rshift = 5;
         nitems = sum32;
@@ -376,16 +405,28 @@ void multi_query_kernel(const Params p) {
   const int rows = n * G;
   const int r0 = rb << rshift, r1 = min(r0 + (1 << rshift), rows);
   const int base_pos = L - n;                                   // position of query token 0
-  const int E = max(0, base_pos + (r1 - 1) / G + 1);            // keys the workgroup reads
-  const int nkb = (E + kKeys - 1) / kKeys;
+  // (MOD: keys that every row of the sequence sees, and the first key that a row sees.)
+  const int prefix = MOD && p.prefix_lens ? min(p.prefix_lens[b], L) : 0;
+  auto first_key = [&](int row) {
+    const int i = row / G;
+    int lo = p.key_start ? max(p.key_start[q0 + i], 0) : 0;
+    if (p.window > 0) lo = max(lo, base_pos + i - p.window + 1);
+    return lo;
+  };
+  auto seen_end = [&](int row) { return max(max(0, base_pos + row / G + 1), prefix); };
+  const int E = MOD ? seen_end(r1 - 1) : max(0, base_pos + (r1 - 1) / G + 1);   // keys the workgroup reads, from 0
   const int wr0 = r0 + (split ? 0 : kTile * kNT * wave), wr1 = min(wr0 + kTile * kNT, r1);
-  const int Ew = wr0 < wr1 ? max(0, base_pos + (wr1 - 1) / G + 1) : 0;       // keys this wave needs
-  const int Ew_full = wr0 < wr1 ? max(0, base_pos + wr0 / G + 1) : 0;       // ... visible to all its rows
+  // Keys this wave needs, and those visible to all its rows.
+  const int Ew = wr0 < wr1 ? (MOD ? seen_end(wr1 - 1) : max(0, base_pos + (wr1 - 1) / G + 1)) : 0;
+  int Ew_full = wr0 < wr1 ? (MOD ? seen_end(wr0) : max(0, base_pos + wr0 / G + 1)) : 0;
 
   // This lane's query rows, one per tile: lanes i and i + 32 share row wr0 + 32 t + i.
   const int i = lane & 31, hh = lane >> 5;
   bool live[kNT];
   int qi[kNT], head[kNT], lim[kNT];
+  int low[kNT];          // MOD: keys [low, lim) are visible
+  float slope[kNT];      // ... and the row's bias a token, in log2 units
+  static_assert(!MOD || kNT == 1, "modified scores: one tile a wave");
 #pragma unroll
   for (int t = 0; t < kNT; ++t) {
     const int row = wr0 + kTile * t + i;
@@ -393,7 +434,36 @@ void multi_query_kernel(const Params p) {
     qi[t] = live[t] ? row / G : 0;
     head[t] = live[t] ? s_qh[g * G + (row - qi[t] * G)] : 0;
     lim[t] = live[t] ? base_pos + qi[t] + 1 : 0;               // keys [0, lim) are visible
+    if constexpr (MOD) {
+      // Rows before token 0 (more rows than tokens) see nothing.
+      const bool there = live[t] && base_pos + qi[t] >= 0;
+      low[t] = there ? first_key(row) : 0;
+      lim[t] = there ? seen_end(row) : 0;
+      slope[t] = live[t] && p.slopes ? p.slopes[head[t]] * 1.4426950408889634f : 0.f;
+      if (low[t] >= lim[t]) low[t] = lim[t] = 0;
+    }
   }
+  // MOD: the blocks start at kb0; the wave's rows see keys from Wlo on, all of them from
+  // Wlo_full on (where one sees nothing, none do).
+  int kb0 = 0, first_page = 0, Wlo = 0, Wlo_full = 0;
+  if constexpr (MOD) {
+    int lo = E;
+#pragma unroll
+    for (int k = 0; k < kMultiRows; k += 64) {
+      const int row = r0 + k + lane;
+      if (row < r1 && base_pos + row / G >= 0) {
+        const int x = first_key(row);
+        if (x < seen_end(row)) lo = min(lo, x);
+      }
+    }
+    lo = wave_min(lo);
+    kb0 = lo / kKeys;
+    first_page = lo / kPage;   // the page before it may be in the first block: not read
+    Wlo = wave_min(lim[0] > 0 ? low[0] : 0x7ffffffe);
+    Wlo_full = wave_max(low[0]);
+    if (__builtin_amdgcn_ballot_w64(live[0] && lim[0] == 0) != 0) Ew_full = 0;
+  }
+  const int nkb = max((E + kKeys - 1) / kKeys - kb0, 0);   // blocks: kb0 + kb, kb < nkb
 
   // Q operands (B of K Q^T): lane 32h + i holds its row's elements [16s + 8h, 16s + 8h + 8).
   bf16x8 qop[kNT][S::KS];
@@ -434,7 +504,7 @@ void multi_query_kernel(const Params p) {
   // Page j of the sequence, K or V, into registers and from there to page `slot` of
   // block buffer `buf`.
   auto page_load = [&](Staged& st, int is_v, int j, int pid) {
-    int tok = min(max(E - j * kPage, 0), kPage);
+    int tok = MOD && j < first_page ? 0 : min(max(E - j * kPage, 0), kPage);
     st.bad = 0;
     if (tok > 0) {
       if ((unsigned)pid >= (unsigned)p.num_pages) {
@@ -507,7 +577,7 @@ void multi_query_kernel(const Params p) {
 #pragma unroll
     for (int h = 0; h < kKH; ++h) {
       const int j = page_index(kb, h);
-      int tok = min(max(E - j * kPage, 0), kPage);
+      int tok = MOD && j < first_page ? 0 : min(max(E - j * kPage, 0), kPage);
       int badp = 0;
       if (tok > 0 && (unsigned)pid[h] >= (unsigned)p.num_pages) {
         tok = 0;
@@ -540,6 +610,8 @@ void multi_query_kernel(const Params p) {
 
   // P^T operands of the current block per tile: key tile kh, key step kk.
   bf16x8 pb[kNT][kKH][2];
+  bool masked = false;   // MOD: this lane's row does not see every key of the current block
+  static_assert(!MOD || kKH == 1, "modified scores: one key tile a block");
   // Online softmax of tile t on block kb: updates (m, l), rescales the tile's
   // accumulators when m moves and leaves the block's P^T operands in pb[t].
   auto softmax = [&](int t, int kb, int buf, const f32x16* sc) {
@@ -559,14 +631,33 @@ void multi_query_kernel(const Params p) {
 #pragma unroll
     for (int kh = 0; kh < kKH; ++kh)
 #pragma unroll
-      for (int j = 0; j < 16; ++j) sv[kh][j] = FP8 ? sc[kh][j] * km[2 * kh + (j >> 3)] : sc[kh][j];
-    if ((kb + 1) * kKeys > Ew_full || bad) {
+      for (int j = 0; j < 16; ++j) {
+        sv[kh][j] = FP8 || MOD ? sc[kh][j] * km[2 * kh + (j >> 3)] : sc[kh][j];
+        if constexpr (MOD) {
+          if (p.cap_log2 > 0.f) sv[kh][j] = cap_score(sv[kh][j], p.cap_log2, p.cap_arg);
+        }
+      }
+    if constexpr (MOD) {
+      if (p.slopes) {
+        const float at = (float)(base_pos + qi[t] - kb * kKeys - 4 * hh);   // position less the key of j = 0
+#pragma unroll
+        for (int kh = 0; kh < kKH; ++kh)
+#pragma unroll
+          for (int j = 0; j < 16; ++j)
+            sv[kh][j] = __builtin_fmaf(-slope[t], __builtin_fabsf(at - (float)(kTile * kh + 8 * (j >> 2) + (j & 3))), sv[kh][j]);
+      }
+      masked = false;
+    }
+    if ((kb + 1) * kKeys > Ew_full || (MOD && kb * kKeys < Wlo_full) || bad) {
 #pragma unroll
       for (int kh = 0; kh < kKH; ++kh)
 #pragma unroll
         for (int j = 0; j < 16; ++j) {
           const int key = kb * kKeys + kTile * kh + 8 * (j >> 2) + 4 * hh + (j & 3);
-          if (key >= lim[t] || s_bad[buf][2 * kh + (j >> 3)]) sv[kh][j] = neg_inf();
+          if ((MOD && key < low[t]) || key >= lim[t] || s_bad[buf][2 * kh + (j >> 3)]) {
+            sv[kh][j] = neg_inf();
+            if constexpr (MOD) masked = true;
+          }
         }
     }
     float mx = neg_inf();
@@ -576,7 +667,7 @@ void multi_query_kernel(const Params p) {
       for (int j = 0; j < 16; j += 2) mx = fmaxf(fmaxf(mx, sv[kh][j]), sv[kh][j + 1]);
     }
     mx = pair_max(mx);
-    if constexpr (!FP8) mx *= km[0];
+    if constexpr (!FP8 && !MOD) mx *= km[0];
     // Lazy rescale: the reference maximum moves only when a score exceeds it by
     // more than 2^kRescaleLog2 (always when it is still -inf and a score is not).
     // A row whose keys are all masked so far keeps m = -inf and alpha = 1.
@@ -589,7 +680,7 @@ void multi_query_kernel(const Params p) {
       for (int c = 0; c < S::DT; ++c) acc[t][c] *= alpha;
     }
     const float mu = (m[t] == neg_inf()) ? 0.f : m[t];
-    const float fk = FP8 ? 1.f : km[0];
+    const float fk = FP8 || MOD ? 1.f : km[0];
 #pragma unroll
     for (int kh = 0; kh < kKH; ++kh) {
       float pr[16];
@@ -644,12 +735,55 @@ void multi_query_kernel(const Params p) {
   };
   static_assert(S::KS == 2 * S::DT, "as many V^T operands as score k-steps");
 
+  // MOD: the infinities and NaN of V that this lane's row sees, a bit an output (NaN: both).
+  // They are noted here, left out of the product, and put into the results at the end.  A
+  // key a turn, its values from LDS: as slow as it is rare.  (Added to the accumulators in
+  // a branch, they made two copies of these: 250 to 450 registers spilled.)
+  uint32_t plus_inf[S::DT / 2] = {}, minus_inf[S::DT / 2] = {};
+  auto note_odd = [&](auto dma, int kb, int buf) __attribute__((always_inline)) {
+    constexpr bool kDma = decltype(dma)::value;
+    typedef uint16_t u16x4_t __attribute__((ext_vector_type(4)));
+#pragma unroll 1
+    for (int R = 0; R < kTile; ++R) {
+      const int key = kb * kKeys + R;
+      const bool sees = key >= low[0] && key < lim[0] && !s_bad[buf][R >> 4];
+      const char* vr = s_v[buf] + R * S::vrs(kDma);
+#pragma unroll
+      for (int c = 0; c < S::DT; ++c)
+#pragma unroll
+        for (int jj = 0; jj < 4; ++jj) {
+          // Elements d = 32c + 8jj + 4hh ..: chunk 4c + jj, byte 8hh in it.
+          const int off = kDma ? 16 * chunk_pos(true, R, 4 * c + jj) + 8 * hh : 2 * (32 * c + 8 * jj + 4 * hh);
+          const u16x4_t x = *(const u16x4_t*)(vr + off);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const uint32_t bit = sees && (x[e] & 0x7F80u) == 0x7F80u ? 1u << (16 * (c & 1) + 4 * jj + e) : 0u;
+            plus_inf[c / 2] |= x[e] == 0xFF80u ? 0u : bit;
+            minus_inf[c / 2] |= x[e] == 0x7F80u ? 0u : bit;
+          }
+        }
+    }
+  };
+  auto put_odd = [&]() __attribute__((always_inline)) {
+    uint32_t any = 0;
+#pragma unroll
+    for (int c = 0; c < S::DT / 2; ++c) any |= plus_inf[c] | minus_inf[c];
+    if (__builtin_amdgcn_ballot_w64(any != 0) == 0) return;
+#pragma unroll
+    for (int c = 0; c < S::DT; ++c)
+#pragma unroll
+      for (int j = 0; j < 16; ++j) {
+        const uint32_t bit = 1u << (16 * (c & 1) + j);
+        acc[0][c][j] += plus_inf[c / 2] & bit ? -neg_inf() : 0.f;
+        acc[0][c][j] += minus_inf[c / 2] & bit ? neg_inf() : 0.f;   // after the other: NaN
+      }
+  };
+
   // Block kb in LDS buffer buf: scores, softmax, P V, for the wave's row tiles.
-  auto compute_block = [&](auto dma, int kb, int buf) {   // dma: the block's layout
-    if (kb * kKeys < Ew) {
+  auto compute_block = [&](auto dma, int kb, int buf) __attribute__((always_inline)) {   // dma: the block's layout
+    if (kb * kKeys < Ew && (!MOD || (kb + 1) * kKeys > Wlo)) {
       // Each K and V operand read serves every row tile of the wave.
       f32x16 sc[kNT][kKH];
-      bf16x8 va[kKH][S::KS];
 #pragma unroll
       for (int kh = 0; kh < kKH; ++kh) {
         bf16x8 ka[S::KS];
@@ -664,8 +798,29 @@ void multi_query_kernel(const Params p) {
       }
 #pragma unroll
       for (int t = 0; t < kNT; ++t) softmax(t, kb, buf, sc[t]);
+      bool any_odd = false;
+      if constexpr (MOD) {
+        // A key that a row does not see has no part in it, whatever its values: an infinity
+        // or NaN of V would turn the product with its zero probability into NaN.
+        if (__builtin_amdgcn_ballot_w64(masked) != 0) {
+          uint32_t odd = 0;
+          constexpr bool kDma = decltype(dma)::value;
+#pragma unroll
+          for (int c = 0; c < D / 8; c += 2)   // two lanes a row
+            odd |= not_finite(*(const u32x4*)(s_v[buf] + (lane >> 1) * S::vrs(kDma) + 16 * (c + (lane & 1))));
+          any_odd = __builtin_amdgcn_ballot_w64(odd != 0) != 0;
+          if (any_odd) note_odd(dma, kb, buf);
+        }
+      }
+      bf16x8 va[kKH][S::KS];
 #pragma unroll
       for (int kh = 0; kh < kKH; ++kh) read_v(dma, va[kh], buf, kh);
+      if constexpr (MOD) {
+        if (any_odd) {
+#pragma unroll
+          for (int s = 0; s < S::KS; ++s) va[0][s] = without_odd(va[0][s]);
+        }
+      }
 #pragma unroll
       for (int kh = 0; kh < kKH; ++kh)
 #pragma unroll
@@ -687,7 +842,7 @@ void multi_query_kernel(const Params p) {
     Staged sk[2], sv[2];
     int ids = 0;
     auto load = [&](int k) {   // the wave's k-th block; past the keys the loads read nothing
-      const int kb = wave + kWaves * k;
+      const int kb = kb0 + wave + kWaves * k;
       if ((k & 31) == 0) ids = bt_vec[min(2 * (kb + kWaves * (lane >> 1)) + (lane & 1), p.max_pages - 1)];
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
@@ -706,7 +861,7 @@ void multi_query_kernel(const Params p) {
       // A wave's LDS operations complete in order; the compiler keeps theirs.
       asm volatile("" ::: "memory");
       load(k + 1);
-      compute_block(std::false_type{}, wave + kWaves * k, wave);
+      compute_block(std::false_type{}, kb0 + wave + kWaves * k, wave);
       asm volatile("" ::: "memory");
     }
     // The waves' states meet in LDS, weighted by their maxima: thread (row, chunk of
@@ -717,6 +872,7 @@ void multi_query_kernel(const Params p) {
     auto part = [&](int w) { return (float*)(w < 2 ? s_k[0] : s_v[0]) + (w & 1) * kTile * RSF; };
     __shared__ float2 s_ml[kWaves][kTile];
     const float lt = pair_sum(l[0]);
+    if constexpr (MOD) put_odd();
     lds_barrier();
     if (wave < nkb) {
 #pragma unroll
@@ -769,22 +925,22 @@ void multi_query_kernel(const Params p) {
     constexpr int kDmaPerBlock = S::LPL * kKH;
     {
       int pid[kKH];
-      page_ids(0, pid);
-      dma_issue(0, 0, pid);
-      page_ids(1, pid);
-      dma_issue(1, 1, pid);
+      page_ids(kb0, pid);
+      dma_issue(kb0, 0, pid);
+      page_ids(kb0 + 1, pid);
+      dma_issue(kb0 + 1, 1, pid);
     }
     int pid_next[kKH];
-    page_ids(2, pid_next);
+    page_ids(kb0 + 2, pid_next);
     dma_barrier<kDmaPerBlock>();
-    for (int kb0 = 0; kb0 < nkb; kb0 += 3) {
+    for (int k3 = 0; k3 < nkb; k3 += 3) {
 #pragma unroll
       for (int u = 0; u < 3; ++u) {
-        const int kb = kb0 + u;
+        const int kb = k3 + u;
         if (kb < nkb) {
-          dma_issue(kb + 2, (u + 2) % 3, pid_next);
-          compute_block(std::true_type{}, kb, u);
-          page_ids(kb + 3, pid_next);
+          dma_issue(kb0 + kb + 2, (u + 2) % 3, pid_next);
+          compute_block(std::true_type{}, kb0 + kb, u);
+          page_ids(kb0 + kb + 3, pid_next);
           dma_barrier<kDmaPerBlock>();
         }
       }
@@ -800,33 +956,34 @@ void multi_query_kernel(const Params p) {
       int pid[kKH];
 #pragma unroll
       for (int u = 0; u < PD; ++u) {
-        page_ids(u, pid);
-        stage_load(u, u, pid);
+        page_ids(kb0 + u, pid);
+        stage_load(kb0 + u, u, pid);
       }
     }
     int pid_next[kKH];
-    page_ids(PD, pid_next);
+    page_ids(kb0 + PD, pid_next);
     stage_write(0, 0);
     __syncthreads();
-    for (int kb0 = 0; kb0 < nkb; kb0 += PD) {
+    for (int kp = 0; kp < nkb; kp += PD) {
 #pragma unroll
       for (int u = 0; u < PD; ++u) {
-        const int kb = kb0 + u;
+        const int kb = kp + u;
         if (kb < nkb) {
           const int buf = kb & 1;
-          stage_load(kb + PD, u, pid_next);
-          compute_block(std::false_type{}, kb, buf);
+          stage_load(kb0 + kb + PD, u, pid_next);
+          compute_block(std::false_type{}, kb0 + kb, buf);
           if (kb + 1 < nkb) stage_write((u + 1) % PD, buf ^ 1);
           // The next page ids are read here: a scalar load shares its completion
           // counter with the LDS reads, so issued earlier it would hold up the
           // first MFMA's operand wait; here the barrier's wait covers it.
-          page_ids(kb + PD + 1, pid_next);
+          page_ids(kb0 + kb + PD + 1, pid_next);
           __syncthreads();
         }
       }
     }
   }
 
+  if constexpr (MOD) put_odd();
   // 4. Normalise and write: lane 32h + i holds O^T[d = 32c + 8jj + 4h + 0..3][its row].
 #pragma unroll
   for (int t = 0; t < kNT; ++t) {
@@ -849,12 +1006,12 @@ void multi_query_kernel(const Params p) {
   }
 }
 
-template <int D, bool FP8, bool SMALL>
+template <int D, bool FP8, bool SMALL, bool MOD = false>
 int launch_multi_t(const Params& p, int grid, void* stream, void* ev_begin, void* ev_end) {
   hipStream_t st = (hipStream_t)stream;
   if (ev_begin && hipEventRecord((hipEvent_t)ev_begin, st) != hipSuccess) return -1;
   const size_t lds = p.batch > 64 ? (sizeof(int2) + sizeof(int32_t)) * (size_t)p.batch : 0;
-  hipLaunchKernelGGL((multi_query_kernel<D, FP8, SMALL>), dim3(grid), dim3(kThreads), lds, st, p);
+  hipLaunchKernelGGL((multi_query_kernel<D, FP8, SMALL, MOD>), dim3(grid), dim3(kThreads), lds, st, p);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return (int)e;
   if (ev_end && hipEventRecord((hipEvent_t)ev_end, st) != hipSuccess) return -1;
@@ -873,6 +1030,21 @@ int launch_multi(KvKind kind, int head_dim, bool small, const Params& p, int gri
                            : (head_dim == 128 ? (small ? launch_multi_t<128, true, S> : launch_multi_t<128, true, false>)
                                               : (small ? launch_multi_t<64, true, S> : launch_multi_t<64, true, false>));
   return launch(p, grid, stream, ev_begin, ev_end);
+}
+
+int launch_scored_multi(KvKind kind, int head_dim, bool small, const Params& p, int grid, void* stream, void* ev_begin,
+                        void* ev_end) {
+  if (kind != KvKind::BF16 && kind != KvKind::FP8) return -1;
+  if constexpr (!kMultiSplits) return -1;   // the tilings that are not built for it
+  else {
+    auto* const launch =
+        kind == KvKind::BF16
+            ? (head_dim == 128 ? (small ? launch_multi_t<128, false, true, true> : launch_multi_t<128, false, false, true>)
+                               : (small ? launch_multi_t<64, false, true, true> : launch_multi_t<64, false, false, true>))
+            : (head_dim == 128 ? (small ? launch_multi_t<128, true, true, true> : launch_multi_t<128, true, false, true>)
+                               : (small ? launch_multi_t<64, true, true, true> : launch_multi_t<64, true, false, true>));
+    return launch(p, grid, stream, ev_begin, ev_end);
+  }
 }
 
 }  // namespace rlda

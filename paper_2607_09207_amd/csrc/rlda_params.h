@@ -91,6 +91,14 @@ struct Params {
   int32_t total_q;
   int32_t max_q_len;           // decode-kernel path: rows per sequence allowed (n_b <= max_q_len)
   int32_t row_chunks;          // decode-kernel path: segments per (sequence, KV head), ceil(max_q_len * G / (16 * tiles))
+  // Modified scores (rl_decode_attn_run_scored).  Scores are in log2 units from the start:
+  // y -> cap_log2 tanh(y / cap_log2), as 1 - 2 / (exp2(cap_arg y) + 1); then y -= slope |pos - t|.
+  float cap_log2;              // cap * log2(e); 0: no cap
+  float cap_arg;               // 2 / cap
+  const float* slopes;         // [Hq] or null
+  int32_t window;              // 0: none
+  const int32_t* key_start;    // [rows] or null
+  const int32_t* prefix_lens;  // [batch] or null
   int16_t q_head[kMaxQHeads];  // q_head[g * G + i] = i-th query head of KV head g
 };
 
@@ -179,6 +187,12 @@ int launch_grouped(KvKind kind, int head_dim, int group, const Params& p, int ng
 // two waves per SIMD; batch <= kTwoWgMaxBatch, nranges twice the CUs): eight waves
 // per CU keep twice the tiles in flight.
 int launch_decode_two(KvKind kind, int head_dim, const Params& p, void* stream, void* ev_begin, void* ev_end);
+// The same with modified scores (bf16 / fp8): one row a sequence, `two` workgroups per CU
+// or one; multi-token rows; the multi-token kernel.
+int launch_scored(KvKind kind, int head_dim, bool two, const Params& p, void* stream, void* ev_begin, void* ev_end);
+int launch_scored_rows(KvKind kind, int head_dim, int tiles, const Params& p, void* stream, void* ev_begin, void* ev_end);
+int launch_scored_multi(KvKind kind, int head_dim, bool small, const Params& p, int grid, void* stream, void* ev_begin,
+                        void* ev_end);
 // KV append: one wave per (sequence, KV head) and cache; one for both where they are one.
 int launch_append(KvKind kind, int head_dim, const Params& p, void* stream);
 // Device address of the static scratch on the current device (kScratchBytes bytes),
@@ -215,6 +229,8 @@ constexpr int kPackMaxBatch = 4096;    // packed grouped runs: per-sequence and 
 constexpr int kPackMaxMembers = 7;     // ... members per pack (3 bits of the page descriptor, 7 = every member)
 constexpr int kPackMaxPages = 32767;   // ... pages per sequence (16-bit LDS entries)
 constexpr int kTwoWgMaxBatch = 512;      // two workgroups per CU (fp8, bf16 d = 64 decode): per-sequence LDS tables of this size
+constexpr int kScoredMaxBatch = 4096;    // multi-token rows with modified scores: one more table
+constexpr int kScoredTwoTileMaxBatch = 1024;   // ... in two tiles
 constexpr int kTwoTileMaxBatch = 2048;   // two-tile multi-token rows: per-sequence LDS tables of this size
                                          // leave room for 32-row merge slots
 
