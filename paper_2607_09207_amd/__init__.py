@@ -84,7 +84,7 @@ class DecodeAttention(CacheOps):
         # The native call path (csrc/fastcall.cpp); it shares the workspaces by device.
         native = _abi.fastcall()
         self._fast = _abi.LEFT_TO_PYTHON if native is None else native.Layer(
-            h.value, self._ws, (num_q_heads, num_kv_heads, head_dim, page_size, max_batch, max_pages_per_seq),
+            h.value, self._ws, self._page_ws, (num_q_heads, num_kv_heads, head_dim, page_size, max_batch, max_pages_per_seq),
             (cfg.q_dtype, cfg.kv_dtype, cfg.out_dtype), self._kv_strides, self.workspace_bytes + 256,
             self.grouped_workspace_bytes + 256)
 
@@ -342,8 +342,13 @@ class DecodeAttention(CacheOps):
         [Hq]) times the distance, and every row seeing the keys from max(key_start[row],
         pos - window + 1) to its own position, or to prefix_lens[b] where that is further
         (int32 device tensors [rows] and [batch]).  Rows that see no key give zeros."""
-        torch = _torch()
         what = "rl_decode_attn_run_scored"
+        if events is None:
+            got = self._fast.scored(q, k_cache, v_cache, block_table, seq_lens, k_scale, v_scale, stream, num_pages, out,
+                                    workspace, q_start, max_q_len, score_cap, slopes, window, key_start, prefix_lens)
+            if got is not None:
+                return self._answer(got, what)
+        torch = _torch()
         cfg = self.config
         if not q.is_cuda:
             self._fail(what, f"q must be on a GPU, got {q.device}")

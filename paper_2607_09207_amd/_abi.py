@@ -134,7 +134,8 @@ class LeftToPython:
     def run(self, *args):
         return None
 
-    grouped = multi = noalloc = append = run
+    grouped = multi = noalloc = append = scored = rotate = append_rotary = run
+    page_grow = page_release = page_fork = page_compact = run
 
 
 LEFT_TO_PYTHON = LeftToPython()
@@ -159,7 +160,8 @@ def fastcall():
         # CPU-only torch builds have no stream lookup; every call is then left to Python.
         raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
         addr = [ctypes.cast(getattr(lib, "rl_decode_attn_" + n), ctypes.c_void_p).value
-                for n in ("run", "run_grouped", "run_multi", "run_noalloc", "append")]
+                for n in ("run", "run_grouped", "run_multi", "run_noalloc", "append", "run_scored", "rotate",
+                          "append_rotary", "page_grow", "page_release", "page_fork", "page_compact")]
         _fastcall.bind(raw, *addr)
         _fast = (lib, _fastcall)
     return _fast[1]

@@ -16,6 +16,8 @@ class CacheSet:
 
     def __init__(self, tensors, array, num_pages, device):
         self.tensors, self.array, self.num_pages, self.device = tensors, array, num_pages, device
+        # As the native call path takes it: number, address, pages, device.
+        self.native = (len(tensors), ctypes.addressof(array), num_pages, None if device is None else device.index)
 
     def __len__(self):
         return len(self.tensors)
@@ -33,8 +35,12 @@ class CacheOps:
         q_start[b+1] - q_start[b] tokens.  positions [n] (int32) replaces the rows' tokens as
         what they are turned by.  q, k_new and v_new may be strided (slices of a fused
         projection); out: a tensor for q (q itself: in place)."""
-        import torch
         what = "rl_decode_attn_append_rotary"
+        got = self._fast.append_rotary(q, k_cache, v_cache, block_table, seq_lens, k_scale, v_scale, stream, num_pages, out,
+                                       workspace, k_new, v_new, freqs, q_start, positions, interleaved, amplitude)
+        if got is not None:
+            return self._answer(got, what)
+        import torch
         fail = lambda msg: self._fail(what, msg)   # noqa: E731
         cfg = self.config
         if not q.is_cuda:
@@ -153,8 +159,11 @@ class CacheOps:
     def page_grow(self, refs, block_table, seq_lens, add=None, *, workspace=None, stream=None):
         """Room for add[b] more tokens of every sequence (None: one each): seq_lens grows, new
         pages are the lowest-numbered ones with refs 0 (rl_decode_attn_page_grow)."""
-        import torch
         what = "rl_decode_attn_page_grow"
+        got = self._fast.page_grow(refs, block_table, seq_lens, add, workspace, stream)
+        if got is not None:
+            return _abi.check(got, what)
+        import torch
         dev, batch, npages, _ = self._page_call(what, refs, block_table, seq_lens, None, workspace, stream)
         if add is not None:
             self._tensor(what, "add", add, torch.int32, (batch,), dev)
@@ -168,6 +177,9 @@ class CacheOps:
         """Rows (int32 list on the device) give up their pages; their lengths become 0
         (rl_decode_attn_page_release)."""
         what = "rl_decode_attn_page_release"
+        got = self._fast.page_release(refs, block_table, seq_lens, rows, workspace, stream)
+        if got is not None:
+            return _abi.check(got, what)
         dev, batch, npages, _ = self._page_call(what, refs, block_table, seq_lens, None, workspace, stream)
         n = self._rows_list(what, "rows", rows, dev)
         with on_device(dev):
@@ -180,6 +192,10 @@ class CacheOps:
         """Empty rows `children` become copies of rows `parents`: full pages shared, the partial
         last page copied in every cache (rl_decode_attn_page_fork)."""
         what = "rl_decode_attn_page_fork"
+        if isinstance(caches, CacheSet):
+            got = self._fast.page_fork(refs, block_table, seq_lens, parents, children, *caches.native, workspace, stream)
+            if got is not None:
+                return _abi.check(got, what)
         dev, batch, npages, cs = self._page_call(what, refs, block_table, seq_lens, caches, workspace, stream)
         n = self._rows_list(what, "parents", parents, dev)
         if self._rows_list(what, "children", children, dev) != n:
@@ -193,8 +209,12 @@ class CacheOps:
     def page_compact(self, refs, block_table, seq_lens, caches=(), *, live=None, workspace=None, stream=None):
         """The live pages move to the front of the pool in every cache; the table and refs
         follow (rl_decode_attn_page_compact).  Returns their number, an int32 tensor of one."""
-        import torch
         what = "rl_decode_attn_page_compact"
+        if isinstance(caches, CacheSet):
+            got = self._fast.page_compact(refs, block_table, seq_lens, *caches.native, live, workspace, stream)
+            if got is not None:
+                return self._answer(got, what)
+        import torch
         dev, batch, npages, cs = self._page_call(what, refs, block_table, seq_lens, caches, workspace, stream)
         with on_device(dev):
             if live is None:

@@ -15,6 +15,7 @@
 
 #include <ATen/TensorSubclassLikeUtils.h>
 #include <ATen/ATen.h>
+#include <c10/core/impl/VirtualGuardImpl.h>
 #include <torch/csrc/autograd/python_variable.h>
 
 #include "rl_decode_attn.h"
@@ -30,6 +31,13 @@ decltype(&rl_decode_attn_run_grouped) g_grouped;
 decltype(&rl_decode_attn_run_multi) g_multi;
 decltype(&rl_decode_attn_run_noalloc) g_noalloc;
 decltype(&rl_decode_attn_append) g_append;
+decltype(&rl_decode_attn_run_scored) g_scored;
+decltype(&rl_decode_attn_rotate) g_rotate;
+decltype(&rl_decode_attn_append_rotary) g_append_rotary;
+decltype(&rl_decode_attn_page_grow) g_page_grow;
+decltype(&rl_decode_attn_page_release) g_page_release;
+decltype(&rl_decode_attn_page_fork) g_page_fork;
+decltype(&rl_decode_attn_page_compact) g_page_compact;
 PyObject* g_raw_stream;   // device index -> current stream (an int)
 
 constexpr int kMaxDevices = 64;
@@ -39,6 +47,7 @@ struct Layer {
   PyObject_HEAD
   rl_decode_attn_t handle;
   PyObject* workspaces;   // dict: device string -> uint8 tensor (the Python object's own)
+  PyObject* page_workspaces;   // dict: (device string, pages) -> uint8 tensor (its own too)
   int64_t hq, hkv, d, page, max_batch, max_pages;
   int64_t stride[3];
   int64_t ws_bytes, grouped_ws_bytes;   // as allocated, alignment room included
@@ -106,6 +115,28 @@ bool as_int(PyObject* o, int64_t none, int64_t* out) {
   return true;
 }
 
+// The stream of an argument: None (the device's current one), a raw handle or an object
+// that holds one.
+bool stream_of(PyObject* o, int dev, void** out) {
+  int64_t s = 0;
+  PyObject* r = nullptr;
+  if (o == Py_None) {
+    PyObject* idx = PyLong_FromLong(dev);
+    r = idx ? PyObject_CallFunctionObjArgs(g_raw_stream, idx, nullptr) : nullptr;
+    Py_XDECREF(idx);
+  } else if (as_int(o, 0, &s)) {
+    *out = (void*)(intptr_t)s;
+    return true;
+  } else {
+    r = PyObject_GetAttrString(o, "cuda_stream");   // a torch.cuda.Stream
+  }
+  const bool ok = r && as_int(r, 0, &s);
+  Py_XDECREF(r);
+  if (!ok) PyErr_Clear();
+  *out = (void*)(intptr_t)s;
+  return ok;
+}
+
 // The arguments common to the methods, in order: k, v, block table, lengths, k scale,
 // v scale, stream, page count; `batch` sequences on device `dev`.
 bool common(const Layer* L, Call& c, PyObject* const* a, int dev, int64_t batch) {
@@ -125,27 +156,17 @@ bool common(const Layer* L, Call& c, PyObject* const* a, int dev, int64_t batch)
   } else if (a[4] != Py_None || a[5] != Py_None) {
     return false;
   }
-  int64_t s = 0;
-  if (a[6] == Py_None) {
-    PyObject* idx = PyLong_FromLong(dev);
-    PyObject* r = idx ? PyObject_CallFunctionObjArgs(g_raw_stream, idx, nullptr) : nullptr;
-    Py_XDECREF(idx);
-    const bool ok = r && as_int(r, 0, &s);
-    Py_XDECREF(r);
-    if (!ok) {
-      PyErr_Clear();
-      return false;
-    }
-  } else if (!as_int(a[6], 0, &s)) {
-    PyObject* r = PyObject_GetAttrString(a[6], "cuda_stream");   // a torch.cuda.Stream
-    const bool ok = r && as_int(r, 0, &s);
-    Py_XDECREF(r);
-    if (!ok) {
-      PyErr_Clear();
-      return false;
-    }
-  }
-  c.stream = (void*)(intptr_t)s;
+  return stream_of(a[6], dev, &c.stream);
+}
+
+bool use_workspace(Call& c, const Tensor* t) {
+  if (!plain(t, c.dev, at::kByte) || !t->is_contiguous()) return false;
+  c.ws = *t;
+  char* p = (char*)t->mutable_data_ptr();
+  c.ws_ptr = (char*)(((uintptr_t)p + 255) / 256 * 256);
+  const int64_t room = t->numel() - (c.ws_ptr - p);
+  if (room < 0) return false;
+  c.ws_room = (size_t)room;
   return true;
 }
 
@@ -160,14 +181,7 @@ bool workspace(const Layer* L, Call& c, PyObject* given, bool grouped) {
     t = o ? tensor(o) : nullptr;
     if (t && t->numel() < (grouped ? L->grouped_ws_bytes : L->ws_bytes)) return false;
   }
-  if (!plain(t, c.dev, at::kByte) || !t->is_contiguous()) return false;
-  c.ws = *t;
-  char* p = (char*)t->mutable_data_ptr();
-  c.ws_ptr = (char*)(((uintptr_t)p + 255) / 256 * 256);
-  const int64_t room = t->numel() - (c.ws_ptr - p);
-  if (room < 0) return false;
-  c.ws_room = (size_t)room;
-  return true;
+  return use_workspace(c, t);
 }
 
 void* ptr(const Tensor* t) { return t ? t->mutable_data_ptr() : nullptr; }
@@ -340,27 +354,319 @@ PyObject* layer_append(PyObject* self, PyObject* const* a, Py_ssize_t n) {
   });
 }
 
+// ------------------------------------------------------------------ modified scores, rotary positions, pages
+
+// The new calls launch on the current device: one on another is left to Python, which
+// makes it the current one.
+bool current(int dev) { return c10::impl::VirtualGuardImpl(c10::DeviceType::CUDA).getDevice().index() == dev; }
+
+bool as_double(PyObject* o, double* out) {
+  if (PyFloat_CheckExact(o)) {
+    *out = PyFloat_AS_DOUBLE(o);
+    return true;
+  }
+  int64_t i = 0;
+  if (o == Py_None || !as_int(o, 0, &i)) return false;
+  *out = (double)i;
+  return true;
+}
+bool as_bool(PyObject* o, int* out) {
+  *out = o == Py_True;
+  return o == Py_True || o == Py_False;
+}
+// A vector argument of n elements, or None (null).
+bool vector_or_none(PyObject* o, int dev, at::ScalarType type, int64_t n, const Tensor** out) {
+  *out = nullptr;
+  return o == Py_None || shaped(*out = tensor(o), dev, type, {n});
+}
+
+// Rows [n][heads][d] as the C ABI takes them.
+bool rows_of(const Tensor* t, int dev, at::ScalarType type, int64_t n, int64_t heads, int64_t d, rl_decode_attn_rows* out) {
+  if (!plain(t, dev, type) || t->dim() != 3) return false;
+  const auto sz = t->sizes(), st = t->strides();
+  if (sz[0] != n || sz[1] != heads || sz[2] != d || (d > 1 && st[2] != 1)) return false;
+  const int64_t per = 16 / (int64_t)t->element_size();
+  void* p = t->mutable_data_ptr();
+  if (((uintptr_t)p & 15) || (n > 1 && st[0] % per) || (heads > 1 && st[1] % per)) return false;
+  *out = {p, st[0], st[1]};
+  return true;
+}
+
+bool rotary_of(PyObject* freqs, PyObject* interleaved, PyObject* amplitude, int inverse, int dev, int64_t d,
+               rl_decode_attn_rotary* out) {
+  const Tensor* f = tensor(freqs);
+  int il = 0;
+  double a = 1.0;
+  if (!plain(f, dev, at::kDouble) || f->dim() != 1 || !f->is_contiguous() || !as_bool(interleaved, &il) || !as_double(amplitude, &a))
+    return false;
+  const int64_t half = f->size(0);
+  if (half < 8 || 2 * half > d || half % 8) return false;
+  *out = {(const double*)f->mutable_data_ptr(), (int32_t)(2 * half), il, (float)a, inverse};
+  return true;
+}
+
+// scored(q, k, v, block_table, seq_lens, k_scale, v_scale, stream, num_pages, out, workspace,
+//        q_start, max_q_len, score_cap, slopes, window, key_start, prefix_lens)
+PyObject* layer_scored(PyObject* self, PyObject* const* a, Py_ssize_t n) {
+  if (n != 18) return PyErr_Format(PyExc_TypeError, "scored takes 18 arguments");
+  const Layer* L = (const Layer*)self;
+  return guarded([&]() -> PyObject* {
+    const Tensor* q = tensor(a[0]);
+    if (!q || !q->is_cuda() || q->dim() != 3 || (a[9] == Py_None && a[7] != Py_None)) return nullptr;
+    const int dev = q->get_device();
+    const int64_t total = q->size(0);
+    const Tensor *qs = nullptr, *slopes, *ks, *pl;
+    int64_t B = total, mq = 0, window = 0;
+    double cap = 0.0;
+    if (a[11] != Py_None) {
+      qs = tensor(a[11]);
+      if (!qs || qs->dim() != 1) return nullptr;
+      B = qs->size(0) - 1;
+      if (!shaped(qs, dev, at::kInt, {B + 1})) return nullptr;
+    }
+    if (total > INT32_MAX || a[12] == Py_None || !as_int(a[12], 0, &mq) || mq < INT32_MIN || mq > INT32_MAX ||
+        !as_double(a[13], &cap) || a[15] == Py_None || !as_int(a[15], 0, &window) || window < INT32_MIN || window > INT32_MAX)
+      return nullptr;
+    Call c;
+    if (!shaped(q, dev, L->q_dtype, {total, L->hq, L->d}) || !vector_or_none(a[14], dev, at::kFloat, L->hq, &slopes) ||
+        !vector_or_none(a[16], dev, at::kInt, total, &ks) || !common(L, c, a + 1, dev, B) ||
+        !vector_or_none(a[17], dev, at::kInt, B, &pl) || !workspace(L, c, a[10], false) || !current(dev))
+      return nullptr;
+    Tensor fresh;
+    const Tensor* o = output(L, a[9], *q, total, fresh);
+    if (!o) return nullptr;
+    const rl_decode_attn_scores sc = {(float)cap, (int32_t)window, (const float*)ptr(slopes), (const int32_t*)ptr(ks),
+                                      (const int32_t*)ptr(pl)};
+    void *qp = ptr(q), *kp = ptr(c.k), *vp = ptr(c.v), *ksp = ptr(c.ks), *vsp = ptr(c.vs), *bp = ptr(c.bt),
+         *lp = ptr(c.lens), *op = ptr(o), *qsp = ptr(qs);
+    WITHOUT_GIL(g_scored(L->handle, &sc, (int32_t)B, (int32_t)c.npages, (int32_t)total, (int32_t)mq, qp, kp, vp,
+                         (const float*)ksp, (const float*)vsp, (const int32_t*)bp, (const int32_t*)lp, (const int32_t*)qsp,
+                         op, c.ws_ptr, c.ws_room, c.stream, nullptr, nullptr));
+    return answer(st, a[9], fresh);
+  });
+}
+
+// append_rotary(q, k, v, block_table, seq_lens, k_scale, v_scale, stream, num_pages, out, workspace,
+//               k_new, v_new, freqs, q_start, positions, interleaved, amplitude)
+PyObject* layer_append_rotary(PyObject* self, PyObject* const* a, Py_ssize_t n) {
+  if (n != 18) return PyErr_Format(PyExc_TypeError, "append_rotary takes 18 arguments");
+  const Layer* L = (const Layer*)self;
+  return guarded([&]() -> PyObject* {
+    const Tensor* q = tensor(a[0]);
+    if (!q || !q->is_cuda() || q->dim() != 3 || (a[9] == Py_None && a[7] != Py_None)) return nullptr;
+    const int dev = q->get_device();
+    const int64_t total = q->size(0);
+    const Tensor *qs = nullptr, *pos;
+    int64_t B = total;
+    if (a[14] != Py_None) {
+      qs = tensor(a[14]);
+      if (!qs || qs->dim() != 1) return nullptr;
+      B = qs->size(0) - 1;
+      if (!shaped(qs, dev, at::kInt, {B + 1})) return nullptr;
+    }
+    Call c;
+    rl_decode_attn_rows rq, rk, rv, ro;
+    rl_decode_attn_rotary rot;
+    if (total > INT32_MAX || !rows_of(q, dev, L->q_dtype, total, L->hq, L->d, &rq) ||
+        !rows_of(tensor(a[11]), dev, L->q_dtype, total, L->hkv, L->d, &rk) ||
+        !rows_of(tensor(a[12]), dev, L->q_dtype, total, L->hkv, L->d, &rv) ||
+        !rotary_of(a[13], a[16], a[17], 0, dev, L->d, &rot) || !vector_or_none(a[15], dev, at::kInt, total, &pos) ||
+        !common(L, c, a + 1, dev, B) || !workspace(L, c, a[10], false) || !current(dev))
+      return nullptr;
+    Tensor fresh;
+    if (a[9] == Py_None) fresh = at::empty({total, L->hq, L->d}, q->options());
+    if (!rows_of(a[9] == Py_None ? &fresh : tensor(a[9]), dev, L->q_dtype, total, L->hq, L->d, &ro)) return nullptr;
+    void *kp = ptr(c.k), *vp = ptr(c.v), *ksp = ptr(c.ks), *vsp = ptr(c.vs), *bp = ptr(c.bt), *lp = ptr(c.lens),
+         *qsp = ptr(qs), *pp = ptr(pos);
+    WITHOUT_GIL(g_append_rotary(L->handle, (int32_t)B, (int32_t)c.npages, (int32_t)total, &rot, &rq, &rk, &rv,
+                                (const int32_t*)qsp, (const int32_t*)pp, kp, vp, (float*)ksp, (float*)vsp,
+                                (const int32_t*)bp, (const int32_t*)lp, &ro, c.ws_ptr, c.ws_room, c.stream));
+    return answer(st, a[9], fresh);
+  });
+}
+
+// rotate(x, positions, freqs, interleaved, amplitude, inverse, out, stream)
+PyObject* rotate(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  if (n != 8) return PyErr_Format(PyExc_TypeError, "rotate takes 8 arguments");
+  return guarded([&]() -> PyObject* {
+    const Tensor* x = tensor(a[0]);
+    if (!x || !x->is_cuda() || x->dim() != 3 || (a[6] == Py_None && a[7] != Py_None)) return nullptr;
+    const auto type = x->scalar_type();
+    if (type != at::kBFloat16 && type != at::kFloat) return nullptr;
+    if (x->requires_grad() && at::GradMode::is_enabled()) return nullptr;   // Python notes it for the backward pass
+    const int dev = x->get_device();
+    const int64_t rows = x->size(0), heads = x->size(1), d = x->size(2);
+    int inverse = 0;
+    rl_decode_attn_rows rx, ro;
+    rl_decode_attn_rotary rot;
+    void* stream = nullptr;
+    const Tensor* pos = tensor(a[1]);
+    if (rows > INT32_MAX || heads > INT32_MAX || d > INT32_MAX || !as_bool(a[5], &inverse) ||
+        !rows_of(x, dev, type, rows, heads, d, &rx) || !shaped(pos, dev, at::kInt, {rows}) ||
+        !rotary_of(a[2], a[3], a[4], inverse, dev, d, &rot) || !stream_of(a[7], dev, &stream) || !current(dev))
+      return nullptr;
+    Tensor fresh;
+    if (a[6] == Py_None) fresh = at::empty({rows, heads, d}, x->options());
+    if (!rows_of(a[6] == Py_None ? &fresh : tensor(a[6]), dev, type, rows, heads, d, &ro)) return nullptr;
+    const int32_t* pp = (const int32_t*)ptr(pos);
+    WITHOUT_GIL(g_rotate(type == at::kFloat ? RLDA_F32 : RLDA_BF16, (int32_t)rows, (int32_t)heads, (int32_t)d, &rx, pp, &rot,
+                         &ro, stream));
+    return answer(st, a[6], fresh);
+  });
+}
+
+// What the page operations share: (refs, block_table, seq_lens), workspace, stream.
+bool page_common(const Layer* L, Call& c, PyObject* const* a, PyObject* ws, PyObject* stream, const Tensor** refs, int64_t* batch) {
+  const Tensor* r = tensor(a[0]);
+  if (!r || !r->is_cuda() || r->dim() != 1) return false;
+  c.dev = r->get_device();
+  c.npages = r->size(0);
+  c.bt = tensor(a[1]);
+  c.lens = tensor(a[2]);
+  if (!c.lens || c.lens->dim() != 1) return false;
+  *batch = c.lens->size(0);
+  if (c.npages > INT32_MAX || *batch > L->max_batch || !shaped(r, c.dev, at::kInt, {c.npages}) ||
+      !shaped(c.bt, c.dev, at::kInt, {*batch, L->max_pages}) || !shaped(c.lens, c.dev, at::kInt, {*batch}))
+    return false;
+  *refs = r;
+  const Tensor* t = nullptr;
+  if (ws != Py_None) {
+    t = tensor(ws);
+  } else {
+    if (c.dev >= kMaxDevices) return false;
+    PyObject* pages = PyLong_FromLongLong(c.npages);
+    PyObject* key = pages ? PyTuple_Pack(2, g_device_key[c.dev], pages) : nullptr;
+    PyObject* o = key ? PyDict_GetItem(L->page_workspaces, key) : nullptr;   // borrowed
+    Py_XDECREF(key);
+    Py_XDECREF(pages);
+    t = o ? tensor(o) : nullptr;
+  }
+  return use_workspace(c, t) && stream_of(stream, c.dev, &c.stream) && current(c.dev);
+}
+
+PyObject* status(rlda_status st) { return PyLong_FromLong((long)st); }
+
+// The caches of a set: their number, the address of the C array, pages, device.
+bool caches_of(PyObject* const* a, const Call& c, int32_t* n, const rl_decode_attn_cache** array) {
+  int64_t num = 0, addr = 0, pages = 0, dev = 0;
+  if (a[0] == Py_None || !as_int(a[0], 0, &num) || num < 0 || num > INT32_MAX) return false;
+  *n = (int32_t)num;
+  if (num == 0) return true;
+  if (!as_int(a[1], 0, &addr) || addr == 0 || !as_int(a[2], -1, &pages) || !as_int(a[3], -1, &dev) || pages < c.npages || dev != c.dev)
+    return false;
+  *array = (const rl_decode_attn_cache*)(intptr_t)addr;
+  return true;
+}
+
+// page_grow(refs, block_table, seq_lens, add, workspace, stream): the status, or None (not taken).
+PyObject* layer_page_grow(PyObject* self, PyObject* const* a, Py_ssize_t n) {
+  if (n != 6) return PyErr_Format(PyExc_TypeError, "page_grow takes 6 arguments");
+  const Layer* L = (const Layer*)self;
+  return guarded([&]() -> PyObject* {
+    Call c;
+    const Tensor *refs, *add;
+    int64_t B;
+    if (!page_common(L, c, a, a[4], a[5], &refs, &B) || !vector_or_none(a[3], c.dev, at::kInt, B, &add)) return nullptr;
+    void *rp = ptr(refs), *bp = ptr(c.bt), *lp = ptr(c.lens), *ap = ptr(add);
+    WITHOUT_GIL(g_page_grow(L->handle, (int32_t)B, (int32_t)c.npages, (int32_t*)rp, (int32_t*)bp, (int32_t*)lp,
+                            (const int32_t*)ap, c.ws_ptr, c.ws_room, c.stream));
+    return status(st);
+  });
+}
+
+// page_release(refs, block_table, seq_lens, rows, workspace, stream)
+PyObject* layer_page_release(PyObject* self, PyObject* const* a, Py_ssize_t n) {
+  if (n != 6) return PyErr_Format(PyExc_TypeError, "page_release takes 6 arguments");
+  const Layer* L = (const Layer*)self;
+  return guarded([&]() -> PyObject* {
+    Call c;
+    const Tensor *refs, *rows = tensor(a[3]);
+    int64_t B;
+    if (!rows || rows->dim() != 1 || rows->size(0) > INT32_MAX || !page_common(L, c, a, a[4], a[5], &refs, &B) ||
+        !shaped(rows, c.dev, at::kInt, {rows->size(0)}))
+      return nullptr;
+    const int32_t count = (int32_t)rows->size(0);
+    void *rp = ptr(refs), *bp = ptr(c.bt), *lp = ptr(c.lens), *wp = ptr(rows);
+    WITHOUT_GIL(g_page_release(L->handle, (int32_t)B, (int32_t)c.npages, (int32_t*)rp, (int32_t*)bp, (int32_t*)lp, count,
+                               (const int32_t*)wp, c.ws_ptr, c.ws_room, c.stream));
+    return status(st);
+  });
+}
+
+// page_fork(refs, block_table, seq_lens, parents, children, caches: number, address, pages, device, workspace, stream)
+PyObject* layer_page_fork(PyObject* self, PyObject* const* a, Py_ssize_t n) {
+  if (n != 11) return PyErr_Format(PyExc_TypeError, "page_fork takes 11 arguments");
+  const Layer* L = (const Layer*)self;
+  return guarded([&]() -> PyObject* {
+    Call c;
+    const Tensor *refs, *par = tensor(a[3]), *kid = tensor(a[4]);
+    int64_t B;
+    int32_t nc = 0;
+    const rl_decode_attn_cache* caches = nullptr;
+    if (!par || par->dim() != 1 || par->size(0) > INT32_MAX || !page_common(L, c, a, a[9], a[10], &refs, &B) ||
+        !shaped(par, c.dev, at::kInt, {par->size(0)}) || !shaped(kid, c.dev, at::kInt, {par->size(0)}) ||
+        !caches_of(a + 5, c, &nc, &caches))
+      return nullptr;
+    const int32_t count = (int32_t)par->size(0);
+    void *rp = ptr(refs), *bp = ptr(c.bt), *lp = ptr(c.lens), *pp = ptr(par), *kp = ptr(kid);
+    WITHOUT_GIL(g_page_fork(L->handle, (int32_t)B, (int32_t)c.npages, (int32_t*)rp, (int32_t*)bp, (int32_t*)lp, count,
+                            (const int32_t*)pp, (const int32_t*)kp, nc, caches, c.ws_ptr, c.ws_room, c.stream));
+    return status(st);
+  });
+}
+
+// page_compact(refs, block_table, seq_lens, caches: number, address, pages, device, live, workspace, stream):
+// the live tensor, a status, or None
+PyObject* layer_page_compact(PyObject* self, PyObject* const* a, Py_ssize_t n) {
+  if (n != 10) return PyErr_Format(PyExc_TypeError, "page_compact takes 10 arguments");
+  const Layer* L = (const Layer*)self;
+  return guarded([&]() -> PyObject* {
+    Call c;
+    const Tensor* refs;
+    int64_t B;
+    int32_t nc = 0;
+    const rl_decode_attn_cache* caches = nullptr;
+    if ((a[7] == Py_None && a[9] != Py_None) || !page_common(L, c, a, a[8], a[9], &refs, &B) || !caches_of(a + 3, c, &nc, &caches))
+      return nullptr;
+    Tensor fresh;
+    if (a[7] == Py_None) fresh = at::empty({1}, refs->options());
+    const Tensor* live = a[7] == Py_None ? &fresh : tensor(a[7]);
+    if (!shaped(live, c.dev, at::kInt, {1})) return nullptr;
+    void *rp = ptr(refs), *bp = ptr(c.bt), *lp = ptr(c.lens), *vp = ptr(live);
+    WITHOUT_GIL(g_page_compact(L->handle, (int32_t)B, (int32_t)c.npages, (int32_t*)rp, (int32_t*)bp, (int32_t*)lp, nc, caches,
+                               (int32_t*)vp, c.ws_ptr, c.ws_room, c.stream));
+    return answer(st, a[7], fresh);
+  });
+}
+
 PyMethodDef layer_methods[] = {
     {"run", (PyCFunction)(void*)layer_run, METH_FASTCALL, nullptr},
     {"grouped", (PyCFunction)(void*)layer_grouped, METH_FASTCALL, nullptr},
     {"multi", (PyCFunction)(void*)layer_multi, METH_FASTCALL, nullptr},
     {"noalloc", (PyCFunction)(void*)layer_noalloc, METH_FASTCALL, nullptr},
     {"append", (PyCFunction)(void*)layer_append, METH_FASTCALL, nullptr},
+    {"scored", (PyCFunction)(void*)layer_scored, METH_FASTCALL, nullptr},
+    {"append_rotary", (PyCFunction)(void*)layer_append_rotary, METH_FASTCALL, nullptr},
+    {"page_grow", (PyCFunction)(void*)layer_page_grow, METH_FASTCALL, nullptr},
+    {"page_release", (PyCFunction)(void*)layer_page_release, METH_FASTCALL, nullptr},
+    {"page_fork", (PyCFunction)(void*)layer_page_fork, METH_FASTCALL, nullptr},
+    {"page_compact", (PyCFunction)(void*)layer_page_compact, METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 
 void layer_dealloc(PyObject* self) {
   Py_XDECREF(((Layer*)self)->workspaces);
+  Py_XDECREF(((Layer*)self)->page_workspaces);
   Py_TYPE(self)->tp_free(self);
 }
 
-// Layer(handle, workspaces, (Hq, Hkv, d, page, max_batch, max_pages), (q, kv, out dtype codes),
+// Layer(handle, workspaces, page workspaces, (Hq, Hkv, d, page, max_batch, max_pages), (q, kv, out dtype codes),
 //       (page, head, slot strides), workspace bytes, grouped workspace bytes)
 PyObject* layer_new(PyTypeObject* type, PyObject* args, PyObject*) {
   unsigned long long handle = 0;
-  PyObject* dict = nullptr;
+  PyObject *dict = nullptr, *pages = nullptr;
   long long v[6], s[3], ws = 0, gws = 0;
   int q = 0, kv = 0, out = 0;
-  if (!PyArg_ParseTuple(args, "KO!(LLLLLL)(iii)(LLL)LL", &handle, &PyDict_Type, &dict, &v[0], &v[1], &v[2], &v[3], &v[4],
+  if (!PyArg_ParseTuple(args, "KO!O!(LLLLLL)(iii)(LLL)LL", &handle, &PyDict_Type, &dict, &PyDict_Type, &pages, &v[0], &v[1], &v[2], &v[3], &v[4],
                         &v[5], &q, &kv, &out, &s[0], &s[1], &s[2], &ws, &gws))
     return nullptr;
   Layer* L = (Layer*)type->tp_alloc(type, 0);
@@ -368,6 +674,8 @@ PyObject* layer_new(PyTypeObject* type, PyObject* args, PyObject*) {
   L->handle = (rl_decode_attn_t)(uintptr_t)handle;
   Py_INCREF(dict);
   L->workspaces = dict;
+  Py_INCREF(pages);
+  L->page_workspaces = pages;
   L->hq = v[0], L->hkv = v[1], L->d = v[2], L->page = v[3], L->max_batch = v[4], L->max_pages = v[5];
   for (int i = 0; i < 3; ++i) L->stride[i] = s[i];
   L->ws_bytes = ws;
@@ -381,12 +689,15 @@ PyObject* layer_new(PyTypeObject* type, PyObject* args, PyObject*) {
 
 PyTypeObject layer_type = {PyVarObject_HEAD_INIT(nullptr, 0)};
 
-// bind(raw_stream, run, grouped, multi, noalloc, append): the stream lookup and the
-// addresses of the loaded library's entry points.
+// bind(raw_stream, run, grouped, multi, noalloc, append, scored, rotate, append_rotary, page_grow,
+// page_release, page_fork, page_compact): the stream lookup and the addresses of the loaded
+// library's entry points.
 PyObject* bind(PyObject*, PyObject* args) {
   PyObject* raw = nullptr;
-  unsigned long long f[5];
-  if (!PyArg_ParseTuple(args, "OKKKKK", &raw, &f[0], &f[1], &f[2], &f[3], &f[4])) return nullptr;
+  unsigned long long f[12];
+  if (!PyArg_ParseTuple(args, "OKKKKKKKKKKKK", &raw, &f[0], &f[1], &f[2], &f[3], &f[4], &f[5], &f[6], &f[7], &f[8], &f[9],
+                        &f[10], &f[11]))
+    return nullptr;
   Py_INCREF(raw);
   Py_XDECREF(g_raw_stream);
   g_raw_stream = raw;
@@ -395,10 +706,19 @@ PyObject* bind(PyObject*, PyObject* args) {
   g_multi = (decltype(g_multi))(uintptr_t)f[2];
   g_noalloc = (decltype(g_noalloc))(uintptr_t)f[3];
   g_append = (decltype(g_append))(uintptr_t)f[4];
+  g_scored = (decltype(g_scored))(uintptr_t)f[5];
+  g_rotate = (decltype(g_rotate))(uintptr_t)f[6];
+  g_append_rotary = (decltype(g_append_rotary))(uintptr_t)f[7];
+  g_page_grow = (decltype(g_page_grow))(uintptr_t)f[8];
+  g_page_release = (decltype(g_page_release))(uintptr_t)f[9];
+  g_page_fork = (decltype(g_page_fork))(uintptr_t)f[10];
+  g_page_compact = (decltype(g_page_compact))(uintptr_t)f[11];
   Py_RETURN_NONE;
 }
 
-PyMethodDef module_methods[] = {{"bind", bind, METH_VARARGS, nullptr}, {nullptr, nullptr, 0, nullptr}};
+PyMethodDef module_methods[] = {{"bind", bind, METH_VARARGS, nullptr},
+                                {"rotate", (PyCFunction)(void*)rotate, METH_FASTCALL, nullptr},
+                                {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module_def = {PyModuleDef_HEAD_INIT, "_fastcall", nullptr, -1, module_methods};
 
 }  // namespace

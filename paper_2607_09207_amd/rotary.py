@@ -117,15 +117,51 @@ def used_on(t, device, stream):
         t.record_stream(stream if hasattr(stream, "cuda_stream") else torch.cuda.ExternalStream(stream, device=device))
 
 
+_turn = None
+
+
+def _function():
+    """The rotation for autograd: its backward is the rotation by the transpose."""
+    global _turn
+    if _turn is None:
+        import torch
+
+        class Turn(torch.autograd.Function):
+            @staticmethod
+            def forward(ctx, x, positions, freqs, interleaved, amplitude, inverse):
+                ctx.save_for_backward(positions, freqs)
+                ctx.how = interleaved, amplitude, inverse
+                return rotate(x, positions, freqs, interleaved=interleaved, amplitude=amplitude, inverse=inverse)
+
+            @staticmethod
+            def backward(ctx, grad):
+                positions, freqs = ctx.saved_tensors
+                interleaved, amplitude, inverse = ctx.how
+                # (A gradient may come broadcast or in any layout.)
+                return rotate(grad.contiguous(), positions, freqs, interleaved=interleaved, amplitude=amplitude,
+                              inverse=not inverse), None, None, None, None, None
+
+        _turn = Turn
+    return _turn
+
+
 def rotate(x, positions, freqs, *, interleaved: bool = False, amplitude: float = 1.0, inverse: bool = False, out=None,
            stream=None):
     """Rows x [n][heads][head_dim] (bf16 or fp32; any row and head strides that keep rows
     16-byte aligned, e.g. a slice of a fused projection) turned by positions [n] (int32), pair j
     by positions * freqs[j] radians (rl_decode_attn_rotate).  freqs: float64 [rot_dim / 2]
-    (rotary_frequencies); elements past rot_dim pass.  inverse=True takes the gradient of
-    the result back to x.  Returns `out` (x itself for in place), or a new tensor."""
-    import torch
+    (rotary_frequencies); elements past rot_dim pass.  inverse=True turns by the transpose:
+    what takes a gradient back (an x that requires grad has it done by autograd; `out` is
+    refused then).  Returns `out` (x itself for in place), or a new tensor."""
     what = "rl_decode_attn_rotate"
+    native = _abi.fastcall()
+    if native is not None:
+        got = native.rotate(x, positions, freqs, interleaved, amplitude, inverse, out, stream)
+        if got is not None:
+            if type(got) is int:
+                _abi.check(got, what)
+            return got
+    import torch
 
     def fail(msg):
         raise _abi.RldaError(-1, f"{what}: {msg}")
@@ -134,6 +170,10 @@ def rotate(x, positions, freqs, *, interleaved: bool = False, amplitude: float =
         fail(f"x must be on a GPU, got {x.device}")
     if x.dtype not in (torch.bfloat16, torch.float32):
         fail(f"x must be bfloat16 or float32, got {x.dtype}")
+    if x.requires_grad and torch.is_grad_enabled():
+        if out is not None or stream is not None:
+            fail("an x that requires grad is turned into a new tensor, on the current stream")
+        return _function().apply(x, positions, freqs, interleaved, amplitude, inverse)
     dev = x.device
     shape = tuple(x.shape)
     check_rows(fail, "x", x, x.dtype, shape, dev)

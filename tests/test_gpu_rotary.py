@@ -143,6 +143,35 @@ def test_inverse_is_the_gradient(torch, interleaved):
         assert (diff - grad[..., i].double()).abs().max() <= room
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_autograd(torch, dtype):
+    """x.grad is the inverse rotation of the gradient, through a slice, a broadcast, and twice."""
+    from paper_2607_09207_amd import RldaError, rotary_frequencies, rotate
+    dt = torch.bfloat16 if dtype == "bf16" else torch.float32
+    freqs, _ = rotary_frequencies(64)
+    fused = torch.randn((50, 6, 128), device="cuda").to(dt).requires_grad_()
+    pos = torch.randint(0, 3000, (50,), device="cuda", dtype=torch.int32)
+    w = torch.randn((50, 4, 128), device="cuda").to(dt)
+    y = rotate(fused[:, 1:5], pos, freqs, amplitude=1.25)
+    assert torch.equal(y.detach(), rotate(fused.detach()[:, 1:5], pos, freqs, amplitude=1.25))
+    (g,) = torch.autograd.grad(y, fused, w, retain_graph=True)
+    assert torch.equal(g[:, 1:5], rotate(w, pos, freqs, amplitude=1.25, inverse=True)) and not g[:, 0].any() and not g[:, 5].any()
+    (g,) = torch.autograd.grad(y.sum(), fused)   # a broadcast gradient
+    assert torch.equal(g[:, 1:5], rotate(torch.ones_like(w), pos, freqs, amplitude=1.25, inverse=True))
+    one = torch.randn((1, 1, 128), device="cuda").to(dt).requires_grad_()
+    rotate(one.expand(50, 4, 128), pos, freqs).backward(w)
+    want = rotate(w, pos, freqs, inverse=True)
+    assert torch.equal(one.grad, want.sum((0, 1), keepdim=True, dtype=want.dtype))
+    v = w.clone().requires_grad_()
+    (g,) = torch.autograd.grad(rotate(fused[:, 1:5], pos, freqs), fused, v, create_graph=True)
+    (g2,) = torch.autograd.grad((g[:, 1:5] * w).sum(), v)
+    assert torch.equal(g2, rotate(w, pos, freqs))
+    with pytest.raises(RldaError):
+        rotate(fused[:, 1:5], pos, freqs, out=w)
+    with torch.no_grad():
+        assert not rotate(fused[:, 1:5], pos, freqs).requires_grad
+
+
 # ------------------------------------------------------------------ rows into the cache
 
 KV = {"f32": ("f32", 4), "bf16": ("bf16", 2), "fp8": ("fp8_e4m3fn", 1)}
