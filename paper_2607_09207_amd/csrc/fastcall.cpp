@@ -15,6 +15,7 @@
 
 #include <ATen/TensorSubclassLikeUtils.h>
 #include <ATen/ATen.h>
+#include <c10/core/GradMode.h>
 #include <c10/core/impl/VirtualGuardImpl.h>
 #include <torch/csrc/autograd/python_variable.h>
 
@@ -493,7 +494,7 @@ PyObject* rotate(PyObject*, PyObject* const* a, Py_ssize_t n) {
     if (!x || !x->is_cuda() || x->dim() != 3 || (a[6] == Py_None && a[7] != Py_None)) return nullptr;
     const auto type = x->scalar_type();
     if (type != at::kBFloat16 && type != at::kFloat) return nullptr;
-    if (x->requires_grad() && at::GradMode::is_enabled()) return nullptr;   // Python notes it for the backward pass
+    if (x->requires_grad() && c10::GradMode::is_enabled()) return nullptr;   // Python notes it for the backward pass
     const int dev = x->get_device();
     const int64_t rows = x->size(0), heads = x->size(1), d = x->size(2);
     int inverse = 0;
