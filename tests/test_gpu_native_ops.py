@@ -100,6 +100,6 @@ def test_pages(torch):
         s.layer.page_grow(*s.args())
         s.layer.page_release(*s.args(), s.cuda([5, 0]))
         live = s.layer.page_compact(*s.args(), s.caches)
-        runs.append([x.clone() for x in s.args()] + [live] + [t for one in s.tensors for t in one])
+        runs.append([x.clone() for x in s.args()] + [live] + [t.view(torch.int16) for one in s.tensors for t in one])
         assert not native or w.taken == w.asked == 5
     assert all(torch.equal(a, b) for a, b in zip(*runs))
