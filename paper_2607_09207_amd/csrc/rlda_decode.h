@@ -466,11 +466,23 @@ struct Mfma {
     for (int s = 0; s < KS; ++s) sc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k_operand(f, s), q.v[s], sc, 0, 0, 0);
     float sv[4], mx = neg_inf();
     bool seen[4], masked = false;
+    if (p.cap_log2 > 0.f) {
+      const float arg = kmul * p.cap_arg;
+      if (wide_cap(p.cap_log2)) {
+#pragma unroll
+        for (int r = 0; r < 4; ++r) sv[r] = cap_score_wide(sc[r], kmul, arg, p.cap_log2);
+      } else {
+#pragma unroll
+        for (int r = 0; r < 4; ++r) sv[r] = cap_score(sc[r], arg, p.cap_log2);
+      }
+    } else {
+#pragma unroll
+      for (int r = 0; r < 4; ++r) sv[r] = sc[r] * kmul;
+    }
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
       const int t = 4 * qg + r;
-      float y = sc[r] * kmul;
-      if (p.cap_log2 > 0.f) y = cap_score(y, p.cap_log2, p.cap_arg);
+      float y = sv[r];
       if (p.slopes) y = __builtin_fmaf(-slope, __builtin_fabsf((float)(rpos - t)), y);
       seen[r] = there && t >= rlo && t < rhi;
       masked = masked || !seen[r];
@@ -498,10 +510,10 @@ struct Mfma {
     }
     VOp v = vo ? *vo : v_operand(f);
     if (__builtin_amdgcn_ballot_w64(masked) != 0) {
-      uint32_t odd = 0;
+      u16x2 top = {0, 0};
 #pragma unroll
-      for (int t = 0; t < DT; ++t) odd |= not_finite(v.a[t]);
-      if (__builtin_amdgcn_ballot_w64(odd != 0) != 0) add_not_finite(v, seen);
+      for (int t = 0; t < DT; ++t) top = magnitude_max(top, __builtin_bit_cast(u32x2, v.a[t]));
+      if (__builtin_amdgcn_ballot_w64(not_finite(top)) != 0) add_not_finite(v, seen);
     }
     const u32x2 hi = {pack_bf16(pr[0] * vmul, pr[1] * vmul), pack_bf16(pr[2] * vmul, pr[3] * vmul)};
     const u32x2 lo = remainders(pr, vmul);
@@ -512,16 +524,6 @@ struct Mfma {
       acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, u32x4{a[0], a[1], b[0], b[1]}), pq,
                                                        acc[t], 0, 0, 0);
     }
-  }
-
-  // Non-zero where one of four bf16 values is an infinity or NaN (their exponent bits are all set).
-  __device__ __forceinline__ static uint32_t not_finite(s16x4 v) {
-    const u32x2 w = __builtin_bit_cast(u32x2, v);
-    uint32_t r = 0;
-#pragma unroll
-    for (int i = 0; i < 2; ++i)
-      r |= (uint32_t)((w[i] & 0x7F80u) == 0x7F80u) | (uint32_t)((w[i] & 0x7F800000u) == 0x7F800000u);
-    return r;
   }
 
   // Add the infinities and NaN of V to the rows that see their keys, and take them out of v:

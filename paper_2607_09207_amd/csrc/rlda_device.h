@@ -100,19 +100,33 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
   return __builtin_bit_cast(uint32_t, v);
 }
 
-// tanh of a score, y -> cap tanh(y / cap) in log2 units (cap_log2 = cap log2(e), cap_arg =
-// 2 / cap): 1 - 2 / (e^(2 y / cap) + 1), exact at both ends.  Its error is 2^-23 of the cap,
-// 8e-6 in a score at a cap of 64.  Wider caps take the odd series where |y| is below a
-// sixteenth of the cap (the next term is 2e-9 of the result): their error stays 2^-20 of the score.
-__device__ __forceinline__ float cap_score(float y, float cap_log2, float cap_arg) {
-  const float t = 1.f - 2.f * __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(y * cap_arg) + 1.f);
-  float r = cap_log2 * t;
-  if (cap_log2 > 64.f * 1.4426950408889634f) {
-    const float x = y * cap_arg * 0.34657359027997264f, x2 = x * x;   // y / cap_log2
-    const float small = y * __builtin_fmaf(x2, __builtin_fmaf(x2, __builtin_fmaf(x2, -17.f / 315.f, 2.f / 15.f), -1.f / 3.f), 1.f);
-    r = __builtin_fabsf(x) < 0.0625f ? small : r;
-  }
-  return r;
+// The largest magnitudes of bf16 values, two at a time: without their signs they order as
+// integers, infinities and NaN above the others.
+typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
+template <class Words>
+__device__ __forceinline__ u16x2 magnitude_max(u16x2 top, Words w) {
+#pragma unroll
+  for (unsigned i = 0; i < sizeof(w) / 4; ++i)
+    top = __builtin_elementwise_max(top, __builtin_bit_cast(u16x2, (uint32_t)w[i] & 0x7FFF7FFFu));
+  return top;
+}
+__device__ __forceinline__ bool not_finite(u16x2 top) { return top[0] >= 0x7F80 || top[1] >= 0x7F80; }
+
+// The cap of a score, y -> cap tanh(y / cap) in log2 units (cap_log2 = cap log2(e)), for
+// y = x * mul and arg = mul * 2 / cap: cap - 2 cap / (e^(2 y / cap) + 1), exact at both ends.
+// Its error is 2^-22 of the cap, 1.5e-5 in a score at a cap of 64 (bf16 products of random
+// signs: a few 1e-6 in the result).
+__device__ __forceinline__ float cap_score(float x, float arg, float cap_log2) {
+  return __builtin_fmaf(-2.f * cap_log2, __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(x * arg) + 1.f), cap_log2);
+}
+
+// Wider caps take the odd series where |y| is below a sixteenth of the cap (the next term is
+// 2e-9 of the result): their error stays 2^-18 of the score.
+__host__ __device__ __forceinline__ bool wide_cap(float cap_log2) { return cap_log2 > 64.f * 1.4426950408889634f; }
+__device__ __forceinline__ float cap_score_wide(float x, float mul, float arg, float cap_log2) {
+  const float z = x * arg * 0.5f * 0.6931471805599453f, z2 = z * z;   // y / cap_log2
+  const float small = x * mul * __builtin_fmaf(z2, __builtin_fmaf(z2, __builtin_fmaf(z2, -17.f / 315.f, 2.f / 15.f), -1.f / 3.f), 1.f);
+  return __builtin_fabsf(z) < 0.0625f ? small : cap_score(x, arg, cap_log2);
 }
 
 }  // namespace

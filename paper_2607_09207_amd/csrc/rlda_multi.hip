@@ -96,8 +96,7 @@ struct MqShape {
 #ifdef RLDA_MQ_WAVES
   static constexpr int WAVES = SMALL ? 2 : RLDA_MQ_WAVES;
 #else
-  // (MOD: the intervals, the bias and the noted infinities are 15 registers more.)
-  static constexpr int WAVES = SMALL ? 2 : kNT == 1 ? (D == 64 ? RLDA_MQ_WAVES_D64 : MOD ? 2 : 3) : 1;
+  static constexpr int WAVES = SMALL ? 2 : kNT == 1 ? (D == 64 ? RLDA_MQ_WAVES_D64 : 3) : 1;
 #endif
   static constexpr int krs(bool dma) { return dma ? 2 * D : 2 * D + RLDA_MQ_KPAD; }   // LDS row stride of the K block (bytes)
   static constexpr int vrs(bool dma) { return dma ? 2 * D : 2 * D + RLDA_MQ_VPAD; }   // ... of the V block
@@ -142,24 +141,6 @@ __device__ __forceinline__ bf16x4 lds_tr_read(const char* p) {
   return __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4*)(__attribute__((address_space(3))) char*)p);
 }
 
-// Non-zero where one of eight bf16 values is an infinity or NaN (their exponent bits are all set).
-__device__ __forceinline__ uint32_t not_finite(u32x4 w) {
-  uint32_t r = 0;
-#pragma unroll
-  for (int i = 0; i < 4; ++i)
-    r |= (uint32_t)((w[i] & 0x7F80u) == 0x7F80u) | (uint32_t)((w[i] & 0x7F800000u) == 0x7F800000u);
-  return r;
-}
-
-// Infinities and NaN turned into zeros.
-__device__ __forceinline__ bf16x8 without_odd(bf16x8 v) {
-  typedef uint16_t u16x8_t __attribute__((ext_vector_type(8)));
-  u16x8_t x = __builtin_bit_cast(u16x8_t, v);
-#pragma unroll
-  for (int e = 0; e < 8; ++e) x[e] = (x[e] & 0x7F80u) == 0x7F80u ? (uint16_t)0 : x[e];
-  return __builtin_bit_cast(bf16x8, x);
-}
-
 // The largest and the smallest of non-negative values over the wave.
 __device__ __forceinline__ int wave_max(int x) { return __builtin_amdgcn_readlane(wave_scan_max(x), 63); }
 __device__ __forceinline__ int wave_min(int x) { return 0x7fffffff - wave_max(0x7fffffff - x); }
@@ -168,7 +149,9 @@ __device__ __forceinline__ int wave_min(int x) { return 0x7fffffff - wave_max(0x
 // score registers, and a row sees the keys of an interval.  The workgroup walks the blocks
 // from the first key that one of its rows sees to the last; a wave skips those that none of
 // its own sees, and masks only the ones that some of its rows sees in part.
-template <int D, bool FP8, bool SMALL, bool MOD = false>
+// WIDE: ... with a wide cap (wide_cap), a kernel of its own: with both forms in one, 20
+// registers spilled, documents under a cap of 50 took 335 us a call and 246 without.
+template <int D, bool FP8, bool SMALL, bool MOD = false, bool WIDE = false>
 __global__ __attribute__((amdgpu_flat_work_group_size(kThreads, kThreads),
                           amdgpu_waves_per_eu(MqShape<D, FP8, SMALL, MOD>::WAVES,
                                               MqShape<D, FP8, SMALL, MOD>::WAVES)))
@@ -182,6 +165,7 @@ void multi_query_kernel(const Params p) {
   __shared__ int32_t s_bad[S::NBUF][2 * kKH];   // page of the block not in the pool (contributes nothing)
   __shared__ int32_t s_scan[kWaves], s_emax[kWaves], s_sum32[kWaves];
   __shared__ int16_t s_qh[kMaxQHeads];
+  __shared__ int32_t s_odd;   // MOD: infinities or NaN of V were cleared
   // Batches above 64, per sequence: {L - n_b (position of query token 0), n_b} (n_b 0
   // when its offsets are inconsistent), and its ordering key.
   extern __shared__ int2 s_sq[];   // [batch], then s_key [batch]
@@ -226,6 +210,7 @@ void multi_query_kernel(const Params p) {
     lmax = __builtin_amdgcn_readlane(wave_scan_max(lmax), 63);
     if (SMALL) sum32 = __builtin_amdgcn_readlane(wave_scan(sum32), 63);
     for (int e = tid; e < Hq; e += kThreads) s_qh[e] = p.q_head[e];
+    if (MOD && tid == 0) s_odd = 0;
     // Ordering key of each sequence's row blocks.  A sequence whose rows see at most an
     // eighth of the largest job's keys apart is dispatched as a group (its row blocks
     // then read its pages together): its key count L; -1: each row block is ordered by
@@ -631,13 +616,18 @@ void multi_query_kernel(const Params p) {
 #pragma unroll
     for (int kh = 0; kh < kKH; ++kh)
 #pragma unroll
-      for (int j = 0; j < 16; ++j) {
-        sv[kh][j] = FP8 || MOD ? sc[kh][j] * km[2 * kh + (j >> 3)] : sc[kh][j];
-        if constexpr (MOD) {
-          if (p.cap_log2 > 0.f) sv[kh][j] = cap_score(sv[kh][j], p.cap_log2, p.cap_arg);
-        }
-      }
+      for (int j = 0; j < 16; ++j) sv[kh][j] = FP8 && !MOD ? sc[kh][j] * km[2 * kh + (j >> 3)] : sc[kh][j];
     if constexpr (MOD) {
+      if (p.cap_log2 > 0.f) {
+        const float arg[2] = {km[0] * p.cap_arg, km[1] * p.cap_arg};
+#pragma unroll
+        for (int j = 0; j < 16; ++j)
+          sv[0][j] = WIDE ? cap_score_wide(sv[0][j], km[j >> 3], arg[j >> 3], p.cap_log2)
+                          : cap_score(sv[0][j], arg[j >> 3], p.cap_log2);
+      } else {
+#pragma unroll
+        for (int j = 0; j < 16; ++j) sv[0][j] *= km[j >> 3];
+      }
       if (p.slopes) {
         const float at = (float)(base_pos + qi[t] - kb * kKeys - 4 * hh);   // position less the key of j = 0
 #pragma unroll
@@ -735,50 +725,6 @@ void multi_query_kernel(const Params p) {
   };
   static_assert(S::KS == 2 * S::DT, "as many V^T operands as score k-steps");
 
-  // MOD: the infinities and NaN of V that this lane's row sees, a bit an output (NaN: both).
-  // They are noted here, left out of the product, and put into the results at the end.  A
-  // key a turn, its values from LDS: as slow as it is rare.  (Added to the accumulators in
-  // a branch, they made two copies of these: 250 to 450 registers spilled.)
-  uint32_t plus_inf[S::DT / 2] = {}, minus_inf[S::DT / 2] = {};
-  auto note_odd = [&](auto dma, int kb, int buf) __attribute__((always_inline)) {
-    constexpr bool kDma = decltype(dma)::value;
-    typedef uint16_t u16x4_t __attribute__((ext_vector_type(4)));
-#pragma unroll 1
-    for (int R = 0; R < kTile; ++R) {
-      const int key = kb * kKeys + R;
-      const bool sees = key >= low[0] && key < lim[0] && !s_bad[buf][R >> 4];
-      const char* vr = s_v[buf] + R * S::vrs(kDma);
-#pragma unroll
-      for (int c = 0; c < S::DT; ++c)
-#pragma unroll
-        for (int jj = 0; jj < 4; ++jj) {
-          // Elements d = 32c + 8jj + 4hh ..: chunk 4c + jj, byte 8hh in it.
-          const int off = kDma ? 16 * chunk_pos(true, R, 4 * c + jj) + 8 * hh : 2 * (32 * c + 8 * jj + 4 * hh);
-          const u16x4_t x = *(const u16x4_t*)(vr + off);
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const uint32_t bit = sees && (x[e] & 0x7F80u) == 0x7F80u ? 1u << (16 * (c & 1) + 4 * jj + e) : 0u;
-            plus_inf[c / 2] |= x[e] == 0xFF80u ? 0u : bit;
-            minus_inf[c / 2] |= x[e] == 0x7F80u ? 0u : bit;
-          }
-        }
-    }
-  };
-  auto put_odd = [&]() __attribute__((always_inline)) {
-    uint32_t any = 0;
-#pragma unroll
-    for (int c = 0; c < S::DT / 2; ++c) any |= plus_inf[c] | minus_inf[c];
-    if (__builtin_amdgcn_ballot_w64(any != 0) == 0) return;
-#pragma unroll
-    for (int c = 0; c < S::DT; ++c)
-#pragma unroll
-      for (int j = 0; j < 16; ++j) {
-        const uint32_t bit = 1u << (16 * (c & 1) + j);
-        acc[0][c][j] += plus_inf[c / 2] & bit ? -neg_inf() : 0.f;
-        acc[0][c][j] += minus_inf[c / 2] & bit ? neg_inf() : 0.f;   // after the other: NaN
-      }
-  };
-
   // Block kb in LDS buffer buf: scores, softmax, P V, for the wave's row tiles.
   auto compute_block = [&](auto dma, int kb, int buf) __attribute__((always_inline)) {   // dma: the block's layout
     if (kb * kKeys < Ew && (!MOD || (kb + 1) * kKeys > Wlo)) {
@@ -798,29 +744,32 @@ void multi_query_kernel(const Params p) {
       }
 #pragma unroll
       for (int t = 0; t < kNT; ++t) softmax(t, kb, buf, sc[t]);
-      bool any_odd = false;
       if constexpr (MOD) {
         // A key that a row does not see has no part in it, whatever its values: an infinity
-        // or NaN of V would turn the product with its zero probability into NaN.
+        // or NaN of V would turn the product with its zero probability into NaN.  Such
+        // values are cleared in the block (another wave may meet either, and clears what
+        // it must itself), and put into the rows that see them at the end.  (Kept apart in
+        // registers here, they cost a wave per SIMD: plain scores 594 us a call and
+        // 448 without.)
         if (__builtin_amdgcn_ballot_w64(masked) != 0) {
-          uint32_t odd = 0;
           constexpr bool kDma = decltype(dma)::value;
-#pragma unroll
+          u16x2 top = {0, 0};
+#pragma unroll 2
           for (int c = 0; c < D / 8; c += 2)   // two lanes a row
-            odd |= not_finite(*(const u32x4*)(s_v[buf] + (lane >> 1) * S::vrs(kDma) + 16 * (c + (lane & 1))));
-          any_odd = __builtin_amdgcn_ballot_w64(odd != 0) != 0;
-          if (any_odd) note_odd(dma, kb, buf);
+            top = magnitude_max(top, *(const u32x4*)(s_v[buf] + (lane >> 1) * S::vrs(kDma) + 16 * (c + (lane & 1))));
+          if (__builtin_amdgcn_ballot_w64(not_finite(top)) != 0) {
+            char* row = s_v[buf] + (lane >> 1) * S::vrs(kDma);
+#pragma unroll 1
+            for (int e = (lane & 1) * (D / 2); e < (lane & 1) * (D / 2) + D / 2; ++e)
+              if ((((uint16_t*)row)[e] & 0x7F80u) == 0x7F80u) ((uint16_t*)row)[e] = 0;
+            if (lane == 0) s_odd = 1;
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+          }
         }
       }
       bf16x8 va[kKH][S::KS];
 #pragma unroll
       for (int kh = 0; kh < kKH; ++kh) read_v(dma, va[kh], buf, kh);
-      if constexpr (MOD) {
-        if (any_odd) {
-#pragma unroll
-          for (int s = 0; s < S::KS; ++s) va[0][s] = without_odd(va[0][s]);
-        }
-      }
 #pragma unroll
       for (int kh = 0; kh < kKH; ++kh)
 #pragma unroll
@@ -829,6 +778,44 @@ void multi_query_kernel(const Params p) {
           for (int t = 0; t < kNT; ++t)
             acc[t][s % S::DT] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(va[kh][s], pb[t][kh][s / S::DT],
                                                                         acc[t][s % S::DT], 0, 0, 0);
+    }
+  };
+
+  // MOD: the infinities and NaN of V that were cleared, into the results of the rows that see
+  // them (every thread calls it, with the results stored).  Every wave looks through the
+  // workgroup's keys and serves a quarter of its rows: as slow as it is rare.
+  auto put_odd = [&]() {
+    __syncthreads();   // the other waves' stores are complete
+    if (uni(s_odd) == 0) return;
+    for (int key = max(kb0 * kKeys, first_page * kPage); key < E; ++key) {
+      const int pid = uni(bt_vec[key / kPage]);
+      if ((unsigned)pid >= (unsigned)p.num_pages) continue;
+      const char* vr = (const char*)p.v + (int64_t)pid * p.stride_page + (int64_t)g * p.stride_head + (int64_t)(key % kPage) * p.stride_slot;
+      float add[D / 64];   // 0, an infinity or NaN
+      bool odd = false;
+#pragma unroll
+      for (int e = 0; e < D / 64; ++e) {
+        const uint32_t x = FP8 ? ((const uint8_t*)vr)[lane + 64 * e] : ((const uint16_t*)vr)[lane + 64 * e];
+        const bool is = FP8 ? (x & 0x7Fu) == 0x7Fu : (x & 0x7F80u) == 0x7F80u;
+        add[e] = !is ? 0.f : FP8 ? __builtin_nanf("") : __uint_as_float(x << 16);
+        odd = odd || is;
+      }
+      if (__builtin_amdgcn_ballot_w64(odd) == 0) continue;
+      for (int row = r0 + wave; row < r1; row += kWaves) {
+        const int i = row / G;
+        if (base_pos + i < 0 || key < first_key(row) || key >= seen_end(row)) continue;
+        const int64_t ob = ((int64_t)(q0 + i) * Hq + s_qh[g * G + (row - i * G)]) * D + lane;
+#pragma unroll
+        for (int e = 0; e < D / 64; ++e) {
+          if (add[e] == 0.f) continue;
+          if (p.out_bf16) {
+            uint16_t* o = (uint16_t*)p.out + ob + 64 * e;
+            *o = __builtin_bit_cast(uint16_t, (__bf16)(__uint_as_float((uint32_t)*o << 16) + add[e]));
+          } else {
+            ((float*)p.out)[ob + 64 * e] += add[e];
+          }
+        }
+      }
     }
   };
 
@@ -872,7 +859,6 @@ void multi_query_kernel(const Params p) {
     auto part = [&](int w) { return (float*)(w < 2 ? s_k[0] : s_v[0]) + (w & 1) * kTile * RSF; };
     __shared__ float2 s_ml[kWaves][kTile];
     const float lt = pair_sum(l[0]);
-    if constexpr (MOD) put_odd();
     lds_barrier();
     if (wave < nkb) {
 #pragma unroll
@@ -885,7 +871,8 @@ void multi_query_kernel(const Params p) {
     if (hh == 0) s_ml[wave][i] = make_float2(m[0], lt);
     lds_barrier();
     const int row = tid >> 3, d0 = (tid & 7) * DPT;
-    if (r0 + row >= r1) return;
+    const bool there = r0 + row < r1;
+    if (!MOD && !there) return;
     float M = neg_inf(), Ls = 0.f, o[DPT];
 #pragma unroll
     for (int w = 0; w < kWaves; ++w) M = fmaxf(M, s_ml[w][row].x);
@@ -910,11 +897,13 @@ void multi_query_kernel(const Params p) {
     const int64_t ob = ((int64_t)(q0 + rq) * Hq + s_qh[g * G + (r0 + row - rq * G)]) * D + d0;
 #pragma unroll
     for (int c = 0; c < DPT; c += 4) {
+      if (MOD && !there) continue;
       if (p.out_bf16)
         *(u32x2*)((uint16_t*)p.out + ob + c) = u32x2{pack_bf16(o[c] * inv, o[c + 1] * inv), pack_bf16(o[c + 2] * inv, o[c + 3] * inv)};
       else
         *(f32x4*)((float*)p.out + ob + c) = f32x4{o[c] * inv, o[c + 1] * inv, o[c + 2] * inv, o[c + 3] * inv};
     }
+    if constexpr (MOD) put_odd();
     return;
   }
   if constexpr (S::DMA) {
@@ -983,14 +972,15 @@ void multi_query_kernel(const Params p) {
     }
   }
 
-  if constexpr (MOD) put_odd();
   // 4. Normalise and write: lane 32h + i holds O^T[d = 32c + 8jj + 4h + 0..3][its row].
 #pragma unroll
   for (int t = 0; t < kNT; ++t) {
     const float lt = pair_sum(l[t]);
     if (!live[t]) continue;
     const float inv = lt > 0.f ? 1.f / lt : 0.f;
-    const int64_t ob = ((int64_t)(q0 + qi[t]) * Hq + head[t]) * D;
+    // (MOD: the head is read again, for a register less in the loop.)
+    const int hd = MOD ? s_qh[g * G + (wr0 + kTile * t + i - qi[t] * G)] : head[t];
+    const int64_t ob = ((int64_t)(q0 + qi[t]) * Hq + hd) * D;
 #pragma unroll
     for (int c = 0; c < S::DT; ++c)
 #pragma unroll
@@ -1004,14 +994,15 @@ void multi_query_kernel(const Params p) {
           *(f32x4*)((float*)p.out + ob + d) = f32x4{o0, o1, o2, o3};
       }
   }
+  if constexpr (MOD) put_odd();
 }
 
-template <int D, bool FP8, bool SMALL, bool MOD = false>
+template <int D, bool FP8, bool SMALL, bool MOD = false, bool WIDE = false>
 int launch_multi_t(const Params& p, int grid, void* stream, void* ev_begin, void* ev_end) {
   hipStream_t st = (hipStream_t)stream;
   if (ev_begin && hipEventRecord((hipEvent_t)ev_begin, st) != hipSuccess) return -1;
   const size_t lds = p.batch > 64 ? (sizeof(int2) + sizeof(int32_t)) * (size_t)p.batch : 0;
-  hipLaunchKernelGGL((multi_query_kernel<D, FP8, SMALL, MOD>), dim3(grid), dim3(kThreads), lds, st, p);
+  hipLaunchKernelGGL((multi_query_kernel<D, FP8, SMALL, MOD, WIDE>), dim3(grid), dim3(kThreads), lds, st, p);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return (int)e;
   if (ev_end && hipEventRecord((hipEvent_t)ev_end, st) != hipSuccess) return -1;
@@ -1032,18 +1023,23 @@ int launch_multi(KvKind kind, int head_dim, bool small, const Params& p, int gri
   return launch(p, grid, stream, ev_begin, ev_end);
 }
 
+namespace {
+template <int D, bool FP8>
+int launch_scored_multi_t(bool small, const Params& p, int grid, void* stream, void* ev_begin, void* ev_end) {
+  auto* const launch = wide_cap(p.cap_log2) ? (small ? launch_multi_t<D, FP8, true, true, true> : launch_multi_t<D, FP8, false, true, true>)
+                                            : (small ? launch_multi_t<D, FP8, true, true> : launch_multi_t<D, FP8, false, true>);
+  return launch(p, grid, stream, ev_begin, ev_end);
+}
+}  // namespace
+
 int launch_scored_multi(KvKind kind, int head_dim, bool small, const Params& p, int grid, void* stream, void* ev_begin,
                         void* ev_end) {
   if (kind != KvKind::BF16 && kind != KvKind::FP8) return -1;
   if constexpr (!kMultiSplits) return -1;   // the tilings that are not built for it
   else {
-    auto* const launch =
-        kind == KvKind::BF16
-            ? (head_dim == 128 ? (small ? launch_multi_t<128, false, true, true> : launch_multi_t<128, false, false, true>)
-                               : (small ? launch_multi_t<64, false, true, true> : launch_multi_t<64, false, false, true>))
-            : (head_dim == 128 ? (small ? launch_multi_t<128, true, true, true> : launch_multi_t<128, true, false, true>)
-                               : (small ? launch_multi_t<64, true, true, true> : launch_multi_t<64, true, false, true>));
-    return launch(p, grid, stream, ev_begin, ev_end);
+    auto* const launch = kind == KvKind::BF16 ? (head_dim == 128 ? launch_scored_multi_t<128, false> : launch_scored_multi_t<64, false>)
+                                              : (head_dim == 128 ? launch_scored_multi_t<128, true> : launch_scored_multi_t<64, true>);
+    return launch(small, p, grid, stream, ev_begin, ev_end);
   }
 }
 
