@@ -378,7 +378,10 @@ rlda_status rl_decode_attn_rotate(rlda_dtype dtype, int32_t rows, int32_t heads,
  * bf16 and f32 caches store the rows rounded once to their type.  fp8 caches keep the rule
  * of rl_decode_attn_append with the call's rows of one page taken together (amax over all
  * of them, the turned K rows in fp32): a page whose slot 0 is among them starts with scale
- * amax / 448; in another the scale is raised, and its earlier rows are re-encoded, once.
+ * amax / 448; in another the scale is raised to that where it has to be, and its earlier
+ * rows are re-encoded, once.  Rows that set the scale are stored as E4M3(448 value / amax),
+ * the others as E4M3(value / scale), in fp32 (the append's value / scale is rounded twice
+ * where it sets the scale: halfway values may be the other neighbour).
  * Rows that no sequence names, rows of sequences with inconsistent q_start entries or a
  * length outside [0, capacity], and rows before token 0 (n_b > seq_lens[b]) are not
  * written, q_out included (flag bit 1, but for rows of no sequence and for an empty

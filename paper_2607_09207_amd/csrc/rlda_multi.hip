@@ -448,7 +448,7 @@ void multi_query_kernel(const Params p) {
     Wlo_full = wave_max(low[0]);
     if (__builtin_amdgcn_ballot_w64(live[0] && lim[0] == 0) != 0) Ew_full = 0;
   }
-  const int nkb = max((E + kKeys - 1) / kKeys - kb0, 0);   // blocks: kb0 + kb, kb < nkb
+  const int nkb = MOD ? max((E + kKeys - 1) / kKeys - kb0, 0) : (E + kKeys - 1) / kKeys;   // blocks: kb0 + kb, kb < nkb
 
   // Q operands (B of K Q^T): lane 32h + i holds its row's elements [16s + 8h, 16s + 8h + 8).
   bf16x8 qop[kNT][S::KS];

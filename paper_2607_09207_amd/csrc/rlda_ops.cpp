@@ -62,11 +62,29 @@ void set_rotary(RotaryParams& p, const rl_decode_attn_rotary& r, int d, int rows
   p.magic_half = magic_of(p.half);
 }
 
-// Workgroups of a window: enough for kWanted in all while every thread has a unit.
-constexpr int kWanted = 2048;
-int parts_of(int64_t windows, int64_t units, int64_t jobs) {
-  const int64_t most = std::max<int64_t>((units + rlda::kThreads - 1) / rlda::kThreads, (jobs + rlda::kWaves - 1) / rlda::kWaves);
-  return (int)std::min(std::max<int64_t>(kWanted / windows, 1), std::max<int64_t>(most, 1));
+// Windows, and workgroups of a window: kWanted that turn rows in all, where the rows give
+// them, none without a unit for its threads.  us a call by kWanted 2048 / 8192: 32768 x 32
+// heads of 128 89.6 / 83.6.  Windows stay small while they are enough, since each of its
+// workgroups takes a window's sines and cosines; fp8 caches have windows of a page where
+// sequences bring several rows, so that few of them hold no page's first row.
+//   Workgroups that write pages: four pages to a wave, or one while they are few.
+//   Inputs beyond kStreamBytes are read past the caches, which they would only pass through
+// (32768 x 32 heads 101 to 84 us); smaller ones are where the projection left them (512
+// tokens, 64/8 heads: 7.8 us, and 9.4 past the caches).
+constexpr int kWanted = 8192, kWantedPages = 2048;
+constexpr int64_t kStreamBytes = 128ll << 20;
+void set_windows(RotaryParams& p, int64_t units_a_row, int64_t jobs_a_row, int64_t bytes_a_row) {
+  const bool paged = jobs_a_row > 0 && p.q_start;
+  p.win = 1;
+  while (p.win < rlda::kRotaryWindow && p.rows >= 2ll * p.win * (paged ? 128 : kWanted)) p.win *= 2;
+  const int64_t windows = ((int64_t)p.rows + p.win - 1) / p.win, n = std::min(p.rows, p.win);
+  auto most = [](int64_t a, int64_t b) { return (a + b - 1) / b; };
+  p.parts = (int)std::max<int64_t>(std::min(kWanted / windows, most(n * units_a_row, rlda::kThreads)), 1);
+  p.stream = p.rows * bytes_a_row > kStreamBytes;
+  if (jobs_a_row > 0) {
+    const int64_t jobs = (paged ? p.win / 8 + 1 : p.win) * jobs_a_row;   // (a window's pages: about)
+    p.page_parts = (int)std::max(most(jobs, 4 * rlda::kWaves), std::min(kWantedPages / windows, most(jobs, rlda::kWaves)));
+  }
 }
 
 }  // namespace
@@ -94,9 +112,7 @@ rlda_status rl_decode_attn_rotate(rlda_dtype dtype, int32_t rows, int32_t heads,
   p.o_rs = out->row_stride;
   p.o_hs = out->head_stride;
   p.positions = positions;
-  const int64_t windows = ((int64_t)rows + rlda::kRotaryWindow - 1) / rlda::kRotaryWindow;
-  p.parts = parts_of(windows, (int64_t)std::min(rows, rlda::kRotaryWindow) * heads * p.units, 0);
-  if (windows * p.parts > INT32_MAX) return RLDA_ERR_UNSUPPORTED;
+  set_windows(p, (int64_t)heads * p.units, 0, (int64_t)heads * head_dim * eb);
   return rlda::launch_rotate(dtype == RLDA_F32, p, stream) == hipSuccess ? RLDA_OK : RLDA_ERR_HIP;
 }
 
@@ -158,12 +174,8 @@ rlda_status rl_decode_attn_append_rotary(rl_decode_attn_t h, int32_t batch, int3
   p.batch = batch;
   p.num_pages = num_pages;
   p.max_pages = c.max_pages_per_seq;
-  const int n = std::min(total_q, rlda::kRotaryWindow);
-  const int64_t windows = ((int64_t)total_q + rlda::kRotaryWindow - 1) / rlda::kRotaryWindow;
-  // fp8 pages: one a row where every sequence brings one, else two a window.
-  const int64_t jobs = h->kind == rlda::KvKind::FP8 ? 2ll * c.num_kv_heads * (q_start ? 2 : n) : 0;
-  p.parts = parts_of(windows, (int64_t)n * c.num_q_heads * p.units, jobs);
-  if (windows * p.parts > INT32_MAX) return RLDA_ERR_UNSUPPORTED;
+  set_windows(p, (int64_t)c.num_q_heads * p.units, h->kind == rlda::KvKind::FP8 ? 2 * c.num_kv_heads : 0,
+              (int64_t)(c.num_q_heads + 2 * c.num_kv_heads) * c.head_dim * eb);
   return rlda::launch_append_rotary(h->kind, c.head_dim, p, stream) == hipSuccess ? RLDA_OK : RLDA_ERR_HIP;
 }
 
@@ -236,6 +248,8 @@ rlda_status page_call(rl_decode_attn_t h, int32_t batch, int32_t num_pages, int3
   p.in_lds = p.group_words == 1;
   return RLDA_OK;
 }
+
+constexpr int kMoveGrid = 2048;   // workgroups of a compaction's copies, whose number the device knows
 
 // Layers of a workgroup: a page pair of a few KiB is too little for one.
 constexpr int kCopyBytes = 32 << 10;
@@ -336,7 +350,7 @@ rlda_status rl_decode_attn_page_compact(rl_decode_attn_t h, int32_t batch, int32
   if ((st = check_caches(h, num_caches, caches, num_pages)) != RLDA_OK) return st;
   p.live_out = live;
   if (rlda::launch_page_compact(p, stream) != hipSuccess) return RLDA_ERR_HIP;
-  return for_caches(h, p, num_caches, caches, [&] { return rlda::launch_page_move(p, kWanted, stream); });
+  return for_caches(h, p, num_caches, caches, [&] { return rlda::launch_page_move(p, kMoveGrid, stream); });
 }
 
 rlda_status rl_decode_attn_page_copy(rl_decode_attn_t h, int32_t num_pages, int32_t count, const int32_t* src,

@@ -102,7 +102,7 @@ struct Params {
   int16_t q_head[kMaxQHeads];  // q_head[g * G + i] = i-th query head of KV head g
 };
 
-constexpr int kRotaryWindow = 16;   // rows of a workgroup's window (rlda_rotary.hip)
+constexpr int kRotaryWindow = 16;   // rows of a workgroup's window at most (rlda_rotary.hip)
 
 // Rotary positions: rows turned alone (hq heads of q to q_out), or q, k_in and v_in on
 // their way into the cache.  Strides of rows and heads in elements.
@@ -129,7 +129,9 @@ struct RotaryParams {
   int32_t units;               // units of a head (rlda_rotary.hip)
   int32_t interleaved, inverse;
   int32_t num_pages, max_pages;
-  int32_t parts;               // workgroups of a window
+  int32_t win;                 // rows of a window, at most kRotaryWindow
+  int32_t parts, page_parts;   // workgroups of it that turn rows, and that write the pages of an fp8 cache
+  int32_t stream;              // rows are read past the caches
   float amplitude;
   uint32_t magic_u, magic_qu, magic_ku, magic_half;   // ceil(2^32 / x) of units, hq units, hkv units, half
 };

@@ -10,19 +10,21 @@
 // fraction of a turn in 32 bits (2^20 positions: 0.06 radians), so it is reduced to a
 // fraction of a turn, and its sine and cosine taken, in 64.
 //
-// Work.  A workgroup takes a window of 16 rows (tokens): it finds their sequences,
+// Work.  A workgroup takes a window of up to 16 rows (tokens): it finds their sequences,
 // positions and cache slots, and takes one sine and cosine a (row, pair) into LDS, shared
 // by every head of the row (one a lane in registers would be repeated by each head).  Then
 // its threads walk the window's 16-byte chunks, a pair of chunks at a time where their
-// elements are turned into each other, four such units in flight.  Few rows take several
-// workgroups to a window (`parts`), each with a share of the units.
+// elements are turned into each other, four such units in flight, the first of them asked
+// for before anything else.  Few rows take small windows, and several workgroups to a
+// window with a share of the units each.
 // Rows are read and written once: what bounds it is bandwidth, and latency on few rows.
 //
 // fp8 caches hold one scale per (page, KV head) that covers every row written so far, so
-// their K and V rows are written a page at a time: one wave per (page, KV head, K or V)
-// turns the page's new rows in registers, finds their largest magnitude, sets or raises
-// the scale (re-encoding the rows before them) and encodes them.  A page belongs to the
-// window that holds its first new row; its rows reach at most 15 past the window.
+// their K and V rows are written a page at a time, by workgroups of their own: one wave per
+// (page, KV head, K or V) turns the page's new rows in registers, finds their largest
+// magnitude, sets or raises the scale (re-encoding the rows before them) and encodes them.
+// A page belongs to the window that holds its first new row; its rows reach at most 15
+// past the window.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -32,9 +34,9 @@
 namespace rlda {
 namespace {
 
-constexpr int kWin = kRotaryWindow;   // rows of a window
-constexpr int kWinRows = 2 * kWin;    // ... and the rows its pages may reach to
-constexpr int kUnroll = 4;            // units in flight a thread
+constexpr int kWin = kRotaryWindow;      // rows of a window at most
+constexpr int kWinRows = 2 * kWin;       // ... and the rows its pages may reach to
+constexpr int kUnroll = 4;               // units in flight a thread
 
 // Eight consecutive elements.
 template <bool F32>
@@ -42,7 +44,11 @@ struct Chunk;
 template <>
 struct Chunk<false> {
   u32x4 r;
-  __device__ __forceinline__ void load(const void* base, int64_t e) { r = *(const u32x4*)((const uint16_t*)base + e); }
+  template <bool STREAM = false>
+  __device__ __forceinline__ void load(const void* base, int64_t e) {
+    const u32x4* at = (const u32x4*)((const uint16_t*)base + e);
+    r = STREAM ? __builtin_nontemporal_load(at) : *at;
+  }
   __device__ __forceinline__ void get(float* x) const {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -59,9 +65,11 @@ struct Chunk<false> {
 template <>
 struct Chunk<true> {
   f32x4 r[2];
+  template <bool STREAM = false>
   __device__ __forceinline__ void load(const void* base, int64_t e) {
-    r[0] = *(const f32x4*)((const float*)base + e);
-    r[1] = *(const f32x4*)((const float*)base + e + 4);
+    const f32x4* at = (const f32x4*)((const float*)base + e);
+    r[0] = STREAM ? __builtin_nontemporal_load(at) : at[0];
+    r[1] = STREAM ? __builtin_nontemporal_load(at + 1) : at[1];
   }
   __device__ __forceinline__ void get(float* x) const {
 #pragma unroll
@@ -111,33 +119,35 @@ __device__ __forceinline__ int unit_chunk(const RotaryParams& p, int u) {
 
 __device__ __forceinline__ uint32_t div_by(uint32_t x, uint32_t magic) { return __umulhi(x, magic); }
 
-// Turn `nrows` rows of `heads` heads (rows[first + r], r < nrows, where ok[r]) and hand
-// every chunk's result to put(row, head, chunk, values).  `part` of `parts` workgroups.
-template <bool F32, bool IL, class Put>
-__device__ __forceinline__ void turn_rows(const RotaryParams& p, const void* x, int64_t rs, int64_t hs, int first,
-                                          int nrows, int heads, uint32_t magic_hu, int part, const uint8_t* ok,
-                                          const float2* cs, Put put) {
-  const int U = p.units, total = nrows * heads * U, step = p.parts * kThreads, h8 = p.half >> 3;
-  for (int i0 = part * kThreads + (int)threadIdx.x; i0 < total; i0 += kUnroll * step) {
-    Chunk<F32> a[kUnroll], b[kUnroll];
-    int row[kUnroll], head[kUnroll], unit[kUnroll];
+// Units i, i + step, .. of `nrows` rows of `heads` heads (rows first + r, r < nrows): asked
+// for, and then turned and handed to put(row, head, chunk, values) where ok[row].
+// STREAM: rows too many for the caches to hold are read past them (set_windows).
+template <bool F32, bool IL, bool STREAM>
+struct Units {
+  Chunk<F32> a[kUnroll], b[kUnroll];
+  int row[kUnroll], head[kUnroll], unit[kUnroll];
+
+  __device__ __forceinline__ void fetch(const RotaryParams& p, const void* x, int64_t rs, int64_t hs, int first, int total,
+                                        int heads, uint32_t magic_hu, int i0, int step) {
 #pragma unroll
     for (int k = 0; k < kUnroll; ++k) {
       const int i = i0 + k * step;
       row[k] = -1;
       if (i >= total) continue;
-      const int r = (int)div_by(i, magic_hu), rem = i - r * heads * U, hd = (int)div_by(rem, p.magic_u);
-      unit[k] = rem - hd * U;
-      head[k] = hd;
-      if (!ok[r]) continue;
+      const int r = (int)div_by(i, magic_hu), rem = i - r * heads * p.units, hd = (int)div_by(rem, p.magic_u);
       row[k] = r;
+      head[k] = hd;
+      unit[k] = rem - hd * p.units;
       const int64_t e = (int64_t)(first + r) * rs + (int64_t)hd * hs + 8 * unit_chunk<IL>(p, unit[k]);
-      a[k].load(x, e);
-      if (!IL && unit_turns<IL>(p, unit[k])) b[k].load(x, e + 8 * h8);
+      a[k].template load<STREAM>(x, e);
+      if (!IL && unit_turns<IL>(p, unit[k])) b[k].template load<STREAM>(x, e + p.half);
     }
+  }
+  template <class Put>
+  __device__ __forceinline__ void finish(const RotaryParams& p, const uint8_t* ok, const float2* cs, Put put) {
 #pragma unroll
     for (int k = 0; k < kUnroll; ++k) {
-      if (row[k] < 0) continue;
+      if (row[k] < 0 || !ok[row[k]]) continue;
       const int u = unit[k], c = unit_chunk<IL>(p, u);
       if (unit_turns<IL>(p, u)) {
         float xa[8], xb[8];
@@ -147,13 +157,13 @@ __device__ __forceinline__ void turn_rows(const RotaryParams& p, const void* x, 
         a[k].set(xa);
         if (!IL) {
           b[k].set(xb);
-          put(row[k], head[k], c + h8, b[k]);
+          put(row[k], head[k], c + (p.half >> 3), b[k]);
         }
       }
       put(row[k], head[k], c, a[k]);
     }
   }
-}
+};
 
 // Cosine and sine (times the amplitude) of rows [0, n) of the window, by all threads.
 __device__ __forceinline__ void angles(const RotaryParams& p, const int32_t* pos, int n, float2* cs) {
@@ -170,13 +180,17 @@ __device__ __forceinline__ void angles(const RotaryParams& p, const int32_t* pos
 }
 
 // ---------------------------------------------------------------- rows alone
-template <bool F32, bool IL>
+template <bool F32, bool IL, bool STREAM>
 __global__ __launch_bounds__(kThreads) void rotate_kernel(const RotaryParams p) {
-  extern __shared__ float2 s_cs[];   // [kWin][half]
+  extern __shared__ float2 s_cs[];   // [win][half]
   __shared__ int32_t s_pos[kWin];
   __shared__ uint8_t s_ok[kWin];
   const int win = blockIdx.x / p.parts, part = blockIdx.x - win * p.parts;
-  const int first = win * kWin, n = min(kWin, p.rows - first);
+  const int first = win * p.win, n = min(p.win, p.rows - first);
+  const int total = n * p.hq * p.units, step = p.parts * kThreads;
+  int i = part * kThreads + threadIdx.x;
+  Units<F32, IL, STREAM> x;
+  x.fetch(p, p.q, p.q_rs, p.q_hs, first, total, p.hq, p.magic_qu, i, step);
   if (threadIdx.x < (uint32_t)n) {
     s_pos[threadIdx.x] = p.positions[first + threadIdx.x];
     s_ok[threadIdx.x] = 1;
@@ -185,10 +199,14 @@ __global__ __launch_bounds__(kThreads) void rotate_kernel(const RotaryParams p) 
   angles(p, s_pos, n, s_cs);
   __syncthreads();
   constexpr int E = F32 ? 4 : 2;
-  turn_rows<F32, IL>(p, p.q, p.q_rs, p.q_hs, first, n, p.hq, p.magic_qu, part, s_ok, s_cs,
-                     [&](int r, int hd, int c, const Chunk<F32>& v) {
-                       v.store((char*)p.q_out + ((int64_t)(first + r) * p.o_rs + (int64_t)hd * p.o_hs + 8 * c) * E);
-                     });
+  for (;;) {
+    x.finish(p, s_ok, s_cs, [&](int r, int hd, int c, const Chunk<F32>& v) {
+      v.store((char*)p.q_out + ((int64_t)(first + r) * p.o_rs + (int64_t)hd * p.o_hs + 8 * c) * E);
+    });
+    i += kUnroll * step;
+    if (i >= total) break;
+    x.fetch(p, p.q, p.q_rs, p.q_hs, first, total, p.hq, p.magic_qu, i, step);
+  }
 }
 
 // ---------------------------------------------------------------- rows into the cache
@@ -217,49 +235,70 @@ __device__ __forceinline__ uint32_t e4m3x2(float a, float b) {
 }
 
 // One page of an fp8 cache, KV head and K or V, by a wave: rows r0 .. r0 + m - 1 of the
-// window into slots s0 .. of the page.  Lane 4 t + c: slot t, units c, c + 4, .. of its row.
+// window into slots s0 .. of the page.  Lane l: chunk l % NC of the slots l / NC, + 64 / NC, ..
+// (a load or store of the wave covers whole rows); its pairs' other halves come from the
+// lanes that hold them.
+//   A row that sets the scale, amax / 448, is encoded from 448 x / amax, one rounding from the
+// value where x / scale has two: ties of bf16 rows stay ties.
 template <int D, bool IL, bool TURN>
 __device__ __forceinline__ void write_page(const RotaryParams& p, const void* x, int64_t rs, int64_t hs, int first, int r0,
                                            int m, int s0, int g, char* page, float* scale, const float2* cs, int lane) {
-  constexpr int NC = D / 8, MU = (NC + 3) / 4;   // chunks of a row, units of a lane at most
-  const int t = lane >> 2, c = lane & 3, r = r0 + t - s0, h8 = p.half >> 3;
-  const bool mine = t >= s0 && t < s0 + m;
-  const int U = TURN ? p.units : NC;
-  float v[MU][2][8];
+  constexpr int NC = D / 8, kStep = 64 / NC, kN = kPage / kStep;   // chunks of a row, rows of an access, accesses
+  const int c = lane % NC, t0 = lane / NC, h8 = p.half >> 3;
+  Chunk<false> raw[kN];
+#pragma unroll
+  for (int j = 0; j < kN; ++j) {
+    const int t = t0 + kStep * j;
+    raw[j].r = u32x4{0u, 0u, 0u, 0u};
+    if (t >= s0 && t < s0 + m) raw[j].load(x, (int64_t)(first + r0 + t - s0) * rs + (int64_t)g * hs + 8 * c);
+  }
+  float s = s0 > 0 ? *scale : 0.f;
+  if (!(s > 0.f) || __builtin_isinf(s)) s = 0.f;
+  // Half pairs: this chunk is the first (side 0) or second half of pairs 8 pair .. + 7, the other half in chunk `other`.
+  const bool turns = TURN && c < (IL ? p.half >> 2 : 2 * h8);
+  const int side = !IL && c >= h8, pair = IL ? 4 * c : 8 * (side ? c - h8 : c);
+  const int other = lane + (turns && !IL ? (side ? -h8 : h8) : 0);
+  float v[kN][8];
   float amax = 0.f;
 #pragma unroll
-  for (int j = 0; j < MU; ++j) {
-    const int u = c + 4 * j;
+  for (int j = 0; j < kN; ++j) {
+    const int t = t0 + kStep * j, r = r0 + t - s0;
+    raw[j].get(v[j]);
+    if constexpr (TURN) {
+      Chunk<false> ob;
+      if constexpr (!IL) {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) v[j][0][e] = v[j][1][e] = 0.f;
-    if (!mine || u >= U) continue;
-    const bool turns = TURN && unit_turns<IL>(p, u);
-    const int64_t at = (int64_t)(first + r) * rs + (int64_t)g * hs + 8 * (TURN ? unit_chunk<IL>(p, u) : u);
-    Chunk<false> a, b;
-    a.load(x, at);
-    a.get(v[j][0]);
-    if (turns) {
-      if (!IL) {
-        b.load(x, at + 8 * h8);
-        b.get(v[j][1]);
+        for (int i = 0; i < 4; ++i) ob.r[i] = (uint32_t)__builtin_amdgcn_ds_bpermute(4 * other, (int)raw[j].r[i]);
       }
-      turn<IL>(v[j][0], v[j][1], cs + r * p.half + (IL ? 4 : 8) * u);
+      if (turns && t >= s0 && t < s0 + m) {
+        const float2* f = cs + r * p.half + pair;
+        if constexpr (IL) {
+          float none[8];
+          turn<true>(v[j], none, f);
+        } else {
+          float o[8];
+          ob.get(o);
+          if (side)
+            turn<false>(o, v[j], f);
+          else
+            turn<false>(v[j], o, f);
+        }
+      }
     }
 #pragma unroll
-    for (int e = 0; e < 8; ++e) amax = fmaxf(amax, fmaxf(fabsf(v[j][0][e]), fabsf(v[j][1][e])));
+    for (int e = 0; e < 8; ++e) amax = fmaxf(amax, fabsf(v[j][e]));
   }
   // Never NaN, and not negative: as an integer in the order of its value.
   amax = __builtin_bit_cast(float, __builtin_amdgcn_readlane(wave_scan_max(__builtin_bit_cast(int, amax)), 63));
-  float s = s0 > 0 ? *scale : 0.f;
-  if (!(s > 0.f) || __builtin_isinf(s)) s = 0.f;
-  float s_new = s;
-  if (s0 == 0 || amax > 448.f * s) {
-    s_new = amax / 448.f;
-    // The page's earlier rows, at the new scale.
+  const bool grows = s0 == 0 || amax > 448.f * s;
+  const float s_new = grows ? amax / 448.f : s;
+  if (grows && s0 > 0) {
+    // The page's earlier rows, at the new scale: four lanes a row.
     const float ratio = s > 0.f ? s / s_new : 0.f;
+    const int t = lane >> 2;
     if (t < s0) {
       constexpr int N = D / 64;   // 16-byte loads of a quarter row
-      u32x4* rp = (u32x4*)(page + (int64_t)t * p.stride_slot + c * (D / 4));
+      u32x4* rp = (u32x4*)(page + (int64_t)t * p.stride_slot + (lane & 3) * (D / 4));
       u32x4 w[N];
 #pragma unroll
       for (int i = 0; i < N; ++i) w[i] = rp[i];
@@ -274,32 +313,39 @@ __device__ __forceinline__ void write_page(const RotaryParams& p, const void* x,
       }
     }
   }
-  char* row = page + (int64_t)t * p.stride_slot;
-  auto put = [&](int ch, const float* f) {
+  // x num / den, correctly rounded: a quotient by the rounded reciprocal, corrected by its
+  // remainder (exact with a correctly rounded reciprocal); by division where the
+  // reciprocal would overflow.
+  const float num = grows ? 448.f : 1.f, den = grows ? amax : s;
+  const bool small = den < 0x1p-100f;
+  const float inv = 1.f / den;
+  auto quotient = [&](float f) {
+    const float n = f * num;
+    if (small) return n / den;
+    const float q = n * inv;
+    return __builtin_fmaf(__builtin_fmaf(-den, q, n), inv, q);
+  };
+#pragma unroll
+  for (int j = 0; j < kN; ++j) {
+    const int t = t0 + kStep * j;
+    if (t < s0 || t >= s0 + m) continue;
     u32x2 w = {0u, 0u};
     if (s_new > 0.f) {
 #pragma unroll
       for (int i = 0; i < 2; ++i)
-        w[i] = e4m3x2(f[4 * i] / s_new, f[4 * i + 1] / s_new) | e4m3x2(f[4 * i + 2] / s_new, f[4 * i + 3] / s_new) << 16;
+        w[i] = e4m3x2(quotient(v[j][4 * i]), quotient(v[j][4 * i + 1])) |
+               e4m3x2(quotient(v[j][4 * i + 2]), quotient(v[j][4 * i + 3])) << 16;
     }
-    *(u32x2*)(row + 8 * ch) = w;
-  };
-#pragma unroll
-  for (int j = 0; j < MU; ++j) {
-    const int u = c + 4 * j;
-    if (!mine || u >= U) continue;
-    const int ch = TURN ? unit_chunk<IL>(p, u) : u;
-    put(ch, v[j][0]);
-    if (TURN && !IL && unit_turns<IL>(p, u)) put(ch + h8, v[j][1]);
+    *(u32x2*)(page + (int64_t)t * p.stride_slot + 8 * c) = w;
   }
   if (lane == 0) *scale = s_new;
 }
 
-template <int D, KvKind KIND, bool IL>
+template <int D, KvKind KIND, bool IL, bool STREAM>
 __global__ __launch_bounds__(kThreads) void append_rotary_kernel(const RotaryParams p) {
   constexpr bool F32 = KIND == KvKind::F32, FP8 = KIND == KvKind::FP8;
   constexpr int E = F32 ? 4 : 2;
-  extern __shared__ float2 s_cs[];   // [kWin, fp8 caches and several rows a sequence: kWinRows][half]
+  extern __shared__ float2 s_cs[];   // [win, fp8 caches and several rows a sequence: win + 15][half]
   __shared__ int32_t s_pos[kWinRows];   // position of the row (its angle)
   __shared__ int32_t s_tok[kWinRows];   // token of its sequence
   __shared__ int32_t s_seq[kWinRows];
@@ -308,10 +354,23 @@ __global__ __launch_bounds__(kThreads) void append_rotary_kernel(const RotaryPar
   __shared__ uint8_t s_ok[kWinRows];    // the row belongs to a sequence and has a position
   __shared__ int32_t s_n;
   const int tid = threadIdx.x, lane = tid & 63, wave = uni(tid >> 6);
-  const int win = blockIdx.x / p.parts, part = blockIdx.x - win * p.parts;
-  const int first = win * kWin, n = min(kWin, p.rows - first);
+  // fp8 caches: a window's workgroups from p.parts on write pages, the others turn q.  They
+  // run together: a token's q, k and v lie behind one another, and read far apart in time
+  // they cost 10 to 20 us of 150 (27,700 rows of 40/8 heads).
+  //   Blocks go round the 8 XCDs, so a window's roles move on by one from window to window:
+  // fixed, they would all be on some of them where their number and 8 share a factor
+  // (3 and 1 of them 174 us, 3 and 2 143).
+  const int all_parts = p.parts + p.page_parts;
+  const int win = blockIdx.x / all_parts, turn_part = (int)((blockIdx.x + (uint32_t)win) % (uint32_t)all_parts);
+  const bool pages = FP8 && turn_part >= p.parts;
+  const int part = turn_part - (pages ? p.parts : 0), parts = pages ? p.page_parts : p.parts;
+  const int first = win * p.win, n = min(p.win, p.rows - first);
   const int cap = p.max_pages * kPage;
-  const int span = FP8 && p.q_start ? min(kWinRows, p.rows - first) : n;   // rows described here
+  const int span = pages && p.q_start ? min(p.win + kPage - 1, p.rows - first) : n;   // rows described here
+  const int total = n * p.hq * p.units, step = parts * kThreads;
+  int i = part * kThreads + tid;
+  Units<F32, IL, STREAM> x;
+  if (!pages) x.fetch(p, p.q, p.q_rs, p.q_hs, first, total, p.hq, p.magic_qu, i, step);
 
   // 1. Every row's sequence, token, position and slot.
   if (wave == 0) {
@@ -362,12 +421,12 @@ __global__ __launch_bounds__(kThreads) void append_rotary_kernel(const RotaryPar
       s_pid[lane] = pid;
       s_pos[lane] = ok ? (p.positions ? p.positions[r] : tok) : 0;
     }
-    // The rows that this window's pages reach to: row i >= 16 continues a page when it is
-    // in the sequence and the page of row 15 (and so on from there).
+    // The rows that this window's pages reach to: a row behind the window continues a page
+    // when it is in the sequence and the page of the window's last row.
     if (lane == 0) s_n = n;
-    if (FP8 && span > kWin) {
-      const int b15 = __builtin_amdgcn_readlane(b, kWin - 1), t15 = __builtin_amdgcn_readlane(tok, kWin - 1);
-      const bool on = ok && b == b15 && t15 >= 0 && lane >= kWin && tok / kPage == t15 / kPage;
+    if (FP8 && span > n) {
+      const int bl = __builtin_amdgcn_readlane(b, n - 1), tl = __builtin_amdgcn_readlane(tok, n - 1);
+      const bool on = ok && b == bl && tl >= 0 && lane >= n && tok / kPage == tl / kPage;
       const uint64_t m = __builtin_amdgcn_ballot_w64(on);
       if (lane == 0) s_n = n + __builtin_popcountll(m);
     }
@@ -376,84 +435,95 @@ __global__ __launch_bounds__(kThreads) void append_rotary_kernel(const RotaryPar
     if (__builtin_amdgcn_ballot_w64((bad & kFlagBadPage) != 0) && part == 0 && lane == 0) atomicOr(p.flags, kFlagBadPage);
   }
   __syncthreads();
-  angles(p, s_pos, uni(s_n), s_cs);
+  if constexpr (FP8) {
+    if (pages) {
+      // 2. The pages whose first new row is in the window.  A row starts a page when its
+      //    token is the page's first, or its sequence's first new one.
+      const int r = lane;
+      const bool here = r < n && s_ok[r];
+      const bool start = here && (s_tok[r] % kPage == 0 || !p.q_start || first + r == p.q_start[s_seq[r]]);
+      const uint64_t starts = __builtin_amdgcn_ballot_w64(start);
+      if (starts == 0) return;
+      const int jobs = __builtin_popcountll(starts) * 2 * p.hkv;
+      const int all = uni(s_n);
+      angles(p, s_pos, all, s_cs);
+      __syncthreads();
+      for (int j = part * kWaves + wave; j < jobs; j += parts * kWaves) {
+        int k = j / (2 * p.hkv);
+        const int gw = j - k * 2 * p.hkv, g = gw >> 1;
+        uint64_t m = starts;
+        for (; k > 0; --k) m &= m - 1;
+        const int r0 = __builtin_ctzll(m), s0 = uni(s_tok[r0]) % kPage;
+        int rows = 1;   // rows of the page: as many as follow in it
+        while (r0 + rows < all && s0 + rows < kPage && s_ok[r0 + rows] && s_seq[r0 + rows] == s_seq[r0]) ++rows;
+        rows = uni(rows);
+        const int pid = uni(s_pid[r0]);
+        if ((uint32_t)pid >= (uint32_t)p.num_pages) continue;
+        const int64_t at = (int64_t)pid * p.stride_page + (int64_t)g * p.stride_head;
+        const int64_t si = (int64_t)pid * p.hkv + g;
+        if (gw & 1)
+          write_page<D, IL, false>(p, p.v_in, p.v_rs, p.v_hs, first, r0, rows, s0, g, (char*)p.v + at, p.v_scale + si, s_cs, lane);
+        else
+          write_page<D, IL, true>(p, p.k_in, p.k_rs, p.k_hs, first, r0, rows, s0, g, (char*)p.k + at, p.k_scale + si, s_cs, lane);
+      }
+      return;
+    }
+  }
+  angles(p, s_pos, n, s_cs);
   __syncthreads();
 
-  // 2. q, and K and V rows of caches that hold them as they are.
-  turn_rows<F32, IL>(p, p.q, p.q_rs, p.q_hs, first, n, p.hq, p.magic_qu, part, s_ok, s_cs,
-                     [&](int r, int hd, int c, const Chunk<F32>& v) {
-                       v.store((char*)p.q_out + ((int64_t)(first + r) * p.o_rs + (int64_t)hd * p.o_hs + 8 * c) * E);
-                     });
+  // 3. q, and K and V rows of caches that hold them as they are.
+  for (;;) {
+    x.finish(p, s_ok, s_cs, [&](int r, int hd, int c, const Chunk<F32>& v) {
+      v.store((char*)p.q_out + ((int64_t)(first + r) * p.o_rs + (int64_t)hd * p.o_hs + 8 * c) * E);
+    });
+    i += kUnroll * step;
+    if (i >= total) break;
+    x.fetch(p, p.q, p.q_rs, p.q_hs, first, total, p.hq, p.magic_qu, i, step);
+  }
   if constexpr (!FP8) {
-    turn_rows<F32, IL>(p, p.k_in, p.k_rs, p.k_hs, first, n, p.hkv, p.magic_ku, part, s_ok, s_cs,
-                       [&](int r, int g, int c, const Chunk<F32>& v) {
-                         if (s_off[r] >= 0) v.store((char*)p.k + s_off[r] + (int64_t)g * p.stride_head + 8 * c * E);
-                       });
+    const int ktotal = n * p.hkv * p.units;
+    for (i = part * kThreads + tid; i < ktotal; i += kUnroll * step) {
+      x.fetch(p, p.k_in, p.k_rs, p.k_hs, first, ktotal, p.hkv, p.magic_ku, i, step);
+      x.finish(p, s_ok, s_cs, [&](int r, int g, int c, const Chunk<F32>& v) {
+        if (s_off[r] >= 0) v.store((char*)p.k + s_off[r] + (int64_t)g * p.stride_head + 8 * c * E);
+      });
+    }
     constexpr int NC = D / 8;
-    const int total = n * p.hkv * NC;
-    for (int i = part * kThreads + tid; i < total; i += p.parts * kThreads) {
+    const int vtotal = n * p.hkv * NC;
+    for (i = part * kThreads + tid; i < vtotal; i += step) {
       const int c = i % NC, rg = i / NC, r = rg / p.hkv, g = rg - r * p.hkv;
       if (!s_ok[r] || s_off[r] < 0) continue;
       Chunk<F32> v;
       v.load(p.v_in, (int64_t)(first + r) * p.v_rs + (int64_t)g * p.v_hs + 8 * c);
       v.store((char*)p.v + s_off[r] + (int64_t)g * p.stride_head + 8 * c * E);
     }
-  } else {
-    // 3. fp8: the pages whose first new row is in the window.  A row starts a page when its
-    //    token is the page's first, or its sequence's first new one.
-    const int r = lane;
-    const bool here = r < n && s_ok[r];
-    const bool start = here && (s_tok[r] % kPage == 0 || !p.q_start || first + r == p.q_start[s_seq[r]]);
-    const uint64_t starts = __builtin_amdgcn_ballot_w64(start);
-    const int jobs = __builtin_popcountll(starts) * 2 * p.hkv;
-    const int all = uni(s_n);
-    for (int j = part * kWaves + wave; j < jobs; j += p.parts * kWaves) {
-      int k = j / (2 * p.hkv);
-      const int gw = j - k * 2 * p.hkv, g = gw >> 1;
-      uint64_t m = starts;
-      for (; k > 0; --k) m &= m - 1;
-      const int r0 = __builtin_ctzll(m), s0 = uni(s_tok[r0]) % kPage;
-      int rows = 1;   // rows of the page: as many as follow in it
-      while (r0 + rows < all && s0 + rows < kPage && s_ok[r0 + rows] && s_seq[r0 + rows] == s_seq[r0]) ++rows;
-      rows = uni(rows);
-      const int pid = uni(s_pid[r0]);
-      if ((uint32_t)pid >= (uint32_t)p.num_pages) continue;
-      const int64_t at = (int64_t)pid * p.stride_page + (int64_t)g * p.stride_head;
-      const int64_t si = (int64_t)pid * p.hkv + g;
-      if (gw & 1)
-        write_page<D, IL, false>(p, p.v_in, p.v_rs, p.v_hs, first, r0, rows, s0, g, (char*)p.v + at, p.v_scale + si, s_cs, lane);
-      else
-        write_page<D, IL, true>(p, p.k_in, p.k_rs, p.k_hs, first, r0, rows, s0, g, (char*)p.k + at, p.k_scale + si, s_cs, lane);
-    }
   }
 }
 
 template <int D, KvKind KIND>
 int launch_append_rotary_t(const RotaryParams& p, hipStream_t st) {
-  const int grid = (p.rows + kWin - 1) / kWin * p.parts;
-  const size_t lds = sizeof(float2) * p.half * (KIND == KvKind::FP8 && p.q_start ? kWinRows : kWin);
-  if (p.interleaved)
-    hipLaunchKernelGGL((append_rotary_kernel<D, KIND, true>), dim3(grid), dim3(kThreads), lds, st, p);
-  else
-    hipLaunchKernelGGL((append_rotary_kernel<D, KIND, false>), dim3(grid), dim3(kThreads), lds, st, p);
+  constexpr bool FP8 = KIND == KvKind::FP8;
+  const int grid = (p.rows + p.win - 1) / p.win * (p.parts + p.page_parts);
+  const int rows = FP8 && p.q_start ? p.win + kPage - 1 : p.win;
+  auto* const kernel = p.interleaved ? (p.stream ? append_rotary_kernel<D, KIND, true, true> : append_rotary_kernel<D, KIND, true, false>)
+                                     : (p.stream ? append_rotary_kernel<D, KIND, false, true> : append_rotary_kernel<D, KIND, false, false>);
+  hipLaunchKernelGGL(kernel, dim3(grid), dim3(kThreads), sizeof(float2) * p.half * rows, st, p);
+  return (int)hipGetLastError();
+}
+
+template <bool F32>
+int launch_rotate_t(const RotaryParams& p, hipStream_t st) {
+  auto* const kernel = p.interleaved ? (p.stream ? rotate_kernel<F32, true, true> : rotate_kernel<F32, true, false>)
+                                     : (p.stream ? rotate_kernel<F32, false, true> : rotate_kernel<F32, false, false>);
+  hipLaunchKernelGGL(kernel, dim3((p.rows + p.win - 1) / p.win * p.parts), dim3(kThreads), sizeof(float2) * p.half * p.win, st, p);
   return (int)hipGetLastError();
 }
 
 }  // namespace
 
 int launch_rotate(bool f32, const RotaryParams& p, void* stream) {
-  const hipStream_t st = (hipStream_t)stream;
-  const int grid = (p.rows + kWin - 1) / kWin * p.parts;
-  const size_t lds = sizeof(float2) * p.half * kWin;
-  if (f32 && p.interleaved)
-    hipLaunchKernelGGL((rotate_kernel<true, true>), dim3(grid), dim3(kThreads), lds, st, p);
-  else if (f32)
-    hipLaunchKernelGGL((rotate_kernel<true, false>), dim3(grid), dim3(kThreads), lds, st, p);
-  else if (p.interleaved)
-    hipLaunchKernelGGL((rotate_kernel<false, true>), dim3(grid), dim3(kThreads), lds, st, p);
-  else
-    hipLaunchKernelGGL((rotate_kernel<false, false>), dim3(grid), dim3(kThreads), lds, st, p);
-  return (int)hipGetLastError();
+  return f32 ? launch_rotate_t<true>(p, (hipStream_t)stream) : launch_rotate_t<false>(p, (hipStream_t)stream);
 }
 
 int launch_append_rotary(KvKind kind, int head_dim, const RotaryParams& p, void* stream) {

@@ -303,7 +303,9 @@ def check(torch, c, freqs, before, q, interleaved, amplitude, positions=None):
                     room = np.maximum(2.0 ** -4 * np.abs(x), 2.0 ** -10 * float(s_new)) * 1.0001 + tol[mine, g] + 1e-6 * np.abs(x)
                     assert (np.abs(got - x) <= room).all(), (name, p, g, np.max(np.abs(got - x) - room))
                 else:
-                    e = e4m3_encode((x.astype(np.float32) / s_new).astype(np.float32)) if s_new > 0 else np.zeros_like(code)
+                    # Rows that set the scale: 448 x / amax (448 x is exact), else x / scale.
+                    f = x.astype(np.float32)
+                    e = e4m3_encode(np.float32(448) * f / amax if grew else f / s_new) if s_new > 0 else np.zeros_like(code)
                     assert np.array_equal(code, e), (name, p, g)
 
 
@@ -333,6 +335,25 @@ def test_append_rotary(torch, kv, d, rows):
 
 
 @pytest.mark.parametrize("kv", ["bf16", "fp8"])
+@pytest.mark.parametrize("n", [2100, 4300, 9000, 17000])
+def test_append_rotary_windows(torch, kv, n):
+    """Enough rows for windows of 2, 4, 8 and 16, cut into sequences of any length."""
+    from paper_2607_09207_amd import rotary_frequencies
+    rng = np.random.default_rng(n)
+    rows = []
+    while sum(rows) < n:
+        rows.append(int(rng.choice([0, 1, 2, 15, 16, 17, 40, 333, 900])))
+    lens = [m + int(rng.integers(0, 40)) for m in rows]
+    say("windows", kv, n, len(rows))
+    c = Case(torch, kv, 4, 2, 64, lens, rows, seed=n, lead=1, behind=2)
+    freqs, _ = rotary_frequencies([64, 32, 48, 16][n % 4], 1e4)
+    before = {x: None if getattr(c, x) is None else getattr(c, x).clone() for x in ("k", "v", "ks", "vs")}
+    q = c.run(freqs)
+    check(torch, c, freqs, before, q, False, 1.0)
+    assert c.layer.read_flags(device=c.q.device) == 0
+
+
+@pytest.mark.parametrize("kv", ["bf16", "fp8"])
 def test_rows_of_nobody_stay(torch, kv):
     """q_start that begins after row 0 and ends before the last row; given positions; q in place."""
     from paper_2607_09207_amd import rotary_frequencies
@@ -352,7 +373,8 @@ def test_rows_of_nobody_stay(torch, kv):
 
 @pytest.mark.parametrize("kv", ["bf16", "fp8"])
 def test_one_token_is_append(torch, kv):
-    """At position 0 nothing turns: the caches and scales append leaves, bit for bit."""
+    """At position 0 nothing turns: the caches and scales append leaves, bit for bit, but for
+    fp8 values halfway between two codes (append rounds value / scale in between)."""
     from paper_2607_09207_amd import rotary_frequencies
     a, b = (Case(torch, kv, 12, 2, 128, LENS1, None, seed=9) for _ in range(2))
     freqs, _ = rotary_frequencies(128)
@@ -361,9 +383,20 @@ def test_one_token_is_append(torch, kv):
     b.layer.append(b.k_new.contiguous(), b.v_new.contiguous(), b.k, b.v, b.block_table, b.seq_lens, k_scale=b.ks, v_scale=b.vs)
     live = torch.tensor([x > 0 for x in LENS1], device="cuda")
     assert torch.equal(q[live], a.q[live])
-    for x in ("k", "v", "ks", "vs"):
-        if getattr(a, x) is not None:
-            assert np.array_equal(raw(getattr(a, x)), raw(getattr(b, x))), x
+    if kv == "fp8":
+        assert torch.equal(a.ks, b.ks) and torch.equal(a.vs, b.vs)
+    for x in ("k", "v"):
+        ra, rb = raw(getattr(a, x)), raw(getattr(b, x))
+        if kv == "bf16":
+            assert np.array_equal(ra, rb), x
+            continue
+        for p, g, s, e in np.argwhere(ra != rb):
+            seq, tok = next((i, t) for _, i, t in a.tokens() if a.table[i, t // PAGE] == p)
+            row = np64(getattr(a, x + "_new"))[seq, g]
+            assert s == tok % PAGE, "an earlier row differs"
+            mid = (e4m3_decode(ra[p, g, s, e]) + e4m3_decode(rb[p, g, s, e])) / 2
+            assert abs(int(ra[p, g, s, e]) - int(rb[p, g, s, e])) == 1
+            assert abs(row[e] * 448 / np.abs(row).max() - mid) <= 2.0 ** -22 * abs(mid), "not halfway between two codes"
 
 
 @pytest.mark.parametrize("kv", ["bf16", "fp8"])
