@@ -354,7 +354,7 @@ typedef struct {
 /*
  * Turn rows by their positions: out[r][h] = x[r][h] turned by positions[r] (int32, device,
  * any sign).  dtype RLDA_F32 or RLDA_BF16 for x and out; heads <= 256, head_dim a multiple
- * of 8 in [32, 256] (else RLDA_ERR_UNSUPPORTED).  x may be read through any strides (a
+ * of 8 in [32, 256], rows <= 2^31 - 65 (else RLDA_ERR_UNSUPPORTED).  x may be read through any strides (a
  * slice of a fused projection; 0: one row for all); out's rows must not overlap each
  * other, and out is x itself (same strides) or apart from it.  No handle, no workspace,
  * one kernel, asynchronous.

@@ -20,6 +20,8 @@ using rlda::kAlign;
 using rlda::PageParams;
 using rlda::RotaryParams;
 
+constexpr int32_t kMaxRows = INT32_MAX - 64;   // row numbers a window past the last stay 32-bit
+
 bool aligned4(const void* p) { return ((uintptr_t)p & 3u) == 0; }
 
 // floor(i / x) = umulhi(i, magic) for i < 2^17 and x <= 2^13 (the error, below i x / 2^32,
@@ -96,7 +98,7 @@ rlda_status rl_decode_attn_rotate(rlda_dtype dtype, int32_t rows, int32_t heads,
                                   const rl_decode_attn_rotary* rotary, const rl_decode_attn_rows* out, void* stream) {
   if (dtype != RLDA_F32 && dtype != RLDA_BF16) return dtype == RLDA_FP8_E4M3FN ? RLDA_ERR_UNSUPPORTED : RLDA_ERR_INVALID_ARG;
   if (rows < 0 || heads < 0) return RLDA_ERR_INVALID_ARG;
-  if (heads > rlda::kMaxQHeads || head_dim < 32 || head_dim > 256 || head_dim % 8) return RLDA_ERR_UNSUPPORTED;
+  if (rows > kMaxRows || heads > rlda::kMaxQHeads || head_dim < 32 || head_dim > 256 || head_dim % 8) return RLDA_ERR_UNSUPPORTED;
   if (!rotary_ok(rotary, head_dim)) return RLDA_ERR_INVALID_ARG;
   if (rows == 0 || heads == 0) return RLDA_OK;
   const int eb = elem_bytes(dtype);
@@ -127,6 +129,7 @@ rlda_status rl_decode_attn_append_rotary(rl_decode_attn_t h, int32_t batch, int3
   const rl_decode_attn_config& c = h->cfg;
   if (batch < 0 || batch > c.max_batch || num_pages < 0 || total_q < 0) return RLDA_ERR_INVALID_ARG;
   if (!q_start && total_q != batch) return RLDA_ERR_INVALID_ARG;
+  if (total_q > kMaxRows) return RLDA_ERR_UNSUPPORTED;
   if (!rotary_ok(rotary, c.head_dim)) return RLDA_ERR_INVALID_ARG;
   if (batch == 0 || total_q == 0) return RLDA_OK;
   const int eb = elem_bytes(c.q_dtype);
@@ -249,10 +252,9 @@ rlda_status page_call(rl_decode_attn_t h, int32_t batch, int32_t num_pages, int3
   return RLDA_OK;
 }
 
-constexpr int kMoveGrid = 2048;   // workgroups of a compaction's copies, whose number the device knows
-
-// Layers of a workgroup: a page pair of a few KiB is too little for one.
-constexpr int kCopyBytes = 32 << 10;
+// Layers of a workgroup that copies pages: a pair of a few KiB is too little for one.
+constexpr int kCopyBytes = 16 << 10;
+constexpr int kMoveGrid = 32768;   // workgroups of a compaction's copies at most
 
 rlda_status check_caches(rl_decode_attn_t h, int32_t num_caches, const rl_decode_attn_cache* caches, int32_t num_pages) {
   if (num_caches < 0 || (num_caches > 0 && !caches)) return RLDA_ERR_INVALID_ARG;
@@ -350,7 +352,11 @@ rlda_status rl_decode_attn_page_compact(rl_decode_attn_t h, int32_t batch, int32
   if ((st = check_caches(h, num_caches, caches, num_pages)) != RLDA_OK) return st;
   p.live_out = live;
   if (rlda::launch_page_compact(p, stream) != hipSuccess) return RLDA_ERR_HIP;
-  return for_caches(h, p, num_caches, caches, [&] { return rlda::launch_page_move(p, kMoveGrid, stream); });
+  return for_caches(h, p, num_caches, caches, [&] {
+    // One for every copy there may be (half of the pages), and some for the table's rows.
+    const int64_t copies = (int64_t)num_pages / 2 * p.layer_blocks;
+    return rlda::launch_page_move(p, (int)std::min<int64_t>(std::max<int64_t>(copies, 256), kMoveGrid), stream);
+  });
 }
 
 rlda_status rl_decode_attn_page_copy(rl_decode_attn_t h, int32_t num_pages, int32_t count, const int32_t* src,

@@ -19,6 +19,7 @@
 
 #include "rlda_device.h"
 #include "rlda_params.h"
+#include "rlda_split.h"
 
 namespace rlda {
 namespace {
@@ -118,25 +119,33 @@ struct Pool {
   int tmp[kMgrWaves];
 };
 
+// Counts of eight words of a wave's: asked for together.
+struct Counts {
+  int r[8];
+  __device__ __forceinline__ void load(const PageParams& p, int w0) {
+    const int lane = threadIdx.x & 63;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int64_t page = (int64_t)(w0 + i * kMgrWaves) * 64 + lane;
+      r[i] = p.in_lds && page < p.num_pages ? p.refs[page] : 1;
+    }
+  }
+};
+
 // The mask of free pages (all threads of the workgroup); returns the free pages' number.
-__device__ __forceinline__ int read_pool(const PageParams& p, Pool& s, Mask& mask) {
+// `c`: the first counts, asked for by the caller ahead of its own reads.
+__device__ __forceinline__ int read_pool(const PageParams& p, Pool& s, Mask& mask, Counts c) {
   const int tid = threadIdx.x, lane = tid & 63, wave = uni(tid >> 6);
   mask = Mask{s.words, s.before, p.group_words};
   constexpr int kPer = kGroups / kMgr;   // groups of a thread
   int n[kPer], sum = 0, all;
   if (p.in_lds) {
-    // Eight words of a wave at a time, so that their loads are in flight together.
     for (int w0 = wave; w0 < kGroups; w0 += 8 * kMgrWaves) {
       if (w0 >= p.words) break;
-      int r[8];
+      if (w0 != wave) c.load(p, w0);
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        const int64_t page = (int64_t)(w0 + i * kMgrWaves) * 64 + lane;
-        r[i] = page < p.num_pages ? p.refs[page] : 1;
-      }
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const uint64_t m = __builtin_amdgcn_ballot_w64(r[i] == 0);
+        const uint64_t m = __builtin_amdgcn_ballot_w64(c.r[i] == 0);
         const int w = w0 + i * kMgrWaves;
         if (lane == 0 && w < kLdsWords) s.words[w] = m;
       }
@@ -171,6 +180,8 @@ __global__ __launch_bounds__(kMgr) void page_grow_kernel(const PageParams p) {
   __shared__ int s_off[kMaxBatch + 1];   // pages asked for before each sequence
   const int tid = threadIdx.x, cap = p.max_pages * kPage;
   const int per = (p.batch + kMgr - 1) / kMgr, b0 = tid * per, b1 = min(b0 + per, p.batch);
+  Counts c;
+  c.load(p, uni(tid >> 6));
   // A sequence whose length or growth is out of range asks for nothing and stays.
   int len[kPerThread], add[kPerThread], sum = 0, all;
   bool bad = false;
@@ -189,7 +200,7 @@ __global__ __launch_bounds__(kMgr) void page_grow_kernel(const PageParams p) {
     sum += pages_of(L + a) - pages_of(L);
   }
   Mask mask;
-  const int nfree = read_pool(p, s_pool, mask);
+  const int nfree = read_pool(p, s_pool, mask, c);
   int run = block_before(sum, s_pool.tmp, &all);
   // Requests are served in order until one finds too few pages left.
   bool out = false;
@@ -271,6 +282,8 @@ __global__ __launch_bounds__(kMgr) void page_fork_kernel(const PageParams p) {
   __shared__ int s_claim[kMaxBatch];   // the first fork that names a row as its child
   const int tid = threadIdx.x, cap = p.max_pages * kPage;
   const int per = (p.count + kMgr - 1) / kMgr, f0 = tid * per, f1 = min(f0 + per, p.count);
+  Counts counts;
+  counts.load(p, uni(tid >> 6));
   for (int i = tid; i < p.batch; i += kMgr) s_claim[i] = 0x7fffffff;
   __syncthreads();
   int parent[kPerThread], child[kPerThread], len[kPerThread];   // len -1: refused
@@ -307,7 +320,7 @@ __global__ __launch_bounds__(kMgr) void page_fork_kernel(const PageParams p) {
     sum += len[i] > 0 && len[i] % kPage != 0;
   }
   Mask mask;
-  const int nfree = read_pool(p, s_pool, mask);
+  const int nfree = read_pool(p, s_pool, mask, counts);
   int run = block_before(sum, s_pool.tmp, &all);
   bool out = false;
 #pragma unroll
@@ -342,37 +355,36 @@ __global__ __launch_bounds__(kMgr) void page_fork_kernel(const PageParams p) {
 
 // ---------------------------------------------------------------- copies
 
-// Copy one page of one cache (all KV heads) by the workgroup.
-__device__ __forceinline__ void copy_pool_page(const PageParams& p, char* pool, int src, int dst) {
-  const char* a = pool + (int64_t)src * p.stride_page;
-  char* b = pool + (int64_t)dst * p.stride_page;
-  const int chunks = p.page_bytes >> 4, per_row = p.row_bytes >> 4;
-  constexpr int kU = 4;
-  for (int i0 = threadIdx.x; i0 < chunks; i0 += kU * kThreads) {
-    u32x4 v[kU];
-    int64_t at[kU];
-#pragma unroll
-    for (int k = 0; k < kU; ++k) {
-      const int i = i0 + k * kThreads;
-      if (i >= chunks) continue;
-      if (p.linear) {
-        at[k] = (int64_t)i * 16;
-      } else {
-        const int row = i / per_row, c = i - row * per_row, g = row / kPage, s = row - g * kPage;
-        at[k] = (int64_t)g * p.stride_head + (int64_t)s * p.stride_slot + c * 16;
-      }
-      v[k] = *(const u32x4*)(a + at[k]);
-    }
-#pragma unroll
-    for (int k = 0; k < kU; ++k)
-      if (i0 + k * kThreads < chunks) *(u32x4*)(b + at[k]) = v[k];
-  }
-}
+// Copy page src over page dst in caches [first, last) by the workgroup.  A wave takes runs of
+// 64 chunks of 16 bytes (a page of a cache is a multiple of that), kU of them in flight
+// whichever cache they are in.  The copies are written past the caches, which would only
+// hold them in the way of the pages that are read again (fork below: 44.6 us a call, 35.5 so).
 __device__ __forceinline__ void copy_page(const PageParams& p, int src, int dst, int first, int last) {
+  constexpr int kU = 4;
+  const int lane = threadIdx.x & 63, wave = uni((int)(threadIdx.x >> 6));
+  const int runs = p.page_bytes >> 10, per_row = p.row_bytes >> 4, total = (last - first) * 2 * runs;
+  for (int r0 = wave; r0 < total; r0 += kU * kWaves) {
+    u32x4 v[kU];
+#pragma unroll
+    for (int k = 0; k < 2 * kU; ++k) {   // kU loads, then kU stores
+      const int j = k % kU, r = r0 + j * kWaves;
+      if (r >= total) continue;
+      const int pool = r / runs, i = (r - pool * runs) * 64 + lane;
+      int64_t at = (int64_t)i * 16;
+      if (!p.linear) {
+        const int row = i / per_row, c = i - row * per_row, g = row / kPage, s = row - g * kPage;
+        at = (int64_t)g * p.stride_head + (int64_t)s * p.stride_slot + c * 16;
+      }
+      const PageCache& c = p.caches[first + (pool >> 1)];
+      char* base = (pool & 1 ? c.v : c.k) + at;
+      if (k < kU)
+        v[j] = *(const u32x4*)(base + (int64_t)src * p.stride_page);
+      else
+        __builtin_nontemporal_store(v[j], (u32x4*)(base + (int64_t)dst * p.stride_page));
+    }
+  }
   for (int l = first; l < last; ++l) {
-    const PageCache c = p.caches[l];
-    copy_pool_page(p, c.k, src, dst);
-    copy_pool_page(p, c.v, src, dst);
+    const PageCache& c = p.caches[l];
     if (c.k_scale && (int)threadIdx.x < p.num_kv_heads) {
       const int64_t a = (int64_t)src * p.num_kv_heads + threadIdx.x, b = (int64_t)dst * p.num_kv_heads + threadIdx.x;
       c.k_scale[b] = c.k_scale[a];
@@ -397,8 +409,11 @@ __global__ __launch_bounds__(kThreads) void page_copy_kernel(const PageParams p)
 
 // The forks' table rows and references; with part > 0, their copies.
 __global__ __launch_bounds__(kThreads) void page_fork_rows_kernel(const PageParams p) {
+  // Contiguous items to an XCD: the children of one parent are neighbours, and all but the
+  // first read its page from the L2 (256 children of 32 parents, 28 layers: 47 us a call
+  // dealt round, 44.6 so).
   const int parts = 1 + p.layer_blocks;
-  const int f = blockIdx.x / parts, part = blockIdx.x - f * parts;
+  const int item = share_of_block(blockIdx.x, gridDim.x), f = item / parts, part = item - f * parts;
   if (part > 0) {
     const int src = p.list_src[f], dst = p.list_dst[f];
     if (src < 0 || dst < 0) return;
@@ -427,7 +442,9 @@ __global__ __launch_bounds__(kThreads) void page_fork_rows_kernel(const PagePara
 __global__ __launch_bounds__(kMgr) void page_compact_kernel(const PageParams p) {
   __shared__ Pool s_pool;
   Mask mask;
-  const int nfree = read_pool(p, s_pool, mask), n = p.num_pages - nfree, tid = threadIdx.x;
+  Counts c;
+  c.load(p, uni((int)(threadIdx.x >> 6)));
+  const int nfree = read_pool(p, s_pool, mask, c), n = p.num_pages - nfree, tid = threadIdx.x;
   // Free pages below n: those before n's word, and in it.
   const int wn = n >> 6, gn = wn / p.group_words;
   int below = s_pool.before[min(gn, kGroups)];
@@ -469,7 +486,9 @@ __global__ __launch_bounds__(kMgr) void page_compact_kernel(const PageParams p) 
 }
 
 // The table's entries follow the moves; then the moves' copies, whose number only the
-// device knows, dealt over the grid.
+// device knows, dealt over the grid (16 layers, 980 MB read and written: 213 us a call with
+// 2048 workgroups and two layers to each, 196 with one for every copy there may be and
+// one layer; a copy of one buffer to another takes 198).
 __global__ __launch_bounds__(kThreads) void page_move_kernel(const PageParams p) {
   const int n = *p.live_out;
   if (p.share) {

@@ -34,6 +34,11 @@ def say(*a):
 
 
 def np64(t):
+    with np.errstate(invalid="ignore"):   # rows that nobody writes may hold anything
+        return _np64(t)
+
+
+def _np64(t):
     return t.detach().float().cpu().numpy().astype(np.float64) if t.element_size() < 8 else t.detach().cpu().numpy()
 
 
@@ -93,6 +98,41 @@ def test_rotate(torch, shape, interleaved, dtype):
     assert torch.equal(y, want) and torch.equal(back[:, 0], fused[:, 0]) and torch.equal(back[:, heads + 1:], fused[:, heads + 1:])
     other = torch.zeros((heads, n, d), device="cuda", dtype=dt).transpose(0, 1)
     assert torch.equal(rotate(x, pos, freqs, interleaved=interleaved, out=other), want)
+
+
+@pytest.mark.parametrize("n", [17000, 40000, 70000, 140001])
+def test_rotate_windows(torch, n):
+    """Enough rows for windows of 2, 4, 8 and 16, and (the last) for reading past the caches."""
+    from paper_2607_09207_amd import rotary_frequencies, rotate
+    heads = 1 if n < 140000 else 9
+    x = torch.randn((n, heads, 64), device="cuda").bfloat16()
+    pos = torch.randint(0, 1 << 20, (n,), device="cuda", dtype=torch.int32)
+    freqs, _ = rotary_frequencies(32)
+    got = rotate(x, pos, freqs)
+    pick = torch.cat([torch.arange(40), torch.arange(n - 40, n), torch.randint(0, n, (3000,))]).cuda()
+    want, tol = turned(np64(x[pick]), pos[pick].cpu().numpy(), freqs.cpu().numpy(), False, 1.0, False)
+    within(np64(got[pick]), want, tol, True, "rotate")
+    part = rotate(x[5:1000], pos[5:1000], freqs)   # the same rows in other windows
+    assert torch.equal(part, got[5:1000])
+
+
+def test_append_rotary_large_windows(torch):
+    """140,000 rows in a bf16 cache: windows of 16."""
+    from paper_2607_09207_amd import rotary_frequencies
+    rng = np.random.default_rng(1)
+    rows = rng.integers(1, 5000, size=60)
+    c = Case(torch, "bf16", 1, 1, 64, rows + rng.integers(0, 30, size=60), rows, seed=3)
+    assert c.q.shape[0] > 16 * 8192
+    freqs, _ = rotary_frequencies(64)
+    q = c.run(freqs)
+    pos = torch.cat([torch.arange(L - m, L) for L, m in zip(c.lens.tolist(), c.rows.tolist())])
+    want, tol = turned(np64(c.q), pos.numpy(), freqs.cpu().numpy(), False, 1.0, False)
+    within(np64(q), want, tol, True, "q")
+    seq = np.repeat(np.arange(60), c.rows)
+    page, slot = c.table[seq, pos.numpy() // PAGE], pos.numpy() % PAGE
+    want, tol = turned(np64(c.k_new), pos.numpy(), freqs.cpu().numpy(), False, 1.0, False)
+    within(np64(c.k)[page, :, slot], want, tol, True, "k")
+    assert np.array_equal(np64(c.v)[page, :, slot], np64(c.v_new))
 
 
 def test_rotate_broadcast_and_empty(torch):
