@@ -754,9 +754,11 @@ void multi_query_kernel(const Params p) {
         if (__builtin_amdgcn_ballot_w64(masked) != 0) {
           constexpr bool kDma = decltype(dma)::value;
           u16x2 top = {0, 0};
-#pragma unroll 2
-          for (int c = 0; c < D / 8; c += 2)   // two lanes a row
-            top = magnitude_max(top, *(const u32x4*)(s_v[buf] + (lane >> 1) * S::vrs(kDma) + 16 * (c + (lane & 1))));
+          // Whole rows at a time: no bank twice.
+          constexpr int NC = D / 8;
+          const char* at = s_v[buf] + lane / NC * S::vrs(kDma) + 16 * (lane % NC);
+#pragma unroll
+          for (int R = 0; R < kTile; R += 64 / NC) top = magnitude_max(top, *(const u32x4*)(at + R * S::vrs(kDma)));
           if (__builtin_amdgcn_ballot_w64(not_finite(top)) != 0) {
             char* row = s_v[buf] + (lane >> 1) * S::vrs(kDma);
 #pragma unroll 1

@@ -85,21 +85,38 @@ struct Chunk<true> {
   }
 };
 
-// Turn a unit: chunks a and b into each other (half pairs, cs of their eight pairs), or
-// chunk a in itself (interleaved, cs of its four pairs).
+// The cosines and sines of a row: unit u turns pairs K u .. K u + K - 1 (half pairs K = 8,
+// interleaved K = 4), and neighbouring lanes turn neighbouring units, so every two pairs
+// of a unit stand beside the same ones of its neighbours: pair K u + r at place
+// (r / 2) 2 (half / K) + 2 u + r % 2.  (In order, eight lanes met in the same banks.)
 template <bool IL>
-__device__ __forceinline__ void turn(float* a, float* b, const float2* cs) {
+__device__ __forceinline__ int place_of(const RotaryParams& p, int pair) {
+  constexpr int K = IL ? 4 : 8;
+  const int u = pair / K, r = pair % K;
+  return (r >> 1) * 2 * (p.half / K) + 2 * u + (r & 1);
+}
+
+// Turn unit u of a row: chunks a and b into each other (half pairs), or chunk a in itself
+// (interleaved).  cs: the row's cosines and sines.
+template <bool IL>
+__device__ __forceinline__ void turn(const RotaryParams& p, float* a, float* b, const float2* cs, int u) {
+  constexpr int K = IL ? 4 : 8;
+  const f32x4* at = (const f32x4*)cs + u;   // two pairs: (cos, sin, cos, sin)
+  const int step = p.half / K;
+  f32x4 f[K / 2];
+#pragma unroll
+  for (int j = 0; j < K / 2; ++j) f[j] = at[j * step];
   if constexpr (IL) {
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      const float c = cs[j].x, s = cs[j].y, x = a[2 * j], y = a[2 * j + 1];
+      const float c = f[j >> 1][2 * (j & 1)], s = f[j >> 1][2 * (j & 1) + 1], x = a[2 * j], y = a[2 * j + 1];
       a[2 * j] = __builtin_fmaf(x, c, -(y * s));
       a[2 * j + 1] = __builtin_fmaf(y, c, x * s);
     }
   } else {
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-      const float c = cs[j].x, s = cs[j].y, x = a[j], y = b[j];
+      const float c = f[j >> 1][2 * (j & 1)], s = f[j >> 1][2 * (j & 1) + 1], x = a[j], y = b[j];
       a[j] = __builtin_fmaf(x, c, -(y * s));
       b[j] = __builtin_fmaf(y, c, x * s);
     }
@@ -153,7 +170,7 @@ struct Units {
         float xa[8], xb[8];
         a[k].get(xa);
         if (!IL) b[k].get(xb);
-        turn<IL>(xa, xb, cs + row[k] * p.half + (IL ? 4 : 8) * u);
+        turn<IL>(p, xa, xb, cs + row[k] * p.half, u);
         a[k].set(xa);
         if (!IL) {
           b[k].set(xb);
@@ -166,6 +183,7 @@ struct Units {
 };
 
 // Cosine and sine (times the amplitude) of rows [0, n) of the window, by all threads.
+template <bool IL>
 __device__ __forceinline__ void angles(const RotaryParams& p, const int32_t* pos, int n, float2* cs) {
   const double turns = 0.15915494309189535;   // 1 / (2 pi)
   for (int i = threadIdx.x; i < n * p.half; i += kThreads) {
@@ -175,14 +193,14 @@ __device__ __forceinline__ void angles(const RotaryParams& p, const int32_t* pos
     double s, c;
     sincospi(2.0 * t, &s, &c);
     const float sn = (float)(s * (double)p.amplitude);
-    cs[i] = make_float2((float)(c * (double)p.amplitude), p.inverse ? -sn : sn);
+    cs[r * p.half + place_of<IL>(p, j)] = make_float2((float)(c * (double)p.amplitude), p.inverse ? -sn : sn);
   }
 }
 
 // ---------------------------------------------------------------- rows alone
 template <bool F32, bool IL, bool STREAM>
 __global__ __launch_bounds__(kThreads) void rotate_kernel(const RotaryParams p) {
-  extern __shared__ float2 s_cs[];   // [win][half]
+  extern __shared__ __align__(16) float2 s_cs[];   // [win][half]
   __shared__ int32_t s_pos[kWin];
   __shared__ uint8_t s_ok[kWin];
   const int win = blockIdx.x / p.parts, part = blockIdx.x - win * p.parts;
@@ -196,7 +214,7 @@ __global__ __launch_bounds__(kThreads) void rotate_kernel(const RotaryParams p) 
     s_ok[threadIdx.x] = 1;
   }
   __syncthreads();
-  angles(p, s_pos, n, s_cs);
+  angles<IL>(p, s_pos, n, s_cs);
   __syncthreads();
   constexpr int E = F32 ? 4 : 2;
   for (;;) {
@@ -254,9 +272,10 @@ __device__ __forceinline__ void write_page(const RotaryParams& p, const void* x,
   }
   float s = s0 > 0 ? *scale : 0.f;
   if (!(s > 0.f) || __builtin_isinf(s)) s = 0.f;
-  // Half pairs: this chunk is the first (side 0) or second half of pairs 8 pair .. + 7, the other half in chunk `other`.
+  // Half pairs: this chunk is the first (side 0) or second half of unit u, the other half in
+  // the lane `other`.
   const bool turns = TURN && c < (IL ? p.half >> 2 : 2 * h8);
-  const int side = !IL && c >= h8, pair = IL ? 4 * c : 8 * (side ? c - h8 : c);
+  const int side = !IL && c >= h8, u = side ? c - h8 : c;
   const int other = lane + (turns && !IL ? (side ? -h8 : h8) : 0);
   float v[kN][8];
   float amax = 0.f;
@@ -271,17 +290,17 @@ __device__ __forceinline__ void write_page(const RotaryParams& p, const void* x,
         for (int i = 0; i < 4; ++i) ob.r[i] = (uint32_t)__builtin_amdgcn_ds_bpermute(4 * other, (int)raw[j].r[i]);
       }
       if (turns && t >= s0 && t < s0 + m) {
-        const float2* f = cs + r * p.half + pair;
+        const float2* f = cs + r * p.half;
         if constexpr (IL) {
           float none[8];
-          turn<true>(v[j], none, f);
+          turn<true>(p, v[j], none, f, u);
         } else {
           float o[8];
           ob.get(o);
           if (side)
-            turn<false>(o, v[j], f);
+            turn<false>(p, o, v[j], f, u);
           else
-            turn<false>(v[j], o, f);
+            turn<false>(p, v[j], o, f, u);
         }
       }
     }
@@ -345,7 +364,7 @@ template <int D, KvKind KIND, bool IL, bool STREAM>
 __global__ __launch_bounds__(kThreads) void append_rotary_kernel(const RotaryParams p) {
   constexpr bool F32 = KIND == KvKind::F32, FP8 = KIND == KvKind::FP8;
   constexpr int E = F32 ? 4 : 2;
-  extern __shared__ float2 s_cs[];   // [win, fp8 caches and several rows a sequence: win + 15][half]
+  extern __shared__ __align__(16) float2 s_cs[];   // [win, fp8 caches and several rows a sequence: win + 15][half]
   __shared__ int32_t s_pos[kWinRows];   // position of the row (its angle)
   __shared__ int32_t s_tok[kWinRows];   // token of its sequence
   __shared__ int32_t s_seq[kWinRows];
@@ -446,7 +465,7 @@ __global__ __launch_bounds__(kThreads) void append_rotary_kernel(const RotaryPar
       if (starts == 0) return;
       const int jobs = __builtin_popcountll(starts) * 2 * p.hkv;
       const int all = uni(s_n);
-      angles(p, s_pos, all, s_cs);
+      angles<IL>(p, s_pos, all, s_cs);
       __syncthreads();
       for (int j = part * kWaves + wave; j < jobs; j += parts * kWaves) {
         int k = j / (2 * p.hkv);
@@ -469,7 +488,7 @@ __global__ __launch_bounds__(kThreads) void append_rotary_kernel(const RotaryPar
       return;
     }
   }
-  angles(p, s_pos, n, s_cs);
+  angles<IL>(p, s_pos, n, s_cs);
   __syncthreads();
 
   // 3. q, and K and V rows of caches that hold them as they are.
