@@ -298,7 +298,7 @@ rlda_status rl_decode_attn_run_multi(rl_decode_attn_t handle, int32_t batch, int
  * Attention with modified scores.  With s = scale q . k for a query row at position `pos`
  * (its token; seq_lens[b] - 1, or as for rl_decode_attn_run_multi) and the key of token t:
  *   score_cap c > 0:   s <- c tanh(s / c)
- *   slopes:            s <- s - slopes[h] |pos - t|         (query head h; any finite value)
+ *   slopes:            s <- s - slopes[h] |pos - t|         (query head h)
  * and the row sees the keys t of one interval only,
  *   max(key_start[row], pos - window + 1, 0) <= t < max(pos + 1, min(prefix_lens[b], seq_lens[b])):
  * a sliding window, documents packed in one sequence, a prefix that every row sees whole.
@@ -308,7 +308,7 @@ rlda_status rl_decode_attn_run_multi(rl_decode_attn_t handle, int32_t batch, int
 typedef struct {
   float score_cap;              /* 0, or in [2^-10, 2^30] */
   int32_t window;               /* keys a row sees up to its own; 0: all */
-  const float* slopes;          /* DEVICE [Hq] fp32 */
+  const float* slopes;          /* DEVICE [Hq] fp32, of any sign, up to 2^64 */
   const int32_t* key_start;     /* DEVICE [total_q] */
   const int32_t* prefix_lens;   /* DEVICE [batch] */
 } rl_decode_attn_scores;
@@ -318,7 +318,7 @@ typedef struct {
  * rl_decode_attn_run_multi (q_start given) with modified scores; arguments, limits, checks
  * and workspace as for these.  Pages below every row's interval are not read, their
  * block-table entries neither.  Supported for bf16 and fp8 caches (RLDA_ERR_UNSUPPORTED
- * for f32).  Rows at negative positions (n_b > seq_lens[b]) give zeros.  One kernel,
+ * for f32), with q_start for batches up to 4096 (RLDA_ERR_UNSUPPORTED).  Rows at negative positions (n_b > seq_lens[b]) give zeros.  One kernel,
  * asynchronous; events: both NULL, or both recorded around it.
  */
 rlda_status rl_decode_attn_run_scored(rl_decode_attn_t handle, const rl_decode_attn_scores* scores, int32_t batch,
@@ -354,9 +354,9 @@ typedef struct {
 /*
  * Turn rows by their positions: out[r][h] = x[r][h] turned by positions[r] (int32, device,
  * any sign).  dtype RLDA_F32 or RLDA_BF16 for x and out; heads <= 256, head_dim a multiple
- * of 8 in [32, 256], rows <= 2^31 - 65 (else RLDA_ERR_UNSUPPORTED).  x may be read through any strides (a
- * slice of a fused projection; 0: one row for all); out's rows must not overlap each
- * other, and out is x itself (same strides) or apart from it.  No handle, no workspace,
+ * of 8 in [32, 256], rows <= 2^27 (else RLDA_ERR_UNSUPPORTED).  x may be read through any
+ * strides (a slice of a fused projection; 0: one row for all); out's rows must not overlap
+ * each other, and out is x itself (same strides) or apart from it.  No handle, no workspace,
  * one kernel, asynchronous.
  */
 rlda_status rl_decode_attn_rotate(rlda_dtype dtype, int32_t rows, int32_t heads, int32_t head_dim,
@@ -387,6 +387,7 @@ rlda_status rl_decode_attn_rotate(rlda_dtype dtype, int32_t rows, int32_t heads,
  * written, q_out included (flag bit 1, but for rows of no sequence and for an empty
  * sequence without q_start); of a token whose page id is outside the pool only q_out is
  * (flag bit 0).  The pages one call writes must each belong to one sequence.
+ * total_q: up to 2^27, and what one launch holds (RLDA_ERR_UNSUPPORTED).
  * workspace: as for rl_decode_attn_run (only its flag word is used).  One kernel, asynchronous.
  */
 rlda_status rl_decode_attn_append_rotary(rl_decode_attn_t handle, int32_t batch, int32_t num_pages, int32_t total_q,
@@ -402,7 +403,11 @@ rlda_status rl_decode_attn_append_rotary(rl_decode_attn_t handle, int32_t batch,
  * (device; 0: free; a page that k rows of the block table use has k), with the block
  * table and the lengths as for rl_decode_attn_run.  Every layer's cache shares that state
  * (page id p means page p of each of them), so taking, sharing and returning pages is one
- * call for all layers, and what moves contents takes a list of caches:
+ * call for all layers, and what moves contents takes a list of caches.
+ *   A row's pages are the first ceil(seq_lens[b] / 16) of its table row, and these calls
+ * change the lengths.  A caller that cuts one back itself (rejected draft tokens) stays
+ * within the row's last page and out of pages that a fork shares: pages behind the length
+ * would stay counted, and a token appended to a shared page be seen by every row that has it.
  */
 typedef struct {
   void* k_cache;
@@ -431,7 +436,7 @@ rlda_status rl_decode_attn_page_grow(rl_decode_attn_t handle, int32_t batch, int
 /*
  * rows[0 .. count) give up their pages: each of a row's pages loses a reference, and the
  * row's length becomes 0 (its table entries stay as they were).  A row named twice is
- * released once.  Row ids outside [0, batch) and lengths out of range: flag bit 1; page
+ * released once; count <= 2^23 (RLDA_ERR_UNSUPPORTED).  Row ids outside [0, batch) and lengths out of range: flag bit 1; page
  * ids outside the pool, and pages that nobody holds: flag bit 0.  One kernel, asynchronous.
  */
 rlda_status rl_decode_attn_page_release(rl_decode_attn_t handle, int32_t batch, int32_t num_pages, int32_t* refs,

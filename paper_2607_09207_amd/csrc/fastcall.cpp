@@ -389,7 +389,7 @@ bool rows_of(const Tensor* t, int dev, at::ScalarType type, int64_t n, int64_t h
   const int64_t per = 16 / (int64_t)t->element_size();
   void* p = t->mutable_data_ptr();
   if (((uintptr_t)p & 15) || (n > 1 && st[0] % per) || (heads > 1 && st[1] % per)) return false;
-  *out = {p, st[0], st[1]};
+  *out = {p, n > 1 ? st[0] : 0, heads > 1 ? st[1] : 0};
   return true;
 }
 
@@ -398,7 +398,7 @@ bool rotary_of(PyObject* freqs, PyObject* interleaved, PyObject* amplitude, int 
   const Tensor* f = tensor(freqs);
   int il = 0;
   double a = 1.0;
-  if (!plain(f, dev, at::kDouble) || f->dim() != 1 || !f->is_contiguous() || !as_bool(interleaved, &il) || !as_double(amplitude, &a))
+  if (!plain(f, dev, at::kDouble) || (f->requires_grad() && c10::GradMode::is_enabled()) || f->dim() != 1 || !f->is_contiguous() || !as_bool(interleaved, &il) || !as_double(amplitude, &a))
     return false;
   const int64_t half = f->size(0);
   if (half < 8 || 2 * half > d || half % 8) return false;
@@ -507,8 +507,16 @@ PyObject* rotate(PyObject*, PyObject* const* a, Py_ssize_t n) {
         !rotary_of(a[2], a[3], a[4], inverse, dev, d, &rot) || !stream_of(a[7], dev, &stream) || !current(dev))
       return nullptr;
     Tensor fresh;
-    if (a[6] == Py_None) fresh = at::empty({rows, heads, d}, x->options());
-    if (!rows_of(a[6] == Py_None ? &fresh : tensor(a[6]), dev, type, rows, heads, d, &ro)) return nullptr;
+    const Tensor* out = &fresh;
+    if (a[6] == Py_None) {
+      fresh = at::empty({rows, heads, d}, x->options());
+    } else {
+      out = tensor(a[6]);
+      if (!out || (out->requires_grad() && c10::GradMode::is_enabled())) return nullptr;
+    }
+    if (!rows_of(out, dev, type, rows, heads, d, &ro)) return nullptr;
+    // A backward pass that saved the given tensor is to notice.
+    if (a[6] != Py_None && !out->is_inference()) out->unsafeGetTensorImpl()->bump_version();
     const int32_t* pp = (const int32_t*)ptr(pos);
     WITHOUT_GIL(g_rotate(type == at::kFloat ? RLDA_F32 : RLDA_BF16, (int32_t)rows, (int32_t)heads, (int32_t)d, &rx, pp, &rot,
                          &ro, stream));

@@ -456,8 +456,7 @@ struct Mfma {
   // part in a row whatever its values: its score is replaced, and where a page with masked
   // keys holds an infinity or NaN in V, which would turn the product with its zero
   // probability into NaN, those values are counted apart.  The probabilities' remainders
-  // enter the product always: us a call without / with them, capped bf16 d 128, four
-  // sequences of 8k to 16k tokens: see compute_mod's caller.
+  // always enter the product: its K of 32 holds the page's 16 keys twice anyway.
   __device__ __forceinline__ void compute_mod(const Params& p, const Frag& f, const VOp* vo, int lane, bool there,
                                               float kmul, float vmul) {
     const int qg = lane >> 4;

@@ -20,7 +20,10 @@ using rlda::kAlign;
 using rlda::PageParams;
 using rlda::RotaryParams;
 
-constexpr int32_t kMaxRows = INT32_MAX - 64;   // row numbers a window past the last stay 32-bit
+constexpr int32_t kMaxRows = 1 << 27;   // the rows of a call (with their launch, below)
+constexpr int32_t kMaxList = 1 << 23;   // rows of a release
+constexpr int64_t kMaxBlocks = (1ll << 32) / rlda::kThreads - 1;   // a launch holds fewer than 2^32 threads
+
 
 bool aligned4(const void* p) { return ((uintptr_t)p & 3u) == 0; }
 
@@ -63,6 +66,8 @@ void set_rotary(RotaryParams& p, const rl_decode_attn_rotary& r, int d, int rows
   p.magic_ku = magic_of((int64_t)p.units * std::max(hkv, 1));
   p.magic_half = magic_of(p.half);
 }
+
+int64_t rotary_blocks(const RotaryParams& p) { return ((int64_t)p.rows + p.win - 1) / p.win * (p.parts + p.page_parts); }
 
 // Windows, and workgroups of a window: kWanted that turn rows in all, where the rows give
 // them, none without a unit for its threads.  us a call by kWanted 2048 / 8192: 32768 x 32
@@ -115,6 +120,7 @@ rlda_status rl_decode_attn_rotate(rlda_dtype dtype, int32_t rows, int32_t heads,
   p.o_hs = out->head_stride;
   p.positions = positions;
   set_windows(p, (int64_t)heads * p.units, 0, (int64_t)heads * head_dim * eb);
+  if (rotary_blocks(p) > kMaxBlocks) return RLDA_ERR_UNSUPPORTED;
   return rlda::launch_rotate(dtype == RLDA_F32, p, stream) == hipSuccess ? RLDA_OK : RLDA_ERR_HIP;
 }
 
@@ -179,6 +185,7 @@ rlda_status rl_decode_attn_append_rotary(rl_decode_attn_t h, int32_t batch, int3
   p.max_pages = c.max_pages_per_seq;
   set_windows(p, (int64_t)c.num_q_heads * p.units, h->kind == rlda::KvKind::FP8 ? 2 * c.num_kv_heads : 0,
               (int64_t)(c.num_q_heads + 2 * c.num_kv_heads) * c.head_dim * eb);
+  if (rotary_blocks(p) > kMaxBlocks) return RLDA_ERR_UNSUPPORTED;
   return rlda::launch_append_rotary(h->kind, c.head_dim, p, stream) == hipSuccess ? RLDA_OK : RLDA_ERR_HIP;
 }
 
@@ -255,6 +262,7 @@ rlda_status page_call(rl_decode_attn_t h, int32_t batch, int32_t num_pages, int3
 // Layers of a workgroup that copies pages: a pair of a few KiB is too little for one.
 constexpr int kCopyBytes = 16 << 10;
 constexpr int kMoveGrid = 32768;   // workgroups of a compaction's copies at most
+constexpr int kCopyGrid = 1 << 20;   // ... of a list's copies
 
 rlda_status check_caches(rl_decode_attn_t h, int32_t num_caches, const rl_decode_attn_cache* caches, int32_t num_pages) {
   if (num_caches < 0 || (num_caches > 0 && !caches)) return RLDA_ERR_INVALID_ARG;
@@ -317,6 +325,7 @@ rlda_status rl_decode_attn_page_release(rl_decode_attn_t h, int32_t batch, int32
   const rlda_status st = page_call(h, batch, num_pages, refs, block_table, seq_lens, workspace, workspace_bytes, p);
   if (st != RLDA_OK) return st;
   if (count < 0 || (count > 0 && (!rows || !aligned4(rows)))) return RLDA_ERR_INVALID_ARG;
+  if (count > kMaxList) return RLDA_ERR_UNSUPPORTED;
   if (count == 0) return RLDA_OK;
   p.count = count;
   p.list_a = rows;
@@ -374,7 +383,9 @@ rlda_status rl_decode_attn_page_copy(rl_decode_attn_t h, int32_t num_pages, int3
   p.count = count;
   p.list_src = const_cast<int32_t*>(src);
   p.list_dst = const_cast<int32_t*>(dst);
-  return for_caches(h, p, num_caches, caches, [&] { return rlda::launch_page_copy(p, stream); });
+  return for_caches(h, p, num_caches, caches, [&] {
+    return rlda::launch_page_copy(p, std::min(count * p.layer_blocks, kCopyGrid), stream);
+  });
 }
 
 }  // extern "C"

@@ -394,17 +394,18 @@ __device__ __forceinline__ void copy_page(const PageParams& p, int src, int dst,
 }
 
 // Pages list_src -> list_dst of `count` pairs in layers of a few, one workgroup per (pair,
-// layers).  Pairs with a page outside the pool are skipped (CHECK: and reported).
-template <bool CHECK>
+// layers) up to the grid.  Pairs with a page outside the pool are skipped and reported.
 __global__ __launch_bounds__(kThreads) void page_copy_kernel(const PageParams p) {
-  const int i = blockIdx.x / p.layer_blocks, part = blockIdx.x - i * p.layer_blocks;
-  const int src = p.list_src[i], dst = p.list_dst[i];
-  if ((uint32_t)src >= (uint32_t)p.num_pages || (uint32_t)dst >= (uint32_t)p.num_pages) {
-    if (CHECK && threadIdx.x == 0) atomicOr(p.flags, kFlagBadPage);
-    return;
+  const int64_t items = (int64_t)p.count * p.layer_blocks;
+  for (int64_t it = blockIdx.x; it < items; it += gridDim.x) {
+    const int i = (int)(it / p.layer_blocks), part = (int)(it - (int64_t)i * p.layer_blocks);
+    const int src = p.list_src[i], dst = p.list_dst[i];
+    if ((uint32_t)src >= (uint32_t)p.num_pages || (uint32_t)dst >= (uint32_t)p.num_pages) {
+      if (threadIdx.x == 0) atomicOr(p.flags, kFlagBadPage);
+    } else if (src != dst) {
+      copy_page(p, src, dst, part * p.block_layers, min((part + 1) * p.block_layers, p.num_caches));
+    }
   }
-  if (src == dst) return;
-  copy_page(p, src, dst, part * p.block_layers, min((part + 1) * p.block_layers, p.num_caches));
 }
 
 // The forks' table rows and references; with part > 0, their copies.
@@ -558,8 +559,8 @@ int launch_page_move(const PageParams& p, int grid, void* stream) {
   return (int)hipGetLastError();
 }
 
-int launch_page_copy(const PageParams& p, void* stream) {
-  hipLaunchKernelGGL((page_copy_kernel<true>), dim3(p.count * p.layer_blocks), dim3(kThreads), 0, (hipStream_t)stream, p);
+int launch_page_copy(const PageParams& p, int grid, void* stream) {
+  hipLaunchKernelGGL(page_copy_kernel, dim3(grid), dim3(kThreads), 0, (hipStream_t)stream, p);
   return (int)hipGetLastError();
 }
 

@@ -247,6 +247,6 @@ int launch_page_fork(const PageParams& p, void* stream);        // which forks s
 int launch_page_fork_rows(const PageParams& p, void* stream);   // their table rows, references and copies
 int launch_page_compact(const PageParams& p, void* stream);     // the moves
 int launch_page_move(const PageParams& p, int grid, void* stream);   // tables and copies
-int launch_page_copy(const PageParams& p, void* stream);
+int launch_page_copy(const PageParams& p, int grid, void* stream);
 
 }  // namespace rlda

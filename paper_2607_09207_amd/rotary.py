@@ -62,7 +62,7 @@ def rotary_frequencies(rot_dim: int, base: float = 10000.0, scaling=None, device
 
 def rows_of(t):
     """Rows [n][heads][d] as the C ABI takes them (d contiguous, or of one element)."""
-    return _abi.Rows(t.data_ptr(), t.stride(0), t.stride(1))
+    return _abi.Rows(t.data_ptr(), t.stride(0) if t.shape[0] > 1 else 0, t.stride(1) if t.shape[1] > 1 else 0)
 
 
 def rotary_of(freqs, interleaved, amplitude, inverse=False):
@@ -89,6 +89,8 @@ def check_freqs(fail, freqs, d, device):
     import torch
     if freqs is None or not freqs.is_cuda or freqs.device != device:
         fail(f"freqs must be on {device}")
+    if freqs.requires_grad and torch.is_grad_enabled():
+        fail("freqs gets no gradient: detach it")
     if freqs.dtype != torch.float64 or freqs.dim() != 1 or not freqs.is_contiguous():
         fail("freqs must be a contiguous float64 vector")
     if not 16 <= 2 * freqs.shape[0] <= d or freqs.shape[0] % 8:
@@ -170,6 +172,8 @@ def rotate(x, positions, freqs, *, interleaved: bool = False, amplitude: float =
         fail(f"x must be on a GPU, got {x.device}")
     if x.dtype not in (torch.bfloat16, torch.float32):
         fail(f"x must be bfloat16 or float32, got {x.dtype}")
+    if out is not None and out.requires_grad and torch.is_grad_enabled():
+        fail("out requires grad")
     if x.requires_grad and torch.is_grad_enabled():
         if out is not None or stream is not None:
             fail("an x that requires grad is turned into a new tensor, on the current stream")
@@ -187,6 +191,8 @@ def rotate(x, positions, freqs, *, interleaved: bool = False, amplitude: float =
             used_on(out, dev, stream)
         else:
             check_rows(fail, "out", out, x.dtype, shape, dev)
+            if not out.is_inference():
+                torch.autograd.graph.increment_version(out)   # a backward pass that saved it is to notice
         xr, outr, rot = rows_of(x), rows_of(out), rotary_of(freqs, interleaved, amplitude, inverse)
         _abi.check(_abi.load().rl_decode_attn_rotate(
             _abi.RLDA_F32 if x.dtype == torch.float32 else _abi.RLDA_BF16, shape[0], shape[1], shape[2], ctypes.byref(xr),

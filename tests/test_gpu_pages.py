@@ -341,6 +341,24 @@ def test_copy(torch, kv, layout, hkv, d):
     s.check("copy of pages out of the pool")
 
 
+def test_copy_more_pairs_than_workgroups(torch):
+    """A list longer than the copies' grid: mostly pages outside the pool, copies at its end."""
+    from paper_2607_09207_amd import DecodeAttention
+    layer = DecodeAttention(1, 1, 64, 4, 8, "bf16", "bf16", "bf16")
+    n = (1 << 20) + 1000
+    k = torch.randint(-9, 9, (1000, 1, 16, 64), device="cuda").to(torch.bfloat16)
+    v = k + 1
+    src = torch.full((n,), -1, dtype=torch.int32, device="cuda")
+    dst = torch.arange(n, dtype=torch.int32, device="cuda")
+    src[-400:] = torch.arange(0, 400, dtype=torch.int32, device="cuda")
+    dst[-400:] = torch.arange(500, 900, dtype=torch.int32, device="cuda")
+    want = k.clone()
+    want[500:900] = k[:400]
+    layer.page_copy(src, dst, [(k, v)])
+    assert torch.equal(k, want) and torch.equal(v, want + 1)
+    assert layer.page_flags(1000, k.device) == 1
+
+
 def test_refusals(torch):
     from paper_2607_09207_amd import RldaError
     s = State(torch, 50, [20, 30], 40, layers=1)

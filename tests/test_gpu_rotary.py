@@ -212,6 +212,73 @@ def test_autograd(torch, dtype):
         assert not rotate(fused[:, 1:5], pos, freqs).requires_grad
 
 
+def test_autograd_refusals_and_versions(torch):
+    """What would go without a gradient is refused; a saved tensor turned in place is noticed."""
+    from paper_2607_09207_amd import RldaError, rotary_frequencies, rotate
+    freqs, _ = rotary_frequencies(64)
+    x = torch.randn((5, 2, 64), device="cuda")
+    pos = torch.arange(5, device="cuda", dtype=torch.int32)
+    grads = x.clone().requires_grad_()
+    with pytest.raises(RldaError):
+        rotate(x, pos, freqs, out=grads)
+    with pytest.raises(RldaError):
+        rotate(x, pos, freqs.clone().requires_grad_())
+    with torch.no_grad():
+        assert rotate(x, pos, freqs, out=grads) is grads
+    w = torch.ones_like(x).requires_grad_()
+    y = w * x
+    assert torch.equal(rotate(x, pos, freqs, out=x), grads)
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        y.sum().backward()
+    with torch.inference_mode():
+        z = x + 1
+        assert rotate(z, pos, freqs, out=z) is z
+
+
+def test_single_rows_of_any_stride(torch):
+    """One row, or one head, of a buffer whose other stride is no multiple of 16 bytes."""
+    from paper_2607_09207_amd import rotary_frequencies, rotate
+    freqs, _ = rotary_frequencies(64)
+    pos = torch.full((1,), 77, device="cuda", dtype=torch.int32)
+    x = torch.randn(1, 2 * 64 + 3, device="cuda").to(torch.bfloat16)[:, :128].view(1, 2, 64)
+    x = x.as_strided((1, 2, 64), (131, 64, 1))
+    assert torch.equal(rotate(x, pos, freqs), rotate(x.clone(memory_format=torch.contiguous_format), pos, freqs))
+    y = torch.randn((3, 1, 64), device="cuda").as_strided((3, 1, 64), (64, 7, 1))
+    assert torch.equal(rotate(y, pos.expand(3).contiguous(), freqs), rotate(y.contiguous().view(3, 1, 64), pos.expand(3).contiguous(), freqs))
+
+
+def test_captured_backward(torch):
+    """Forward and backward in one graph, replayed, with eager work between."""
+    from paper_2607_09207_amd import rotary_frequencies, rotate
+    freqs, amp = rotary_frequencies(128)
+    x = torch.randn((40, 3, 128), device="cuda").to(torch.bfloat16).requires_grad_()
+    w = torch.randn((40, 3, 128), device="cuda").to(torch.bfloat16)
+    pos = torch.randint(0, 9000, (40,), device="cuda", dtype=torch.int32)
+
+    def step():
+        y = rotate(x, pos, freqs, interleaved=True)
+        return y.detach(), torch.autograd.grad(y, x, w)[0]
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step()
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        y, g = step()
+    for i in range(3):
+        with torch.no_grad():
+            x.copy_(torch.randn((40, 3, 128), device="cuda"))
+        w.copy_(torch.randn((40, 3, 128), device="cuda"))
+        pos.add_(1000 * i)
+        y.zero_(), g.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        want, grad = step()
+        assert torch.equal(y, want) and torch.equal(g, grad)
+
+
 # ------------------------------------------------------------------ rows into the cache
 
 KV = {"f32": ("f32", 4), "bf16": ("bf16", 2), "fp8": ("fp8_e4m3fn", 1)}

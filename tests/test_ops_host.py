@@ -222,3 +222,22 @@ def test_frequencies():
                 lambda: F(64, 1e4, dict(how, context=0))):
         with pytest.raises(ValueError):
             bad()
+
+
+def test_sizes_beyond_a_launch(lib, handles):  # noqa: F811
+    """What one launch cannot hold is refused before it."""
+    assert rotate(lib, rows=2 ** 27 + 1) == UNSUPPORTED
+    h = handles["bf16"]
+    assert append(lib, h, total=2 ** 27 + 1, q_start=P) == UNSUPPORTED
+    # 2^23 windows of two workgroups (rows and pages) and more.
+    assert append(lib, handles["fp8"], total=2 ** 27, q_start=P) == UNSUPPORTED
+    ws = page_bytes(lib, h, 10)
+    assert lib.rl_decode_attn_page_release(h, 4, 10, P, P, P, 2 ** 23 + 1, P, P, ws, None) == UNSUPPORTED
+
+
+def test_scored_rows_of_large_batches(lib):  # noqa: F811
+    st, h = create(lib, cfg(num_q_heads=8, num_kv_heads=2, max_batch=8192, max_pages_per_seq=8, kv_dtype=_abi.RLDA_BF16))
+    assert st == 0
+    for mq in (0, 1, 4, 100):
+        assert scored(lib, h, batch=4097, total=4097, q_start=P, max_q=mq) == UNSUPPORTED
+    lib.rl_decode_attn_destroy(h)
