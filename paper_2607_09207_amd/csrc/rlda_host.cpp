@@ -173,6 +173,7 @@ void set_scores(rlda::Params& p, const rl_decode_attn_scores& s) {
   p.window = s.window;
   p.key_start = s.key_start;
   p.prefix_lens = s.prefix_lens;
+  p.group_magic = (uint32_t)(((1ull << 32) + p.group - 1) / p.group);
 }
 
 // group_size == 0: plain run; > 0: grouped run with prefix_pages.  With `mem` the

@@ -165,6 +165,7 @@ void multi_query_kernel(const Params p) {
   __shared__ int32_t s_bad[S::NBUF][2 * kKH];   // page of the block not in the pool (contributes nothing)
   __shared__ int32_t s_scan[kWaves], s_emax[kWaves], s_sum32[kWaves];
   __shared__ int16_t s_qh[kMaxQHeads];
+  __shared__ int2 s_item;     // MOD: the workgroup's sequence and row block
   __shared__ int32_t s_odd;   // MOD: infinities or NaN of V were cleared
   // Batches above 64, per sequence: {L - n_b (position of query token 0), n_b} (n_b 0
   // when its offsets are inconsistent), and its ordering key.
@@ -185,12 +186,14 @@ void multi_query_kernel(const Params p) {
   //    sequences took 9.2 to 11.5 us, and 7.1 to 8.8 so; whole prompts (32 x 512 tokens,
   //    12/2 heads) 58.2 and 53.5 us; chunks of long sequences 1420 and 1390 us.
   int2 sq0 = make_int2(0, 0);   // the sequence of this lane: {L - n_b, n_b}
-  int key0 = -1;                // its ordering key (below)
+  int key0 = -1, q00 = 0;       // its ordering key (below), its first row
   int nitems = 0, emax = 0;     // row blocks; the most keys any sequence's rows see
   bool split = false;           // SMALL: 32 rows to a workgroup, its waves split the keys
   int rshift = kMultiRowsLog2;  // log2 of a row block's rows
   {
     int sum = 0, sum32 = 0, bad = 0, lmax = 0;   // 128-row blocks, 32-row blocks
+    static_assert(kMaxQHeads <= kThreads, "one query head per thread");
+    const int16_t qh = tid < Hq ? p.q_head[tid] : (int16_t)0;
     const bool many = batch > 64;
     for (int b = many ? tid : lane; b < batch; b += kThreads) {
       const int q0 = p.q_start[b], q1 = p.q_start[b + 1];
@@ -200,6 +203,7 @@ void multi_query_kernel(const Params p) {
       if (!ok || L < 0 || L > cap || n > L) bad = 1;
       L = min(max(L, 0), cap);
       sq0 = make_int2(L - n, n);
+      q00 = q0;
       if (many) s_sq[b] = sq0;
       sum += (n * G + kMultiRows - 1) / kMultiRows;
       if (SMALL) sum32 += (n * G + kTile - 1) / kTile;
@@ -209,7 +213,7 @@ void multi_query_kernel(const Params p) {
     sum = __builtin_amdgcn_readlane(wave_scan(sum), 63);
     lmax = __builtin_amdgcn_readlane(wave_scan_max(lmax), 63);
     if (SMALL) sum32 = __builtin_amdgcn_readlane(wave_scan(sum32), 63);
-    for (int e = tid; e < Hq; e += kThreads) s_qh[e] = p.q_head[e];
+    if (tid < Hq) s_qh[tid] = qh;
     if (MOD && tid == 0) s_odd = 0;
     // Ordering key of each sequence's row blocks.  A sequence whose rows see at most an
     // eighth of the largest job's keys apart is dispatched as a group (its row blocks
@@ -275,7 +279,7 @@ void multi_query_kernel(const Params p) {
   //    past the set's end return).  Item t is found by a search on the key count, three
   //    points a step: with C(x) the items having at least x keys (a closed form per
   //    sequence, summed across the wave), its key count x* is the largest x with C(x) > t.
-  //    Every wave finds it (no barrier).
+  //    Every wave finds it (no barrier; but see `searches`).
   const int u = blockIdx.x, xcd = u & 7;
   const bool by_head = Hkv % 8 == 0, by_class = Hkv == 4;
   const int ncls = by_class ? 8 / Hkv : 1, my_cls = by_class ? xcd / Hkv : 0;
@@ -296,40 +300,52 @@ void multi_query_kernel(const Params p) {
     const int rr = rank % (2 * ncls);
     mine = (rr < ncls ? rr : 2 * ncls - 1 - rr) == my_cls;
   }
-  // Row blocks of sequence `sq` with at least x >= 1 keys (E is non-decreasing in rb).
-  auto at_least = [&](int2 sq, int key, int x) -> int {
-    const int nrb = blocks_of(sq.y * G);
-    if (key >= 0) return key >= x ? nrb : 0;   // dispatched as a group
-    if (x - 1 <= sq.x) return nrb;             // E >= x iff (r1 - 1) / G >= k
-    const uint32_t k = (uint32_t)(x - 1) - (uint32_t)sq.x;
-    return k < (uint32_t)sq.y ? nrb - (int)((uint32_t)G * k >> rshift) : 0;   // ... iff r1 > G k
+  // Row blocks of a sequence with at least x >= 1 keys (E is non-decreasing in rb): E >= x
+  // iff (r1 - 1) / G >= k, k = x - 1 - (L - n), iff r1 > G k: nrb - G max(k, 0) / (rows of a
+  // block) where k < n.  A sequence dispatched as a group has E = key in all of them.
+  // (Without branches: a workgroup's search took 4.2 us with them, 2.9 so.)
+  struct Seq {
+    int nrb, base, end;
   };
-  // f({L - n, n}, key) of each of the set's sequences that this lane holds (the first 64
-  // in registers), and a lane's count summed over the wave.
+  auto seq_of = [&](int2 sq, int key, bool in) -> Seq {
+    return Seq{in ? blocks_of(sq.y * G) : 0, key >= 0 ? key - 1 : sq.x, !in ? INT32_MIN : key >= 0 ? 1 : sq.y};
+  };
+  auto at_least = [&](const Seq& q, int x) -> int {
+    const int k = x - 1 - q.base;
+    const int c = q.nrb - (int)(__umul24((uint32_t)G, (uint32_t)max(k, 0)) >> rshift);   // (G n < 2^24)
+    return k < q.end ? c : 0;
+  };
+  // f(sequence) of each of the set's that this lane holds (the first 64 in registers), and a
+  // lane's count summed over the wave.
   auto in_set = [&](int b) { return b < batch && (by_class && batch > 64 ? b % ncls == my_cls : mine); };
+  const Seq seq0 = seq_of(sq0, key0, in_set(lane));
   auto each = [&](auto f) {
-    if (in_set(lane)) f(sq0, key0);
+    f(seq0);
     for (int b = lane + 64; b < batch; b += 64)
-      if (in_set(b)) f(s_sq[b], s_key[b]);
+      if (in_set(b)) f(seq_of(s_sq[b], s_key[b], true));
   };
   auto total = [&](int c) { return __builtin_amdgcn_readlane(wave_scan(c), 63); };
   int set_items = 0;
-  each([&](int2 sq, int) { set_items += blocks_of(sq.y * G); });
+  each([&](const Seq& q) { set_items += q.nrb; });
   set_items = total(set_items) * hx;
 
   if (t_first >= set_items) return;
   const int v = t_first / hx, hsub = t_first - v * hx;
   int b = 0, rb = 0;
-  {
+  // MOD: one wave of the workgroup searches, a different one in the workgroups that share a
+  // CU, and the others leave it the issue slots (16384 tokens of packed documents of 100 /
+  // 900 tokens: 103 / 182 us a call, and 109 / 188 with every wave searching).
+  const bool searches = !MOD || wave == ((t_first + (t_first >> 5)) & (kWaves - 1));
+  if (searches) {
     int lo = 0, hi = emax + 1, chi = 0;   // C(lo) > v >= C(hi) = chi
     while (hi - lo > 1) {
       // Three points strictly between where there is room (else some coincide).
       const int d = hi - lo, x2 = lo + (d >> 1), x1 = lo + max(d >> 2, 1), x3 = min(x2 + max(d >> 2, 1), hi - 1);
       int c1 = 0, c2 = 0, c3 = 0;
-      each([&](int2 sq, int key) {
-        c1 += at_least(sq, key, x1);
-        c2 += at_least(sq, key, x2);
-        c3 += at_least(sq, key, x3);
+      each([&](const Seq& q) {
+        c1 += at_least(q, x1);
+        c2 += at_least(q, x2);
+        c3 += at_least(q, x3);
       });
       c1 = total(c1);
       c2 = total(c2);
@@ -357,20 +373,15 @@ void multi_query_kernel(const Params p) {
     int j = v - chi, found = 0;
     for (int b0 = 0; b0 < batch && !found; b0 += 64) {
       const int bb = b0 + lane;
-      int c1 = 0, c2 = 0, nrb = 0;
-      if (in_set(bb)) {
-        const int2 sq = b0 ? s_sq[bb] : sq0;
-        const int key = b0 ? s_key[bb] : key0;
-        nrb = blocks_of(sq.y * G);
-        c1 = lo > 0 ? at_least(sq, key, lo) : nrb;
-        c2 = at_least(sq, key, lo + 1);
-      }
+      Seq q = seq0;
+      if (b0) q = in_set(bb) ? seq_of(s_sq[bb], s_key[bb], true) : seq_of(make_int2(0, 0), -1, false);
+      const int c1 = lo > 0 ? at_least(q, lo) : q.nrb, c2 = at_least(q, lo + 1);
       const int eq = c1 - c2, incl = wave_scan(eq);
       const uint64_t hit = __builtin_amdgcn_ballot_w64(j >= incl - eq && j < incl);
       if (hit) {
         const int src = __builtin_ctzll(hit);
         b = __builtin_amdgcn_readlane(bb, src);
-        rb = __builtin_amdgcn_readlane(nrb - c2 - 1, src) - (j - __builtin_amdgcn_readlane(incl - eq, src));
+        rb = __builtin_amdgcn_readlane(q.nrb - c2 - 1, src) - (j - __builtin_amdgcn_readlane(incl - eq, src));
         found = 1;
       } else {
         j -= __builtin_amdgcn_readlane(incl, 63);
@@ -378,11 +389,17 @@ void multi_query_kernel(const Params p) {
     }
     b = uni(b);
     rb = uni(rb);
+    if (MOD && lane == 0) s_item = make_int2(b, rb);
+  }
+  if constexpr (MOD) {
+    lds_barrier();
+    b = uni(s_item.x);
+    rb = uni(s_item.y);
   }
   // The KV head: rotated by the sequence, so that every XCD serves every head (the
   // head fixes the page tiles' offset, and with it their HBM channels).
   const int g = by_head ? ((xcd + b) & 7) + 8 * hsub : (by_class ? (xcd + b) % Hkv : hsub);
-  const int q0 = p.q_start[b];
+  const int q0 = batch > 64 ? p.q_start[b] : __builtin_amdgcn_readlane(q00, b);
   const int2 sqb = batch > 64 ? make_int2(uni(s_sq[b].x), uni(s_sq[b].y))
                               : make_int2(__builtin_amdgcn_readlane(sq0.x, b), __builtin_amdgcn_readlane(sq0.y, b));
   const int n = sqb.y;
@@ -392,13 +409,14 @@ void multi_query_kernel(const Params p) {
   const int base_pos = L - n;                                   // position of query token 0
   // (MOD: keys that every row of the sequence sees, and the first key that a row sees.)
   const int prefix = MOD && p.prefix_lens ? min(p.prefix_lens[b], L) : 0;
+  auto token_of = [&](int row) { return MOD ? (int)(G == 1 ? row : __umulhi(row, p.group_magic)) : row / G; };
   auto first_key = [&](int row) {
-    const int i = row / G;
+    const int i = token_of(row);
     int lo = p.key_start ? max(p.key_start[q0 + i], 0) : 0;
     if (p.window > 0) lo = max(lo, base_pos + i - p.window + 1);
     return lo;
   };
-  auto seen_end = [&](int row) { return max(max(0, base_pos + row / G + 1), prefix); };
+  auto seen_end = [&](int row) { return max(max(0, base_pos + token_of(row) + 1), prefix); };
   const int E = MOD ? seen_end(r1 - 1) : max(0, base_pos + (r1 - 1) / G + 1);   // keys the workgroup reads, from 0
   const int wr0 = r0 + (split ? 0 : kTile * kNT * wave), wr1 = min(wr0 + kTile * kNT, r1);
   // Keys this wave needs, and those visible to all its rows.
@@ -416,7 +434,7 @@ void multi_query_kernel(const Params p) {
   for (int t = 0; t < kNT; ++t) {
     const int row = wr0 + kTile * t + i;
     live[t] = row < wr1;
-    qi[t] = live[t] ? row / G : 0;
+    qi[t] = live[t] ? token_of(row) : 0;
     head[t] = live[t] ? s_qh[g * G + (row - qi[t] * G)] : 0;
     lim[t] = live[t] ? base_pos + qi[t] + 1 : 0;               // keys [0, lim) are visible
     if constexpr (MOD) {
@@ -428,28 +446,6 @@ void multi_query_kernel(const Params p) {
       if (low[t] >= lim[t]) low[t] = lim[t] = 0;
     }
   }
-  // MOD: the blocks start at kb0; the wave's rows see keys from Wlo on, all of them from
-  // Wlo_full on (where one sees nothing, none do).
-  int kb0 = 0, first_page = 0, Wlo = 0, Wlo_full = 0;
-  if constexpr (MOD) {
-    int lo = E;
-#pragma unroll
-    for (int k = 0; k < kMultiRows; k += 64) {
-      const int row = r0 + k + lane;
-      if (row < r1 && base_pos + row / G >= 0) {
-        const int x = first_key(row);
-        if (x < seen_end(row)) lo = min(lo, x);
-      }
-    }
-    lo = wave_min(lo);
-    kb0 = lo / kKeys;
-    first_page = lo / kPage;   // the page before it may be in the first block: not read
-    Wlo = wave_min(lim[0] > 0 ? low[0] : 0x7ffffffe);
-    Wlo_full = wave_max(low[0]);
-    if (__builtin_amdgcn_ballot_w64(live[0] && lim[0] == 0) != 0) Ew_full = 0;
-  }
-  const int nkb = MOD ? max((E + kKeys - 1) / kKeys - kb0, 0) : (E + kKeys - 1) / kKeys;   // blocks: kb0 + kb, kb < nkb
-
   // Q operands (B of K Q^T): lane 32h + i holds its row's elements [16s + 8h, 16s + 8h + 8).
   bf16x8 qop[kNT][S::KS];
   {
@@ -462,6 +458,28 @@ void multi_query_kernel(const Params p) {
         qop[t][s] = __builtin_bit_cast(bf16x8, __builtin_amdgcn_raw_buffer_load_b128(rq, off + 16 * (2 * s + hh), 0, 0));
     }
   }
+
+  // MOD: the blocks start at kb0; the wave's rows see keys from Wlo on, all of them from
+  // Wlo_full on (where one sees nothing, none do).
+  int kb0 = 0, first_page = 0, Wlo = 0, Wlo_full = 0;
+  if constexpr (MOD) {
+    int lo = E;
+#pragma unroll
+    for (int k = 0; k < kMultiRows; k += 64) {
+      const int row = r0 + k + lane;
+      if (row < r1 && base_pos + token_of(row) >= 0) {
+        const int x = first_key(row);
+        if (x < seen_end(row)) lo = min(lo, x);
+      }
+    }
+    lo = wave_min(lo);
+    kb0 = lo / kKeys;
+    first_page = lo / kPage;   // the page before it may be in the first block: not read
+    Wlo = wave_min(lim[0] > 0 ? low[0] : 0x7ffffffe);
+    Wlo_full = wave_max(low[0]);
+    if (__builtin_amdgcn_ballot_w64(live[0] && lim[0] == 0) != 0) Ew_full = 0;
+  }
+  const int nkb = MOD ? max((E + kKeys - 1) / kKeys - kb0, 0) : (E + kKeys - 1) / kKeys;   // blocks: kb0 + kb, kb < nkb
 
   // Staging: wave w brings pages (w & 1) + 2h, h < kKH, of each block's K (w < 2)
   // or V (w >= 2).
@@ -787,8 +805,9 @@ void multi_query_kernel(const Params p) {
   // them (every thread calls it, with the results stored).  Every wave looks through the
   // workgroup's keys and serves a quarter of its rows: as slow as it is rare.
   auto put_odd = [&]() {
-    __syncthreads();   // the other waves' stores are complete
+    lds_barrier();   // s_odd; the stores need not have ended
     if (uni(s_odd) == 0) return;
+    __syncthreads();   // the other waves' stores have
     for (int key = max(kb0 * kKeys, first_page * kPage); key < E; ++key) {
       const int pid = uni(bt_vec[key / kPage]);
       if ((unsigned)pid >= (unsigned)p.num_pages) continue;

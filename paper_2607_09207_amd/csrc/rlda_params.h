@@ -99,6 +99,7 @@ struct Params {
   int32_t window;              // 0: none
   const int32_t* key_start;    // [rows] or null
   const int32_t* prefix_lens;  // [batch] or null
+  uint32_t group_magic;        // floor(i / group) = umulhi(i, group_magic) for i < 2^24, group > 1
   int16_t q_head[kMaxQHeads];  // q_head[g * G + i] = i-th query head of KV head g
 };
 
