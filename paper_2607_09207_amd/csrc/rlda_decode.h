@@ -464,7 +464,9 @@ struct Mfma {
 #pragma unroll
     for (int s = 0; s < KS; ++s) sc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k_operand(f, s), q.v[s], sc, 0, 0, 0);
     float sv[4], mx = neg_inf();
-    bool seen[4], masked = false;
+    // Most pages are seen whole by every row: no masks there (`masked` is uniform).
+    const bool masked = __builtin_amdgcn_ballot_w64(!there || rlo > 0 || rhi < kPage) != 0;
+    const auto sees = [&](int lo, int hi, int t) { return there && t >= lo && t < hi; };
     if (p.cap_log2 > 0.f) {
       const float arg = kmul * p.cap_arg;
       if (wide_cap(p.cap_log2)) {
@@ -478,16 +480,18 @@ struct Mfma {
 #pragma unroll
       for (int r = 0; r < 4; ++r) sv[r] = sc[r] * kmul;
     }
+    if (p.slopes) {
+      const float at = (float)(rpos - 4 * qg);
 #pragma unroll
-    for (int r = 0; r < 4; ++r) {
-      const int t = 4 * qg + r;
-      float y = sv[r];
-      if (p.slopes) y = __builtin_fmaf(-slope, __builtin_fabsf((float)(rpos - t)), y);
-      seen[r] = there && t >= rlo && t < rhi;
-      masked = masked || !seen[r];
-      sv[r] = seen[r] ? y : neg_inf();
-      mx = fmaxf(mx, sv[r]);
+      for (int r = 0; r < 4; ++r) sv[r] = __builtin_fmaf(-slope, __builtin_fabsf(at - (float)r), sv[r]);
     }
+    const int lo0 = rlo, hi0 = rhi;
+    if (masked) {
+#pragma unroll
+      for (int r = 0; r < 4; ++r) sv[r] = sees(lo0, hi0, 4 * qg + r) ? sv[r] : neg_inf();
+    }
+#pragma unroll
+    for (int r = 0; r < 4; ++r) mx = fmaxf(mx, sv[r]);
     rlo -= kPage;
     rhi -= kPage;
     rpos -= kPage;
@@ -508,11 +512,16 @@ struct Mfma {
       l += pr[r];
     }
     VOp v = vo ? *vo : v_operand(f);
-    if (__builtin_amdgcn_ballot_w64(masked) != 0) {
+    if (masked) {
       u16x2 top = {0, 0};
 #pragma unroll
       for (int t = 0; t < DT; ++t) top = magnitude_max(top, __builtin_bit_cast(u32x2, v.a[t]));
-      if (__builtin_amdgcn_ballot_w64(not_finite(top)) != 0) add_not_finite(v, seen);
+      if (__builtin_amdgcn_ballot_w64(not_finite(top)) != 0) {
+        bool seen[4];
+#pragma unroll
+        for (int r = 0; r < 4; ++r) seen[r] = sees(lo0, hi0, 4 * qg + r);
+        add_not_finite(v, seen);
+      }
     }
     const u32x2 hi = {pack_bf16(pr[0] * vmul, pr[1] * vmul), pack_bf16(pr[2] * vmul, pr[3] * vmul)};
     const u32x2 lo = remainders(pr, vmul);
@@ -548,11 +557,11 @@ struct Mfma {
       const f32x4 cu = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(up, sees, zero, 0, 0, 0);
       const f32x4 cd = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(down, sees, zero, 0, 0, 0);
       const f32x4 cn = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(nan, sees, zero, 0, 0, 0);
+      // A count to an infinity, or 0.  (Comparisons kept a hundred masks alive.)
+      const auto many = [](float n) { return __builtin_amdgcn_ldexpf(n, 255); };
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
-        if (cu[r] > 0.f) acc[t][r] -= neg_inf();
-        if (cd[r] > 0.f) acc[t][r] += neg_inf();
-        if (cn[r] > 0.f) acc[t][r] = __builtin_nanf("");
+        acc[t][r] += many(cu[r]) - many(cd[r]) + 0.f * many(cn[r]);
       }
     }
   }
