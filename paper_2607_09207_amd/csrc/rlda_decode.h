@@ -474,7 +474,7 @@ struct Mfma {
         for (int r = 0; r < 4; ++r) sv[r] = cap_score_wide(sc[r], kmul, arg, p.cap_log2);
       } else {
 #pragma unroll
-        for (int r = 0; r < 4; ++r) sv[r] = cap_score(sc[r], arg, p.cap_log2);
+        for (int r = 0; r < 4; ++r) sv[r] = cap_score(sc[r], arg, p.cap_log2, p.cap_log2);
       }
     } else {
 #pragma unroll

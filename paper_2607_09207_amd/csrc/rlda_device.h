@@ -116,8 +116,9 @@ __device__ __forceinline__ bool not_finite(u16x2 top) { return top[0] >= 0x7F80 
 // y = x * mul and arg = mul * 2 / cap: cap - 2 cap / (e^(2 y / cap) + 1), exact at both ends.
 // Its error is 2^-22 of the cap, 1.5e-5 in a score at a cap of 64 (bf16 products of random
 // signs: a few 1e-6 in the result).
-__device__ __forceinline__ float cap_score(float x, float arg, float cap_log2) {
-  return __builtin_fmaf(-2.f * cap_log2, __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(x * arg) + 1.f), cap_log2);
+// top: cap_log2, and what the caller adds to the score (at no cost).
+__device__ __forceinline__ float cap_score(float x, float arg, float cap_log2, float top) {
+  return __builtin_fmaf(-2.f * cap_log2, __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(x * arg) + 1.f), top);
 }
 
 // Wider caps take the odd series where |y| is below a sixteenth of the cap (the next term is
@@ -126,7 +127,7 @@ __host__ __device__ __forceinline__ bool wide_cap(float cap_log2) { return cap_l
 __device__ __forceinline__ float cap_score_wide(float x, float mul, float arg, float cap_log2) {
   const float z = x * arg * 0.5f * 0.6931471805599453f, z2 = z * z;   // y / cap_log2
   const float small = x * mul * __builtin_fmaf(z2, __builtin_fmaf(z2, __builtin_fmaf(z2, -17.f / 315.f, 2.f / 15.f), -1.f / 3.f), 1.f);
-  return __builtin_fabsf(z) < 0.0625f ? small : cap_score(x, arg, cap_log2);
+  return __builtin_fabsf(z) < 0.0625f ? small : cap_score(x, arg, cap_log2, cap_log2);
 }
 
 }  // namespace

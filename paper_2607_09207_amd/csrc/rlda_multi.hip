@@ -533,7 +533,15 @@ void multi_query_kernel(const Params p) {
     }
     if constexpr (FP8) st.scale = tok > 0 ? (is_v ? p.v_scale : p.k_scale)[(int64_t)pid * Hkv + g] : 0.f;
   };
-  auto page_write = [&](const Staged& st, int is_v, int buf, int slot) {
+  auto page_write = [&](Staged& st, int is_v, int buf, int slot) {
+    if constexpr (MOD && FP8) {
+      // A page of zeros (scales up to 2^-100 count as 0) has scale 1: the softmax takes its log.
+      if (is_v && uni((int)(st.scale <= 0x1p-100f)) != 0) {
+        st.scale = 1.f;
+#pragma unroll
+        for (int k = 0; k < S::LPL; ++k) st.r[k] = u32x4{0u, 0u, 0u, 0u};
+      }
+    }
     char* dst = is_v ? s_v[buf] : s_k[buf];
     const int RS = is_v ? S::vrs(false) : S::krs(false);
 #pragma unroll
@@ -627,12 +635,22 @@ void multi_query_kernel(const Params p) {
   auto softmax = [&](int t, int kb, int buf, const f32x16* sc) {
     // Lane 32h + i holds S^T[key 32kh + 8(j/4) + 4h + j%4][row i] of key tile kh,
     // j < 16: page 2kh for j < 8, 2kh + 1 above.
-    float km[2 * kKH], vm[2 * kKH];
+    // MOD, fp8: V's scales enter the exponent, exp2(y + log2 v - m), and the sum takes the
+    // weights over v: the row's largest weight is a power of two where m is its own, and has no
+    // rounding (p v rounded: 2.4e-3 and up to 2.7e-3 of a result that bf16 itself holds to
+    // 1.7e-3), and a product less for every weight.
+    constexpr bool kExpScale = MOD && FP8;
+    float km[2 * kKH], vm[2 * kKH], iv[2 * kKH];
     int bad = 0;
 #pragma unroll
     for (int q = 0; q < 2 * kKH; ++q) {
       km[q] = FP8 ? p.scale_log2 * s_scale[buf][q] : p.scale_log2;
       vm[q] = FP8 ? s_scale[buf][2 * kKH + q] : 1.f;
+      iv[q] = 1.f;
+      if constexpr (kExpScale) {   // (taken once, where the pages are written to LDS, they cost 13 us of 228)
+        iv[q] = __builtin_amdgcn_rcpf(vm[q]);
+        vm[q] = __builtin_amdgcn_logf(vm[q]);   // log2
+      }
       bad |= s_bad[buf][q];
     }
     // bf16: one positive factor for the whole block, so the maximum is taken on the
@@ -647,11 +665,11 @@ void multi_query_kernel(const Params p) {
         const float arg[2] = {km[0] * p.cap_arg, km[1] * p.cap_arg};
 #pragma unroll
         for (int j = 0; j < 16; ++j)
-          sv[0][j] = WIDE ? cap_score_wide(sv[0][j], km[j >> 3], arg[j >> 3], p.cap_log2)
-                          : cap_score(sv[0][j], arg[j >> 3], p.cap_log2);
+          sv[0][j] = WIDE ? cap_score_wide(sv[0][j], km[j >> 3], arg[j >> 3], p.cap_log2) + (kExpScale ? vm[j >> 3] : 0.f)
+                          : cap_score(sv[0][j], arg[j >> 3], p.cap_log2, p.cap_log2 + (kExpScale ? vm[j >> 3] : 0.f));
       } else {
 #pragma unroll
-        for (int j = 0; j < 16; ++j) sv[0][j] *= km[j >> 3];
+        for (int j = 0; j < 16; ++j) sv[0][j] = kExpScale ? __builtin_fmaf(sv[0][j], km[j >> 3], vm[j >> 3]) : sv[0][j] * km[j >> 3];
       }
       if (p.slopes) {
         const float at = (float)(base_pos + qi[t] - kb * kKeys - 4 * hh);   // position less the key of j = 0
@@ -702,13 +720,13 @@ void multi_query_kernel(const Params p) {
 #pragma unroll
       for (int j = 0; j < 16; ++j) {
         pr[j] = __builtin_amdgcn_exp2f(__builtin_fmaf(sv[kh][j], fk, -mu));
-        l[t] += pr[j];
+        l[t] = kExpScale ? __builtin_fmaf(pr[j], iv[2 * kh + (j >> 3)], l[t]) : l[t] + pr[j];
       }
       // P^T operand of key step kk: K position 8h + e is key 16kk + 8(e/4) + 4h + e%4
       // of the key tile.
 #pragma unroll
       for (int kk = 0; kk < 2; ++kk) {
-        const float v = vm[2 * kh + kk];
+        const float v = kExpScale ? 1.f : vm[2 * kh + kk];
         const u32x4 w = {pack_bf16(pr[8 * kk] * v, pr[8 * kk + 1] * v), pack_bf16(pr[8 * kk + 2] * v, pr[8 * kk + 3] * v),
                          pack_bf16(pr[8 * kk + 4] * v, pr[8 * kk + 5] * v), pack_bf16(pr[8 * kk + 6] * v, pr[8 * kk + 7] * v)};
         pb[t][kh][kk] = __builtin_bit_cast(bf16x8, w);

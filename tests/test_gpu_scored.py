@@ -287,6 +287,17 @@ def test_odd_values_in_masked_places(torch, kv, d):
             c.check(mod, few, f"documents, odd {what}", max_q_len=max(rows) if few else 0)
 
 
+@pytest.mark.parametrize("rows,kw", [(None, {}), ([4, 3, 5], dict(max_q_len=5)), ([90, 70, 60], {})])
+def test_pages_of_zeros(torch, rows, kw):
+    """fp8 pages whose V scale is 0: their keys count, with values of 0."""
+    c = Case(torch, "fp8", 8, 2, 128, [300, 90, 77], rows, seed=4)
+    for b, j in ((0, 0), (0, 7), (0, 18), (1, 5), (2, 0), (2, 1), (2, 2), (2, 3), (2, 4)):
+        c.vs[int(c.table[b, j])] = 0.0
+    for mod in (dict(), dict(score_cap=10.0), dict(window=40)):
+        got = c.check(mod, rows is None or max(rows) < 16, "zeros", **kw)
+        assert not got[2 if rows is None else slice(int(c.start[2]), None)].any()
+
+
 @pytest.mark.parametrize("kv", ["bf16", "fp8"])
 def test_pages_below_the_window_are_not_read(torch, kv):
     for rows, few in ((None, True), ([3, 4], True), ([40, 30], False)):
