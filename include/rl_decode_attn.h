@@ -319,8 +319,9 @@ typedef struct {
  * and workspace as for these.  Pages below every row's interval are not read, their
  * block-table entries neither.  Supported for bf16 and fp8 caches (RLDA_ERR_UNSUPPORTED
  * for f32), with q_start for batches up to 4096 (RLDA_ERR_UNSUPPORTED).  fp8: the scales of
- * pages that are read are finite, and those of V pages up to 2^-100 may count as 0.  Rows at negative positions (n_b > seq_lens[b]) give zeros.  One kernel,
- * asynchronous; events: both NULL, or both recorded around it.
+ * pages that are read are finite, and those of V pages up to 2^-100 may count as 0.  Rows
+ * at negative positions (n_b > seq_lens[b]) give zeros.  One kernel, asynchronous; events:
+ * both NULL, or both recorded around it.
  */
 rlda_status rl_decode_attn_run_scored(rl_decode_attn_t handle, const rl_decode_attn_scores* scores, int32_t batch,
                                       int32_t num_pages, int32_t total_q, int32_t max_q_len, const void* q,

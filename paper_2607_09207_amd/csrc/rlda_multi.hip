@@ -149,10 +149,10 @@ __device__ __forceinline__ int wave_min(int x) { return 0x7fffffff - wave_max(0x
 // score registers, and a row sees the keys of an interval.  The workgroup walks the blocks
 // from the first key that one of its rows sees to the last; a wave skips those that none of
 // its own sees, and masks only the ones that some of its rows sees in part.
-//   16384 tokens (28/4 heads, bf16) in documents of 900 under a cap of 50: 212 us (103 GFLOP
-// on the keys that are seen, 487 TFLOP/s), of which a window of one key takes 88: 235 MB of q
+//   16384 tokens (28/4 heads, bf16) in documents of 900 under a cap of 50: 210 us (103 GFLOP
+// on the keys that are seen, 492 TFLOP/s), of which a window of one key takes 88: 235 MB of q
 // and out and 3584 workgroups' starts and ends.  4096 tokens (40/8 heads, fp8) with a bias
-// and prefixes: 222 us (147 GFLOP, 664 TFLOP/s).  The matrix cores are busy for 20 to 26% of
+// and prefixes: 225 us (147 GFLOP, 655 TFLOP/s).  The matrix cores are busy for 20 to 26% of
 // it: what bounds it is the chain of a block, score, cap or bias, softmax, product, at three
 // waves per SIMD; a tenth fewer VALU operations (the maximum subtracted by the multiply-adds
 // before it) took as long, and so did priorities of the waves (s_setprio) in either phase.

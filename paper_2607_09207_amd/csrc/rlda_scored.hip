@@ -6,8 +6,9 @@
 // own length.
 // Reading the keys bounds it, as it does the plain kernel, and the scores' operations hide
 // behind that: 64 sequences of a long-tailed cache (28/4 heads, 482 MB) with a bias 85 us, 5.6
-// TB/s, without 84; 4 of up to 16384 tokens under a cap 33, without 31; 128 fp8 sequences, a
-// window of 4096 and a cap 150 us (800 MB, 5.3 TB/s).
+// TB/s, without 84; 4 of up to 16384 tokens under a cap 31.5, without 31; 128 fp8 sequences, a
+// window of 4096 and a cap 139 us (800 MB, 5.8 TB/s; 150 with masks and a bias of 0 computed on
+// every page).
 #include "rlda_decode.h"
 #include "rlda_params.h"
 
