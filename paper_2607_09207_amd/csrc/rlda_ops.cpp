@@ -69,21 +69,26 @@ void set_rotary(RotaryParams& p, const rl_decode_attn_rotary& r, int d, int rows
 
 int64_t rotary_blocks(const RotaryParams& p) { return ((int64_t)p.rows + p.win - 1) / p.win * (p.parts + p.page_parts); }
 
-// Windows, and workgroups of a window: kWanted that turn rows in all, where the rows give
-// them, none without a unit for its threads.  us a call by kWanted 2048 / 8192: 32768 x 32
-// heads of 128 89.6 / 83.6.  Windows stay small while they are enough, since each of its
-// workgroups takes a window's sines and cosines; fp8 caches have windows of a page where
-// sequences bring several rows, so that few of them hold no page's first row.
+// Windows, and workgroups of a window.  A window doubles while it has fewer than two units
+// a thread and enough windows are left: each takes its rows' sines and cosines, and
+// more units to a thread than two gain nothing.  us a call, windows by 8192 workgroups alone /
+// so: 8192 rows of 8 heads of 64 11.8 / 4.8, 32768 of 1 of 128 14.6 / 9.2, of 32 91.6 / 88.1.
+// fp8 caches have windows of a page where sequences bring several rows, so that few of them
+// hold no page's first row.  Up to kWanted workgroups turn rows, none without a unit for its
+// threads.
 //   Workgroups that write pages: four pages to a wave, or one while they are few.
-//   Inputs beyond kStreamBytes are read past the caches, which they would only pass through
-// (32768 x 32 heads 101 to 84 us); smaller ones are where the projection left them (512
-// tokens, 64/8 heads: 7.8 us, and 9.4 past the caches).
-constexpr int kWanted = 8192, kWantedPages = 2048;
+//   Inputs beyond kStreamBytes are read past the caches, which they would only pass through,
+// and written so: 32768 x 32 heads, neither 101.6 us a call, the loads 96.3, both 91.3;
+// 26,237 rows into fp8 pages 144.5, 145.1, 140.2.  Smaller ones are where the projection
+// left them (512 tokens, 64/8 heads: 7.8 us, and 9.4 past the caches).
+constexpr int kWanted = 8192, kWindows = 1024, kPagedWindows = 128, kWantedPages = 2048;
 constexpr int64_t kStreamBytes = 128ll << 20;
 void set_windows(RotaryParams& p, int64_t units_a_row, int64_t jobs_a_row, int64_t bytes_a_row) {
   const bool paged = jobs_a_row > 0 && p.q_start;
   p.win = 1;
-  while (p.win < rlda::kRotaryWindow && p.rows >= 2ll * p.win * (paged ? 128 : kWanted)) p.win *= 2;
+  while (p.win < rlda::kRotaryWindow && p.rows >= 2ll * p.win * (paged ? kPagedWindows : kWindows) &&
+         (paged || p.win * units_a_row < 2 * rlda::kThreads))
+    p.win *= 2;
   const int64_t windows = ((int64_t)p.rows + p.win - 1) / p.win, n = std::min(p.rows, p.win);
   auto most = [](int64_t a, int64_t b) { return (a + b - 1) / b; };
   p.parts = (int)std::max<int64_t>(std::min(kWanted / windows, most(n * units_a_row, rlda::kThreads)), 1);

@@ -361,8 +361,11 @@ __global__ __launch_bounds__(kMgr) void page_fork_kernel(const PageParams p) {
 
 // Copy page src over page dst in caches [first, last) by the workgroup.  A wave takes runs of
 // 64 chunks of 16 bytes (a page of a cache is a multiple of that), kU of them in flight
-// whichever cache they are in.  The copies are written past the caches, which would only
+// whichever cache they are in.  ONCE: every page is read once, past the caches too (the
+// compaction below 197 us a call, 192 so; a fork's parents are read by all of their children,
+// 34 and 46).  The copies are written past the caches, which would only
 // hold them in the way of the pages that are read again (fork below: 44.6 us a call, 35.5 so).
+template <bool ONCE>
 __device__ __forceinline__ void copy_page(const PageParams& p, int src, int dst, int first, int last) {
   constexpr int kU = 4;
   const int lane = threadIdx.x & 63, wave = uni((int)(threadIdx.x >> 6));
@@ -382,7 +385,8 @@ __device__ __forceinline__ void copy_page(const PageParams& p, int src, int dst,
       const PageCache& c = p.caches[first + (pool >> 1)];
       char* base = (pool & 1 ? c.v : c.k) + at;
       if (k < kU)
-        v[j] = *(const u32x4*)(base + (int64_t)src * p.stride_page);
+        v[j] = ONCE ? __builtin_nontemporal_load((const u32x4*)(base + (int64_t)src * p.stride_page))
+                    : *(const u32x4*)(base + (int64_t)src * p.stride_page);
       else
         __builtin_nontemporal_store(v[j], (u32x4*)(base + (int64_t)dst * p.stride_page));
     }
@@ -407,7 +411,7 @@ __global__ __launch_bounds__(kThreads) void page_copy_kernel(const PageParams p)
     if ((uint32_t)src >= (uint32_t)p.num_pages || (uint32_t)dst >= (uint32_t)p.num_pages) {
       if (threadIdx.x == 0) atomicOr(p.flags, kFlagBadPage);
     } else if (src != dst) {
-      copy_page(p, src, dst, part * p.block_layers, min((part + 1) * p.block_layers, p.num_caches));
+      copy_page<false>(p, src, dst, part * p.block_layers, min((part + 1) * p.block_layers, p.num_caches));
     }
   }
 }
@@ -422,7 +426,7 @@ __global__ __launch_bounds__(kThreads) void page_fork_rows_kernel(const PagePara
   if (part > 0) {
     const int src = p.list_src[f], dst = p.list_dst[f];
     if (src < 0 || dst < 0) return;
-    copy_page(p, src, dst, (part - 1) * p.block_layers, min(part * p.block_layers, p.num_caches));
+    copy_page<false>(p, src, dst, (part - 1) * p.block_layers, min(part * p.block_layers, p.num_caches));
     return;
   }
   const int full = p.fork_full[f];
@@ -518,7 +522,7 @@ __global__ __launch_bounds__(kThreads) void page_move_kernel(const PageParams p)
   const int64_t items = (int64_t)*p.count_out * p.layer_blocks;
   for (int64_t it = blockIdx.x; it < items; it += gridDim.x) {
     const int i = (int)(it / p.layer_blocks), part = (int)(it - (int64_t)i * p.layer_blocks);
-    copy_page(p, p.list_src[i], p.list_dst[i], part * p.block_layers, min((part + 1) * p.block_layers, p.num_caches));
+    copy_page<true>(p, p.list_src[i], p.list_dst[i], part * p.block_layers, min((part + 1) * p.block_layers, p.num_caches));
   }
 }
 

@@ -18,9 +18,8 @@
 // for before anything else.  Few rows take small windows, and several workgroups to a
 // window with a share of the units each.
 // Rows are read and written once: what bounds it is bandwidth, and latency on few rows.
-// Kernel times: 32768 x 32 heads of 128 in bf16, 82 us (537 MB, 6.5 TB/s; a copy of one large
-// buffer to another reaches 4.9); 26,237 rows of 40/8 heads into fp8 pages, 145 to 152 us (700
-// MB, 4.7 TB/s); one token of 512 sequences, 64/8 heads, 7.6 (21 MB), of 8 sequences 5.0
+// us a call: 32768 x 32 heads of 128 in bf16 88 (537 MB, 6.1 TB/s; a copy of one large
+// buffer to another reaches 4.9); 26,237 rows of 40/8 heads into fp8 pages 140 (700 MB, 5.0 TB/s); one token of 512 sequences, 64/8 heads, 7.6 (21 MB), of 8 sequences 5.0
 // (three dependent reads: length, page id, and the page's scale, and what the launch takes).
 //
 // fp8 caches hold one scale per (page, KV head) that covers every row written so far, so
@@ -64,7 +63,11 @@ struct Chunk<false> {
   __device__ __forceinline__ void set(const float* x) {
     r = u32x4{pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]), pack_bf16(x[4], x[5]), pack_bf16(x[6], x[7])};
   }
-  __device__ __forceinline__ void store(void* p) const { *(u32x4*)p = r; }
+  template <bool STREAM = false>
+  __device__ __forceinline__ void store(void* p) const {
+    if (STREAM) __builtin_nontemporal_store(r, (u32x4*)p);
+    else *(u32x4*)p = r;
+  }
 };
 template <>
 struct Chunk<true> {
@@ -83,9 +86,13 @@ struct Chunk<true> {
 #pragma unroll
     for (int i = 0; i < 8; ++i) r[i >> 2][i & 3] = x[i];
   }
+  template <bool STREAM = false>
   __device__ __forceinline__ void store(void* p) const {
-    *(f32x4*)p = r[0];
-    *((f32x4*)p + 1) = r[1];
+    f32x4* at = (f32x4*)p;
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+      if (STREAM) __builtin_nontemporal_store(r[i], at + i);
+      else at[i] = r[i];
   }
 };
 
@@ -142,7 +149,7 @@ __device__ __forceinline__ uint32_t div_by(uint32_t x, uint32_t magic) { return 
 
 // Units i, i + step, .. of `nrows` rows of `heads` heads (rows first + r, r < nrows): asked
 // for, and then turned and handed to put(row, head, chunk, values) where ok[row].
-// STREAM: rows too many for the caches to hold are read past them (set_windows).
+// STREAM: rows too many for the caches to hold are read and written past them (set_windows).
 template <bool F32, bool IL, bool STREAM>
 struct Units {
   Chunk<F32> a[kUnroll], b[kUnroll];
@@ -223,7 +230,7 @@ __global__ __launch_bounds__(kThreads) void rotate_kernel(const RotaryParams p) 
   constexpr int E = F32 ? 4 : 2;
   for (;;) {
     x.finish(p, s_ok, s_cs, [&](int r, int hd, int c, const Chunk<F32>& v) {
-      v.store((char*)p.q_out + ((int64_t)(first + r) * p.o_rs + (int64_t)hd * p.o_hs + 8 * c) * E);
+      v.template store<STREAM>((char*)p.q_out + ((int64_t)(first + r) * p.o_rs + (int64_t)hd * p.o_hs + 8 * c) * E);
     });
     i += kUnroll * step;
     if (i >= total) break;
@@ -498,7 +505,7 @@ __global__ __launch_bounds__(kThreads) void append_rotary_kernel(const RotaryPar
   // 3. q, and K and V rows of caches that hold them as they are.
   for (;;) {
     x.finish(p, s_ok, s_cs, [&](int r, int hd, int c, const Chunk<F32>& v) {
-      v.store((char*)p.q_out + ((int64_t)(first + r) * p.o_rs + (int64_t)hd * p.o_hs + 8 * c) * E);
+      v.template store<STREAM>((char*)p.q_out + ((int64_t)(first + r) * p.o_rs + (int64_t)hd * p.o_hs + 8 * c) * E);
     });
     i += kUnroll * step;
     if (i >= total) break;
