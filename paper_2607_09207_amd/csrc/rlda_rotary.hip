@@ -344,14 +344,16 @@ __device__ __forceinline__ void write_page(const RotaryParams& p, const void* x,
     }
   }
   // x num / den, correctly rounded: a quotient by the rounded reciprocal, corrected by its
-  // remainder (exact with a correctly rounded reciprocal); by division where the
-  // reciprocal would overflow.
-  const float num = grows ? 448.f : 1.f, den = grows ? amax : s;
-  const bool small = den < 0x1p-100f;
+  // remainder (exact with a correctly rounded reciprocal); by division where the reciprocal
+  // or the remainder would leave the range, both sides of it 2^16 smaller where 448 x would
+  // overflow (a magnitude beside which 2^-110 is a zero byte), and where den is infinite.
+  const float den_of = grows ? amax : s;
+  const bool wide = den_of > 0x1p100f, divide = den_of < 0x1p-100f || wide;
+  const float num = (grows ? 448.f : 1.f) * (wide ? 0x1p-16f : 1.f), den = wide ? den_of * 0x1p-16f : den_of;
   const float inv = 1.f / den;
   auto quotient = [&](float f) {
     const float n = f * num;
-    if (small) return n / den;
+    if (divide) return n / den;
     const float q = n * inv;
     return __builtin_fmaf(__builtin_fmaf(-den, q, n), inv, q);
   };

@@ -506,6 +506,44 @@ def test_one_token_is_append(torch, kv):
             assert abs(row[e] * 448 / np.abs(row).max() - mid) <= 2.0 ** -22 * abs(mid), "not halfway between two codes"
 
 
+@pytest.mark.parametrize("rows", [None, [7, 20, 3]], ids=["one", "chunks"])
+def test_large_rows_in_fp8(torch, rows):
+    """Rows near the largest bf16 value, and (of V) beside an infinity: E4M3(448 value / amax) or
+    E4M3(value / scale), as the quotients are in 64 bits (448 value overflows in 32)."""
+    from paper_2607_09207_amd import rotary_frequencies
+    freqs, _ = rotary_frequencies(64)
+    for big in (7e35, 8e35, 1e37, 3.3e38):
+        say("large rows", rows, big)
+        c = Case(torch, "fp8", 4, 2, 64, [40, 20, 35], rows, seed=6)
+        n = c.q.shape[0]
+        # Magnitudes from the largest down to 2^-20 of it: codes of every size.
+        g = torch.Generator("cuda").manual_seed(1)
+        for t in (c.k_new, c.v_new):
+            size = torch.exp2(-20 * torch.rand(t.shape, device="cuda", generator=g))
+            t.copy_(torch.where(torch.rand(t.shape, device="cuda", generator=g) < 0.5, -big, big) * size)
+            t[..., 5] = big
+        c.v_new[n - 1, 1, 9] = float("inf")
+        old = {x: getattr(c, x + "s").clone().cpu().numpy() for x in "kv"}
+        c.run(freqs, positions=torch.zeros(n, dtype=torch.int32, device="cuda"))
+        rows_of = {}
+        for r, b, t in c.tokens():
+            rows_of.setdefault(int(c.table[b, t // PAGE]), []).append((t % PAGE, r))
+        for name in "kv":
+            new, code = np64(getattr(c, name + "_new")), raw(getattr(c, name))
+            scale = getattr(c, name + "s").cpu().numpy().astype(np.float64)
+            for p, of in rows_of.items():
+                for g in range(c.hkv):
+                    x = np.stack([new[r, g] for _, r in of])
+                    amax = np.abs(x).max()
+                    assert of[0][0] == 0 or amax > 448 * float(old[name][p, g])   # they set the scale
+                    assert scale[p, g] == np.float32(amax) / np.float32(448) if np.isfinite(amax) else np.isinf(scale[p, g])
+                    got = np.stack([code[p, g, s] for s, _ in of])
+                    if np.isfinite(amax):
+                        assert np.array_equal(got, e4m3_encode(448.0 * x / amax)), (name, p, g)
+                    else:
+                        assert np.array_equal((got & 0x7F) == 0x7F, np.isinf(x)) and not (got[np.isfinite(x)] & 0x7F).any()
+
+
 @pytest.mark.parametrize("kv", ["bf16", "fp8"])
 def test_bad_rows_are_flagged_and_skipped(torch, kv):
     from paper_2607_09207_amd import rotary_frequencies
