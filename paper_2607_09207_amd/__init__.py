@@ -70,6 +70,7 @@ class DecodeAttention(CacheOps):
         P, d = page_size, head_dim
         self._kv_strides = (tuple(int(x) for x in kv_strides) if kv_strides is not None
                             else (num_kv_heads * P * d, P * d, d))
+        self._geometry = (cfg.kv_dtype, num_kv_heads, P, d, self._kv_strides)   # of its caches (CacheSet)
         h = ctypes.c_void_p()
         _abi.check(lib.rl_decode_attn_create(ctypes.byref(cfg), ctypes.byref(h)), "rl_decode_attn_create")
         self._lib, self._h, self.config = lib, h, cfg

@@ -12,10 +12,11 @@ from .rotary import check_freqs, check_rows, on_device, raw_stream, rotary_of, r
 
 class CacheSet:
     """The caches of the layers that share one pool's page ids, checked once
-    (DecodeAttention.caches)."""
+    (DecodeAttention.caches), for layers whose caches are of the same `geometry`."""
 
-    def __init__(self, tensors, array, num_pages, device):
+    def __init__(self, tensors, array, num_pages, device, geometry):
         self.tensors, self.array, self.num_pages, self.device = tensors, array, num_pages, device
+        self.geometry = geometry
         # As the native call path takes it: number, address, pages, device.
         self.native = (len(tensors), ctypes.addressof(array), num_pages, None if device is None else device.index)
 
@@ -24,6 +25,13 @@ class CacheSet:
 
 
 class CacheOps:
+    def _check_set(self, what, caches):
+        """The page operations copy by their own layer's page size and strides."""
+        if len(caches) and caches.geometry != self._geometry:
+            self._fail(what, f"the caches are of (dtype, KV heads, page size, head_dim, strides) {caches.geometry}, "
+                             f"the layer's of {self._geometry}")
+        return caches
+
     # ---------------------------------------------------------------- rotary positions
 
     def append_rotary(self, q, k_new, v_new, k_cache, v_cache, block_table, seq_lens, freqs, *, q_start=None,
@@ -109,7 +117,8 @@ class CacheOps:
     def caches(self, layers, num_pages: Optional[int] = None):
         """The caches of the layers that share one pool's page ids, as the page operations
         take them: [(k_cache, v_cache), ...], or (k_cache, v_cache, k_scale, v_scale) for
-        fp8.  Checked here once; the set keeps the tensors."""
+        fp8.  Checked here once; the set keeps the tensors.  Every layer whose caches have
+        the same dtype, heads and strides takes the set."""
         what = "caches"
         layers = [tuple(x) for x in layers]
         fp8 = self.config.kv_dtype == _abi.RLDA_FP8_E4M3FN
@@ -117,7 +126,7 @@ class CacheOps:
             if len(x) != (4 if fp8 else 2):
                 self._fail(what, "a cache is (k_cache, v_cache), with (.., k_scale, v_scale) for fp8")
         if not layers:
-            return CacheSet([], (_abi.Cache * 1)(), None, None)
+            return CacheSet([], (_abi.Cache * 1)(), None, None, self._geometry)
         dev = layers[0][0].device
         if num_pages is None:
             num_pages = int(layers[0][0].shape[0])
@@ -126,7 +135,7 @@ class CacheOps:
             k, v, ks, vs = x if fp8 else x + (None, None)
             self._check_cache(what, k, v, ks, vs, num_pages, dev)
             array[i] = _abi.Cache(k.data_ptr(), v.data_ptr(), ks.data_ptr() if fp8 else None, vs.data_ptr() if fp8 else None)
-        return CacheSet(layers, array, num_pages, dev)
+        return CacheSet(layers, array, num_pages, dev, self._geometry)
 
     def _page_call(self, what, refs, block_table, seq_lens, caches, workspace, stream):
         """Checks that the page operations share; (device, batch, pages, caches, workspace)."""
@@ -139,6 +148,8 @@ class CacheOps:
         self._check_table(what, block_table, seq_lens, batch, dev)
         if caches is not None and not isinstance(caches, CacheSet):
             caches = self.caches(caches, npages)
+        if caches is not None:
+            self._check_set(what, caches)
         if caches is not None and len(caches) and (caches.device != dev or caches.num_pages < npages):
             self._fail(what, f"the caches hold {caches.num_pages} pages on {caches.device}, refs {npages} on {dev}")
         return dev, batch, npages, caches
@@ -192,7 +203,7 @@ class CacheOps:
         """Empty rows `children` become copies of rows `parents`: full pages shared, the partial
         last page copied in every cache (rl_decode_attn_page_fork)."""
         what = "rl_decode_attn_page_fork"
-        if isinstance(caches, CacheSet):
+        if isinstance(caches, CacheSet) and caches.geometry == self._geometry:
             got = self._fast.page_fork(refs, block_table, seq_lens, parents, children, *caches.native, workspace, stream)
             if got is not None:
                 return _abi.check(got, what)
@@ -210,7 +221,7 @@ class CacheOps:
         """The live pages move to the front of the pool in every cache; the table and refs
         follow (rl_decode_attn_page_compact).  Returns their number, an int32 tensor of one."""
         what = "rl_decode_attn_page_compact"
-        if isinstance(caches, CacheSet):
+        if isinstance(caches, CacheSet) and caches.geometry == self._geometry:
             got = self._fast.page_compact(refs, block_table, seq_lens, *caches.native, live, workspace, stream)
             if got is not None:
                 return self._answer(got, what)
@@ -230,7 +241,7 @@ class CacheOps:
     def page_copy(self, src, dst, caches, *, workspace=None, stream=None):
         """Page src[i] over page dst[i] in every cache (rl_decode_attn_page_copy)."""
         what = "rl_decode_attn_page_copy"
-        cs = caches if isinstance(caches, CacheSet) else self.caches(caches)
+        cs = self._check_set(what, caches) if isinstance(caches, CacheSet) else self.caches(caches)
         if not len(cs):
             self._fail(what, "caches is empty")
         n = self._rows_list(what, "src", src, cs.device)

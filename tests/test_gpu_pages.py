@@ -383,6 +383,30 @@ def test_refusals(torch):
     s.check("refusals")
 
 
+def test_a_set_of_another_layer(torch):
+    """A set is taken by a layer with caches of the same geometry, by both call paths, and
+    refused by any other, before anything is launched."""
+    from paper_2607_09207_amd import DecodeAttention, RldaError, _abi
+    s = State(torch, 50, [20, 30, 0], 40, "bf16", 2, 64, layers=2)
+    like = DecodeAttention(8, 2, 64, 3, 40, "bf16", "bf16", "bf16")
+    others = [DecodeAttention(8, 2, 64, 3, 40, "bf16", "fp8_e4m3fn", "f32"), DecodeAttention(8, 4, 64, 3, 40),
+              DecodeAttention(8, 2, 128, 3, 40), DecodeAttention(8, 2, 64, 3, 40, kv_strides=(2048, 64, 128))]
+    one = s.cuda([1])
+    for layer in others:
+        for fast in (layer._fast, _abi.LEFT_TO_PYTHON):
+            layer.page_workspace(50, "cuda:0")
+            layer._fast = fast
+            for call in (lambda: layer.page_fork(*s.args(), one, s.cuda([2]), s.caches),
+                         lambda: layer.page_compact(*s.args(), s.caches), lambda: layer.page_copy(one, s.cuda([2]), s.caches)):
+                with pytest.raises(RldaError, match="caches are of"):
+                    call()
+        layer.page_compact(*s.args(), s.layer.caches([]), live=s.cuda([0]))   # of none: any layer's
+    s2 = State(torch, 50, [20, 30, 0], 40, "bf16", 2, 64, layers=2)
+    like.page_fork(*s2.args(), one, s2.cuda([2]), s2.caches)
+    s2.model.fork([1], [2])
+    s2.check("another layer of the same geometry")
+
+
 def test_graph_and_streams(torch):
     """Release, fork and grow captured into one graph and replayed; the same on another stream."""
     def steps(s, stream=None):

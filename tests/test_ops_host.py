@@ -192,6 +192,27 @@ def test_python_refuses_host_tensors():
             call()
 
 
+def test_a_set_of_another_layer():
+    """A set holds addresses: a layer whose pages differ refuses it (here before it looks at
+    the lists, so without a GPU)."""
+    import torch
+
+    from paper_2607_09207_amd import DecodeAttention, RldaError
+    from paper_2607_09207_amd.cache_ops import CacheSet
+    bf16 = DecodeAttention(8, 2, 128, 4, 8, "bf16", "bf16", "bf16")
+    same = DecodeAttention(4, 2, 128, 9, 3, "bf16", "bf16", "f32")
+    k = torch.zeros((5, 2, 16, 128), dtype=torch.bfloat16)
+    cs = CacheSet([(k, k)], (_abi.Cache * 1)(), 5, k.device, bf16._geometry)
+    one = torch.zeros(1, dtype=torch.int32)
+    for other in (DecodeAttention(8, 2, 128, 4, 8, "bf16", "fp8_e4m3fn", "bf16"), DecodeAttention(8, 4, 128, 4, 8),
+                  DecodeAttention(8, 2, 64, 4, 8), DecodeAttention(8, 2, 128, 4, 8, kv_strides=(4096, 128, 256))):
+        with pytest.raises(RldaError, match="caches are of"):
+            other.page_copy(one, one, cs)
+        with pytest.raises(RldaError, match="caches are of"):
+            other._check_set("page_fork", cs)
+    assert same._check_set("page_fork", cs) is cs
+
+
 def test_frequencies():
     import torch
 
