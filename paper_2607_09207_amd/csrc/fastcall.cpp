@@ -15,6 +15,7 @@
 
 #include <ATen/TensorSubclassLikeUtils.h>
 #include <ATen/ATen.h>
+#include <c10/core/AutogradState.h>
 #include <c10/core/GradMode.h>
 #include <c10/core/impl/VirtualGuardImpl.h>
 #include <torch/csrc/autograd/python_variable.h>
@@ -393,12 +394,19 @@ bool rows_of(const Tensor* t, int dev, at::ScalarType type, int64_t n, int64_t h
   return true;
 }
 
+// A tensor whose derivatives are asked for, by either mode: Python notes it or refuses it.
+bool derived(const Tensor& t) {
+  return (t.requires_grad() && c10::GradMode::is_enabled()) ||
+         (c10::AutogradState::get_tls_state().get_fw_grad_mode() && t._fw_grad(0).defined());
+}
+
 bool rotary_of(PyObject* freqs, PyObject* interleaved, PyObject* amplitude, int inverse, int dev, int64_t d,
                rl_decode_attn_rotary* out) {
   const Tensor* f = tensor(freqs);
   int il = 0;
   double a = 1.0;
-  if (!plain(f, dev, at::kDouble) || (f->requires_grad() && c10::GradMode::is_enabled()) || f->dim() != 1 || !f->is_contiguous() || !as_bool(interleaved, &il) || !as_double(amplitude, &a))
+  if (!plain(f, dev, at::kDouble) || derived(*f) || f->dim() != 1 || !f->is_contiguous() || !as_bool(interleaved, &il) ||
+      !as_double(amplitude, &a))
     return false;
   const int64_t half = f->size(0);
   if (half < 8 || 2 * half > d || half % 8) return false;
@@ -494,7 +502,7 @@ PyObject* rotate(PyObject*, PyObject* const* a, Py_ssize_t n) {
     if (!x || !x->is_cuda() || x->dim() != 3 || (a[6] == Py_None && a[7] != Py_None)) return nullptr;
     const auto type = x->scalar_type();
     if (type != at::kBFloat16 && type != at::kFloat) return nullptr;
-    if (x->requires_grad() && c10::GradMode::is_enabled()) return nullptr;   // Python notes it for the backward pass
+    if (derived(*x)) return nullptr;
     const int dev = x->get_device();
     const int64_t rows = x->size(0), heads = x->size(1), d = x->size(2);
     int inverse = 0;
@@ -512,7 +520,7 @@ PyObject* rotate(PyObject*, PyObject* const* a, Py_ssize_t n) {
       fresh = at::empty({rows, heads, d}, x->options());
     } else {
       out = tensor(a[6]);
-      if (!out || (out->requires_grad() && c10::GradMode::is_enabled())) return nullptr;
+      if (!out || derived(*out)) return nullptr;
     }
     if (!rows_of(out, dev, type, rows, heads, d, &ro)) return nullptr;
     // A backward pass that saved the given tensor is to notice.

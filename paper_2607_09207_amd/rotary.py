@@ -89,12 +89,18 @@ def check_freqs(fail, freqs, d, device):
     import torch
     if freqs is None or not freqs.is_cuda or freqs.device != device:
         fail(f"freqs must be on {device}")
-    if freqs.requires_grad and torch.is_grad_enabled():
+    if (freqs.requires_grad and torch.is_grad_enabled()) or has_tangent(freqs):
         fail("freqs gets no gradient: detach it")
     if freqs.dtype != torch.float64 or freqs.dim() != 1 or not freqs.is_contiguous():
         fail("freqs must be a contiguous float64 vector")
     if not 16 <= 2 * freqs.shape[0] <= d or freqs.shape[0] % 8:
         fail(f"freqs turns {2 * freqs.shape[0]} elements: a multiple of 16 up to head_dim {d} is supported")
+
+
+def has_tangent(t):
+    """Whether t is a dual tensor (forward-mode derivatives), which requires_grad does not say."""
+    from torch.autograd import forward_ad
+    return forward_ad.unpack_dual(t).tangent is not None
 
 
 def on_device(device):
@@ -123,7 +129,8 @@ _turn = None
 
 
 def _function():
-    """The rotation for autograd: its backward is the rotation by the transpose."""
+    """The rotation for autograd: its backward is the rotation by the transpose, and its
+    forward-mode derivative, as it is linear, itself."""
     global _turn
     if _turn is None:
         import torch
@@ -132,8 +139,9 @@ def _function():
             @staticmethod
             def forward(ctx, x, positions, freqs, interleaved, amplitude, inverse):
                 ctx.save_for_backward(positions, freqs)
+                ctx.save_for_forward(positions, freqs)
                 ctx.how = interleaved, amplitude, inverse
-                return rotate(x, positions, freqs, interleaved=interleaved, amplitude=amplitude, inverse=inverse)
+                return _rotate(x, positions, freqs, interleaved, amplitude, inverse, None, None)
 
             @staticmethod
             def backward(ctx, grad):
@@ -142,6 +150,13 @@ def _function():
                 # (A gradient may come broadcast or in any layout.)
                 return rotate(grad.contiguous(), positions, freqs, interleaved=interleaved, amplitude=amplitude,
                               inverse=not inverse), None, None, None, None, None
+
+            @staticmethod
+            def jvp(ctx, tangent, *_):
+                positions, freqs = ctx.saved_tensors
+                interleaved, amplitude, inverse = ctx.how
+                return rotate(tangent.contiguous(), positions, freqs, interleaved=interleaved, amplitude=amplitude,
+                              inverse=inverse)
 
         _turn = Turn
     return _turn
@@ -153,31 +168,46 @@ def rotate(x, positions, freqs, *, interleaved: bool = False, amplitude: float =
     16-byte aligned, e.g. a slice of a fused projection) turned by positions [n] (int32), pair j
     by positions * freqs[j] radians (rl_decode_attn_rotate).  freqs: float64 [rot_dim / 2]
     (rotary_frequencies); elements past rot_dim pass.  inverse=True turns by the transpose:
-    what takes a gradient back (an x that requires grad has it done by autograd; `out` is
-    refused then).  Returns `out` (x itself for in place), or a new tensor."""
-    what = "rl_decode_attn_rotate"
+    what takes a gradient back (an x that requires grad, or has a tangent, has its derivative
+    done by autograd; `out` is refused then).  Returns `out` (x itself for in place), or a new tensor."""
     native = _abi.fastcall()
     if native is not None:
         got = native.rotate(x, positions, freqs, interleaved, amplitude, inverse, out, stream)
         if got is not None:
             if type(got) is int:
-                _abi.check(got, what)
+                _abi.check(got, _WHAT)
             return got
     import torch
-
-    def fail(msg):
-        raise _abi.RldaError(-1, f"{what}: {msg}")
-
-    if not x.is_cuda:
-        fail(f"x must be on a GPU, got {x.device}")
-    if x.dtype not in (torch.bfloat16, torch.float32):
-        fail(f"x must be bfloat16 or float32, got {x.dtype}")
-    if out is not None and out.requires_grad and torch.is_grad_enabled():
-        fail("out requires grad")
-    if x.requires_grad and torch.is_grad_enabled():
+    if out is not None and ((out.requires_grad and torch.is_grad_enabled()) or has_tangent(out)):
+        _refuse("out requires grad")
+    if (x.requires_grad and torch.is_grad_enabled()) or has_tangent(x):
         if out is not None or stream is not None:
-            fail("an x that requires grad is turned into a new tensor, on the current stream")
+            _refuse("an x that requires grad is turned into a new tensor, on the current stream")
+        _check_type(x)
         return _function().apply(x, positions, freqs, interleaved, amplitude, inverse)
+    return _rotate(x, positions, freqs, interleaved, amplitude, inverse, out, stream)
+
+
+_WHAT = "rl_decode_attn_rotate"
+
+
+def _refuse(msg):
+    raise _abi.RldaError(-1, f"{_WHAT}: {msg}")
+
+
+def _check_type(x):
+    import torch
+    if not x.is_cuda:
+        _refuse(f"x must be on a GPU, got {x.device}")
+    if x.dtype not in (torch.bfloat16, torch.float32):
+        _refuse(f"x must be bfloat16 or float32, got {x.dtype}")
+
+
+def _rotate(x, positions, freqs, interleaved, amplitude, inverse, out, stream):
+    """rotate() without derivatives."""
+    import torch
+    fail = _refuse
+    _check_type(x)
     dev = x.device
     shape = tuple(x.shape)
     check_rows(fail, "x", x, x.dtype, shape, dev)
@@ -196,5 +226,5 @@ def rotate(x, positions, freqs, *, interleaved: bool = False, amplitude: float =
         xr, outr, rot = rows_of(x), rows_of(out), rotary_of(freqs, interleaved, amplitude, inverse)
         _abi.check(_abi.load().rl_decode_attn_rotate(
             _abi.RLDA_F32 if x.dtype == torch.float32 else _abi.RLDA_BF16, shape[0], shape[1], shape[2], ctypes.byref(xr),
-            positions.data_ptr(), ctypes.byref(rot), ctypes.byref(outr), raw_stream(dev, stream)), what)
+            positions.data_ptr(), ctypes.byref(rot), ctypes.byref(outr), raw_stream(dev, stream)), _WHAT)
     return out

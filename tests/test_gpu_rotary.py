@@ -235,6 +235,39 @@ def test_autograd_refusals_and_versions(torch):
         assert rotate(z, pos, freqs, out=z) is z
 
 
+@pytest.mark.parametrize("native", [True, False], ids=["native", "python"])
+def test_forward_mode(torch, native, monkeypatch):
+    """A dual tensor's tangent is turned as its value is (the rotation is linear), also where it
+    requires grad; a tangent that would be lost is refused."""
+    import torch.autograd.forward_ad as fwd
+
+    from paper_2607_09207_amd import RldaError, _abi, rotary_frequencies, rotate
+    if not native:
+        monkeypatch.setattr(_abi, "fastcall", lambda: None)
+    freqs, _ = rotary_frequencies(64)
+    x, t = (torch.randn((5, 2, 64), device="cuda") for _ in range(2))
+    pos = torch.arange(5, device="cuda", dtype=torch.int32)
+    kw = dict(interleaved=True, amplitude=1.5)
+    y, ty = rotate(x, pos, freqs, **kw), rotate(t, pos, freqs, **kw)
+    leaf = x.clone().requires_grad_()
+    with fwd.dual_level():
+        for v in (x, leaf):
+            got = fwd.unpack_dual(rotate(fwd.make_dual(v, t), pos, freqs, **kw))
+            assert torch.equal(got.primal, y) and torch.equal(got.tangent, ty)
+        assert torch.equal(torch.autograd.grad(got.primal, leaf, t)[0], rotate(t, pos, freqs, inverse=True, **kw))
+        # (a tangent of any layout, and the tangent of the inverse)
+        wide = torch.randn((2, 64, 5), device="cuda").permute(2, 0, 1)
+        got = fwd.unpack_dual(rotate(fwd.make_dual(x, wide), pos, freqs, inverse=True)).tangent
+        assert torch.equal(got, rotate(wide.contiguous(), pos, freqs, inverse=True))
+        dual = fwd.make_dual(x, t)
+        for bad in (lambda: rotate(dual, pos, freqs, out=torch.empty_like(x)), lambda: rotate(x, pos, freqs, out=dual),
+                    lambda: rotate(dual, pos, freqs, stream=torch.cuda.current_stream()),
+                    lambda: rotate(x, pos, fwd.make_dual(freqs, freqs))):
+            with pytest.raises(RldaError):
+                bad()
+        assert fwd.unpack_dual(rotate(x, pos, freqs)).tangent is None
+
+
 def test_single_rows_of_any_stride(torch):
     """One row, or one head, of a buffer whose other stride is no multiple of 16 bytes."""
     from paper_2607_09207_amd import rotary_frequencies, rotate
