@@ -7,7 +7,7 @@ import ctypes
 from typing import Optional
 
 from . import _abi
-from .rotary import check_freqs, check_rows, on_device, raw_stream, rotary_of, rows_of, used_on
+from .rotary import check_freqs, check_rows, derived, mark_written, on_device, raw_stream, rotary_of, rows_of, used_on
 
 
 class CacheSet:
@@ -42,7 +42,8 @@ class CacheOps:
         row a sequence (token seq_lens[b] - 1), or, with q_start [batch + 1], its last
         q_start[b+1] - q_start[b] tokens.  positions [n] (int32) replaces the rows' tokens as
         what they are turned by.  q, k_new and v_new may be strided (slices of a fused
-        projection); out: a tensor for q (q itself: in place)."""
+        projection); out: a tensor for q (q itself: in place).  No gradient goes through the
+        cache: rows that require grad, or have a tangent, are refused."""
         what = "rl_decode_attn_append_rotary"
         got = self._fast.append_rotary(q, k_cache, v_cache, block_table, seq_lens, k_scale, v_scale, stream, num_pages, out,
                                        workspace, k_new, v_new, freqs, q_start, positions, interleaved, amplitude)
@@ -58,6 +59,9 @@ class CacheOps:
         check_rows(fail, "q", q, qd, (n, cfg.num_q_heads, d), dev)
         check_rows(fail, "k_new", k_new, qd, (n, cfg.num_kv_heads, d), dev)
         check_rows(fail, "v_new", v_new, qd, (n, cfg.num_kv_heads, d), dev)
+        for name, t in (("q", q), ("k_new", k_new), ("v_new", v_new), ("out", out)):
+            if t is not None and derived(t):
+                fail(f"{name} gets no gradient here: detach it (rotate has one)")
         check_freqs(fail, freqs, d, dev)
         batch = n
         if q_start is not None:
@@ -76,6 +80,7 @@ class CacheOps:
                 used_on(out, dev, stream)
             else:
                 check_rows(fail, "out", out, qd, (n, cfg.num_q_heads, d), dev)
+                mark_written(out)
             ws = workspace if workspace is not None else self._own_workspace(dev, stream)
             self._check_workspace(what, ws, dev)
             wp = self._aligned_ptr(ws)

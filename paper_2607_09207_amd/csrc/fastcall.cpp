@@ -400,6 +400,11 @@ bool derived(const Tensor& t) {
          (c10::AutogradState::get_tls_state().get_fw_grad_mode() && t._fw_grad(0).defined());
 }
 
+// A backward pass that saved a tensor written here is to notice.
+void mark_written(const Tensor& t) {
+  if (!t.is_inference()) t.unsafeGetTensorImpl()->bump_version();
+}
+
 bool rotary_of(PyObject* freqs, PyObject* interleaved, PyObject* amplitude, int inverse, int dev, int64_t d,
                rl_decode_attn_rotary* out) {
   const Tensor* f = tensor(freqs);
@@ -476,15 +481,18 @@ PyObject* layer_append_rotary(PyObject* self, PyObject* const* a, Py_ssize_t n) 
     Call c;
     rl_decode_attn_rows rq, rk, rv, ro;
     rl_decode_attn_rotary rot;
+    const Tensor *kn = tensor(a[11]), *vn = tensor(a[12]), *given = a[9] == Py_None ? nullptr : tensor(a[9]);
     if (total > INT32_MAX || !rows_of(q, dev, L->q_dtype, total, L->hq, L->d, &rq) ||
-        !rows_of(tensor(a[11]), dev, L->q_dtype, total, L->hkv, L->d, &rk) ||
-        !rows_of(tensor(a[12]), dev, L->q_dtype, total, L->hkv, L->d, &rv) ||
+        !rows_of(kn, dev, L->q_dtype, total, L->hkv, L->d, &rk) ||
+        !rows_of(vn, dev, L->q_dtype, total, L->hkv, L->d, &rv) || derived(*q) || derived(*kn) || derived(*vn) ||
         !rotary_of(a[13], a[16], a[17], 0, dev, L->d, &rot) || !vector_or_none(a[15], dev, at::kInt, total, &pos) ||
         !common(L, c, a + 1, dev, B) || !workspace(L, c, a[10], false) || !current(dev))
       return nullptr;
     Tensor fresh;
     if (a[9] == Py_None) fresh = at::empty({total, L->hq, L->d}, q->options());
-    if (!rows_of(a[9] == Py_None ? &fresh : tensor(a[9]), dev, L->q_dtype, total, L->hq, L->d, &ro)) return nullptr;
+    if (!rows_of(a[9] == Py_None ? &fresh : given, dev, L->q_dtype, total, L->hq, L->d, &ro) || (given && derived(*given)))
+      return nullptr;
+    if (given) mark_written(*given);
     void *kp = ptr(c.k), *vp = ptr(c.v), *ksp = ptr(c.ks), *vsp = ptr(c.vs), *bp = ptr(c.bt), *lp = ptr(c.lens),
          *qsp = ptr(qs), *pp = ptr(pos);
     WITHOUT_GIL(g_append_rotary(L->handle, (int32_t)B, (int32_t)c.npages, (int32_t)total, &rot, &rq, &rk, &rv,
@@ -523,8 +531,7 @@ PyObject* rotate(PyObject*, PyObject* const* a, Py_ssize_t n) {
       if (!out || derived(*out)) return nullptr;
     }
     if (!rows_of(out, dev, type, rows, heads, d, &ro)) return nullptr;
-    // A backward pass that saved the given tensor is to notice.
-    if (a[6] != Py_None && !out->is_inference()) out->unsafeGetTensorImpl()->bump_version();
+    if (a[6] != Py_None) mark_written(*out);
     const int32_t* pp = (const int32_t*)ptr(pos);
     WITHOUT_GIL(g_rotate(type == at::kFloat ? RLDA_F32 : RLDA_BF16, (int32_t)rows, (int32_t)heads, (int32_t)d, &rx, pp, &rot,
                          &ro, stream));

@@ -89,7 +89,7 @@ def check_freqs(fail, freqs, d, device):
     import torch
     if freqs is None or not freqs.is_cuda or freqs.device != device:
         fail(f"freqs must be on {device}")
-    if (freqs.requires_grad and torch.is_grad_enabled()) or has_tangent(freqs):
+    if derived(freqs):
         fail("freqs gets no gradient: detach it")
     if freqs.dtype != torch.float64 or freqs.dim() != 1 or not freqs.is_contiguous():
         fail("freqs must be a contiguous float64 vector")
@@ -97,10 +97,19 @@ def check_freqs(fail, freqs, d, device):
         fail(f"freqs turns {2 * freqs.shape[0]} elements: a multiple of 16 up to head_dim {d} is supported")
 
 
-def has_tangent(t):
-    """Whether t is a dual tensor (forward-mode derivatives), which requires_grad does not say."""
+def derived(t):
+    """Whether t's derivatives are asked for: backwards, or (a dual tensor, of which requires_grad
+    says nothing) forwards."""
+    import torch
     from torch.autograd import forward_ad
-    return forward_ad.unpack_dual(t).tangent is not None
+    return (t.requires_grad and torch.is_grad_enabled()) or forward_ad.unpack_dual(t).tangent is not None
+
+
+def mark_written(t):
+    """A backward pass that saved t is to notice that it was written."""
+    import torch
+    if not t.is_inference():
+        torch.autograd.graph.increment_version(t)
 
 
 def on_device(device):
@@ -177,10 +186,9 @@ def rotate(x, positions, freqs, *, interleaved: bool = False, amplitude: float =
             if type(got) is int:
                 _abi.check(got, _WHAT)
             return got
-    import torch
-    if out is not None and ((out.requires_grad and torch.is_grad_enabled()) or has_tangent(out)):
+    if out is not None and derived(out):
         _refuse("out requires grad")
-    if (x.requires_grad and torch.is_grad_enabled()) or has_tangent(x):
+    if derived(x):
         if out is not None or stream is not None:
             _refuse("an x that requires grad is turned into a new tensor, on the current stream")
         _check_type(x)
@@ -221,8 +229,7 @@ def _rotate(x, positions, freqs, interleaved, amplitude, inverse, out, stream):
             used_on(out, dev, stream)
         else:
             check_rows(fail, "out", out, x.dtype, shape, dev)
-            if not out.is_inference():
-                torch.autograd.graph.increment_version(out)   # a backward pass that saved it is to notice
+            mark_written(out)
         xr, outr, rot = rows_of(x), rows_of(out), rotary_of(freqs, interleaved, amplitude, inverse)
         _abi.check(_abi.load().rl_decode_attn_rotate(
             _abi.RLDA_F32 if x.dtype == torch.float32 else _abi.RLDA_BF16, shape[0], shape[1], shape[2], ctypes.byref(xr),

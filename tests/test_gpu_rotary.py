@@ -635,6 +635,50 @@ def test_refusals(torch):
         c.layer.append_rotary(*args, q_start=torch.zeros(5, dtype=torch.int32, device="cuda"))
 
 
+@pytest.mark.parametrize("native", [True, False], ids=["native", "python"])
+@pytest.mark.parametrize("rows", [None, [3, 2]], ids=["one", "chunks"])
+def test_append_rotary_derivatives_and_versions(torch, rows, native):
+    """Rows whose gradient or tangent would be lost are refused, before anything is written; a
+    saved tensor turned in place is noticed."""
+    import torch.autograd.forward_ad as fwd
+
+    from paper_2607_09207_amd import RldaError, _abi, rotary_frequencies
+    freqs, _ = rotary_frequencies(64)
+    c = Case(torch, "bf16", 4, 2, 64, [20, 35], rows, seed=3)
+    c.layer.workspace(c.q.device)
+    if not native:
+        c.layer._fast = _abi.LEFT_TO_PYTHON
+    k, v = c.k.clone(), c.v.clone()
+    for name in ("q", "k_new", "v_new"):
+        plain = getattr(c, name)
+        setattr(c, name, plain.clone().requires_grad_())
+        with pytest.raises(RldaError, match=f"{name} gets no gradient"):
+            c.run(freqs)
+        with fwd.dual_level():
+            setattr(c, name, fwd.make_dual(plain.clone(), torch.ones_like(plain)))
+            with pytest.raises(RldaError, match=f"{name} gets no gradient"):
+                c.run(freqs)
+        setattr(c, name, plain)
+    leaf = torch.empty_like(c.q).requires_grad_()
+    with pytest.raises(RldaError, match="out gets no gradient"):
+        c.run(freqs, out=leaf)
+    assert torch.equal(c.k, k) and torch.equal(c.v, v)
+    want = c.run(freqs)
+    with torch.no_grad():   # no derivatives are asked for here
+        c.q = c.q.clone().requires_grad_()
+        assert torch.equal(c.run(freqs), want) and c.run(freqs, out=leaf) is leaf and torch.equal(leaf, want)
+    c.q = c.q.detach()
+    w = torch.ones_like(c.q).requires_grad_()
+    y = w * c.q
+    assert torch.equal(c.run(freqs, out=c.q), want)
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        y.sum().backward()
+    with torch.inference_mode():
+        z = want + 1
+        c.q = z
+        assert c.run(freqs, out=z) is z
+
+
 def test_other_stream_and_graph(torch):
     """A call on another stream, and one captured and replayed, with eager work between."""
     from paper_2607_09207_amd import rotary_frequencies
