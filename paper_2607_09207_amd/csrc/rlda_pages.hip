@@ -533,11 +533,11 @@ __global__ __launch_bounds__(kThreads) void page_move_kernel(const PageParams p)
       int32_t* row = p.block_table + (int64_t)b * p.max_pages;
       for (int j = threadIdx.x; j < pages_of(L); j += kThreads) {
         const int page = row[j];
-        if (page < n && page >= 0) continue;
-        // A page out of the pool, or one that a row names and nothing counts.
+        // A page out of the pool, or one that a row names and nothing counts: below n too, where
+        // a moved page may just have taken its place.
         if ((uint32_t)page >= (uint32_t)p.num_pages || (p.mask[page >> 6] >> (page & 63) & 1))
           atomicOr(p.flags, kFlagBadPage);
-        else
+        else if (page >= n)
           row[j] = p.map[page];
       }
     }

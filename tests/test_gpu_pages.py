@@ -326,6 +326,31 @@ def test_compact_odd_tables(torch):
     assert s.layer.page_flags(100, s.refs.device) == 3
 
 
+@pytest.mark.parametrize("npages", [100, 131072 + 700])
+def test_compact_flags_every_uncounted_page(torch, npages):
+    """An entry whose page nothing counts stays and is flagged, wherever its page is: below the
+    live pages' number (another page moves into it) or above."""
+    for above in (False, True):
+        s = State(torch, npages, [320, 320], 40, layers=1, kv="fp8", hkv=1, seed=10)
+        # Two pages at the front and the last one are held by row 1, whatever their numbers were.
+        lo, hi = 2, npages - 1
+        for b, j, page in ((1, 0, lo), (1, 1, hi)):
+            old = int(s.table[b, j])
+            where = (s.table[:, :20] == page).nonzero()
+            if len(where):
+                s.table[where[0, 0], where[0, 1]] = old
+            else:
+                s.refs[old] = 0
+            s.table[b, j] = page
+            s.refs[page] = 1
+        page, j = (hi, 1) if above else (lo, 0)
+        s.refs[page] = 0
+        n = int(s.layer.page_compact(*s.args(), s.caches))
+        assert n == 39 and int(s.refs[:n].min()) == 1 and int(s.refs.sum()) == 39
+        assert int(s.table[1, j]) == page
+        assert s.layer.page_flags(npages, s.refs.device) == 1, above
+
+
 @pytest.mark.parametrize("kv,layout,hkv,d", LAYOUTS)
 def test_copy(torch, kv, layout, hkv, d):
     s = State(torch, 60, [5], 40, kv, hkv, d, 2, layout, seed=11)
