@@ -14,7 +14,7 @@ from typing import Optional
 
 from . import _abi
 from .cache_ops import CacheOps
-from .rotary import on_device, raw_stream, rotary_frequencies, rotate, used_on
+from .rotary import empty_on, on_device, raw_stream, rotary_frequencies, rotate
 
 __all__ = ["DecodeAttention", "decode_attention", "rotate", "rotary_frequencies", "RldaError", "library_path"]
 
@@ -222,8 +222,7 @@ class DecodeAttention(CacheOps):
         if not q.is_cuda:
             self._fail(what, f"q must be on a GPU, got {q.device}")
         if out is None:
-            odt = torch.float32 if cfg.out_dtype == _abi.RLDA_F32 else torch.bfloat16
-            out = torch.empty((B, cfg.num_q_heads, cfg.head_dim), dtype=odt, device=q.device)
+            out = empty_on((B, cfg.num_q_heads, cfg.head_dim), _torch_dtype(cfg.out_dtype), q.device, stream)
         npages = int(k_cache.shape[0]) if num_pages is None else int(num_pages)
         self._check_rows(what, q, out, B, q.device)
         self._check_table(what, block_table, seq_lens, B, q.device)
@@ -272,8 +271,7 @@ class DecodeAttention(CacheOps):
         if not q.is_cuda:
             self._fail(what, f"q must be on a GPU, got {q.device}")
         if out is None:
-            odt = torch.float32 if cfg.out_dtype == _abi.RLDA_F32 else torch.bfloat16
-            out = torch.empty((B, cfg.num_q_heads, cfg.head_dim), dtype=odt, device=q.device)
+            out = empty_on((B, cfg.num_q_heads, cfg.head_dim), _torch_dtype(cfg.out_dtype), q.device, stream)
         npages = int(k_cache.shape[0]) if num_pages is None else int(num_pages)
         self._check_rows(what, q, out, B, q.device)
         self._check_table(what, block_table, seq_lens, B, q.device)
@@ -311,8 +309,7 @@ class DecodeAttention(CacheOps):
         if not q.is_cuda:
             self._fail(what, f"q must be on a GPU, got {q.device}")
         if out is None:
-            odt = torch.float32 if cfg.out_dtype == _abi.RLDA_F32 else torch.bfloat16
-            out = torch.empty((total, cfg.num_q_heads, cfg.head_dim), dtype=odt, device=q.device)
+            out = empty_on((total, cfg.num_q_heads, cfg.head_dim), _torch_dtype(cfg.out_dtype), q.device, stream)
         npages = int(k_cache.shape[0]) if num_pages is None else int(num_pages)
         self._check_rows(what, q, out, total, q.device)
         self._tensor(what, "q_start", q_start, torch.int32, (B + 1,), q.device)
@@ -373,8 +370,7 @@ class DecodeAttention(CacheOps):
                 self._tensor(what, name, t, dt, (n,), dev)
         with on_device(dev):
             if out is None:
-                out = torch.empty((total, cfg.num_q_heads, cfg.head_dim), dtype=_torch_dtype(cfg.out_dtype), device=dev)
-                used_on(out, dev, stream)
+                out = empty_on((total, cfg.num_q_heads, cfg.head_dim), _torch_dtype(cfg.out_dtype), dev, stream)
             ws = workspace if workspace is not None else self._own_workspace(dev, stream)
             self._check_workspace(what, ws, dev)
             ptr = lambda t: None if t is None else t.data_ptr()   # noqa: E731

@@ -7,7 +7,7 @@ import ctypes
 from typing import Optional
 
 from . import _abi
-from .rotary import check_freqs, check_rows, derived, mark_written, on_device, raw_stream, rotary_of, rows_of, used_on
+from .rotary import check_freqs, check_rows, derived, empty_on, mark_written, on_device, raw_stream, rotary_of, rows_of
 
 
 class CacheSet:
@@ -76,8 +76,7 @@ class CacheOps:
         self._check_cache(what, k_cache, v_cache, k_scale, v_scale, npages, dev)
         with on_device(dev):
             if out is None:
-                out = torch.empty((n, cfg.num_q_heads, d), dtype=qd, device=dev)
-                used_on(out, dev, stream)
+                out = empty_on((n, cfg.num_q_heads, d), qd, dev, stream)
             else:
                 check_rows(fail, "out", out, qd, (n, cfg.num_q_heads, d), dev)
                 mark_written(out)
@@ -234,8 +233,7 @@ class CacheOps:
         dev, batch, npages, cs = self._page_call(what, refs, block_table, seq_lens, caches, workspace, stream)
         with on_device(dev):
             if live is None:
-                live = torch.empty(1, dtype=torch.int32, device=dev)
-                used_on(live, dev, stream)
+                live = empty_on((1,), torch.int32, dev, stream)
             self._tensor(what, "live", live, torch.int32, (1,), dev)
             args = self._page_ws_args(what, npages, dev, workspace, stream)
             _abi.check(self._lib.rl_decode_attn_page_compact(

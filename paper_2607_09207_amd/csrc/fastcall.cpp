@@ -188,10 +188,30 @@ bool workspace(const Layer* L, Call& c, PyObject* given, bool grouped) {
 
 void* ptr(const Tensor* t) { return t ? t->mutable_data_ptr() : nullptr; }
 
+// A tensor that a call on `stream` writes and the caller then has (`given`: the stream as the
+// caller gave it).  On another stream than the current one, memory of that stream's own:
+// memory of the current stream's might still be in use by what is queued there.  And it is
+// not given out again before what is then queued on the current stream is done.
+Tensor empty_on(at::IntArrayRef shape, at::TensorOptions how, int dev, PyObject* given, void* stream) {
+  void* now = stream;
+  if (given != Py_None && !stream_of(Py_None, dev, &now)) throw std::runtime_error("no current stream");
+  if (now == stream) return at::empty(shape, how);
+  const c10::impl::VirtualGuardImpl impl(c10::DeviceType::CUDA);
+  // A stream's handle names it, as torch.cuda.ExternalStream does (0: the default stream).
+  struct Guard {
+    const c10::impl::VirtualGuardImpl& impl;
+    c10::Stream old;
+    ~Guard() { impl.exchangeStream(old); }
+  } guard{impl, impl.exchangeStream(c10::Stream::unpack3((int64_t)(intptr_t)stream, (c10::DeviceIndex)dev, c10::DeviceType::CUDA))};
+  Tensor t = at::empty(shape, how);
+  t.record_stream(guard.old);
+  return t;
+}
+
 // The output given, or a new tensor (rows, Hq, d) held by `fresh`.
-const Tensor* output(const Layer* L, PyObject* given, const Tensor& q, int64_t rows, Tensor& fresh) {
+const Tensor* output(const Layer* L, PyObject* given, const Tensor& q, int64_t rows, PyObject* stream, const Call& c, Tensor& fresh) {
   if (given == Py_None) {
-    fresh = at::empty({rows, L->hq, L->d}, at::TensorOptions().dtype(L->out_dtype).device(q.device()));
+    fresh = empty_on({rows, L->hq, L->d}, at::TensorOptions().dtype(L->out_dtype).device(q.device()), c.dev, stream, c.stream);
     return &fresh;
   }
   const Tensor* o = tensor(given);
@@ -240,7 +260,7 @@ PyObject* layer_run(PyObject* self, PyObject* const* a, Py_ssize_t n) {
     if (!shaped(q, dev, L->q_dtype, {B, L->hq, L->d}) || !common(L, c, a + 1, dev, B) || !workspace(L, c, a[10], false))
       return nullptr;
     Tensor fresh;
-    const Tensor* o = output(L, a[9], *q, B, fresh);
+    const Tensor* o = output(L, a[9], *q, B, a[7], c, fresh);
     if (!o) return nullptr;
     void *qp = ptr(q), *kp = ptr(c.k), *vp = ptr(c.v), *ksp = ptr(c.ks), *vsp = ptr(c.vs), *bp = ptr(c.bt),
          *lp = ptr(c.lens), *op = ptr(o);
@@ -270,7 +290,7 @@ PyObject* layer_grouped(PyObject* self, PyObject* const* a, Py_ssize_t n) {
         !shaped(pp, dev, at::kInt, {(B + gs - 1) / gs}) || !workspace(L, c, a[10], true))
       return nullptr;
     Tensor fresh;
-    const Tensor* o = output(L, a[9], *q, B, fresh);
+    const Tensor* o = output(L, a[9], *q, B, a[7], c, fresh);
     if (!o) return nullptr;
     void *qp = ptr(q), *kp = ptr(c.k), *vp = ptr(c.v), *ksp = ptr(c.ks), *vsp = ptr(c.vs), *bp = ptr(c.bt),
          *lp = ptr(c.lens), *op = ptr(o), *ppp = ptr(pp);
@@ -299,7 +319,7 @@ PyObject* layer_multi(PyObject* self, PyObject* const* a, Py_ssize_t n) {
         !common(L, c, a + 1, dev, B) || !workspace(L, c, a[10], false))
       return nullptr;
     Tensor fresh;
-    const Tensor* o = output(L, a[9], *q, total, fresh);
+    const Tensor* o = output(L, a[9], *q, total, a[7], c, fresh);
     if (!o) return nullptr;
     void *qp = ptr(q), *kp = ptr(c.k), *vp = ptr(c.v), *ksp = ptr(c.ks), *vsp = ptr(c.vs), *bp = ptr(c.bt),
          *lp = ptr(c.lens), *op = ptr(o), *qsp = ptr(qs);
@@ -324,7 +344,7 @@ PyObject* layer_noalloc(PyObject* self, PyObject* const* a, Py_ssize_t n) {
     if (a[10] != Py_None && !shaped(flags = tensor(a[10]), dev, at::kInt, {1})) return nullptr;
     if (!shaped(q, dev, L->q_dtype, {B, L->hq, L->d}) || !common(L, c, a + 1, dev, B)) return nullptr;
     Tensor fresh;
-    const Tensor* o = output(L, a[9], *q, B, fresh);
+    const Tensor* o = output(L, a[9], *q, B, a[7], c, fresh);
     if (!o) return nullptr;
     void *qp = ptr(q), *kp = ptr(c.k), *vp = ptr(c.v), *ksp = ptr(c.ks), *vsp = ptr(c.vs), *bp = ptr(c.bt),
          *lp = ptr(c.lens), *op = ptr(o), *fp = ptr(flags);
@@ -447,7 +467,7 @@ PyObject* layer_scored(PyObject* self, PyObject* const* a, Py_ssize_t n) {
         !vector_or_none(a[17], dev, at::kInt, B, &pl) || !workspace(L, c, a[10], false) || !current(dev))
       return nullptr;
     Tensor fresh;
-    const Tensor* o = output(L, a[9], *q, total, fresh);
+    const Tensor* o = output(L, a[9], *q, total, a[7], c, fresh);
     if (!o) return nullptr;
     const rl_decode_attn_scores sc = {(float)cap, (int32_t)window, (const float*)ptr(slopes), (const int32_t*)ptr(ks),
                                       (const int32_t*)ptr(pl)};

@@ -127,11 +127,21 @@ def raw_stream(device, stream):
     return getattr(stream, "cuda_stream", stream)
 
 
-def used_on(t, device, stream):
-    """A tensor made here and used on the caller's stream: its memory waits for it."""
+def empty_on(shape, dtype, device, stream):
+    """A tensor that a call on `stream` (None: the current one) writes and the caller then has.
+    Memory of that stream's own: memory of the current stream's might still be in use by what
+    is queued there.  And it is not given out again before what is then queued on the
+    current stream, where the caller is taken to read it, is done."""
     import torch
-    if stream is not None:
-        t.record_stream(stream if hasattr(stream, "cuda_stream") else torch.cuda.ExternalStream(stream, device=device))
+    current = torch.cuda.current_stream(device)
+    if stream is None or raw_stream(device, stream) == current.cuda_stream:
+        return torch.empty(shape, dtype=dtype, device=device)
+    if not hasattr(stream, "cuda_stream"):
+        stream = torch.cuda.ExternalStream(stream, device=device) if stream else torch.cuda.default_stream(device)
+    with torch.cuda.stream(stream):
+        t = torch.empty(shape, dtype=dtype, device=device)
+    t.record_stream(current)
+    return t
 
 
 _turn = None
@@ -225,8 +235,7 @@ def _rotate(x, positions, freqs, interleaved, amplitude, inverse, out, stream):
         fail(f"positions must be a contiguous int32 tensor of {shape[0]} on {dev}")
     with on_device(dev):
         if out is None:
-            out = torch.empty(shape, dtype=x.dtype, device=dev)
-            used_on(out, dev, stream)
+            out = empty_on(shape, x.dtype, dev, stream)
         else:
             check_rows(fail, "out", out, x.dtype, shape, dev)
             mark_written(out)
