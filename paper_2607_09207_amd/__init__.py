@@ -80,7 +80,7 @@ class DecodeAttention(CacheOps):
         _abi.check(lib.rl_decode_attn_grouped_workspace_size(h, ctypes.byref(n)),
                    "rl_decode_attn_grouped_workspace_size")
         self.grouped_workspace_bytes = int(n.value)
-        self._ws = {}
+        self._ws, self._outgrown = {}, []
         self._page_ws = {}
         # The native call path (csrc/fastcall.cpp); it shares the workspaces by device.
         native = _abi.fastcall()
@@ -98,14 +98,15 @@ class DecodeAttention(CacheOps):
 
     def workspace(self, device, grouped: bool = False):
         """Zero-filled workspace for `device`, allocated once and reused (grown once
-        for grouped calls, which need more)."""
-        torch = _torch()
+        for grouped calls, which need more).  A call to be captured into a graph finds it
+        made before."""
         key = str(device)
         need = (self.grouped_workspace_bytes if grouped else self.workspace_bytes) + 256
         ws = self._ws.get(key)
         if ws is None or ws.numel() < need:
-            ws = torch.zeros(need, dtype=torch.uint8, device=device)
-            self._ws[key] = ws
+            if ws is not None:
+                self._outgrown.append(ws)   # a graph, or a call that still runs, may use it
+            ws = self._ws[key] = self._zeroed(need, device)
         return ws
 
     @staticmethod
@@ -371,7 +372,7 @@ class DecodeAttention(CacheOps):
         with on_device(dev):
             if out is None:
                 out = empty_on((total, cfg.num_q_heads, cfg.head_dim), _torch_dtype(cfg.out_dtype), dev, stream)
-            ws = workspace if workspace is not None else self._own_workspace(dev, stream)
+            ws = workspace if workspace is not None else self.workspace(dev)
             self._check_workspace(what, ws, dev)
             ptr = lambda t: None if t is None else t.data_ptr()   # noqa: E731
             sc = _abi.Scores(float(score_cap), int(window), ptr(slopes), ptr(key_start), ptr(prefix_lens))

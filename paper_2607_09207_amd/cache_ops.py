@@ -80,7 +80,7 @@ class CacheOps:
             else:
                 check_rows(fail, "out", out, qd, (n, cfg.num_q_heads, d), dev)
                 mark_written(out)
-            ws = workspace if workspace is not None else self._own_workspace(dev, stream)
+            ws = workspace if workspace is not None else self.workspace(dev)
             self._check_workspace(what, ws, dev)
             wp = self._aligned_ptr(ws)
             ptr = lambda t: None if t is None else t.data_ptr()   # noqa: E731
@@ -92,12 +92,14 @@ class CacheOps:
                 ws.numel() - (wp - ws.data_ptr()), raw_stream(dev, stream)), what)
         return out
 
-    def _own_workspace(self, device, stream):
-        """The layer's workspace; a new one is zero before the caller's stream uses it."""
-        new = str(device) not in self._ws
-        ws = self.workspace(device)
-        if new:
-            _zero_before(device, stream)
+    def _zeroed(self, nbytes, device):
+        """Zeroed device memory for calls on any stream: the fill is waited for."""
+        import torch
+        if torch.cuda.is_current_stream_capturing():
+            self._fail("workspace", "none is made during a graph's capture, which would clear it, with its flags, in "
+                                    "every replay: call workspace() or page_workspace() before")
+        ws = torch.zeros(nbytes, dtype=torch.uint8, device=device)
+        torch.cuda.current_stream(ws.device).synchronize()
         return ws
 
     # ---------------------------------------------------------------- pages
@@ -105,7 +107,8 @@ class CacheOps:
     def page_workspace(self, num_pages: int, device, stream=None):
         """Workspace of the page operations on a pool of `num_pages`, allocated (and zeroed)
         once.  Calls that may overlap need separate ones (`workspace=`); a call to be
-        captured into a graph finds it made before."""
+        captured into a graph finds it made before.  (`stream` makes no difference: it is
+        zero for every stream.)"""
         import torch
         key = (str(torch.device(device)), int(num_pages))
         ws = self._page_ws.get(key)
@@ -113,9 +116,7 @@ class CacheOps:
             n = ctypes.c_size_t()
             _abi.check(self._lib.rl_decode_attn_page_workspace_size(self._h, int(num_pages), ctypes.byref(n)),
                        "rl_decode_attn_page_workspace_size")
-            ws = torch.zeros(n.value + 256, dtype=torch.uint8, device=device)
-            _zero_before(ws.device, stream)
-            self._page_ws[key] = ws
+            ws = self._page_ws[key] = self._zeroed(n.value + 256, device)
         return ws
 
     def caches(self, layers, num_pages: Optional[int] = None):
@@ -159,7 +160,7 @@ class CacheOps:
         return dev, batch, npages, caches
 
     def _page_ws_args(self, what, npages, dev, workspace, stream):
-        ws = workspace if workspace is not None else self.page_workspace(npages, dev, stream)
+        ws = workspace if workspace is not None else self.page_workspace(npages, dev)
         self._check_workspace(what, ws, dev)
         wp = self._aligned_ptr(ws)
         return wp, ws.numel() - (wp - ws.data_ptr()), raw_stream(dev, stream)
@@ -259,12 +260,3 @@ class CacheOps:
         """The flags the page operations raised (waits for the stream)."""
         ws = workspace if workspace is not None else self.page_workspace(num_pages, device)
         return self.read_flags(workspace=ws, stream=stream)
-
-
-def _zero_before(device, stream):
-    """A workspace was just zeroed on the current stream: the caller's stream waits for it."""
-    import torch
-    if stream is None:
-        return
-    st = stream if hasattr(stream, "wait_stream") else torch.cuda.ExternalStream(stream, device=device)
-    st.wait_stream(torch.cuda.current_stream(device))

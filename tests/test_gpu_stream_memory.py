@@ -36,12 +36,13 @@ def make_calls(torch):
     state.layer.page_workspace(60, state.refs.device)
     args = lambda c: (c.q, c.k, c.v, c.block_table, c.seq_lens)   # noqa: E731
     pp = torch.zeros(3, dtype=torch.int32, device="cuda")
+    cap = few.mods(0)[1]
     calls = {
         "run": lambda s: one.layer(*args(one), stream=s),
         "grouped": lambda s: one.layer(*args(one), group_size=1, prefix_pages=pp, stream=s),
         "noalloc": lambda s: one.layer.run_noalloc(*args(one), stream=s),
         "multi": lambda s: few.layer.multi(*args(few), few.q_start, stream=s),
-        "scored": lambda s: few.run(few.mods(0)[1], stream=s),
+        "scored": lambda s: few.run(cap, stream=s),
         "append_rotary": lambda s: app.run(freqs, stream=s),
         "rotate": lambda s: rotate(x, pos, freqs, stream=s),
         "page_compact": lambda s: state.layer.page_compact(*state.args(), state.caches, stream=s),
@@ -107,3 +108,58 @@ def test_the_default_stream_by_its_handle(torch):
             a, b = calls[name](0), calls[name](torch.cuda.default_stream())
             torch.cuda.synchronize()
             assert torch.equal(a, b), name
+
+
+def test_workspaces_are_zero_for_every_stream(torch):
+    """A workspace is handed out with its zeros in it, whatever its maker's stream has queued."""
+    from paper_2607_09207_amd import DecodeAttention
+    layer = DecodeAttention(8, 2, 64, 4, 8)
+    dev = torch.device("cuda:0")
+    for make in (lambda: layer.workspace(dev), lambda: layer.workspace(dev, grouped=True), lambda: layer.page_workspace(50, dev)):
+        torch.cuda._sleep(20_000_000)
+        ws = make()
+        assert torch.cuda.current_stream().query()
+        with torch.cuda.stream(torch.cuda.Stream()):
+            assert not ws.any()
+
+
+def test_a_graph_keeps_its_workspace(torch):
+    """A graph captured on the plain workspace, replayed after grouped calls took a larger one."""
+    from test_gpu_scored import Case
+    c = Case(torch, "bf16", 8, 2, 64, [5000, 33, 3000], None, seed=1)
+    want = c.layer(c.q, c.k, c.v, c.block_table, c.seq_lens)
+    old = c.layer.workspace(c.q.device)
+    size, at = old.numel(), old.data_ptr()
+    out = torch.empty_like(want)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        c.layer(c.q, c.k, c.v, c.block_table, c.seq_lens, out=out)
+    del old
+    pp = torch.zeros(3, dtype=torch.int32, device="cuda")
+    c.layer(c.q, c.k, c.v, c.block_table, c.seq_lens, group_size=1, prefix_pages=pp)
+    assert c.layer.workspace(c.q.device).numel() > size
+    junk = [torch.full((size,), 255, dtype=torch.uint8, device="cuda") for _ in range(4)]
+    assert all(t.data_ptr() != at for t in junk)
+    for _ in range(3):
+        out.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, want) and all((t == 255).all() for t in junk)
+
+
+def test_no_workspace_is_made_in_a_capture(torch):
+    from paper_2607_09207_amd import RldaError
+    calls, layers = make_calls(torch)
+    for layer in layers:
+        layer._ws.clear()
+        layer._page_ws.clear()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        for name in ("run", "grouped", "multi", "scored", "append_rotary", "page_compact"):
+            with pytest.raises(RldaError, match="workspace"):
+                calls[name](None)
+    for name in NAMES:
+        calls[name](None)
+    torch.cuda.synchronize()
+    assert all(layer.read_flags(device="cuda:0") == 0 for layer in layers)
