@@ -14,7 +14,7 @@ from typing import Optional
 
 from . import _abi
 from .cache_ops import CacheOps
-from .rotary import empty_on, on_device, raw_stream, rotary_frequencies, rotate
+from .rotary import device_of, empty_on, on_device, raw_stream, rotary_frequencies, rotate
 
 __all__ = ["DecodeAttention", "decode_attention", "rotate", "rotary_frequencies", "RldaError", "library_path"]
 
@@ -100,6 +100,7 @@ class DecodeAttention(CacheOps):
         """Zero-filled workspace for `device`, allocated once and reused (grown once
         for grouped calls, which need more).  A call to be captured into a graph finds it
         made before."""
+        device = device_of(device)
         key = str(device)
         need = (self.grouped_workspace_bytes if grouped else self.workspace_bytes) + 256
         ws = self._ws.get(key)

@@ -7,7 +7,7 @@ import ctypes
 from typing import Optional
 
 from . import _abi
-from .rotary import check_freqs, check_rows, derived, empty_on, mark_written, on_device, raw_stream, rotary_of, rows_of
+from .rotary import check_freqs, check_rows, derived, device_of, empty_on, mark_written, on_device, raw_stream, rotary_of, rows_of
 
 
 class CacheSet:
@@ -109,8 +109,8 @@ class CacheOps:
         once.  Calls that may overlap need separate ones (`workspace=`); a call to be
         captured into a graph finds it made before.  (`stream` makes no difference: it is
         zero for every stream.)"""
-        import torch
-        key = (str(torch.device(device)), int(num_pages))
+        device = device_of(device)
+        key = (str(device), int(num_pages))
         ws = self._page_ws.get(key)
         if ws is None:
             n = ctypes.c_size_t()
@@ -257,6 +257,11 @@ class CacheOps:
                 self._h, cs.num_pages, n, src.data_ptr(), dst.data_ptr(), len(cs), cs.array, *args), what)
 
     def page_flags(self, num_pages: int, device, workspace=None, stream=None) -> int:
-        """The flags the page operations raised (waits for the stream)."""
-        ws = workspace if workspace is not None else self.page_workspace(num_pages, device)
+        """The flags the page operations raised on a pool of `num_pages` (waits for the stream)."""
+        ws = workspace
+        if ws is None:
+            device = device_of(device)
+            ws = self._page_ws.get((str(device), int(num_pages)))
+            if ws is None:
+                self._fail("page_flags", f"no page operation had a workspace for {num_pages} pages on {device}")
         return self.read_flags(workspace=ws, stream=stream)

@@ -112,6 +112,13 @@ def mark_written(t):
         torch.autograd.graph.increment_version(t)
 
 
+def device_of(device):
+    """The device meant, with its index: "cuda" (and None) is the current one."""
+    import torch
+    d = torch.device("cuda" if device is None else device)
+    return torch.device("cuda", torch.cuda.current_device()) if d.type == "cuda" and d.index is None else d
+
+
 def on_device(device):
     """A context in which `device` is the current one (nothing where it is already)."""
     import contextlib

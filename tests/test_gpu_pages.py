@@ -429,7 +429,30 @@ def test_a_set_of_another_layer(torch):
     s2 = State(torch, 50, [20, 30, 0], 40, "bf16", 2, 64, layers=2)
     like.page_fork(*s2.args(), one, s2.cuda([2]), s2.caches)
     s2.model.fork([1], [2])
+    s2.layer = like   # whose flags they are
     s2.check("another layer of the same geometry")
+
+
+def test_devices_without_an_index(torch):
+    """"cuda" is the current device: the same workspaces, and the same flags."""
+    from paper_2607_09207_amd import RldaError
+    s = State(torch, 10, [20, 30], 40, layers=1)
+    layer = s.layer
+    for none in ((10, "cuda"), (10, "cuda:0")):   # no operation yet
+        with pytest.raises(RldaError, match="no page operation"):
+            layer.page_flags(*none)
+    ws = layer.page_workspace(10, "cuda")
+    s.layer.page_grow(*s.args(), s.cuda([600, 0]))
+    for device in ("cuda", "cuda:0", torch.device("cuda"), 0, None):
+        assert layer.page_flags(10, device) == 16
+        assert layer.page_workspace(10, device) is ws
+    with pytest.raises(RldaError, match="no page operation"):
+        layer.page_flags(11, "cuda")
+    assert len(layer._page_ws) == 1
+    own = layer.workspace("cuda")
+    own[own.data_ptr() % 256 and 256 - own.data_ptr() % 256] = 8
+    for device in ("cuda", "cuda:0", torch.device("cuda"), 0, None):
+        assert layer.workspace(device) is own and layer.read_flags(device=device) == 8
 
 
 def test_graph_and_streams(torch):
