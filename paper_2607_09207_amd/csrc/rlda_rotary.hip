@@ -411,8 +411,28 @@ __global__ __launch_bounds__(kThreads) void append_rotary_kernel(const RotaryPar
     bool ok = lane < span;
     uint32_t bad = 0;
     if (p.q_start) {
+      // The last sequence that begins at or before the row: of the next 64 (asked for together)
+      // as many as begin there, and behind 64 empty ones a search of its own.
       b = sequence_of(p.q_start, p.batch, first, lane);
-      while (ok && b < p.batch - 1 && p.q_start[b + 1] <= r) ++b;
+      const int next = b + 1 + lane < p.batch ? p.q_start[b + 1 + lane] : 0x7fffffff;
+      if (uni(next) < first + span) {   // (else every row is in that one)
+        int k = 0;
+#pragma unroll
+        for (int w = 32; w >= 1; w >>= 1) k += __shfl(next, k + w - 1) <= r ? w : 0;
+        k += __shfl(next, k) <= r;
+        b += k;
+        if (ok && k == 64) {
+          int hi = b + 1;
+          for (int w = 2; hi < p.batch && p.q_start[hi] <= r; w <<= 1) {
+            b = hi;
+            hi = min(hi + w, p.batch);
+          }
+          while (hi - b > 1) {   // q_start[b] <= r < q_start[hi]
+            const int mid = (b + hi) >> 1;
+            if (p.q_start[mid] <= r) b = mid; else hi = mid;
+          }
+        }
+      }
       if (ok) {
         q0 = p.q_start[b];
         q1 = p.q_start[b + 1];

@@ -9,6 +9,8 @@ bits: at 2^20 positions three roundings of 2^-53 of at most 2^18 turns, 2^-34 tu
 3 2^-34 2 pi < 2^-29 of |x| + |y| covers.  E4M3: half a step is 2^-4 of the value, or 2^-10
 of the scale below the normal range.
 """
+import math
+
 import numpy as np
 import pytest
 
@@ -491,6 +493,41 @@ def test_append_rotary_windows(torch, kv, n):
     q = c.run(freqs)
     check(torch, c, freqs, before, q, False, 1.0)
     assert c.layer.read_flags(device=c.q.device) == 0
+
+
+@pytest.mark.parametrize("kv", ["bf16", "fp8"])
+def test_append_rotary_between_empty_sequences(torch, kv):
+    """Rows of neighbours with runs of sequences that bring none between them, shorter and
+    longer than a wave; and what such runs cost: next to nothing."""
+    from paper_2607_09207_amd import rotary_frequencies
+    freqs, _ = rotary_frequencies(64, 1e4)
+    for gaps in ([0, 1, 62, 63, 64, 65, 3], [200, 64, 0, 0, 127, 128, 129, 1000], [5, 3000, 1]):
+        rows = []
+        for i, gap in enumerate(gaps):
+            rows += [0] * gap + [[1, 2, 17, 1][i % 4]]
+        rows += [0] * gaps[0]
+        lens = [m and m + i % 23 for i, m in enumerate(rows)]
+        say("empty sequences", kv, gaps)
+        c = Case(torch, kv, 4, 2, 64, lens, rows, seed=len(rows), lead=2, behind=1)
+        before = {x: None if getattr(c, x) is None else getattr(c, x).clone() for x in ("k", "v", "ks", "vs")}
+        check(torch, c, freqs, before, c.run(freqs), False, 1.0)
+        assert c.layer.read_flags(device=c.q.device) == 0
+
+    def us(rows):
+        c = Case(torch, kv, 4, 2, 64, [40 if m else 0 for m in rows], rows, seed=1)
+        best = math.inf
+        for _ in range(5):
+            a, b = (torch.cuda.Event(enable_timing=True) for _ in range(2))
+            a.record()
+            for _ in range(20):
+                c.run(freqs)
+            b.record()
+            torch.cuda.synchronize()
+            best = min(best, a.elapsed_time(b) * 50)
+        return best
+    alone, among = us([1] * 8), us(([0] * 1000 + [1]) * 8)
+    say("8 rows", kv, alone, "us, with 8000 empty sequences among them", among)
+    assert among < 10 * alone   # (one after the other they took 94 times as long)
 
 
 @pytest.mark.parametrize("kv", ["bf16", "fp8"])
