@@ -151,6 +151,14 @@ def empty_on(shape, dtype, device, stream):
     return t
 
 
+def _laid_out(t):
+    """A gradient or tangent as rotate takes it: it may come broadcast, in any layout, or as a
+    contiguous piece of another tensor that begins anywhere in it."""
+    import torch
+    t = t.contiguous()
+    return t if t.data_ptr() % 16 == 0 else t.clone(memory_format=torch.contiguous_format)
+
+
 _turn = None
 
 
@@ -173,15 +181,14 @@ def _function():
             def backward(ctx, grad):
                 positions, freqs = ctx.saved_tensors
                 interleaved, amplitude, inverse = ctx.how
-                # (A gradient may come broadcast or in any layout.)
-                return rotate(grad.contiguous(), positions, freqs, interleaved=interleaved, amplitude=amplitude,
+                return rotate(_laid_out(grad), positions, freqs, interleaved=interleaved, amplitude=amplitude,
                               inverse=not inverse), None, None, None, None, None
 
             @staticmethod
             def jvp(ctx, tangent, *_):
                 positions, freqs = ctx.saved_tensors
                 interleaved, amplitude, inverse = ctx.how
-                return rotate(tangent.contiguous(), positions, freqs, interleaved=interleaved, amplitude=amplitude,
+                return rotate(_laid_out(tangent), positions, freqs, interleaved=interleaved, amplitude=amplitude,
                               inverse=inverse)
 
         _turn = Turn

@@ -270,6 +270,29 @@ def test_forward_mode(torch, native, monkeypatch):
         assert fwd.unpack_dual(rotate(x, pos, freqs)).tangent is None
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_gradients_that_begin_anywhere(torch, dtype):
+    """A gradient that is a contiguous piece of another one (of a concatenation) is not aligned
+    as rows have to be; a tangent neither."""
+    import torch.autograd.forward_ad as fwd
+
+    from paper_2607_09207_amd import rotary_frequencies, rotate
+    freqs, _ = rotary_frequencies(32)
+    dt = torch.bfloat16 if dtype == "bf16" else torch.float32
+    x = torch.randn((5, 2, 32), device="cuda").to(dt).requires_grad_()
+    pos = torch.arange(5, device="cuda", dtype=torch.int32)
+    head = torch.zeros(3, device="cuda", dtype=dt, requires_grad=True)
+    w = torch.randn(3 + x.numel(), device="cuda").to(dt)
+    y = torch.cat([head, rotate(x, pos, freqs).flatten()])
+    piece = w[3:].view(5, 2, 32)
+    assert piece.data_ptr() % 16 != 0
+    y.backward(w)
+    assert torch.equal(x.grad, rotate(piece.clone(), pos, freqs, inverse=True)) and torch.equal(head.grad, w[:3])
+    with fwd.dual_level():
+        got = fwd.unpack_dual(rotate(fwd.make_dual(x.detach(), piece), pos, freqs)).tangent
+        assert torch.equal(got, rotate(piece.clone(), pos, freqs))
+
+
 def test_single_rows_of_any_stride(torch):
     """One row, or one head, of a buffer whose other stride is no multiple of 16 bytes."""
     from paper_2607_09207_amd import rotary_frequencies, rotate
