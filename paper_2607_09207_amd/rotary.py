@@ -55,6 +55,7 @@ def rotary_frequencies(rot_dim: int, base: float = 10000.0, scaling=None, device
         lo = max(math.floor(pair(fast)), 0)
         hi = min(math.ceil(pair(slow)), rot_dim - 1)
         keep = 1.0 - ((j - lo) / max(hi - lo, 1e-3)).clamp(0.0, 1.0)
+        keep[j >= hi] = 0.0   # (over a short context even the first pair: lo and hi coincide)
         freqs = freqs * keep + freqs / s * (1.0 - keep)
         amplitude = float(scaling.get("amplitude", 0.1 * math.log(s) + 1.0 if s > 1.0 else 1.0))
     return freqs.to(device), amplitude

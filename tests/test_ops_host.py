@@ -245,6 +245,22 @@ def test_frequencies():
             bad()
 
 
+def test_ramp_of_short_contexts():
+    """A pair that turns `slow` times or less over the context is slowed down, the first one too."""
+    import torch
+
+    from paper_2607_09207_amd import rotary_frequencies as F
+    f, _ = F(64, 1e4, device="cpu")
+    for n in (1, 6, 6.28, 7, 30, 200):
+        g, _ = F(64, 1e4, {"type": "ramp", "factor": 16.0, "context": n, "fast": 32, "slow": 1}, "cpu")
+        turns = n * f / (2 * math.pi)
+        slow = turns <= 1
+        at = 32 * math.log(n / (2 * math.pi)) / math.log(1e4)   # the pair that turns once
+        slow &= torch.arange(32) >= math.ceil(at)
+        assert slow.any() and torch.allclose(g[slow] * 16, f[slow], rtol=1e-14)
+        assert (g <= f).all() and (g * 16 >= f * (1 - 1e-14)).all() and (g[1:] < g[:-1]).all()
+
+
 def test_sizes_beyond_a_launch(lib, handles):  # noqa: F811
     """What one launch cannot hold is refused before it."""
     assert rotate(lib, rows=2 ** 27 + 1) == UNSUPPORTED
