@@ -370,6 +370,8 @@ class DecodeAttention(CacheOps):
                                ("prefix_lens", prefix_lens, torch.int32, B)):
             if t is not None:
                 self._tensor(what, name, t, dt, (n,), dev)
+        if score_cap and not ctypes.c_float(score_cap).value:
+            self._fail(what, f"score_cap {score_cap} is 0 in fp32: no cap")
         with on_device(dev):
             if out is None:
                 out = empty_on((total, cfg.num_q_heads, cfg.head_dim), _torch_dtype(cfg.out_dtype), dev, stream)

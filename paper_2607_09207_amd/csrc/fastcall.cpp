@@ -459,7 +459,7 @@ PyObject* layer_scored(PyObject* self, PyObject* const* a, Py_ssize_t n) {
       if (!shaped(qs, dev, at::kInt, {B + 1})) return nullptr;
     }
     if (total > INT32_MAX || a[12] == Py_None || !as_int(a[12], 0, &mq) || mq < INT32_MIN || mq > INT32_MAX ||
-        !as_double(a[13], &cap) || a[15] == Py_None || !as_int(a[15], 0, &window) || window < INT32_MIN || window > INT32_MAX)
+        !as_double(a[13], &cap) || (cap != 0.0 && (float)cap == 0.f) || a[15] == Py_None || !as_int(a[15], 0, &window) || window < INT32_MIN || window > INT32_MAX)
       return nullptr;
     Call c;
     if (!shaped(q, dev, L->q_dtype, {total, L->hq, L->d}) || !vector_or_none(a[14], dev, at::kFloat, L->hq, &slopes) ||

@@ -387,3 +387,17 @@ def test_stream_and_graph(torch):
             torch.cuda.synchronize()
             assert torch.equal(out, want)
             assert torch.equal(c.run(mod, **kw), want)
+
+
+@pytest.mark.parametrize("native", [True, False], ids=["native", "python"])
+def test_caps_out_of_range(torch, native):
+    """A cap that fp32 holds as 0 is refused as any other below the range, and does not mean none."""
+    from paper_2607_09207_amd import RldaError, _abi
+    c = Case(torch, "bf16", 8, 2, 64, [90, 33])
+    c.layer.workspace(c.q.device)
+    if not native:
+        c.layer._fast = _abi.LEFT_TO_PYTHON
+    for cap in (1e-50, -1e-50, 1e-46, 1e-30, 2.0 ** -11, -1.0, math.nan, math.inf, 1e300, 2.0 ** 31):
+        with pytest.raises(RldaError):
+            c.run(dict(score_cap=cap))
+    assert torch.equal(c.run(dict(score_cap=0)), c.run(dict(score_cap=-0.0)))
