@@ -85,12 +85,12 @@ __device__ __forceinline__ f32x2 fp8x2_to_f32(uint32_t w, bool hi_half) {
 #endif
 constexpr bool kFp8Direct = RLDA_FP8_DIRECT;   // fp8 -> bf16 operands in one conversion per pair
 
-// Two e4m3 values (bytes 0, 1, or 2, 3 with hi_half) to a bf16 pair, low half first.
-// Every e4m3 value is a bf16 value, and the scale is one, so the conversion is exact.
-__device__ __forceinline__ uint32_t fp8x2_to_bf16x2(uint32_t w, bool hi_half) {
+// Two e4m3 values (bytes 0, 1, or 2, 3 with hi_half), times `power`, a power of two from 2^-100
+// on, to a bf16 pair, low half first.  These are bf16 values, so the conversion is exact.
+__device__ __forceinline__ uint32_t fp8x2_to_bf16x2(uint32_t w, bool hi_half, float power = 1.0f) {
   typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
-  const bf16x2 v = hi_half ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.0f, true)
-                           : __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.0f, false);
+  const bf16x2 v = hi_half ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, power, true)
+                           : __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, power, false);
   return __builtin_bit_cast(uint32_t, v);
 }
 

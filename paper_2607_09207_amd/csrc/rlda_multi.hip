@@ -534,12 +534,19 @@ void multi_query_kernel(const Params p) {
     if constexpr (FP8) st.scale = tok > 0 ? (is_v ? p.v_scale : p.k_scale)[(int64_t)pid * Hkv + g] : 0.f;
   };
   auto page_write = [&](Staged& st, int is_v, int buf, int slot) {
+    float power = 1.f;
     if constexpr (MOD && FP8) {
-      // A page of zeros (scales up to 2^-100 count as 0) has scale 1: the softmax takes its log.
-      if (is_v && uni((int)(st.scale <= 0x1p-100f)) != 0) {
-        st.scale = 1.f;
+      // V's scale is 2^e f, f in [1, 2): the values take 2^e here, the softmax f (see there).  A
+      // page of zeros (scales up to 2^-100 count as 0) has scale 1.
+      if (is_v) {
+        if (uni((int)(st.scale <= 0x1p-100f)) != 0) {
+          st.scale = 1.f;
 #pragma unroll
-        for (int k = 0; k < S::LPL; ++k) st.r[k] = u32x4{0u, 0u, 0u, 0u};
+          for (int k = 0; k < S::LPL; ++k) st.r[k] = u32x4{0u, 0u, 0u, 0u};
+        }
+        const uint32_t x = __float_as_uint(st.scale);
+        power = __uint_as_float(x & 0x7F800000u);
+        st.scale = __uint_as_float((x & 0x007FFFFFu) | 0x3F800000u);
       }
     }
     char* dst = is_v ? s_v[buf] : s_k[buf];
@@ -555,12 +562,12 @@ void multi_query_kernel(const Params p) {
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           if constexpr (kFp8Direct) {
-            w[2 * e] = fp8x2_to_bf16x2(st.r[k][e], false);
-            w[2 * e + 1] = fp8x2_to_bf16x2(st.r[k][e], true);
+            w[2 * e] = fp8x2_to_bf16x2(st.r[k][e], false, power);
+            w[2 * e + 1] = fp8x2_to_bf16x2(st.r[k][e], true, power);
           } else {
             const f32x2 a = fp8x2_to_f32(st.r[k][e], false), bb = fp8x2_to_f32(st.r[k][e], true);
-            w[2 * e] = pack_bf16(a[0], a[1]);
-            w[2 * e + 1] = pack_bf16(bb[0], bb[1]);
+            w[2 * e] = pack_bf16(a[0] * power, a[1] * power);
+            w[2 * e + 1] = pack_bf16(bb[0] * power, bb[1] * power);
           }
         }
         *(u32x4*)(rowp + 32 * c) = u32x4{w[0], w[1], w[2], w[3]};
@@ -635,10 +642,12 @@ void multi_query_kernel(const Params p) {
   auto softmax = [&](int t, int kb, int buf, const f32x16* sc) {
     // Lane 32h + i holds S^T[key 32kh + 8(j/4) + 4h + j%4][row i] of key tile kh,
     // j < 16: page 2kh for j < 8, 2kh + 1 above.
-    // MOD, fp8: V's scales enter the exponent, exp2(y + log2 v - m), and the sum takes the
-    // weights over v: the row's largest weight is a power of two where m is its own, and has no
-    // rounding (p v rounded: 2.4e-3 and up to 2.7e-3 of a result that bf16 itself holds to
-    // 1.7e-3), and a product less for every weight.
+    // MOD, fp8: V's scales v (what is left of them in [1, 2), the powers of two being in the
+    // values) enter the exponent, exp2(y + log2 v - m), and the sum takes the weights over v:
+    // no weight is lost, however far apart the scales of two pages are, and the row's largest
+    // weight is a power of two where m is its own, and has no rounding (p v rounded: 2.4e-3 and
+    // up to 2.7e-3 of a result that bf16 itself holds to 1.7e-3), and a product less for every
+    // weight.
     constexpr bool kExpScale = MOD && FP8;
     float km[2 * kKH], vm[2 * kKH], iv[2 * kKH];
     int bad = 0;

@@ -298,6 +298,21 @@ def test_pages_of_zeros(torch, rows, kw):
         assert not got[2 if rows is None else slice(int(c.start[2]), None)].any()
 
 
+@pytest.mark.parametrize("rows,kw", [(None, {}), ([4, 3, 5], dict(max_q_len=5)), ([90, 70, 60], {}), ([290, 80, 70], {})])
+def test_scales_far_apart(torch, rows, kw):
+    """fp8 pages of one sequence whose V scales differ by up to 2^180: a key's weight in the sum
+    does not depend on its page's scale."""
+    for d, (hq, hkv) in ((64, (8, 2)), (128, (28, 4))):
+        c = Case(torch, "fp8", hq, hkv, d, [300, 90, 77], rows, seed=4)
+        g = torch.Generator("cuda").manual_seed(7)
+        c.vs.copy_(torch.exp2(180 * torch.rand(c.vs.shape, device="cuda", generator=g) - 90))
+        few = rows is None or max(rows) < 16
+        for q in (c.q, torch.zeros_like(c.q)):   # (and all weights alike)
+            c.q = q
+            for mod in (dict(), dict(score_cap=10.0), dict(score_cap=300.0), dict(window=40)):
+                c.check(mod, few, f"scales far apart {d} {rows}", **kw)
+
+
 @pytest.mark.parametrize("kv", ["bf16", "fp8"])
 def test_pages_below_the_window_are_not_read(torch, kv):
     for rows, few in ((None, True), ([3, 4], True), ([40, 30], False)):
