@@ -467,19 +467,26 @@ void multi_query_kernel(const Params p) {
   }
 
   // MOD: the blocks start at kb0; the wave's rows see keys from Wlo on, all of them from
-  // Wlo_full on (where one sees nothing, none do).
-  int kb0 = 0, first_page = 0, Wlo = 0, Wlo_full = 0;
+  // Wlo_full on (where one sees nothing, none do), and the workgroup's the keys of
+  // [Glo_full, G_full).
+  int kb0 = 0, first_page = 0, Wlo = 0, Wlo_full = 0, Glo_full = 0, G_full = 0;
   if constexpr (MOD) {
-    int lo = E;
+    int lo = E, last = 0;
+    bool none = false;
 #pragma unroll
     for (int k = 0; k < kMultiRows; k += 64) {
       const int row = r0 + k + lane;
-      if (row < r1 && base_pos + token_of(row) >= 0) {
-        const int x = first_key(row);
-        if (x < seen_end(row)) lo = min(lo, x);
+      if (row < r1) {
+        const int x = base_pos + token_of(row) >= 0 ? first_key(row) : E;
+        const bool sees = x < seen_end(row);
+        if (sees) lo = min(lo, x);
+        if (sees) last = max(last, x);
+        none = none || !sees;
       }
     }
     lo = wave_min(lo);
+    Glo_full = wave_max(last);
+    G_full = __builtin_amdgcn_ballot_w64(none) != 0 ? 0 : seen_end(r0);
     kb0 = lo / kKeys;
     first_page = lo / kPage;   // the page before it may be in the first block: not read
     Wlo = wave_min(lim[0] > 0 ? low[0] : 0x7ffffffe);
@@ -635,7 +642,6 @@ void multi_query_kernel(const Params p) {
 
   // P^T operands of the current block per tile: key tile kh, key step kk.
   bf16x8 pb[kNT][kKH][2];
-  bool masked = false;   // MOD: this lane's row does not see every key of the current block
   static_assert(!MOD || kKH == 1, "modified scores: one key tile a block");
   // Online softmax of tile t on block kb: updates (m, l), rescales the tile's
   // accumulators when m moves and leaves the block's P^T operands in pb[t].
@@ -688,7 +694,6 @@ void multi_query_kernel(const Params p) {
           for (int j = 0; j < 16; ++j)
             sv[kh][j] = __builtin_fmaf(-slope[t], __builtin_fabsf(at - (float)(kTile * kh + 8 * (j >> 2) + (j & 3))), sv[kh][j]);
       }
-      masked = false;
     }
     if ((kb + 1) * kKeys > Ew_full || (MOD && kb * kKeys < Wlo_full) || bad) {
 #pragma unroll
@@ -696,10 +701,7 @@ void multi_query_kernel(const Params p) {
 #pragma unroll
         for (int j = 0; j < 16; ++j) {
           const int key = kb * kKeys + kTile * kh + 8 * (j >> 2) + 4 * hh + (j & 3);
-          if ((MOD && key < low[t]) || key >= lim[t] || s_bad[buf][2 * kh + (j >> 3)]) {
-            sv[kh][j] = neg_inf();
-            if constexpr (MOD) masked = true;
-          }
+          if ((MOD && key < low[t]) || key >= lim[t] || s_bad[buf][2 * kh + (j >> 3)]) sv[kh][j] = neg_inf();
         }
     }
     float mx = neg_inf();
@@ -798,12 +800,12 @@ void multi_query_kernel(const Params p) {
       for (int t = 0; t < kNT; ++t) softmax(t, kb, buf, sc[t]);
       if constexpr (MOD) {
         // A key that a row does not see has no part in it, whatever its values: an infinity
-        // or NaN of V would turn the product with its zero probability into NaN.  Such
-        // values are cleared in the block (another wave may meet either, and clears what
-        // it must itself), and put into the rows that see them at the end.  (Kept apart in
-        // registers here, they cost a wave per SIMD: plain scores 594 us a call and
-        // 448 without.)
-        if (__builtin_amdgcn_ballot_w64(masked) != 0) {
+        // or NaN of V would turn the product with its zero probability into NaN.  In blocks that
+        // one of the workgroup's rows does not see whole such values are cleared, by every wave
+        // before it reads them (the waves write the same zeros), and put into the rows that see
+        // them at the end.  (Kept apart in registers here, they cost a wave per SIMD: plain
+        // scores 594 us a call and 448 without.)
+        if ((kb + 1) * kKeys > G_full || kb * kKeys < Glo_full) {
           constexpr bool kDma = decltype(dma)::value;
           u16x2 top = {0, 0};
           // Whole rows at a time: no bank twice.

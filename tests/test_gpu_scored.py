@@ -287,6 +287,24 @@ def test_odd_values_in_masked_places(torch, kv, d):
             c.check(mod, few, f"documents, odd {what}", max_q_len=max(rows) if few else 0)
 
 
+@pytest.mark.parametrize("kv", ["bf16", "fp8"])
+def test_odd_values_that_weigh_nothing(torch, kv):
+    """Rows of one workgroup of which some see an infinity, with a weight that fp32 holds as 0,
+    and the others do not: the same result every time, and infinite in the rows that see it."""
+    for hq, hkv, lens, rows in ((8, 2, [340, 300], [100, 60]), (28, 4, [700] * 9, [290] * 9), (8, 1, [500], [40])):
+        c = Case(torch, kv, hq, hkv, 128, lens, rows, seed=3)
+        start = []
+        for b, (L, m) in enumerate(zip(lens, rows)):
+            at = 30 + 3 * b
+            poison(c, b, at, at + 2, "v")
+            # Every third row begins behind them (the first keys weigh 2^-577 and less in all of them).
+            start += [at + 2 if i % 3 == 2 else 0 for i in range(m)]
+        mod = dict(key_start=torch.tensor(start, dtype=torch.int32, device="cuda"), slopes=torch.full((hq,), 4.0, device="cuda"))
+        first = c.check(mod, False, f"odd values of no weight {kv} {hq}/{hkv}")
+        for _ in range(5):
+            assert torch.equal(c.run(mod).double().nan_to_num(7.0), first.nan_to_num(7.0))
+
+
 @pytest.mark.parametrize("rows,kw", [(None, {}), ([4, 3, 5], dict(max_q_len=5)), ([90, 70, 60], {})])
 def test_pages_of_zeros(torch, rows, kw):
     """fp8 pages whose V scale is 0: their keys count, with values of 0."""
