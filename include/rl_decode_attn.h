@@ -405,7 +405,8 @@ rlda_status rl_decode_attn_append_rotary(rl_decode_attn_t handle, int32_t batch,
  * (device; 0: free; a page that k rows of the block table use has k), with the block
  * table and the lengths as for rl_decode_attn_run.  Every layer's cache shares that state
  * (page id p means page p of each of them), so taking, sharing and returning pages is one
- * call for all layers, and what moves contents takes a list of caches.
+ * call for all layers, and what moves contents takes a list of caches, all of the handle's
+ * dtype, heads and strides (layers with others have a pool of their own).
  *   A row's pages are the first ceil(seq_lens[b] / 16) of its table row, and these calls
  * change the lengths.  A caller that cuts one back itself (rejected draft tokens) stays
  * within the row's last page and out of pages that a fork shares: pages behind the length

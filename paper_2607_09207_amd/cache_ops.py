@@ -123,7 +123,8 @@ class CacheOps:
         """The caches of the layers that share one pool's page ids, as the page operations
         take them: [(k_cache, v_cache), ...], or (k_cache, v_cache, k_scale, v_scale) for
         fp8.  Checked here once; the set keeps the tensors.  Every layer whose caches have
-        the same dtype, heads and strides takes the set."""
+        the same dtype, heads and strides takes the set; layers with others need a pool (counts,
+        table and page ids) of their own."""
         what = "caches"
         layers = [tuple(x) for x in layers]
         fp8 = self.config.kv_dtype == _abi.RLDA_FP8_E4M3FN

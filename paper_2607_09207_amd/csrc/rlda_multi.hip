@@ -149,13 +149,21 @@ __device__ __forceinline__ int wave_min(int x) { return 0x7fffffff - wave_max(0x
 // score registers, and a row sees the keys of an interval.  The workgroup walks the blocks
 // from the first key that one of its rows sees to the last; a wave skips those that none of
 // its own sees, and masks only the ones that some of its rows sees in part.
-//   16384 tokens (28/4 heads, bf16) in documents of 900 under a cap of 50: 210 us (103 GFLOP
-// on the keys that are seen, 492 TFLOP/s), of which a window of one key takes 88: 235 MB of q
+//   16384 tokens (28/4 heads, bf16) in documents of 900 under a cap of 50: 212 us (103 GFLOP
+// on the keys that are seen, 488 TFLOP/s), of which a window of one key takes 88: 235 MB of q
 // and out and 3584 workgroups' starts and ends.  4096 tokens (40/8 heads, fp8) with a bias
-// and prefixes: 225 us (147 GFLOP, 655 TFLOP/s).  The matrix cores are busy for 20 to 26% of
-// it: what bounds it is the chain of a block, score, cap or bias, softmax, product, at three
-// waves per SIMD; a tenth fewer VALU operations (the maximum subtracted by the multiply-adds
-// before it) took as long, and so did priorities of the waves (s_setprio) in either phase.
+// and prefixes: 224 us (147 GFLOP, 656 TFLOP/s).  Both with the clock that a few hundred calls
+// bring; a process's first calls take 250 and 270.  A SIMD's three wave slots are filled for
+// 78 and 76% of the time (the items are dealt heaviest first by causal keys, which is not
+// what these rows see), its VALU issues for 51 and 60%, its matrix core is busy for 20 and
+// 26%: what bounds it is the chain of a block, score, cap or bias, softmax, product, and the
+// slots that stand empty; a tenth fewer VALU operations (the maximum subtracted by the
+// multiply-adds before it) took as long, and so did priorities of the waves (s_setprio) in
+// either phase.
+//   The probabilities enter the product as one bf16 value each, as in the plain call: 2.2e-3
+// (fp8 with its prefixes 2.0e-3) of a result, which bf16 itself holds to 1.65e-3.  With their
+// remainders in a second product the results are at those 1.65e-3, and the calls take 308
+// and 303 us; with a sum of the rounded values 2.0e-3 and 1.9e-3, and 220 and 233 us.
 // WIDE: ... with a wide cap (wide_cap), a kernel of its own: with both forms in one, 20
 // registers spilled, documents under a cap of 50 took 335 us a call and 246 without.
 template <int D, bool FP8, bool SMALL, bool MOD = false, bool WIDE = false>

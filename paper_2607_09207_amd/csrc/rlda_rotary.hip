@@ -18,9 +18,12 @@
 // for before anything else.  Few rows take small windows, and several workgroups to a
 // window with a share of the units each.
 // Rows are read and written once: what bounds it is bandwidth, and latency on few rows.
-// us a call: 32768 x 32 heads of 128 in bf16 88 (537 MB, 6.1 TB/s; a copy of one large
-// buffer to another reaches 4.9); 26,237 rows of 40/8 heads into fp8 pages 140 (700 MB, 5.0 TB/s); one token of 512 sequences, 64/8 heads, 7.6 (21 MB), of 8 sequences 5.0
-// (three dependent reads: length, page id, and the page's scale, and what the launch takes).
+// us a call: 32768 x 32 heads of 128 in bf16 89 (537 MB, 6.0 TB/s; a copy of one large
+// buffer to another reaches 4.9); 26,237 rows of 40/8 heads into fp8 pages 140 (700 MB, 5.0
+// TB/s), into bf16 ones 155 (752 MB, 4.8 TB/s); one token of 512 sequences, 64/8 heads, 7.5 (21 MB),
+// of 8 sequences 5.2 (the launch takes 3.8).  Few rows wait: for their length, then the page
+// id, then the angles, which could run beside that; bf16 and f32 caches then ask for K once
+// q is stored, and for V once K is.
 //
 // fp8 caches hold one scale per (page, KV head) that covers every row written so far, so
 // their K and V rows are written a page at a time, by workgroups of their own: one wave per
