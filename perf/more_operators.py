@@ -322,6 +322,11 @@ def _page_values(s, cache, scale, page):
     return x if scale is None else x * scale[page][..., None, None]
 
 
+def _over_127(x):
+    """The quotient, rounded once (a number as the divisor would be a product with its reciprocal)."""
+    return x / torch.full_like(x, 127)
+
+
 def _bounds(s):
     lens = s["seq_lens"].long()
     last = (lens - 1) // PAGE
@@ -332,7 +337,7 @@ def _bounds(s):
     x = _page_values(s, s["k"], s["ks"], page)
     there = ((j * PAGE)[:, :, None] + torch.arange(PAGE, device=DEV) < lens[:, None, None])[:, :, None, :, None]
     hi, lo = x.masked_fill(~there, -math.inf).amax(dim=3), x.masked_fill(~there, math.inf).amin(dim=3)
-    scale = torch.maximum(hi.abs(), lo.abs()).amax(dim=-1) / 127
+    scale = _over_127(torch.maximum(hi.abs(), lo.abs()).amax(dim=-1))
     by = torch.where(scale > 0, scale, 1.0)[..., None]
     s["bounds"][page] = torch.stack([(lo / by).floor().clamp_min(-127), (hi / by).ceil().clamp_max(127)], dim=-2).to(torch.int8)
     s["bound_scale"][page] = scale
@@ -353,7 +358,7 @@ def _select(s):
     B, n, S, hkv, d = len(s["seq_lens"]), s["most"], s["span"], c["hkv"], c["d"]
     G = c["hq"] // hkv
     q = s["q"].float()
-    sq = q.abs().amax(dim=-1, keepdim=True) / 127
+    sq = _over_127(q.abs().amax(dim=-1, keepdim=True))
     q8 = torch.where(sq > 0, (q / torch.where(sq > 0, sq, 1.0)).round(), 0.0)
     rows = torch.zeros((B, n, c["hq"], 2 * d + 1), device=DEV)
     rows[s["seq"], s["row_of"]] = torch.cat([q8.clamp_max(0), q8.clamp_min(0), sq], dim=-1)
