@@ -485,6 +485,117 @@ rlda_status rl_decode_attn_page_copy(rl_decode_attn_t handle, int32_t num_pages,
                                      const int32_t* dst, int32_t num_caches, const rl_decode_attn_cache* caches,
                                      void* workspace, size_t workspace_bytes, void* stream);
 
+/*
+ * A long cache read in part.  Every query row reads, of each KV head, only the pages whose
+ * keys may match it best: rl_decode_attn_page_bounds keeps bounds of every page's keys as
+ * tokens are appended, rl_decode_attn_select_pages chooses by them,
+ * rl_decode_attn_run_selected attends over what was chosen.
+ *
+ * Bounds of page p for KV head g, over its tokens' keys k_t (fp8: decode(byte) * k_scale):
+ *   s = max |k_t[d]| / 127,
+ *   lo[d] = max(floor(min_t k_t[d] / s), -127),  hi[d] = min(ceil(max_t k_t[d] / s), 127)
+ * in fp32, so s lo <= k_t <= s hi up to that rounding; s = 0 has bounds of 0, and a page with an
+ * infinity or NaN has s = +inf and bounds of 0.
+ *   bounds       [num_pages][Hkv][2][head_dim] int8 (lo, then hi), 16-byte aligned
+ *   bound_scale  [num_pages][Hkv] fp32
+ *   first        [batch] int32 device: the pages from that of token first[b] (0 <= first[b] <=
+ *                seq_lens[b]) on are computed; NULL: the page of the last token alone
+ * Whatever writes a page calls for its bounds again: an append (NULL, or the first token
+ * appended), and page ids whose contents rl_decode_attn_page_compact or _copy moved.  The pages
+ * that one call computes belong to one sequence each, or are full.
+ * Every kv_dtype.  A length out of range, or first[b]: flag bit 1; a page id outside the
+ * pool: skipped, flag bit 0.  workspace: as for rl_decode_attn_run (only its flag word is
+ * used).  One kernel, asynchronous.
+ */
+rlda_status rl_decode_attn_page_bounds(rl_decode_attn_t handle, int32_t batch, int32_t num_pages, const void* k_cache,
+                                       const float* k_scale, const int32_t* block_table, const int32_t* seq_lens,
+                                       const int32_t* first, int8_t* bounds, float* bound_scale, void* workspace,
+                                       size_t workspace_bytes, void* stream);
+
+/*
+ * The pages that every (query row, KV head) reads.  Rows are as for rl_decode_attn_run_scored:
+ * q_start NULL (total_q = batch): one a sequence; given: sequence b's last n_b tokens.  Of the
+ * n = ceil(tokens up to the row's own / 16) pages that a row sees, the first `sink` and the
+ * last `recent` (>= 1) are chosen, and of the others the best by
+ *   score(p) = s_p max_i (u_i sq_i),   u_i = sum_d max(q8_i[d] lo_p[d], q8_i[d] hi_p[d])
+ * over the KV head's query heads i, up to `budget` (>= sink + recent) together; equal scores
+ * go to the lower page.  q8 = rint(q / sq), sq = max |q| / 127 of the (row, head), in fp32; the
+ * sum is one of integers and exact.  A head whose q holds an infinity or NaN counts as 0;
+ * a page whose s is not finite is chosen before all others, one outside the pool after them.
+ *   pages   [total_q][Hkv][budget] int32: indices of the row's pages, ascending, then -1
+ *   counts  [total_q][Hkv] int32: min(n, budget)
+ * Rows that no sequence names, and those of inconsistent q_start entries (flag bit 1), are not
+ * written; rows before token 0 (n_b > seq_lens[b], flag bit 1) choose nothing.
+ * max_pages_per_seq up to 32768 (else RLDA_ERR_UNSUPPORTED).  workspace: as for
+ * rl_decode_attn_run.  One kernel, asynchronous.
+ */
+rlda_status rl_decode_attn_select_pages(rl_decode_attn_t handle, int32_t batch, int32_t num_pages, int32_t total_q,
+                                        int32_t budget, int32_t sink, int32_t recent, const void* q, const int8_t* bounds,
+                                        const float* bound_scale, const int32_t* block_table, const int32_t* seq_lens,
+                                        const int32_t* q_start, int32_t* pages, int32_t* counts, void* workspace,
+                                        size_t workspace_bytes, void* stream);
+
+/*
+ * rl_decode_attn_run over listed pages: row r reads, for the query heads of KV head g, the keys
+ * up to its own position in the pages pages[r][g][0 .. counts[r][g]), indices into its
+ * sequence's block-table row (any order; one named twice counts twice).  An empty list gives
+ * zeros.  Entries that are none of the row's pages are skipped (flag bit 0), counts beyond
+ * min(the row's pages, budget) are cut back to it.  Rows and rows without a sequence as
+ * for rl_decode_attn_select_pages; rows before token 0 give zeros.
+ * Every kv_dtype; total_q <= 4096 (RLDA_ERR_UNSUPPORTED).  Other arguments, checks and the
+ * workspace as for rl_decode_attn_run.  One kernel, asynchronous; events: both NULL, or both
+ * recorded around it.
+ */
+rlda_status rl_decode_attn_run_selected(rl_decode_attn_t handle, int32_t batch, int32_t num_pages, int32_t total_q,
+                                        int32_t budget, const int32_t* pages, const int32_t* counts, const void* q,
+                                        const void* k_cache, const void* v_cache, const float* k_scale, const float* v_scale,
+                                        const int32_t* block_table, const int32_t* seq_lens, const int32_t* q_start,
+                                        void* out, void* workspace, size_t workspace_bytes, void* stream, void* event_begin,
+                                        void* event_end);
+
+/*
+ * A long cache kept in part: decode attention that adds up how much of the softmax goes to
+ * every page, and eviction of the pages that got the least.
+ *
+ * rl_decode_attn_run (q_start NULL), or of several rows a sequence (its last n_b tokens, each
+ * attending up to its own position), and for every page j of a sequence that has rows
+ *   weights[b][j] <- decay weights[b][j] + sum over its rows, query heads and the page's keys of
+ *                    the softmax's probabilities
+ * in fp32, in one order.  decay in [0, 1]; with 0 the old weights are not read.
+ *   weights  [batch][max_pages_per_seq] fp32; entries at or past a sequence's pages stay as they
+ *            were.  A row of the table that is given to another sequence starts with zeros
+ *            (the caller's).
+ * Every kv_dtype; total_q <= 4096 (RLDA_ERR_UNSUPPORTED).  A row whose scores are NaN makes its
+ * sequence's weights NaN.  workspace: >= rl_decode_attn_weighed_workspace_size(total_q) bytes, with
+ * the rules of rl_decode_attn_run (whose calls it serves too).  Two kernels, asynchronous;
+ * events: both NULL, or both recorded around them.
+ */
+rlda_status rl_decode_attn_weighed_workspace_size(rl_decode_attn_t handle, int32_t total_q, size_t* bytes);
+rlda_status rl_decode_attn_run_weighed(rl_decode_attn_t handle, int32_t batch, int32_t num_pages, int32_t total_q,
+                                       float* weights, float decay, const void* q, const void* k_cache, const void* v_cache,
+                                       const float* k_scale, const float* v_scale, const int32_t* block_table,
+                                       const int32_t* seq_lens, const int32_t* q_start, void* out, void* workspace,
+                                       size_t workspace_bytes, void* stream, void* event_begin, void* event_end);
+
+/*
+ * Every sequence of more than `budget` (>= sink + recent) pages keeps its first `sink`, its last
+ * `recent` (>= 1), and the heaviest of the others (NaN: heaviest; equal weights: the lower
+ * page); the rest leave the block-table row and lose a reference each, as in
+ * rl_decode_attn_page_release, and dropped[b] (int32 device) says how many, 0 where none.  Entries
+ * and weights of the others move up in order, weights[b] of the places that fell empty become
+ * 0, seq_lens[b] shrinks by 16 a page.  The last page, alone in not being full, always stays.
+ * Keys keep the positions they were turned by: tokens appended afterwards are given theirs
+ * (`positions` of rl_decode_attn_append_rotary), and rows that shared a prompt's pages no
+ * longer do where these calls dropped unlike ones (rl_decode_attn_run_grouped).
+ * max_pages_per_seq up to 32768 (RLDA_ERR_UNSUPPORTED).  Lengths out of range: the row stays
+ * (flag bit 1); page ids outside the pool, or held by nobody, among the dropped: flag bit 0.
+ * workspace: of the page operations.  One kernel, asynchronous.
+ */
+rlda_status rl_decode_attn_page_evict(rl_decode_attn_t handle, int32_t batch, int32_t num_pages, int32_t* refs,
+                                      int32_t* block_table, int32_t* seq_lens, float* weights, int32_t budget, int32_t sink,
+                                      int32_t recent, int32_t* dropped, void* workspace, size_t workspace_bytes,
+                                      void* stream);
+
 /* Flags raised by device-side contract checks since the workspace was zeroed
  * (bit 0: page id outside [0, num_pages); bit 1: seq_len beyond capacity;
  * bit 2: a group's shared prompt clamped to its shortest member; bit 3: a

@@ -14,6 +14,7 @@ from typing import Optional
 
 from . import _abi
 from .cache_ops import CacheOps
+from .partial import PartialCache
 from .rotary import device_of, empty_on, on_device, raw_stream, rotary_frequencies, rotate
 
 __all__ = ["DecodeAttention", "decode_attention", "rotate", "rotary_frequencies", "RldaError", "library_path"]
@@ -41,7 +42,7 @@ def _dtype_code(t) -> int:
     raise TypeError(f"unsupported dtype {t}")
 
 
-class DecodeAttention(CacheOps):
+class DecodeAttention(CacheOps, PartialCache):
     """A configured decode-attention layer (a library handle).
 
     k_cache / v_cache passed to __call__ are 4-D tensors of shape
@@ -81,11 +82,11 @@ class DecodeAttention(CacheOps):
                    "rl_decode_attn_grouped_workspace_size")
         self.grouped_workspace_bytes = int(n.value)
         self._ws, self._outgrown = {}, []
-        self._page_ws = {}
+        self._page_ws, self._weighed_ws = {}, {}
         # The native call path (csrc/fastcall.cpp); it shares the workspaces by device.
         native = _abi.fastcall()
         self._fast = _abi.LEFT_TO_PYTHON if native is None else native.Layer(
-            h.value, self._ws, self._page_ws, (num_q_heads, num_kv_heads, head_dim, page_size, max_batch, max_pages_per_seq),
+            h.value, self._ws, self._page_ws, self._weighed_ws, (num_q_heads, num_kv_heads, head_dim, page_size, max_batch, max_pages_per_seq),
             (cfg.q_dtype, cfg.kv_dtype, cfg.out_dtype), self._kv_strides, self.workspace_bytes + 256,
             self.grouped_workspace_bytes + 256)
 

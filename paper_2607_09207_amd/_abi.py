@@ -16,7 +16,9 @@ EXPORTS = ["rl_decode_attn_create", "rl_decode_attn_workspace_size", "rl_decode_
            "rl_decode_attn_append", "rl_decode_attn_run_multi", "rl_decode_attn_run_noalloc",
            "rl_decode_attn_run_scored", "rl_decode_attn_rotate", "rl_decode_attn_append_rotary", "rl_decode_attn_page_workspace_size",
            "rl_decode_attn_page_grow", "rl_decode_attn_page_release", "rl_decode_attn_page_fork",
-           "rl_decode_attn_page_compact", "rl_decode_attn_page_copy",
+           "rl_decode_attn_page_compact", "rl_decode_attn_page_copy", "rl_decode_attn_page_bounds",
+           "rl_decode_attn_select_pages", "rl_decode_attn_run_selected", "rl_decode_attn_weighed_workspace_size",
+           "rl_decode_attn_run_weighed", "rl_decode_attn_page_evict",
            "rl_decode_attn_read_flags", "rl_decode_attn_destroy", "rl_decode_attn_strerror"]
 
 
@@ -112,8 +114,16 @@ def load() -> ctypes.CDLL:
         lib.rl_decode_attn_page_fork.argtypes = state + [i32, vp, vp] + caches + [vp, sz, vp]
         lib.rl_decode_attn_page_compact.argtypes = state + caches + [vp, vp, sz, vp]
         lib.rl_decode_attn_page_copy.argtypes = [vp, i32, i32, vp, vp] + caches + [vp, sz, vp]
+        f32 = ctypes.c_float
+        lib.rl_decode_attn_page_bounds.argtypes = [vp, i32, i32] + [vp] * 7 + [vp, sz, vp]
+        lib.rl_decode_attn_select_pages.argtypes = [vp] + [i32] * 6 + [vp] * 8 + [vp, sz, vp]
+        lib.rl_decode_attn_run_selected.argtypes = [vp] + [i32] * 4 + [vp] * 11 + [vp, sz, vp, vp, vp]
+        lib.rl_decode_attn_weighed_workspace_size.argtypes = [vp, i32, ctypes.POINTER(sz)]
+        lib.rl_decode_attn_run_weighed.argtypes = [vp] + [i32] * 3 + [vp, f32] + [vp] * 9 + [vp, sz, vp, vp, vp]
+        lib.rl_decode_attn_page_evict.argtypes = state + [vp, i32, i32, i32, vp, vp, sz, vp]
         for name in ("rotate", "append_rotary", "page_workspace_size", "page_grow", "page_release", "page_fork",
-                     "page_compact", "page_copy"):
+                     "page_compact", "page_copy", "page_bounds", "select_pages", "run_selected", "weighed_workspace_size",
+                     "run_weighed", "page_evict"):
             getattr(lib, "rl_decode_attn_" + name).restype = ctypes.c_int
         lib.rl_decode_attn_read_flags.argtypes = [vp, vp, vp, ctypes.POINTER(ctypes.c_uint32)]
         lib.rl_decode_attn_read_flags.restype = ctypes.c_int
@@ -136,6 +146,7 @@ class LeftToPython:
 
     grouped = multi = noalloc = append = scored = rotate = append_rotary = run
     page_grow = page_release = page_fork = page_compact = run
+    page_bounds = select_pages = selected = weighed = page_evict = run
 
 
 LEFT_TO_PYTHON = LeftToPython()
@@ -161,7 +172,8 @@ def fastcall():
         raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
         addr = [ctypes.cast(getattr(lib, "rl_decode_attn_" + n), ctypes.c_void_p).value
                 for n in ("run", "run_grouped", "run_multi", "run_noalloc", "append", "run_scored", "rotate",
-                          "append_rotary", "page_grow", "page_release", "page_fork", "page_compact")]
+                          "append_rotary", "page_grow", "page_release", "page_fork", "page_compact", "page_bounds",
+                          "select_pages", "run_selected", "weighed_workspace_size", "run_weighed", "page_evict")]
         _fastcall.bind(raw, *addr)
         _fast = (lib, _fastcall)
     return _fast[1]

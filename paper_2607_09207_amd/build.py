@@ -13,7 +13,8 @@ LIB = os.path.join(HERE, "librl_decode_attn.so")
 SOURCES = [os.path.join(CSRC, "rlda_kernels.hip"), os.path.join(CSRC, "rlda_multi.hip"),
            os.path.join(CSRC, "rlda_host.cpp"), os.path.join(CSRC, "rlda_rotary.hip"),
            os.path.join(CSRC, "rlda_pages.hip"), os.path.join(CSRC, "rlda_ops.cpp"),
-           os.path.join(CSRC, "rlda_scored.hip")]
+           os.path.join(CSRC, "rlda_scored.hip"), os.path.join(CSRC, "rlda_listed.hip"),
+           os.path.join(CSRC, "rlda_select.hip")]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 # Read-bandwidth reference kernels (bench support, not the attention path).
 PROBE_SOURCES = [os.path.join(CSRC, "hbm_probe.hip")]

@@ -40,6 +40,12 @@ decltype(&rl_decode_attn_page_grow) g_page_grow;
 decltype(&rl_decode_attn_page_release) g_page_release;
 decltype(&rl_decode_attn_page_fork) g_page_fork;
 decltype(&rl_decode_attn_page_compact) g_page_compact;
+decltype(&rl_decode_attn_page_bounds) g_page_bounds;
+decltype(&rl_decode_attn_select_pages) g_select_pages;
+decltype(&rl_decode_attn_run_selected) g_selected;
+decltype(&rl_decode_attn_weighed_workspace_size) g_weighed_size;
+decltype(&rl_decode_attn_run_weighed) g_weighed;
+decltype(&rl_decode_attn_page_evict) g_page_evict;
 PyObject* g_raw_stream;   // device index -> current stream (an int)
 
 constexpr int kMaxDevices = 64;
@@ -50,6 +56,7 @@ struct Layer {
   rl_decode_attn_t handle;
   PyObject* workspaces;   // dict: device string -> uint8 tensor (the Python object's own)
   PyObject* page_workspaces;   // dict: (device string, pages) -> uint8 tensor (its own too)
+  PyObject* weighed_workspaces;   // dict: device string -> uint8 tensor (its own too)
   int64_t hq, hkv, d, page, max_batch, max_pages;
   int64_t stride[3];
   int64_t ws_bytes, grouped_ws_bytes;   // as allocated, alignment room included
@@ -683,6 +690,198 @@ PyObject* layer_page_compact(PyObject* self, PyObject* const* a, Py_ssize_t n) {
   });
 }
 
+// ------------------------------------------------------------------ a cache read and kept in part
+
+// q [total][Hq][d] of `batch` sequences, one row each or by q_start.
+bool rows_call(const Layer* L, PyObject* q_arg, PyObject* qs_arg, const Tensor** q, const Tensor** qs, int* dev, int64_t* total,
+               int64_t* batch) {
+  const Tensor* t = *q = tensor(q_arg);
+  *qs = nullptr;
+  if (!t || !t->is_cuda() || t->dim() != 3 || t->size(0) > INT32_MAX || derived(*t)) return false;
+  *dev = t->get_device();
+  *total = *batch = t->size(0);
+  if (qs_arg != Py_None) {
+    const Tensor* s = *qs = tensor(qs_arg);
+    if (!s || s->dim() != 1) return false;
+    *batch = s->size(0) - 1;
+    if (!shaped(s, *dev, at::kInt, {*batch + 1})) return false;
+  }
+  return shaped(t, *dev, L->q_dtype, {*total, L->hq, L->d}) && current(*dev);
+}
+
+bool bounds_ok(const Layer* L, const Tensor* b, const Tensor* s, int dev, int64_t npages) {
+  return plain(b, dev, at::kChar) && b->dim() == 4 && b->size(0) >= npages && b->size(1) == L->hkv && b->size(2) == 2 &&
+         b->size(3) == L->d && b->is_contiguous() && scale_ok(L, s, dev, npages);
+}
+
+bool host_int(PyObject* o, int32_t* out) {
+  int64_t x = 0;
+  if (o == Py_None || !as_int(o, 0, &x) || x < INT32_MIN || x > INT32_MAX) return false;
+  *out = (int32_t)x;
+  return true;
+}
+bool budget_of(PyObject* const* a, int32_t* budget, int32_t* sink, int32_t* recent) {
+  return host_int(a[0], budget) && host_int(a[1], sink) && host_int(a[2], recent) && *sink >= 0 && *recent >= 1 &&
+         (int64_t)*sink + *recent <= *budget;
+}
+
+// page_bounds(k, block_table, seq_lens, k_scale, stream, num_pages, workspace, bounds, bound_scale, first): the
+// status, or None (not taken).
+PyObject* layer_page_bounds(PyObject* self, PyObject* const* a, Py_ssize_t n) {
+  if (n != 10) return PyErr_Format(PyExc_TypeError, "page_bounds takes 10 arguments");
+  const Layer* L = (const Layer*)self;
+  return guarded([&]() -> PyObject* {
+    const Tensor *lens = tensor(a[2]), *k = tensor(a[0]), *bounds = tensor(a[7]), *bscale = tensor(a[8]), *first;
+    if (!k || !k->is_cuda() || !lens || lens->dim() != 1) return nullptr;
+    const int dev = k->get_device();
+    const int64_t B = lens->size(0);
+    PyObject* const args[8] = {a[0], a[0], a[1], a[2], a[3], a[3], a[4], a[5]};   // (K alone)
+    Call c;
+    if (!common(L, c, args, dev, B) || !bounds_ok(L, bounds, bscale, dev, c.npages) || !vector_or_none(a[9], dev, at::kInt, B, &first) ||
+        !workspace(L, c, a[6], false) || !current(dev))
+      return nullptr;
+    void *kp = ptr(c.k), *ksp = ptr(c.ks), *bp = ptr(c.bt), *lp = ptr(c.lens), *fp = ptr(first), *op = ptr(bounds), *sp = ptr(bscale);
+    WITHOUT_GIL(g_page_bounds(L->handle, (int32_t)B, (int32_t)c.npages, kp, (const float*)ksp, (const int32_t*)bp, (const int32_t*)lp,
+                              (const int32_t*)fp, (int8_t*)op, (float*)sp, c.ws_ptr, c.ws_room, c.stream));
+    return status(st);
+  });
+}
+
+// select_pages(q, bounds, bound_scale, block_table, seq_lens, stream, num_pages, pages, counts, workspace, q_start,
+//              budget, sink, recent): (pages, counts), a status, or None
+PyObject* layer_select_pages(PyObject* self, PyObject* const* a, Py_ssize_t n) {
+  if (n != 14) return PyErr_Format(PyExc_TypeError, "select_pages takes 14 arguments");
+  const Layer* L = (const Layer*)self;
+  return guarded([&]() -> PyObject* {
+    const Tensor *q, *qs, *bounds = tensor(a[1]), *bscale = tensor(a[2]);
+    int dev;
+    int64_t total, B;
+    int32_t budget, sink, recent;
+    Call c;
+    if (!rows_call(L, a[0], a[10], &q, &qs, &dev, &total, &B) || !budget_of(a + 11, &budget, &sink, &recent) || !bounds ||
+        bounds->dim() != 4 || !as_int(a[6], bounds->size(0), &c.npages) || c.npages < 0 || c.npages > INT32_MAX ||
+        !bounds_ok(L, bounds, bscale, dev, c.npages) || B < 0 || B > L->max_batch)
+      return nullptr;
+    c.dev = dev;
+    c.bt = tensor(a[3]);
+    c.lens = tensor(a[4]);
+    if (!shaped(c.bt, dev, at::kInt, {B, L->max_pages}) || !shaped(c.lens, dev, at::kInt, {B}) || !stream_of(a[5], dev, &c.stream) ||
+        !workspace(L, c, a[9], false))
+      return nullptr;
+    Tensor fresh[2];
+    const Tensor* out[2];
+    const std::vector<int64_t> shape[2] = {{total, L->hkv, budget}, {total, L->hkv}};
+    for (int i = 0; i < 2; ++i) {
+      if (a[7 + i] == Py_None) {
+        fresh[i] = empty_on(shape[i], c.lens->options(), dev, a[5], c.stream);
+        out[i] = &fresh[i];
+      } else if (!shaped(out[i] = tensor(a[7 + i]), dev, at::kInt, shape[i])) {
+        return nullptr;
+      }
+    }
+    void *qp = ptr(q), *op = ptr(bounds), *sp = ptr(bscale), *bp = ptr(c.bt), *lp = ptr(c.lens), *qsp = ptr(qs), *pp = ptr(out[0]),
+         *cp = ptr(out[1]);
+    WITHOUT_GIL(g_select_pages(L->handle, (int32_t)B, (int32_t)c.npages, (int32_t)total, budget, sink, recent, qp, (const int8_t*)op,
+                               (const float*)sp, (const int32_t*)bp, (const int32_t*)lp, (const int32_t*)qsp, (int32_t*)pp,
+                               (int32_t*)cp, c.ws_ptr, c.ws_room, c.stream));
+    if (st != RLDA_OK) return status(st);
+    PyObject* r[2];
+    for (int i = 0; i < 2; ++i) r[i] = answer(st, a[7 + i], fresh[i]);
+    PyObject* both = r[0] && r[1] ? PyTuple_Pack(2, r[0], r[1]) : nullptr;
+    Py_XDECREF(r[0]);
+    Py_XDECREF(r[1]);
+    return both;
+  });
+}
+
+// selected(q, k, v, block_table, seq_lens, k_scale, v_scale, stream, num_pages, out, workspace, q_start, pages, counts)
+PyObject* layer_selected(PyObject* self, PyObject* const* a, Py_ssize_t n) {
+  if (n != 14) return PyErr_Format(PyExc_TypeError, "selected takes 14 arguments");
+  const Layer* L = (const Layer*)self;
+  return guarded([&]() -> PyObject* {
+    const Tensor *q, *qs, *pages = tensor(a[12]), *counts = tensor(a[13]);
+    int dev;
+    int64_t total, B;
+    Call c;
+    if (!rows_call(L, a[0], a[11], &q, &qs, &dev, &total, &B) || !pages || pages->dim() != 3 || pages->size(2) > INT32_MAX ||
+        !shaped(pages, dev, at::kInt, {total, L->hkv, pages->size(2)}) || !shaped(counts, dev, at::kInt, {total, L->hkv}) ||
+        !common(L, c, a + 1, dev, B) || !workspace(L, c, a[10], false))
+      return nullptr;
+    Tensor fresh;
+    const Tensor* o = output(L, a[9], *q, total, a[7], c, fresh);
+    if (!o) return nullptr;
+    const int32_t budget = (int32_t)pages->size(2);
+    void *qp = ptr(q), *kp = ptr(c.k), *vp = ptr(c.v), *ksp = ptr(c.ks), *vsp = ptr(c.vs), *bp = ptr(c.bt), *lp = ptr(c.lens),
+         *op = ptr(o), *qsp = ptr(qs), *pp = ptr(pages), *cp = ptr(counts);
+    WITHOUT_GIL(g_selected(L->handle, (int32_t)B, (int32_t)c.npages, (int32_t)total, budget, (const int32_t*)pp, (const int32_t*)cp,
+                           qp, kp, vp, (const float*)ksp, (const float*)vsp, (const int32_t*)bp, (const int32_t*)lp,
+                           (const int32_t*)qsp, op, c.ws_ptr, c.ws_room, c.stream, nullptr, nullptr));
+    return answer(st, a[9], fresh);
+  });
+}
+
+// weighed(q, k, v, block_table, seq_lens, k_scale, v_scale, stream, num_pages, out, workspace, q_start, weights, decay)
+PyObject* layer_weighed(PyObject* self, PyObject* const* a, Py_ssize_t n) {
+  if (n != 14) return PyErr_Format(PyExc_TypeError, "weighed takes 14 arguments");
+  const Layer* L = (const Layer*)self;
+  return guarded([&]() -> PyObject* {
+    const Tensor *q, *qs, *weights = tensor(a[12]);
+    int dev;
+    int64_t total, B;
+    double decay = 0.0;
+    Call c;
+    size_t need = 0;
+    if (!rows_call(L, a[0], a[11], &q, &qs, &dev, &total, &B) || !as_double(a[13], &decay) || !(decay >= 0.0 && decay <= 1.0) ||
+        !shaped(weights, dev, at::kFloat, {B, L->max_pages}) || derived(*weights) || !common(L, c, a + 1, dev, B) ||
+        dev >= kMaxDevices || g_weighed_size(L->handle, (int32_t)total, &need) != RLDA_OK)
+      return nullptr;
+    const Tensor* ws = nullptr;
+    if (a[10] != Py_None) {
+      ws = tensor(a[10]);
+    } else {
+      PyObject* o = PyDict_GetItem(L->weighed_workspaces, g_device_key[dev]);   // borrowed
+      ws = o ? tensor(o) : nullptr;
+      if (ws && ws->numel() < (int64_t)need + 256) return nullptr;
+    }
+    if (!use_workspace(c, ws)) return nullptr;
+    Tensor fresh;
+    const Tensor* o = output(L, a[9], *q, total, a[7], c, fresh);
+    if (!o) return nullptr;
+    mark_written(*weights);
+    void *qp = ptr(q), *kp = ptr(c.k), *vp = ptr(c.v), *ksp = ptr(c.ks), *vsp = ptr(c.vs), *bp = ptr(c.bt), *lp = ptr(c.lens),
+         *op = ptr(o), *qsp = ptr(qs), *wp = ptr(weights);
+    WITHOUT_GIL(g_weighed(L->handle, (int32_t)B, (int32_t)c.npages, (int32_t)total, (float*)wp, (float)decay, qp, kp, vp,
+                          (const float*)ksp, (const float*)vsp, (const int32_t*)bp, (const int32_t*)lp, (const int32_t*)qsp, op,
+                          c.ws_ptr, c.ws_room, c.stream, nullptr, nullptr));
+    return answer(st, a[9], fresh);
+  });
+}
+
+// page_evict(refs, block_table, seq_lens, weights, budget, sink, recent, dropped, workspace, stream): the dropped
+// tensor, a status, or None
+PyObject* layer_page_evict(PyObject* self, PyObject* const* a, Py_ssize_t n) {
+  if (n != 10) return PyErr_Format(PyExc_TypeError, "page_evict takes 10 arguments");
+  const Layer* L = (const Layer*)self;
+  return guarded([&]() -> PyObject* {
+    Call c;
+    const Tensor *refs, *weights = tensor(a[3]);
+    int64_t B;
+    int32_t budget, sink, recent;
+    if (!budget_of(a + 4, &budget, &sink, &recent) || !page_common(L, c, a, a[8], a[9], &refs, &B) ||
+        !shaped(weights, c.dev, at::kFloat, {B, L->max_pages}) || derived(*weights))
+      return nullptr;
+    Tensor fresh;
+    if (a[7] == Py_None) fresh = empty_on({B}, refs->options(), c.dev, a[9], c.stream);
+    const Tensor* dropped = a[7] == Py_None ? &fresh : tensor(a[7]);
+    if (!shaped(dropped, c.dev, at::kInt, {B})) return nullptr;
+    mark_written(*weights);
+    void *rp = ptr(refs), *bp = ptr(c.bt), *lp = ptr(c.lens), *wp = ptr(weights), *dp = ptr(dropped);
+    WITHOUT_GIL(g_page_evict(L->handle, (int32_t)B, (int32_t)c.npages, (int32_t*)rp, (int32_t*)bp, (int32_t*)lp, (float*)wp, budget,
+                             sink, recent, (int32_t*)dp, c.ws_ptr, c.ws_room, c.stream));
+    return answer(st, a[7], fresh);
+  });
+}
+
 PyMethodDef layer_methods[] = {
     {"run", (PyCFunction)(void*)layer_run, METH_FASTCALL, nullptr},
     {"grouped", (PyCFunction)(void*)layer_grouped, METH_FASTCALL, nullptr},
@@ -695,22 +894,29 @@ PyMethodDef layer_methods[] = {
     {"page_release", (PyCFunction)(void*)layer_page_release, METH_FASTCALL, nullptr},
     {"page_fork", (PyCFunction)(void*)layer_page_fork, METH_FASTCALL, nullptr},
     {"page_compact", (PyCFunction)(void*)layer_page_compact, METH_FASTCALL, nullptr},
+    {"page_bounds", (PyCFunction)(void*)layer_page_bounds, METH_FASTCALL, nullptr},
+    {"select_pages", (PyCFunction)(void*)layer_select_pages, METH_FASTCALL, nullptr},
+    {"selected", (PyCFunction)(void*)layer_selected, METH_FASTCALL, nullptr},
+    {"weighed", (PyCFunction)(void*)layer_weighed, METH_FASTCALL, nullptr},
+    {"page_evict", (PyCFunction)(void*)layer_page_evict, METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 
 void layer_dealloc(PyObject* self) {
   Py_XDECREF(((Layer*)self)->workspaces);
   Py_XDECREF(((Layer*)self)->page_workspaces);
+  Py_XDECREF(((Layer*)self)->weighed_workspaces);
   Py_TYPE(self)->tp_free(self);
 }
 
-// Layer(handle, workspaces, page workspaces, (Hq, Hkv, d, page, max_batch, max_pages), (q, kv, out dtype codes),
+// Layer(handle, workspaces, page workspaces, workspaces of weighed, (Hq, Hkv, d, page, max_batch, max_pages), (q, kv, out dtype codes),
 //       (page, head, slot strides), workspace bytes, grouped workspace bytes)
 PyObject* layer_new(PyTypeObject* type, PyObject* args, PyObject*) {
   unsigned long long handle = 0;
-  PyObject *dict = nullptr, *pages = nullptr;
+  PyObject *dict = nullptr, *pages = nullptr, *weighed = nullptr;
   long long v[6], s[3], ws = 0, gws = 0;
   int q = 0, kv = 0, out = 0;
-  if (!PyArg_ParseTuple(args, "KO!O!(LLLLLL)(iii)(LLL)LL", &handle, &PyDict_Type, &dict, &PyDict_Type, &pages, &v[0], &v[1], &v[2], &v[3], &v[4],
+  if (!PyArg_ParseTuple(args, "KO!O!O!(LLLLLL)(iii)(LLL)LL", &handle, &PyDict_Type, &dict, &PyDict_Type, &pages, &PyDict_Type,
+                        &weighed, &v[0], &v[1], &v[2], &v[3], &v[4],
                         &v[5], &q, &kv, &out, &s[0], &s[1], &s[2], &ws, &gws))
     return nullptr;
   Layer* L = (Layer*)type->tp_alloc(type, 0);
@@ -720,6 +926,8 @@ PyObject* layer_new(PyTypeObject* type, PyObject* args, PyObject*) {
   L->workspaces = dict;
   Py_INCREF(pages);
   L->page_workspaces = pages;
+  Py_INCREF(weighed);
+  L->weighed_workspaces = weighed;
   L->hq = v[0], L->hkv = v[1], L->d = v[2], L->page = v[3], L->max_batch = v[4], L->max_pages = v[5];
   for (int i = 0; i < 3; ++i) L->stride[i] = s[i];
   L->ws_bytes = ws;
@@ -734,13 +942,14 @@ PyObject* layer_new(PyTypeObject* type, PyObject* args, PyObject*) {
 PyTypeObject layer_type = {PyVarObject_HEAD_INIT(nullptr, 0)};
 
 // bind(raw_stream, run, grouped, multi, noalloc, append, scored, rotate, append_rotary, page_grow,
-// page_release, page_fork, page_compact): the stream lookup and the addresses of the loaded
+// page_release, page_fork, page_compact, page_bounds, select_pages, selected, weighed_size,
+// weighed, page_evict): the stream lookup and the addresses of the loaded
 // library's entry points.
 PyObject* bind(PyObject*, PyObject* args) {
   PyObject* raw = nullptr;
-  unsigned long long f[12];
-  if (!PyArg_ParseTuple(args, "OKKKKKKKKKKKK", &raw, &f[0], &f[1], &f[2], &f[3], &f[4], &f[5], &f[6], &f[7], &f[8], &f[9],
-                        &f[10], &f[11]))
+  unsigned long long f[18];
+  if (!PyArg_ParseTuple(args, "OKKKKKKKKKKKKKKKKKK", &raw, &f[0], &f[1], &f[2], &f[3], &f[4], &f[5], &f[6], &f[7], &f[8], &f[9],
+                        &f[10], &f[11], &f[12], &f[13], &f[14], &f[15], &f[16], &f[17]))
     return nullptr;
   Py_INCREF(raw);
   Py_XDECREF(g_raw_stream);
@@ -757,6 +966,12 @@ PyObject* bind(PyObject*, PyObject* args) {
   g_page_release = (decltype(g_page_release))(uintptr_t)f[9];
   g_page_fork = (decltype(g_page_fork))(uintptr_t)f[10];
   g_page_compact = (decltype(g_page_compact))(uintptr_t)f[11];
+  g_page_bounds = (decltype(g_page_bounds))(uintptr_t)f[12];
+  g_select_pages = (decltype(g_select_pages))(uintptr_t)f[13];
+  g_selected = (decltype(g_selected))(uintptr_t)f[14];
+  g_weighed_size = (decltype(g_weighed_size))(uintptr_t)f[15];
+  g_weighed = (decltype(g_weighed))(uintptr_t)f[16];
+  g_page_evict = (decltype(g_page_evict))(uintptr_t)f[17];
   Py_RETURN_NONE;
 }
 

@@ -102,6 +102,13 @@ __device__ __forceinline__ float token_sum(float x) {
 
 // ---------------------------------------------------------------- helpers
 
+// What a call's rows read.  kSequences: the pages of their sequences.  kListed: every query
+// row (unit of the work list) the pages that its (row, KV head) lists.  kWeighed: every query
+// row all pages up to its position, and each page's share of the softmax is kept.
+enum RowsForm { kSequences, kListed, kWeighed };
+
+__device__ __forceinline__ float log2_of(float x) { return __builtin_amdgcn_logf(x); }   // v_log_f32 is base 2
+
 __device__ __forceinline__ int64_t owner_of(int64_t x, int W, int64_t C) {
   // Largest u with floor(u*C/W) <= x: the share holding cost x.
   return ((x + 1) * (int64_t)W - 1) / C;
@@ -124,6 +131,14 @@ __device__ __forceinline__ void store_row(const Params& p, int b, int qh, int d0
 template <int D, int DPT = D / 16>
 __device__ __forceinline__ void store_out(const Params& p, int b, int qh, int d0, const float* o, float inv) {
   store_row<D, DPT>(p, b, qh, d0, o, inv);
+}
+
+// kWeighed: log2 of the sum of exp2(score) over a row's keys, and over one page's of them.
+__device__ __forceinline__ void store_row_lse(const Params& p, int row, int qh, float m, float l) {
+  p.row_lse[(int64_t)row * p.num_q_heads + qh] = m + log2_of(l);
+}
+__device__ __forceinline__ void store_page_lse(const Params& p, int row, int qh, int page, float lse) {
+  p.page_lse[((int64_t)row * p.num_q_heads + qh) * p.max_pages + page] = lse;
 }
 
 // Query heads of each KV head (a copy of Params::q_head, filled at kernel start):
@@ -196,7 +211,7 @@ __device__ __forceinline__ void merge_batches(const Params& p, const PartialRsrc
 // A segment cut into many pieces (a long sequence over few workgroups' worth of
 // other work) is merged 16 pieces per round trip (8 when a thread holds 16 outputs);
 // the common 2-4 pieces, 4 at a time.
-template <int D, int DPT = D / 16>
+template <int D, int DPT = D / 16, bool WEIGH = false>
 __device__ __forceinline__ void merge_pieces(const Params& p, int orow, int qh, int h, int d0, int64_t u_first,
                                              int64_t u_last) {
   const PartialRsrc rs = PartialRsrc::of<D>(p);
@@ -207,6 +222,9 @@ __device__ __forceinline__ void merge_pieces(const Params& p, int orow, int qh, 
     merge_batches<D, (DPT <= 8 ? 16 : 8), DPT>(p, rs, h, d0, u_first, u_last, M, Ls, o);
   else
     merge_batches<D, 4, DPT>(p, rs, h, d0, u_first, u_last, M, Ls, o);
+  if constexpr (WEIGH) {
+    if (d0 == 0) store_row_lse(p, orow, qh, M, Ls);
+  }
   store_out<D, DPT>(p, orow, qh, d0, o, Ls > 0.f ? 1.f / Ls : 0.f);
 }
 
@@ -255,6 +273,7 @@ struct Mfma {
   // counted from the page's first token; the row's bias a token, in log2 units.
   int rlo, rhi, rpos;
   float slope;
+  float page;   // kWeighed: the last page's part of the row's sum, log2
 
   __device__ __forceinline__ static int chunk_of(int qg, int s) {
     return FP8 ? 8 * (s >> 1) + 2 * qg + (s & 1) : 4 * s + qg;
@@ -570,13 +589,13 @@ struct Mfma {
   // multi-token rows: tokens of the page and after it, up to 31, less `shift`).
   //   Remainders: the probabilities enter the product as a bf16 value and a bf16
   // remainder.  kAlways: in one product; kByCall: where `exact` (0 or ~0, uniform) says so.
-  template <bool MULTI = false, Remainders REM = kByCall>
+  template <bool MULTI = false, Remainders REM = kByCall, bool WEIGH = false>
   __device__ __forceinline__ void compute(const Frag& f, int lane, int valid_tokens, float kmul, float vmul,
                                           uint64_t exact = 0) {
-    compute_with<MULTI, REM>(f, nullptr, lane, valid_tokens, kmul, vmul, exact);
+    compute_with<MULTI, REM, WEIGH>(f, nullptr, lane, valid_tokens, kmul, vmul, exact);
   }
   // ... with the page's V operands built once by the caller (vo), or here (null).
-  template <bool MULTI = false, Remainders REM = kByCall>
+  template <bool MULTI = false, Remainders REM = kByCall, bool WEIGH = false>
   __device__ __forceinline__ void compute_with(const Frag& f, const VOp* vo, int lane, int valid_tokens, float kmul,
                                                float vmul, uint64_t exact) {
     const int qg = lane >> 4;
@@ -624,6 +643,7 @@ struct Mfma {
       ps += pr[r];
     }
     l += ps;
+    if constexpr (WEIGH) page = mu + log2_of(group_sum(ps));   // no key: -inf
     const u32x2 pb = {pack_bf16(pr[0] * vmul, pr[1] * vmul), pack_bf16(pr[2] * vmul, pr[3] * vmul)};
     const VOp v = vo ? *vo : v_operand(f);
     if constexpr (REM == kAlways) {
@@ -769,11 +789,20 @@ struct Mfma {
     store_row<D, 4 * DT>(p, q0 + rr / G, s_qhead[g * G + rr % G], 4 * DT * qg, o, lt > 0.f ? 1.f / lt : 0.f);
   }
 
+  // kWeighed: the page's part for every row of the tile.
+  __device__ __forceinline__ void put_page(const Params& p, int b, int g, int j, int lane) const {
+    if (lane < p.group) store_page_lse(p, b, s_qhead[g * p.group + lane], j, page);
+  }
+
   // A piece this wave covered entirely: normalise and write its rows.
+  template <bool WEIGH = false>
   __device__ __forceinline__ void write_out(const Params& p, int b, int g, int lane) const {
     const int i = lane & 15, qg = lane >> 4;
     const float lt = group_sum(l);
     if (i >= p.group) return;
+    if constexpr (WEIGH) {
+      if (qg == 0) store_row_lse(p, b, s_qhead[g * p.group + i], m, lt);
+    }
     float o[4 * DT];
 #pragma unroll
     for (int r = 0; r < 4; ++r)
@@ -805,6 +834,7 @@ struct Valu {
   float acc[GM][CW];
   float qv[GM][CW];
   float m[GM], l[GM];
+  float page[GM];   // kWeighed: the last page's part of each row's sum, log2
   int off;
 
   __device__ __forceinline__ void setup(const Params&, int lane, int32_t ss) {
@@ -838,7 +868,7 @@ struct Valu {
     for (int s = 0; s < NL; ++s) f.v[s] = RowLoad<16>::load(rv, off + 16 * s);
   }
 
-  template <bool MULTI = false, Remainders REM = kByCall>
+  template <bool MULTI = false, Remainders REM = kByCall, bool WEIGH = false>
   __device__ __forceinline__ void compute(const Frag& f, int lane, int valid_tokens, float kmul, float, uint64_t = 0) {
     const int t = lane >> 2;
     const bool valid = t < valid_tokens;
@@ -856,6 +886,7 @@ struct Valu {
       const float pr = __builtin_amdgcn_exp2f(s - mu);
       l[h] = l[h] * alpha + pr;
       m[h] = mn;
+      if constexpr (WEIGH) page[h] = mu + log2_of(token_sum(pr));
 #pragma unroll
       for (int j = 0; j < CW; ++j) acc[h][j] = acc[h][j] * alpha + pr * __uint_as_float(f.v[j >> 2][j & 3]);
     }
@@ -888,11 +919,23 @@ struct Valu {
     }
   }
 
+  __device__ __forceinline__ void put_page(const Params& p, int b, int g, int j, int lane) const {
+#pragma unroll
+    for (int h = 0; h < GM; ++h)
+      if (h < p.group && lane == 0) store_page_lse(p, b, s_qhead[g * p.group + h], j, page[h]);
+  }
+
+  template <bool WEIGH = false>
   __device__ __forceinline__ void write_out(const Params& p, int b, int g, int lane) {
     const int c = lane & 3;
     float lt[GM];
     reduce_tokens(lt);
     if (lane >= 4) return;
+    if constexpr (WEIGH) {
+#pragma unroll
+      for (int h = 0; h < GM; ++h)
+        if (h < p.group && c == 0) store_row_lse(p, b, s_qhead[g * p.group + h], m[h], lt[h]);
+    }
 #pragma unroll
     for (int h = 0; h < GM; ++h)
       if (h < p.group) store_row<D, CW>(p, b, s_qhead[g * p.group + h], c * CW, acc[h], lt[h] > 0.f ? 1.f / lt[h] : 0.f);
@@ -916,6 +959,24 @@ constexpr int kInfoChunkShift = 30;     // multi-token run: the segment's 16-row
 constexpr int kInfoActShift = 29;       // packed grouped run: the pack member whose rows the page serves (3 bits;
 constexpr int kActAll = 7;              // kActAll: a prompt page, every member's rows); the pack index has 12 bits
 
+// The j-th page that (row, KV head) reads, of a row of sequence `seq` that sees L tokens:
+// (page id as read, tokens of it that count).  A list's entries that are none of the row's
+// pages, and places past its count, hold no token.
+template <RowsForm ROWS>
+__device__ __forceinline__ int2 row_page(const Params& p, int row, int seq, int g, int j, int L) {
+  int at = j;
+  if constexpr (ROWS == kListed) {
+    const int64_t list = (int64_t)row * p.num_kv_heads + g;
+    if (j >= p.list_counts[list]) return make_int2(0, 0);
+    at = p.list[list * p.budget + j];
+    if (at < 0 || at >= (L + kPage - 1) / kPage) {
+      atomicOr(p.flags, kFlagBadPage);
+      return make_int2(0, 0);
+    }
+  }
+  return make_int2(p.block_table[(int64_t)seq * p.max_pages + at], min(kPage, L - kPage * at));
+}
+
 // The page id is returned as read; it is checked where it is used, so that
 // nothing waits for these loads until the chunk is consumed.
 struct StreamChunk {
@@ -935,7 +996,8 @@ struct StreamChunk {
 // part), then each member's own pages in member order (only that member's rows).
 // Modified scores (MOD): a sequence's pages begin with the first one that a row sees:
 // page s_first[b], or (one row a sequence) the page of token s_ppre[b].
-template <bool MULTI, bool PACK, bool MOD>
+// Query rows as units (ROWS): row b of sequence s_ppre[b] sees s_first[b] tokens.
+template <bool MULTI, bool PACK, bool MOD, RowsForm ROWS>
 __device__ __forceinline__ StreamChunk fetch_chunk(const Params& p, const int32_t* s_pre, const uint8_t* s_tail,
                                                    const int32_t* s_ppre, const uint16_t* s_nfull,
                                                    const int16_t* s_gpp, const int32_t* s_first, int nunits, int base, int w0, int w1,
@@ -987,6 +1049,12 @@ __device__ __forceinline__ StreamChunk fetch_chunk(const Params& p, const int32_
       c.info = tok | flags | (act << kInfoActShift);
       return c;
     }
+    if constexpr (ROWS != kSequences) {
+      const int2 at = row_page<ROWS>(p, b, s_ppre[b], g, j, s_first[b]);
+      c.pid = at.x;
+      c.info = at.y | flags;
+      return c;
+    }
     const int tok = (j == nb - 1) ? s_tail[b] : (MULTI ? (j == nb - 2 ? min(kPage + s_tail[b], 31) : 31) : kPage);
     // Prompt pages handled by the prompt pass (grouped runs), or pages that no row sees.
     const int pp = MOD ? (MULTI ? s_first[b] : s_ppre[b] / kPage) : MULTI ? 0 : s_ppre[b];
@@ -1005,6 +1073,34 @@ __device__ __forceinline__ int2 seen_keys(const Params& p, int b, int row, int p
   if (p.prefix_lens) hi = max(hi, min(p.prefix_lens[b], L));
   // Rows before token 0 (more rows than tokens) see nothing.
   return pos < 0 || lo >= hi ? make_int2(L, L) : make_int2(lo, hi);
+}
+
+// Query rows as units, with q_start: marks in s_seq every row that begins a sequence's rows
+// with 1 + that sequence, and returns the largest mark before row `lo`, the first of the
+// thread's rows [lo, hi).  (All threads; marks of inconsistent offsets are found out where
+// they are used.)
+__device__ __forceinline__ int rows_before(const Params& p, int32_t* s_seq, int32_t* s_scan, int rows, int cap, int lo, int hi,
+                                           int* bad) {
+  const int tid = threadIdx.x, lane = tid & 63, wave = uni(tid >> 6);
+  for (int i = tid; i < rows; i += kThreads) s_seq[i] = 0;
+  __syncthreads();
+  for (int b = tid; b < p.batch; b += kThreads) {
+    const int q0 = p.q_start[b], q1 = p.q_start[b + 1], L = p.seq_lens[b];
+    const bool ok = q0 >= 0 && q0 <= q1 && q1 <= p.total_q;
+    if (!ok || L < 0 || L > cap || q1 - q0 > L) *bad = 1;
+    if (ok && q0 < q1) atomicMax(&s_seq[q0], b + 1);
+  }
+  __syncthreads();
+  int most = 0;
+  for (int i = lo; i < hi; ++i) most = max(most, s_seq[i]);
+  const int incl = wave_scan_max(most);
+  int before = __shfl_up(incl, 1);
+  if (lane == 0) before = 0;
+  if (lane == 63) s_scan[wave] = incl;
+  __syncthreads();
+  for (int w = 0; w < wave; ++w) before = max(before, s_scan[w]);
+  __syncthreads();   // s_scan is used again
+  return before;
 }
 
 // ---------------------------------------------------------------- whole segments
@@ -1026,7 +1122,8 @@ __device__ __forceinline__ int2 seen_keys(const Params& p, int b, int row, int p
 // running a stream that ends with a NaN again without remainders instead cost 0.4 us a
 // call in the check alone.)
 //   MOD: modified scores; the segment's pages are the sequence's from token `lo`'s on.
-template <class Pol, bool MOD>
+//   ROWS: b is a query row that sees `tail` tokens of sequence `lo`.
+template <class Pol, bool MOD, RowsForm ROWS>
 __device__ __forceinline__ void whole_segment(const Params& p, int b, int g, int nb, int tail,
                                               float (*sacc)[16][Pol::kD + 4], float (*sml)[16][2], int lo, float slope) {
   constexpr int D = Pol::kD, kDepth = Pol::kDepth;
@@ -1034,7 +1131,11 @@ __device__ __forceinline__ void whole_segment(const Params& p, int b, int g, int
   const int j0 = nb * wave / kWaves, j1 = nb * (wave + 1) / kWaves;
   const int first = MOD ? lo / kPage : 0;
   const int32_t* bt = p.block_table + (int64_t)b * p.max_pages + first;
-  int pid = j0 < j1 ? bt[j0 + min(lane, j1 - j0 - 1)] : -1;
+  int2 row_at = make_int2(-1, 0);
+  if constexpr (ROWS != kSequences) {
+    if (j0 < j1) row_at = row_page<ROWS>(p, b, lo, g, j0 + min(lane, j1 - j0 - 1), tail);
+  }
+  int pid = ROWS != kSequences ? row_at.x : j0 < j1 ? bt[j0 + min(lane, j1 - j0 - 1)] : -1;
   Pol st;
   st.setup(p, lane, p.stride_slot);
   typename Pol::QOp qo;
@@ -1046,7 +1147,12 @@ __device__ __forceinline__ void whole_segment(const Params& p, int b, int g, int
   }
   for (int cb = j0; cb < j1; cb += kChunk) {
     const int cn = min(kChunk, j1 - cb);
-    if (cb > j0) pid = bt[cb + min(lane, cn - 1)];
+    if constexpr (ROWS != kSequences) {
+      if (cb > j0) row_at = row_page<ROWS>(p, b, lo, g, cb + min(lane, cn - 1), tail);
+      pid = row_at.x;
+    } else {
+      if (cb > j0) pid = bt[cb + min(lane, cn - 1)];
+    }
     typename Pol::Frag fr[kDepth];
     float skm[kDepth], svm[kDepth];
     int sval[kDepth];
@@ -1059,7 +1165,10 @@ __device__ __forceinline__ void whole_segment(const Params& p, int b, int g, int
           pk = -1;
         }
       }
-      val = pk < 0 ? 0 : (cb + k == nb - 1 ? tail : kPage);
+      if constexpr (ROWS != kSequences)
+        val = pk < 0 ? 0 : __builtin_amdgcn_readlane(row_at.y, k & (kChunk - 1));
+      else
+        val = pk < 0 ? 0 : (cb + k == nb - 1 ? tail : kPage);
       const int64_t po = (pk >= 0) ? (int64_t)pk * p.stride_page + (int64_t)g * p.stride_head : 0;
       const uint32_t nrec = val > 0 ? (uint32_t)((val - 1) * p.stride_slot + D * Pol::kEB) : 0u;
       ks = 1.f;
@@ -1083,7 +1192,8 @@ __device__ __forceinline__ void whole_segment(const Params& p, int b, int g, int
           if constexpr (MOD)
             st.compute_mod(p, fr[k], nullptr, lane, sval[k] > 0, p.scale_log2 * skm[k], svm[k]);
           else
-            st.template compute<false, kAlways>(fr[k], lane, sval[k], p.scale_log2 * skm[k], svm[k]);
+            st.template compute<false, kAlways, ROWS == kWeighed>(fr[k], lane, sval[k], p.scale_log2 * skm[k], svm[k]);
+          if constexpr (ROWS == kWeighed) st.put_page(p, b, g, cb + i + k, lane);
         }
       }
     }
@@ -1112,6 +1222,9 @@ __device__ __forceinline__ void whole_segment(const Params& p, int b, int g, int
 #pragma unroll
       for (int e = 0; e < 4; ++e) o[c + e] += a * v[e];
     }
+  }
+  if constexpr (ROWS == kWeighed) {
+    if (d0 == 0) store_row_lse(p, b, s_qhead[g * p.group + h], M, Ls);
   }
   store_out<D, DPT>(p, b, s_qhead[g * p.group + h], d0, o, Ls > 0.f ? 1.f / Ls : 0.f);
 }
@@ -1152,10 +1265,15 @@ struct PromptState<Pol, false> {
 // MOD: modified scores (rl_decode_attn_run_scored): a cap, a bias by distance, and the keys
 // of every row an interval.  The pages below every row's interval are left out of the list
 // before it is cut; inside it each row's interval is carried relative to the page.
-template <class Pol, bool MULTI = false, int NT = 1, bool PACK = false, bool PROMPT = false, int WPE = 1, bool MOD = false>
+// ROWS: the units are query rows, each with the pages that it lists for the KV head
+// (rl_decode_attn_run_selected: min(its pages, budget) places of the list), or all of its
+// pages, whose parts of the softmax are kept (rl_decode_attn_run_weighed).
+template <class Pol, bool MULTI = false, int NT = 1, bool PACK = false, bool PROMPT = false, int WPE = 1, bool MOD = false,
+          RowsForm ROWS = kSequences>
 __global__ __attribute__((amdgpu_flat_work_group_size(kThreads, kThreads), amdgpu_waves_per_eu(WPE, WPE)))
 void decode_attention_kernel(const Params p) {
   static_assert(!MOD || !(PACK || PROMPT), "modified scores: plain and multi-token rows");
+  static_assert(ROWS == kSequences || !(MULTI || PACK || PROMPT || MOD), "query rows as units: plain scores");
   static_assert(NT == 1 || (MULTI && NT == 2), "two row tiles only for multi-token rows");
   static_assert(!PACK || MULTI, "packed grouped runs use the multi-token row machinery");
   static_assert(!(PACK && NT == 2), "packed grouped runs hold one tile");
@@ -1167,6 +1285,7 @@ void decode_attention_kernel(const Params p) {
   static_assert(!(PROMPT && (MULTI || PACK)), "the prompt-pass state belongs to plain grouped launches");
   static_assert(WPE == 1 || (WPE == 2 && !MULTI && !PACK && !PROMPT), "two waves per SIMD: plain runs only");
   constexpr int kB = WPE == 2 ? kTwoWgMaxBatch
+                     : ROWS != kSequences ? kRowsMax
                      : PACK   ? kPackMaxBatch
                      : NT == 2 ? (MOD ? kScoredTwoTileMaxBatch : kTwoTileMaxBatch)
                                : (MOD && MULTI ? kScoredMaxBatch : kMaxBatch);
@@ -1177,7 +1296,8 @@ void decode_attention_kernel(const Params p) {
   // (q_start[b] << 5) | n_b.  Packed grouped runs: (first member << 5) | members.
   // Modified scores, one row a sequence: the first token it sees.
   __shared__ int32_t s_ppre[kB];
-  __shared__ int32_t s_first[MOD && MULTI ? kB : 1];   // modified scores: the first page that a row sees
+  // Query rows as units: s_ppre holds a row's sequence (-1: none), s_first the tokens it sees.
+  __shared__ int32_t s_first[(MOD && MULTI) || ROWS != kSequences ? kB : 1];   // modified scores: the first page that a row sees
   __shared__ float s_slope[MOD ? kMaxQHeads : 1];      // ... bias a token of every query head, in log2 units
   // Packed grouped runs: pages of each sequence, and the clamped prompt pages of each group.
   __shared__ uint16_t s_nfull[PACK ? kB : 1];
@@ -1210,7 +1330,7 @@ void decode_attention_kernel(const Params p) {
   auto chunk_of_info = [](int info) { return PACK ? 0 : (info >> kInfoChunkShift) & 3; };
 
   // Units of the flattened list: sequences, or packs (packed grouped runs).
-  const int nunits = PACK ? p.pack_units : batch;
+  const int nunits = PACK ? p.pack_units : ROWS != kSequences ? p.total_q : batch;
   // Packed grouped runs whose groups are aligned runs of the lanes (a power-of-two
   // group size up to 64 dividing the batch, a power-of-two pack size dividing it,
   // at most one sequence per thread): the group clamps and the pack sums are
@@ -1310,7 +1430,35 @@ void decode_attention_kernel(const Params p) {
       const int per = (nunits + kThreads - 1) / kThreads;
       const int lo = min(tid * per, nunits), hi = min(lo + per, nunits);
       int sum = 0, cnt = 0, most = 0, bad = 0;   // pages, non-empty units, the largest unit
+      int seq_at = 0;   // query rows as units: 1 + the sequence of the last row before b
+      if constexpr (ROWS != kSequences) {
+        if (p.q_start) seq_at = rows_before(p, s_ppre, s_scan, nunits, cap, lo, hi, &bad);
+      }
       for (int b = lo; b < hi; ++b) {
+        if constexpr (ROWS != kSequences) {
+          int seq = b, L;
+          if (p.q_start) {
+            seq_at = max(seq_at, s_ppre[b]);
+            seq = seq_at - 1;
+            const int q0 = seq >= 0 ? p.q_start[seq] : 0, q1 = seq >= 0 ? p.q_start[seq + 1] : 0;
+            if (b < q0 || b >= q1 || q1 > p.total_q) seq = -1;
+            L = seq >= 0 ? min(max(p.seq_lens[seq], 0), cap) - (q1 - 1 - b) : 0;
+          } else {
+            L = p.seq_lens[b];
+            if (L < 0 || L > cap) bad = 1;
+            L = min(L, cap);
+          }
+          L = max(L, 0);   // (a row before token 0 sees nothing)
+          int n = (L + kPage - 1) / kPage;
+          if constexpr (ROWS == kListed) n = min(n, p.budget);
+          s_ppre[b] = seq;
+          s_first[b] = L;
+          s_pre[b + 1] = n;
+          sum += n;
+          cnt += n > 0;
+          most = max(most, n);
+          continue;
+        }
         if constexpr (PACK) {
           // Pack b: members b0 .. b0 + np - 1 of group i; the prompt once, then each member's own pages.
           const int gs = p.group_size, P = p.pack, ppg = (gs + P - 1) / P;
@@ -1416,6 +1564,9 @@ void decode_attention_kernel(const Params p) {
   //    normalised prompt-pass result when the prompt is the whole sequence.
   for (int b = blockIdx.x; b < nunits; b += W) {
     if (s_pre[b + 1] != s_pre[b]) continue;
+    if constexpr (ROWS != kSequences) {
+      if (s_ppre[b] < 0) continue;   // a row of no sequence
+    }
     if constexpr (MULTI) {
       // Rows of a sequence with no keys (none, or rows claimed past an empty cache).
       const int nq = s_ppre[b] & 31, q0 = s_ppre[b] >> 5;
@@ -1430,7 +1581,7 @@ void decode_attention_kernel(const Params p) {
       continue;
     }
     const int n = p.num_q_heads * D;
-    const bool prompt = !MOD && s_ppre[b] > 0;
+    const bool prompt = !MOD && ROWS == kSequences && s_ppre[b] > 0;
     for (int e = tid; e < n; e += kThreads) {
       float v = 0.f;
       if (prompt) {
@@ -1489,8 +1640,8 @@ void decode_attention_kernel(const Params p) {
     const int gv = u - wunit * Hs, pre = uni(s_pre[wunit]), nb = uni(s_pre[wunit + 1]) - pre;
     if constexpr (!MULTI && !PROMPT) {
       if (nb > 0)
-        whole_segment<Pol, MOD>(p, wunit, gv, nb, uni(s_tail[wunit]), s_acc, s_ml, MOD ? uni(s_ppre[wunit]) : 0,
-                                row_slope(gv, lane & 15));
+        whole_segment<Pol, MOD, ROWS>(p, wunit, gv, nb, uni(ROWS != kSequences ? s_first[wunit] : s_tail[wunit]), s_acc, s_ml,
+                                      MOD || ROWS != kSequences ? uni(s_ppre[wunit]) : 0, row_slope(gv, lane & 15));
       return;
     }
     r0 = Hs * pre + gv * nb;
@@ -1562,11 +1713,12 @@ void decode_attention_kernel(const Params p) {
     // The unit of a chunk's last position bounds the units of the next chunk from below.
     auto unit_of_info = [](int info) { return (info >> kInfoSeqShift) & (PACK ? 4095 : 8191); };
     auto fetch = [&](int base, int hint) {
-      return base < w1 ? fetch_chunk<MULTI, PACK, MOD>(p, s_pre, s_tail, s_ppre, s_nfull, s_gpp, s_first, nunits, base, w0,
+      return base < w1 ? fetch_chunk<MULTI, PACK, MOD, ROWS>(p, s_pre, s_tail, s_ppre, s_nfull, s_gpp, s_first, nunits, base, w0,
                                                        w1, lane, Hs, nrc, hint)
                        : StreamChunk{-1, 0};
     };
     bool began = false;   // the segment being accumulated began inside this quarter
+    int jpage = 0;        // kWeighed: the page within it
     StreamChunk cur = fetch(w0, wunit), nxt = {-1, 0};
     if constexpr (kIdsWaited) {
       if (cn > kChunk) nxt = fetch(w0 + kChunk, unit_of_info(__builtin_amdgcn_readlane(cur.info, kChunk - 1)));
@@ -1716,6 +1868,13 @@ void decode_attention_kernel(const Params p) {
             st.template compute_with<true>(f, &vo, lane, info & kInfoTok, p.scale_log2 * km, vm, exact);
             st2.template compute_with<true>(f, &vo, lane, info & kInfoTok, p.scale_log2 * km, vm, exact);
           }
+        } else if constexpr (ROWS == kWeighed) {
+          if (info & (kInfoFirst | kInfoStart)) {
+            const int pre = s_pre[b];
+            jpage = w0 + k - Hs * pre - g * (s_pre[b + 1] - pre);
+          }
+          st.template compute<false, kByCall, true>(f, lane, info & kInfoTok, p.scale_log2 * km, vm, exact);
+          st.put_page(p, b, g, jpage++, lane);
         } else
           st.compute(f, lane, info & kInfoTok, p.scale_log2 * km, vm, exact);
         if (info & (kInfoLast | kInfoEnd)) {
@@ -1726,7 +1885,7 @@ void decode_attention_kernel(const Params p) {
               st.write_out_multi(p, s_ppre[b] >> 5, s_ppre[b] & 31, g, rb, lane);
               if constexpr (NT == 2) st2.write_out_multi(p, s_ppre[b] >> 5, s_ppre[b] & 31, g, rb + 16, lane);
             } else {
-              st.write_out(p, b, g, lane);
+              st.template write_out<ROWS == kWeighed>(p, b, g, lane);
             }
           } else {
             const int slot = 2 * wave + (ended ? 0 : 1);
@@ -1824,6 +1983,9 @@ void decode_attention_kernel(const Params p) {
       const bool whole = seg_start >= r0 && seg_end <= r1;
       if (h < seg_rows(b, g)) {
         if (whole) {
+          if constexpr (ROWS == kWeighed) {
+            if (d0 == 0) store_row_lse(p, out_row(b, g), qh_cur, M, Ls);
+          }
           store_out<D, DPT>(p, out_row(b, g), qh_cur, d0, o, Ls > 0.f ? 1.f / Ls : 0.f);
         } else {
           const PartialRsrc rs = PartialRsrc::of<D>(p);
@@ -1897,17 +2059,18 @@ void decode_attention_kernel(const Params p) {
     const int pre_b = s_pre[b], nb = s_pre[b + 1] - pre_b;
     const int64_t seg_start = (int64_t)Hs * pre_b + (int64_t)g * nb;
     if (h < seg_rows(b, g))
-      merge_pieces<D, DPT>(p, out_row(b, g), out_head(g), h, d0, owner_of(cost_of(seg_start, b, g), Wn, C),
+      merge_pieces<D, DPT, ROWS == kWeighed>(p, out_row(b, g), out_head(g), h, d0, owner_of(cost_of(seg_start, b, g), Wn, C),
                            owner_of(cost_of(seg_start + nb - 1, b, g), Wn, C));
     if (tid == 0) atomicExch(p.counters + sgi, 0u);
   }
 }
 
-template <class Pol, bool MULTI = false, int NT = 1, bool PACK = false, bool PROMPT = false, int WPE = 1, bool MOD = false>
+template <class Pol, bool MULTI = false, int NT = 1, bool PACK = false, bool PROMPT = false, int WPE = 1, bool MOD = false,
+          RowsForm ROWS = kSequences>
 int launch(const Params& p, void* stream, void* ev_begin, void* ev_end) {
   hipStream_t st = (hipStream_t)stream;
   if (ev_begin && hipEventRecord((hipEvent_t)ev_begin, st) != hipSuccess) return -1;
-  hipLaunchKernelGGL((decode_attention_kernel<Pol, MULTI, NT, PACK, PROMPT, WPE, MOD>), dim3(p.nranges), dim3(kThreads),
+  hipLaunchKernelGGL((decode_attention_kernel<Pol, MULTI, NT, PACK, PROMPT, WPE, MOD, ROWS>), dim3(p.nranges), dim3(kThreads),
                      0, st, p);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return (int)e;

@@ -444,9 +444,127 @@ rlda_status multi_impl(rl_decode_attn_t h, const rl_decode_attn_scores* scores, 
   return RLDA_OK;
 }
 
+// Query rows as units: the pages they list, or (`weigh`) all with the pages' weights.
+rlda_status rows_impl(rl_decode_attn_t h, bool weigh, int32_t batch, int32_t num_pages, int32_t total_q, int32_t budget,
+                      const int32_t* pages, const int32_t* counts, float* weights, float decay, const void* q,
+                      const void* k_cache, const void* v_cache, const float* k_scale, const float* v_scale,
+                      const int32_t* block_table, const int32_t* seq_lens, const int32_t* q_start, void* out, void* workspace,
+                      size_t workspace_bytes, void* stream, void* event_begin, void* event_end) {
+  if (!h || (!event_begin) != (!event_end)) return RLDA_ERR_INVALID_ARG;
+  const rl_decode_attn_config& c = h->cfg;
+  if (batch < 0 || batch > c.max_batch || num_pages < 0 || total_q < 0) return RLDA_ERR_INVALID_ARG;
+  if (!q_start && total_q != batch) return RLDA_ERR_INVALID_ARG;
+  if (!weigh && budget < 1) return RLDA_ERR_INVALID_ARG;
+  if (weigh && !(decay >= 0.f && decay <= 1.f)) return RLDA_ERR_INVALID_ARG;
+  if (total_q > rlda::kRowsMax) return RLDA_ERR_UNSUPPORTED;
+  // The kernel numbers (row, KV head, page) units in 32-bit integers, as it does sequences.
+  const int64_t most = weigh ? c.max_pages_per_seq : std::min(budget, c.max_pages_per_seq);
+  if ((int64_t)total_q * (most + rlda::kStartCost) * c.num_kv_heads > INT32_MAX) return RLDA_ERR_UNSUPPORTED;
+  if (batch == 0 || total_q == 0) return RLDA_OK;
+  if (!q || !block_table || !seq_lens || !out) return RLDA_ERR_INVALID_ARG;
+  if (weigh ? !weights : !pages || !counts) return RLDA_ERR_INVALID_ARG;
+  if (num_pages > 0 && (!k_cache || !v_cache)) return RLDA_ERR_INVALID_ARG;
+  if (!aligned16(q) || !aligned16(k_cache) || !aligned16(v_cache) || !aligned16(out)) return RLDA_ERR_INVALID_ARG;
+  if (((uintptr_t)block_table & 3u) || ((uintptr_t)seq_lens & 3u) || ((uintptr_t)q_start & 3u) || ((uintptr_t)pages & 3u) ||
+      ((uintptr_t)counts & 3u) || ((uintptr_t)weights & 3u))
+    return RLDA_ERR_INVALID_ARG;
+  const bool fp8 = h->kind == rlda::KvKind::FP8;
+  if (fp8 && num_pages > 0 && (!k_scale || !v_scale || ((uintptr_t)k_scale & 3u) || ((uintptr_t)v_scale & 3u)))
+    return RLDA_ERR_INVALID_ARG;
+  const WsLayout wl = layout_of(h);
+  const rlda::WeighedLayout ww = rlda::weighed_layout(h, total_q);
+  if (!workspace || ((uintptr_t)workspace % kAlign)) return RLDA_ERR_WORKSPACE;
+  if (workspace_bytes < (weigh ? ww.total : wl.total)) return RLDA_ERR_WORKSPACE;
+
+  int dev = 0;
+  if (hipGetDevice(&dev) != hipSuccess) return RLDA_ERR_HIP;
+  // Workgroups as in a plain run (run_impl).
+  const bool half_pages = fp8 || (h->kind == rlda::KvKind::BF16 && c.head_dim == 64);
+  const bool two = half_pages && total_q <= rlda::kTwoWgMaxBatch;
+  int ranges = c.num_work_ranges;
+  if (ranges == 0) {
+    ranges = cu_count(dev);
+    if (ranges <= 0) return RLDA_ERR_HIP;
+    if (two) ranges *= 2;
+  }
+  ranges = std::min(std::min(ranges, h->ws_ranges), rlda::kMaxRanges);
+  const int64_t max_units = (int64_t)total_q * c.num_kv_heads * most;
+  if (ranges > max_units) ranges = (int)max_units;
+
+  char* ws = (char*)workspace;
+  rlda::Params p;
+  memset(&p, 0, sizeof p);
+  p.q = q;
+  p.k = k_cache;
+  p.v = v_cache;
+  p.k_scale = k_scale;
+  p.v_scale = v_scale;
+  p.block_table = block_table;
+  p.seq_lens = seq_lens;
+  p.q_start = q_start;
+  p.total_q = total_q;
+  p.out = out;
+  p.flags = (uint32_t*)(ws + wl.flags);
+  p.counters = (uint32_t*)(ws + wl.counters);
+  p.call_tag = next_call_tag();
+  p.part_ml = (float*)(ws + wl.part_ml);
+  p.part_acc = (float*)(ws + wl.part_acc);
+  p.part_rows = h->group;
+  const int eb = elem_bytes(c.kv_dtype);
+  p.stride_page = h->stride_page * eb;
+  p.stride_head = h->stride_head * eb;
+  p.stride_slot = (int32_t)(h->stride_slot * eb);
+  p.batch = batch;
+  p.num_pages = num_pages;
+  p.num_q_heads = c.num_q_heads;
+  p.num_kv_heads = c.num_kv_heads;
+  p.group = h->group;
+  p.max_pages = c.max_pages_per_seq;
+  p.nranges = ranges;
+  p.inv_ranges = c.num_work_ranges > 0 ? 0.f : 1.0f / (float)ranges;
+  p.scale_log2 = h->scale * 1.4426950408889634f;
+  p.out_bf16 = c.out_dtype == RLDA_BF16;
+  memcpy(p.q_head, h->q_head, sizeof p.q_head);
+  p.list = pages;
+  p.list_counts = counts;
+  p.budget = budget;
+  p.weights = weights;
+  p.decay = decay;
+  p.page_lse = (float*)(ws + ww.page_lse);
+  p.row_lse = (float*)(ws + ww.row_lse);
+  auto* const launch = weigh ? rlda::launch_weighed : rlda::launch_selected;
+  return launch(h->kind, c.head_dim, h->group, two, p, stream, event_begin, event_end) == hipSuccess ? RLDA_OK : RLDA_ERR_HIP;
+}
+
 }  // namespace
 
 extern "C" {
+
+rlda_status rl_decode_attn_run_selected(rl_decode_attn_t h, int32_t batch, int32_t num_pages, int32_t total_q, int32_t budget,
+                                        const int32_t* pages, const int32_t* counts, const void* q, const void* k_cache,
+                                        const void* v_cache, const float* k_scale, const float* v_scale,
+                                        const int32_t* block_table, const int32_t* seq_lens, const int32_t* q_start,
+                                        void* out, void* workspace, size_t workspace_bytes, void* stream, void* event_begin,
+                                        void* event_end) {
+  return rows_impl(h, false, batch, num_pages, total_q, budget, pages, counts, nullptr, 0.f, q, k_cache, v_cache, k_scale, v_scale,
+                   block_table, seq_lens, q_start, out, workspace, workspace_bytes, stream, event_begin, event_end);
+}
+
+rlda_status rl_decode_attn_weighed_workspace_size(rl_decode_attn_t h, int32_t total_q, size_t* bytes) {
+  if (!h || !bytes || total_q < 0) return RLDA_ERR_INVALID_ARG;
+  if (total_q > rlda::kRowsMax) return RLDA_ERR_UNSUPPORTED;
+  *bytes = rlda::weighed_layout(h, total_q).total;
+  return RLDA_OK;
+}
+
+rlda_status rl_decode_attn_run_weighed(rl_decode_attn_t h, int32_t batch, int32_t num_pages, int32_t total_q, float* weights,
+                                       float decay, const void* q, const void* k_cache, const void* v_cache,
+                                       const float* k_scale, const float* v_scale, const int32_t* block_table,
+                                       const int32_t* seq_lens, const int32_t* q_start, void* out, void* workspace,
+                                       size_t workspace_bytes, void* stream, void* event_begin, void* event_end) {
+  return rows_impl(h, true, batch, num_pages, total_q, 0, nullptr, nullptr, weights, decay, q, k_cache, v_cache, k_scale, v_scale,
+                   block_table, seq_lens, q_start, out, workspace, workspace_bytes, stream, event_begin, event_end);
+}
 
 rlda_status rl_decode_attn_run(rl_decode_attn_t h, int32_t batch, int32_t num_pages, const void* q,
                                const void* k_cache, const void* v_cache, const float* k_scale,

@@ -394,3 +394,141 @@ rlda_status rl_decode_attn_page_copy(rl_decode_attn_t h, int32_t num_pages, int3
 }
 
 }  // extern "C"
+
+// ---------------------------------------------------------------- bounds, choice, eviction
+
+namespace {
+
+using rlda::SelectParams;
+
+void set_select(rl_decode_attn_t h, SelectParams& p) {
+  const rl_decode_attn_config& c = h->cfg;
+  memset(&p, 0, sizeof p);
+  p.max_pages = c.max_pages_per_seq;
+  p.num_q_heads = c.num_q_heads;
+  p.num_kv_heads = c.num_kv_heads;
+  p.group = h->group;
+  memcpy(p.q_head, h->q_head, sizeof p.q_head);
+}
+
+bool budget_ok(int32_t budget, int32_t sink, int32_t recent) {
+  return sink >= 0 && recent >= 1 && (int64_t)sink + recent <= budget;
+}
+
+// Workgroups of a choice: several to a (row, KV head) while that leaves CUs idle, none with
+// less than kPiecePages of the longest sequence there may be.
+constexpr int kWantedChoices = 512, kPiecePages = 512;
+
+}  // namespace
+
+extern "C" {
+
+rlda_status rl_decode_attn_page_bounds(rl_decode_attn_t h, int32_t batch, int32_t num_pages, const void* k_cache,
+                                       const float* k_scale, const int32_t* block_table, const int32_t* seq_lens,
+                                       const int32_t* first, int8_t* bounds, float* bound_scale, void* workspace,
+                                       size_t workspace_bytes, void* stream) {
+  if (!h) return RLDA_ERR_INVALID_ARG;
+  const rl_decode_attn_config& c = h->cfg;
+  if (batch < 0 || batch > c.max_batch || num_pages < 0) return RLDA_ERR_INVALID_ARG;
+  if (batch == 0) return RLDA_OK;
+  if (!block_table || !seq_lens || !aligned4(block_table) || !aligned4(seq_lens) || !aligned4(first)) return RLDA_ERR_INVALID_ARG;
+  if (num_pages > 0 && (!k_cache || !bounds || !bound_scale)) return RLDA_ERR_INVALID_ARG;
+  if (!aligned16(k_cache) || !aligned16(bounds) || !aligned4(bound_scale)) return RLDA_ERR_INVALID_ARG;
+  if (h->kind == rlda::KvKind::FP8 && num_pages > 0 && (!k_scale || !aligned4(k_scale))) return RLDA_ERR_INVALID_ARG;
+  const rlda::WsLayout wl = rlda::layout_of(h);
+  if (!workspace || ((uintptr_t)workspace % kAlign)) return RLDA_ERR_WORKSPACE;
+  if (workspace_bytes < wl.total) return RLDA_ERR_WORKSPACE;
+  SelectParams p;
+  set_select(h, p);
+  p.k = k_cache;
+  p.k_scale = k_scale;
+  p.bounds = bounds;
+  p.bound_scale = bound_scale;
+  p.block_table = const_cast<int32_t*>(block_table);
+  p.seq_lens = const_cast<int32_t*>(seq_lens);
+  p.first = first;
+  p.flags = (uint32_t*)((char*)workspace + wl.flags);
+  const int eb = elem_bytes(c.kv_dtype);
+  p.stride_page = h->stride_page * eb;
+  p.stride_head = h->stride_head * eb;
+  p.stride_slot = (int32_t)(h->stride_slot * eb);
+  p.batch = batch;
+  p.num_pages = num_pages;
+  return rlda::launch_page_bounds(h->kind, c.head_dim, p, stream) == hipSuccess ? RLDA_OK : RLDA_ERR_HIP;
+}
+
+rlda_status rl_decode_attn_select_pages(rl_decode_attn_t h, int32_t batch, int32_t num_pages, int32_t total_q, int32_t budget,
+                                        int32_t sink, int32_t recent, const void* q, const int8_t* bounds,
+                                        const float* bound_scale, const int32_t* block_table, const int32_t* seq_lens,
+                                        const int32_t* q_start, int32_t* pages, int32_t* counts, void* workspace,
+                                        size_t workspace_bytes, void* stream) {
+  if (!h) return RLDA_ERR_INVALID_ARG;
+  const rl_decode_attn_config& c = h->cfg;
+  if (batch < 0 || batch > c.max_batch || num_pages < 0 || total_q < 0) return RLDA_ERR_INVALID_ARG;
+  if (!q_start && total_q != batch) return RLDA_ERR_INVALID_ARG;
+  if (!budget_ok(budget, sink, recent)) return RLDA_ERR_INVALID_ARG;
+  if (c.max_pages_per_seq > rlda::kSelectMaxPages) return RLDA_ERR_UNSUPPORTED;
+  if (batch == 0 || total_q == 0) return RLDA_OK;
+  if (!q || !block_table || !seq_lens || !pages || !counts || !aligned16(q)) return RLDA_ERR_INVALID_ARG;
+  if (!aligned4(block_table) || !aligned4(seq_lens) || !aligned4(q_start) || !aligned4(pages) || !aligned4(counts))
+    return RLDA_ERR_INVALID_ARG;
+  if (num_pages > 0 && (!bounds || !bound_scale)) return RLDA_ERR_INVALID_ARG;
+  if (!aligned16(bounds) || !aligned4(bound_scale)) return RLDA_ERR_INVALID_ARG;
+  const rlda::WsLayout wl = rlda::layout_of(h);
+  if (!workspace || ((uintptr_t)workspace % kAlign)) return RLDA_ERR_WORKSPACE;
+  if (workspace_bytes < wl.total) return RLDA_ERR_WORKSPACE;
+  SelectParams p;
+  set_select(h, p);
+  p.q = q;
+  p.bounds = const_cast<int8_t*>(bounds);
+  p.bound_scale = const_cast<float*>(bound_scale);
+  p.block_table = const_cast<int32_t*>(block_table);
+  p.seq_lens = const_cast<int32_t*>(seq_lens);
+  p.q_start = q_start;
+  p.pages = pages;
+  p.counts = counts;
+  char* ws = (char*)workspace;
+  p.flags = (uint32_t*)(ws + wl.flags);
+  p.counters = (uint32_t*)(ws + wl.counters);
+  p.keys = (uint32_t*)(ws + wl.part_acc);   // where an attention call keeps its partial results
+  p.batch = batch;
+  p.num_pages = num_pages;
+  p.total_q = total_q;
+  p.budget = budget;
+  p.sink = sink;
+  p.recent = recent;
+  const int64_t segs = (int64_t)total_q * c.num_kv_heads;
+  p.pieces = 1;
+  if (segs <= (int64_t)rlda::counters_of(h) && segs * c.max_pages_per_seq * (int64_t)sizeof(uint32_t) <= (int64_t)(wl.total - wl.part_acc))
+    p.pieces = (int)std::max<int64_t>(std::min<int64_t>(kWantedChoices / segs, c.max_pages_per_seq / kPiecePages), 1);
+  if (segs * p.pieces * 512 > (1ll << 32) - 1) return RLDA_ERR_UNSUPPORTED;   // threads of a launch
+  return rlda::launch_select_pages(c.q_dtype == RLDA_F32, c.head_dim, p, stream) == hipSuccess ? RLDA_OK : RLDA_ERR_HIP;
+}
+
+rlda_status rl_decode_attn_page_evict(rl_decode_attn_t h, int32_t batch, int32_t num_pages, int32_t* refs,
+                                      int32_t* block_table, int32_t* seq_lens, float* weights, int32_t budget, int32_t sink,
+                                      int32_t recent, int32_t* dropped, void* workspace, size_t workspace_bytes, void* stream) {
+  PageParams pp;
+  const rlda_status st = page_call(h, batch, num_pages, refs, block_table, seq_lens, workspace, workspace_bytes, pp);
+  if (st != RLDA_OK) return st;
+  if (!budget_ok(budget, sink, recent)) return RLDA_ERR_INVALID_ARG;
+  if (h->cfg.max_pages_per_seq > rlda::kSelectMaxPages) return RLDA_ERR_UNSUPPORTED;
+  if (batch == 0) return RLDA_OK;
+  if (!weights || !dropped || !aligned4(weights) || !aligned4(dropped)) return RLDA_ERR_INVALID_ARG;
+  SelectParams p;
+  set_select(h, p);
+  p.refs = refs;
+  p.block_table = block_table;
+  p.seq_lens = seq_lens;
+  p.weights = weights;
+  p.dropped = dropped;
+  p.flags = pp.flags;
+  p.batch = batch;
+  p.num_pages = num_pages;
+  p.budget = budget;
+  p.sink = sink;
+  p.recent = recent;
+  return rlda::launch_page_evict(p, stream) == hipSuccess ? RLDA_OK : RLDA_ERR_HIP;
+}
+
+}  // extern "C"

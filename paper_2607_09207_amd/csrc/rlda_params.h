@@ -101,6 +101,14 @@ struct Params {
   const int32_t* prefix_lens;  // [batch] or null
   uint32_t group_magic;        // floor(i / group) = umulhi(i, group_magic) for i < 2^24, group > 1
   int16_t q_head[kMaxQHeads];  // q_head[g * G + i] = i-th query head of KV head g
+  // Query rows as units (rl_decode_attn_run_selected, rl_decode_attn_run_weighed).
+  const int32_t* list;         // [rows][Hkv][budget] indices of the sequence's pages
+  const int32_t* list_counts;  // [rows][Hkv]
+  float* page_lse;             // [rows][Hq][max_pages] log2 of a page's sum of exp2(score)
+  float* row_lse;              // [rows][Hq] ... and of the row's
+  float* weights;              // [batch][max_pages]
+  float decay;
+  int32_t budget;
 };
 
 constexpr int kRotaryWindow = 16;   // rows of a workgroup's window at most (rlda_rotary.hip)
@@ -196,6 +204,11 @@ int launch_scored(KvKind kind, int head_dim, bool two, const Params& p, void* st
 int launch_scored_rows(KvKind kind, int head_dim, int tiles, const Params& p, void* stream, void* ev_begin, void* ev_end);
 int launch_scored_multi(KvKind kind, int head_dim, bool small, const Params& p, int grid, void* stream, void* ev_begin,
                         void* ev_end);
+// Query rows as units (rlda_listed.hip): over the listed pages; over all pages with their weights.
+int launch_selected(KvKind kind, int head_dim, int group, bool two, const Params& p, void* stream, void* ev_begin,
+                    void* ev_end);
+int launch_weighed(KvKind kind, int head_dim, int group, bool two, const Params& p, void* stream, void* ev_begin,
+                   void* ev_end);
 // KV append: one wave per (sequence, KV head) and cache; one for both where they are one.
 int launch_append(KvKind kind, int head_dim, const Params& p, void* stream);
 // Device address of the static scratch on the current device (kScratchBytes bytes),
@@ -234,8 +247,40 @@ constexpr int kPackMaxPages = 32767;   // ... pages per sequence (16-bit LDS ent
 constexpr int kTwoWgMaxBatch = 512;      // two workgroups per CU (fp8, bf16 d = 64 decode): per-sequence LDS tables of this size
 constexpr int kScoredMaxBatch = 4096;    // multi-token rows with modified scores: one more table
 constexpr int kScoredTwoTileMaxBatch = 1024;   // ... in two tiles
+constexpr int kRowsMax = 4096;           // query rows as units: per-row LDS tables of this size
 constexpr int kTwoTileMaxBatch = 2048;   // two-tile multi-token rows: per-sequence LDS tables of this size
                                          // leave room for 32-row merge slots
+
+// Bounds of the keys of pages, the choice of pages by them, and eviction (rlda_select.hip).
+constexpr int kSelectMaxPages = 32768;   // pages of a row: a choice holds their keys in LDS
+struct SelectParams {
+  const void* q;               // choice: [rows][Hq][D]
+  const void* k;               // bounds: the K pool, as in Params
+  const float* k_scale;
+  int8_t* bounds;              // [num_pages][Hkv][2][D]: the lower bounds, the upper ones
+  float* bound_scale;          // [num_pages][Hkv]
+  int32_t* block_table;        // [batch][max_pages]
+  int32_t* seq_lens;           // [batch]
+  const int32_t* q_start;      // [batch + 1], or null: one row a sequence
+  const int32_t* first;        // bounds: [batch] first token that may be new, or null: the last
+  int32_t* pages;              // choice: [rows][Hkv][budget]
+  int32_t* counts;             // choice: [rows][Hkv]
+  uint32_t* keys;              // choice, cut: [rows * Hkv][max_pages] order keys
+  uint32_t* counters;          // ... [rows * Hkv] finished pieces, zero between calls
+  float* weights;              // eviction: [batch][max_pages]
+  int32_t* refs;               // ... [num_pages]
+  int32_t* dropped;            // ... [batch]
+  uint32_t* flags;
+  int64_t stride_page, stride_head;   // bytes
+  int32_t stride_slot;                // bytes
+  int32_t batch, total_q, num_pages, max_pages, num_q_heads, num_kv_heads, group;
+  int32_t budget, sink, recent;
+  int32_t pieces;              // choice: workgroups of a (row, KV head)
+  int16_t q_head[kMaxQHeads];
+};
+int launch_page_bounds(KvKind kind, int head_dim, const SelectParams& p, void* stream);
+int launch_select_pages(bool q_f32, int head_dim, const SelectParams& p, void* stream);
+int launch_page_evict(const SelectParams& p, void* stream);
 
 // Rotary positions (rlda_rotary.hip).
 int launch_rotate(bool f32, const RotaryParams& p, void* stream);

@@ -1,0 +1,933 @@
+"""A cache read in part and kept in part (page_bounds, select_pages, selected, weighed, page_evict)
+on the GPU.
+
+Bounds, choices and evictions are compared exactly: bounds are quotients of fp32 numbers rounded
+to whole ones (one IEEE division and a floor or ceiling on both sides), a choice's scores are
+whole numbers below 2^24 times two fp32 factors in one order.
+
+Tolerance of an attention output o = sum_t p_t v_t, with A = sum_t p_t |v_t|: every p_t is off by a
+factor that has
+  - the error of its score: the product of d terms accumulated in fp32, d 2^-24 of |q| |k| scale,
+    and 2^-21 of the score for the log2 units; twice, for the maximum's too;
+  - the exponential's 2^-21, the sum's n 2^-24 (n terms of one sign) and the product's n 2^-24;
+  - its rounding to bf16, 2^-8 (f32 caches: none).
+A bf16 output adds half a step, 2^-8 |o|.  A page's weight has the scores' errors, the
+exponentials', twice the sums', and half a step, 2^-24, of the two logarithms (times ln 2), of
+the additions over the rows and heads (one of each, all of one sign) and of the update (two).
+"""
+import math
+
+import numpy as np
+import pytest
+
+pytestmark = pytest.mark.gpu
+
+PAGE = 16
+NAN = {"bf16": 0x7FC0, "fp8": 0x7F, "f32": 0x7FC00000}
+
+
+@pytest.fixture(scope="module")
+def torch():
+    import torch
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    from paper_2607_09207_amd import _abi
+    _abi.load()
+    return torch
+
+
+def raw_type(torch, kv):
+    return {"bf16": torch.int16, "fp8": torch.uint8, "f32": torch.int32}[kv]
+
+
+class Case:
+    """Sequences on a pool of their own; slots past their ends, and pages nobody uses, hold NaN."""
+
+    def __init__(self, torch, kv, hq, hkv, d, lens, rows=None, layout="head", seed=0, out="f32", ranges=0, max_batch=None,
+                 extra_pages=0, head_map=None, spare=2):
+        from paper_2607_09207_amd import DecodeAttention
+        self.torch, self.kv, self.hq, self.hkv, self.d, self.G = torch, kv, hq, hkv, d, hq // hkv
+        rng = np.random.default_rng(seed)
+        g = self.gen = torch.Generator("cuda").manual_seed(seed)
+        self.lens = np.asarray(lens, np.int64)
+        self.rows = np.ones(len(lens), np.int64) if rows is None else np.asarray(rows, np.int64)
+        self.start = np.concatenate([[0], np.cumsum(self.rows)])
+        self.used = -(-self.lens // PAGE)
+        self.mp = int(max(1, self.used.max() if len(lens) else 1)) + extra_pages
+        self.npages = int(self.used.sum()) + spare
+        perm = rng.permutation(self.npages)
+        self.table = np.full((len(lens), self.mp), -1, np.int32)
+        at = 0
+        for b, u in enumerate(self.used):
+            self.table[b, :u] = perm[at:at + u]
+            at += u
+        qd = torch.float32 if kv == "f32" else torch.bfloat16
+        self.q = (torch.randn((int(self.start[-1]), hq, d), device="cuda", generator=g) * 2).to(qd)
+        shape = (self.npages, hkv, PAGE, d) if layout == "head" else (self.npages, PAGE, hkv, d)
+        view = (lambda t: t) if layout == "head" else (lambda t: t.transpose(1, 2))
+
+        def pool():
+            x = torch.randn(shape, device="cuda", generator=g)
+            if kv != "fp8":
+                return view(x.to(qd)), None
+            s = torch.rand((self.npages, hkv), device="cuda", generator=g) * 0.02 + 0.005
+            sx = s[:, :, None, None] if layout == "head" else s[:, None, :, None]
+            return view((x / sx).clamp(-448, 448).to(torch.float8_e4m3fn)), s
+        (self.k, self.ks), (self.v, self.vs) = pool(), pool()
+        spare = np.ones((self.npages, PAGE), bool)
+        for b, L in enumerate(self.lens):
+            for j in range(self.used[b]):
+                spare[self.table[b, j], :min(PAGE, L - j * PAGE)] = False
+        for t in (self.k, self.v):
+            t.view(raw_type(torch, kv)).transpose(1, 2)[torch.from_numpy(spare).cuda()] = NAN[kv]
+        self.block_table = torch.from_numpy(self.table).cuda()
+        self.seq_lens = torch.from_numpy(self.lens.astype(np.int32)).cuda()
+        self.q_start = None if rows is None else torch.from_numpy(self.start.astype(np.int32)).cuda()
+        self.kv_of = [h // self.G for h in range(hq)] if head_map is None else head_map
+        self.layer = DecodeAttention(hq, hkv, d, max_batch or max(len(lens), 1), self.mp, qd,
+                                     {"bf16": "bf16", "fp8": "fp8_e4m3fn", "f32": "f32"}[kv], out, kv_head_of_q=head_map,
+                                     kv_strides=self.k.stride()[:3], num_work_ranges=ranges)
+        self.bounds = torch.full((self.npages, hkv, 2, d), 55, dtype=torch.int8, device="cuda")
+        self.bscale = torch.full((self.npages, hkv), -3.0, device="cuda")
+
+    def cache(self):
+        return self.k, self.v, self.block_table, self.seq_lens
+
+    def scales(self):
+        return dict(k_scale=self.ks, v_scale=self.vs)
+
+    def make_bounds(self, first=None, **kw):
+        self.layer.page_bounds(self.k, self.block_table, self.seq_lens, self.bounds, self.bscale, first=first,
+                               k_scale=self.ks, **kw)
+
+    def all_bounds(self):
+        self.make_bounds(first=self.torch.zeros(len(self.lens), dtype=self.torch.int32, device="cuda"))
+
+    def values(self, t, s, page):
+        """Page `page` of a cache, [Hkv][16][d] in fp32."""
+        x = t[page].contiguous()
+        x = x.view(raw_type(self.torch, self.kv)).view(t.dtype).float()
+        return x if s is None else x * s[page][:, None, None]
+
+    def select(self, budget, **kw):
+        return self.layer.select_pages(self.q, self.bounds, self.bscale, self.block_table, self.seq_lens, budget,
+                                       q_start=self.q_start, **kw)
+
+    def attend(self, pages, counts, **kw):
+        return self.layer.selected(self.q, *self.cache(), pages, counts, q_start=self.q_start, **self.scales(), **kw)
+
+    def weigh(self, weights, **kw):
+        return self.layer.weighed(self.q, *self.cache(), weights, q_start=self.q_start, **self.scales(), **kw)
+
+    def row_list(self):
+        """(row, sequence, tokens it sees)."""
+        return [(int(self.start[b]) + i, b, int(L) - int(n) + i + 1) for b, (L, n) in enumerate(zip(self.lens, self.rows))
+                for i in range(int(n))]
+
+    def flags(self, ws=None):
+        self.torch.cuda.synchronize()
+        return self.layer.read_flags(device="cuda:0") if ws is None else self.layer.read_flags(workspace=ws)
+
+    # The attention of every row over the keys in keys[row][g], in float64: outputs, their tolerances,
+    # and per row the probabilities [Hq][tokens] with their factors of error.
+    def want(self, keys):
+        torch, d = self.torch, self.d
+        n = self.q.shape[0]
+        o = torch.zeros((n, self.hq, d), dtype=torch.float64, device="cuda")
+        tol, parts = torch.zeros_like(o), {}
+        for r, b, L in self.row_list():
+            if L <= 0:
+                continue
+            pages = [self.values(self.k, self.ks, int(p)) for p in self.table[b, :-(-L // PAGE)]]
+            k = torch.cat(pages, dim=1)[:, :L].double()
+            v = torch.cat([self.values(self.v, self.vs, int(p)) for p in self.table[b, :-(-L // PAGE)]], dim=1)[:, :L].double()
+            kv = torch.tensor(self.kv_of, device="cuda")
+            k, v, q = k[kv].contiguous(), v[kv].contiguous(), self.q[r].double()       # [Hq][L][d], [Hq][d]
+            x = (k * q[:, None]).sum(-1) / math.sqrt(d)
+            seen = torch.zeros((self.hq, L), device="cuda", dtype=torch.float64)      # how often a key counts
+            for h in range(self.hq):
+                for j in keys(r, self.kv_of[h], L):
+                    seen[h, j * PAGE:(j + 1) * PAGE] += 1
+            err = d * 2.0 ** -24 * q.norm(dim=-1)[:, None] * k.norm(dim=-1) / math.sqrt(d) + 2.0 ** -21 * x.abs()
+            err = torch.where(seen > 0, err, 0.0).amax(-1, keepdim=True)
+            x = x.masked_fill(seen == 0, -math.inf)
+            top = x.amax(-1, keepdim=True)
+            top = torch.where(top.isfinite(), top, 0.0)
+            e = torch.exp(x - top) * seen
+            z = e.sum(-1, keepdim=True)
+            p = torch.where(z > 0, e / z.clamp_min(1e-300), 0.0)
+            o[r] = (p[:, :, None] * v).sum(1)
+            a = (p[:, :, None] * v.abs()).sum(1)
+            f = 2 * err + 2.0 ** -20 + 2 * L * 2.0 ** -24
+            tol[r] = a * (f + (0.0 if self.kv == "f32" else 2.0 ** -8))
+            logs = (top.abs() / math.log(2) + (L + 1.0) ** 0.5) * 2.0 ** -23      # |log2 of sums| of 1 to L terms, and of pages
+            small = torch.log2(p.clamp_min(1e-38)).abs() * 2.0 ** -23
+            parts[r] = (p, f + logs + small)
+        return o, tol, parts
+
+    def check(self, got, o, tol, out="f32"):
+        if out == "bf16":
+            tol = tol + 2.0 ** -8 * o.abs()
+        bad = ~((got.double() - o).abs() <= tol + 1e-30)
+        assert not bad.any(), (int(bad.sum()), float(((got.double() - o).abs() / (tol + 1e-30))[bad].max()))
+
+
+LAYOUTS = [("bf16", 28, 4, 128), ("fp8", 40, 8, 128), ("bf16", 12, 2, 64), ("fp8", 16, 1, 64), ("bf16", 3, 3, 128),
+           ("f32", 4, 4, 128), ("f32", 4, 2, 64)]
+
+
+# ---------------------------------------------------------------- bounds
+
+def over_127(x):
+    """The quotient, rounded once (a number as the divisor would be a product with its reciprocal)."""
+    return x / x.new_full(x.shape, 127)
+
+
+def plain_bounds(torch, x):
+    """x [Hkv][tokens][d] fp32: (bounds [Hkv][2][d], scale [Hkv])."""
+    if not bool(x.isfinite().all()):
+        odd = ~x.isfinite().flatten(1).all(-1)
+    else:
+        odd = torch.zeros(x.shape[0], dtype=torch.bool, device=x.device)
+    y = torch.where(odd[:, None, None], 0.0, x)
+    s = over_127(y.abs().amax(dim=(1, 2)))
+    by = torch.where(s > 0, s, 1.0)[:, None]
+    zero = (s == 0)[:, None]
+    lo = torch.where(zero, 0.0, (y.amin(1) / by).floor().clamp_min(-127))
+    hi = torch.where(zero, 0.0, (y.amax(1) / by).ceil().clamp_max(127))
+    return torch.stack([lo, hi], 1).to(torch.int8), torch.where(odd, math.inf, s)
+
+
+def expect_bounds(c, first, b0, s0):
+    want, scale = b0.clone(), s0.clone()
+    for b, L in enumerate(c.lens):
+        L = int(L)
+        if L == 0:
+            continue
+        j0 = (L - 1) // PAGE if first is None else first[b] // PAGE
+        for j in range(j0, -(-L // PAGE)):
+            page = int(c.table[b, j])
+            x = c.values(c.k, c.ks, page)[:, :min(PAGE, L - j * PAGE)]
+            want[page], scale[page] = plain_bounds(c.torch, x)
+    return want, scale
+
+
+@pytest.mark.parametrize("layout", ["head", "slot"])
+@pytest.mark.parametrize("kv,hq,hkv,d", LAYOUTS)
+def test_bounds(torch, kv, hq, hkv, d, layout):
+    c = Case(torch, kv, hq, hkv, d, [1, 0, 15, 16, 17, 250, 33, 700], layout=layout, seed=d + hq)
+    for first in (None, [0] * 8, [1, 0, 3, 16, 16, 100, 32, 511]):
+        b0, s0 = c.bounds.clone(), c.bscale.clone()
+        c.make_bounds(None if first is None else torch.tensor(first, dtype=torch.int32, device="cuda"))
+        want, scale = expect_bounds(c, first, b0, s0)
+        torch.cuda.synchronize()
+        assert torch.equal(c.bounds, want) and torch.equal(c.bscale, scale), first
+    # s lo <= k <= s hi, up to the roundings of s and of a quotient below 128.
+    for b, L in enumerate(c.lens):
+        for j in range(c.used[b]):
+            page = int(c.table[b, j])
+            x = c.values(c.k, c.ks, page)[:, :min(PAGE, int(L) - j * PAGE)].double()
+            s = c.bscale[page].double()[:, None]
+            lo, hi = c.bounds[page, :, 0].double() * s, c.bounds[page, :, 1].double() * s
+            slack = 128 * 2.0 ** -22 * s
+            assert (x.amin(1) >= lo - slack).all() and (x.amax(1) <= hi + slack).all()
+    assert c.flags() == 0
+
+
+@pytest.mark.parametrize("kv,hq,hkv,d", [("bf16", 8, 2, 128), ("fp8", 8, 2, 64), ("f32", 2, 2, 64)])
+def test_bounds_of_odd_keys(torch, kv, hq, hkv, d):
+    """Zeros, the type's largest values, infinities and NaN; an fp8 page's scale that is negative,
+    0, infinite."""
+    c = Case(torch, kv, hq, hkv, d, [PAGE * 6], seed=3)
+    t = [int(x) for x in c.table[0]]
+    c.k[t[0]] = 0
+    c.k.view(raw_type(torch, kv))[t[1], 0, 5, 7] = NAN[kv]
+    if kv != "fp8":
+        c.k[t[2], 1, 3, 0] = math.inf
+        c.k[t[3], 0, 0, 1] = -math.inf
+        c.k[t[4], 0, 2, 2] = torch.finfo(c.k.dtype).max
+        c.k[t[4], 0, 2, 3] = -torch.finfo(c.k.dtype).max
+        c.k[t[5], 0] = -0.0
+    else:
+        c.ks[t[2], 0], c.ks[t[3], 0], c.ks[t[4], 1], c.ks[t[5], 0] = -0.01, 0.0, math.inf, 1e38
+    c.all_bounds()
+    want, scale = expect_bounds(c, [0], c.bounds, c.bscale)
+    torch.cuda.synchronize()
+    assert torch.equal(c.bscale, scale) and torch.equal(c.bounds, want)
+    assert c.bscale[t[1], 0] == math.inf and c.bscale[t[1], 1] < math.inf and c.flags() == 0
+
+
+def test_bounds_of_wrong_tables(torch):
+    c = Case(torch, "bf16", 8, 2, 64, [40, 50, 60], seed=4)
+    c.block_table[0, 1], c.block_table[1, 3] = -7, c.npages
+    c.seq_lens[2] = PAGE * c.mp + 1
+    b0 = c.bounds.clone()
+    c.all_bounds()
+    assert c.flags() == 3
+    for page in c.table[2][:4]:
+        assert torch.equal(c.bounds[int(page)], b0[int(page)])
+    c = Case(torch, "bf16", 8, 2, 64, [40, 50, 60], seed=4)
+    c.make_bounds(torch.tensor([-1, 51, 60], dtype=torch.int32, device="cuda"))
+    assert c.flags() == 2
+
+
+# ---------------------------------------------------------------- choice
+
+def plain_choice(c, budget, sink, recent):
+    """Pages of every (row, KV head), in Python floats and fp32 factors."""
+    torch, d = c.torch, c.d
+    pages = np.full((c.q.shape[0], c.hkv, budget), -1, np.int32)
+    counts = np.zeros((c.q.shape[0], c.hkv), np.int32)
+    q = c.q.float()
+    fine = q.isfinite().all(-1, keepdim=True)
+    q = torch.where(fine, q, 0.0)
+    sq = over_127(q.abs().amax(-1, keepdim=True))
+    q8 = torch.where(sq > 0, (q / torch.where(sq > 0, sq, 1.0)).round(), 0.0).double()
+    for r, b, L in c.row_list():
+        n = max(-(-L // PAGE), 0)
+        page = torch.from_numpy(c.block_table[b, :n].cpu().numpy().astype(np.int64)).cuda()
+        there = (page >= 0) & (page < c.npages)
+        page = torch.where(there, page, 0)
+        for g in range(c.hkv):
+            heads = [h for h in range(c.hq) if c.kv_of[h] == g]
+            lo, hi = c.bounds[page, g, 0].double(), c.bounds[page, g, 1].double()     # [n][d]
+            s = c.bscale[page, g]
+            u = torch.stack([(torch.maximum(q8[r, h] * lo, q8[r, h] * hi)).sum(-1).float() * sq[r, h] for h in heads]).amax(0)
+            x = torch.where(s.isfinite(), u * s, math.inf)
+            x = torch.where(there, x, -math.inf).cpu().numpy()
+            kept = [j for j in range(n) if j < sink or j >= n - recent]
+            rest = sorted((j for j in range(n) if j not in set(kept)), key=lambda j: (-x[j], j))
+            got = sorted(kept + rest[:max(budget - len(kept), 0)]) if n > budget else list(range(n))
+            pages[r, g, :len(got)] = got
+            counts[r, g] = len(got)
+    return pages, counts
+
+
+@pytest.mark.parametrize("budget,sink,recent", [(1, 0, 1), (4, 1, 2), (16, 4, 4), (16, 8, 8), (40, 0, 1), (100, 1, 1)])
+@pytest.mark.parametrize("kv,hq,hkv,d", LAYOUTS)
+def test_choice(torch, kv, hq, hkv, d, budget, sink, recent):
+    c = Case(torch, kv, hq, hkv, d, [1, 0, 16, 17, 250, 64, 1000, 790], seed=budget + d)
+    c.all_bounds()
+    pages, counts = c.select(budget, sink=sink, recent=recent)
+    want_pages, want_counts = plain_choice(c, budget, sink, recent)
+    torch.cuda.synchronize()
+    assert np.array_equal(counts.cpu().numpy(), want_counts)
+    assert np.array_equal(pages.cpu().numpy(), want_pages)
+    assert c.flags() == 0
+
+
+@pytest.mark.parametrize("kv,hq,hkv,d", [("bf16", 28, 4, 128), ("fp8", 8, 1, 64), ("f32", 4, 4, 64)])
+def test_choice_of_several_rows(torch, kv, hq, hkv, d):
+    rows = [3, 0, 1, 5, 17, 0, 40, 2]
+    c = Case(torch, kv, hq, hkv, d, [300, 0, 1, 5, 400, 31, 700, 33], rows, seed=7, max_batch=300)
+    c.all_bounds()
+    pages, counts = c.select(12, sink=1, recent=2)
+    want_pages, want_counts = plain_choice(c, 12, 1, 2)
+    torch.cuda.synchronize()
+    assert np.array_equal(counts.cpu().numpy(), want_counts) and np.array_equal(pages.cpu().numpy(), want_pages)
+    assert c.flags() == 0
+
+
+@pytest.mark.parametrize("n,max_pages,rows", [(5000, 5000, 1), (700, 9000, 1), (2600, 2600, 3), (20000, 32768, 1)])
+def test_choice_of_long_rows(torch, n, max_pages, rows):
+    """Cut over several workgroups; tables beyond what the small form holds."""
+    c = Case(torch, "bf16", 4, 1, 64, [PAGE * n - 3, 900], [rows, rows], seed=n, extra_pages=max_pages - n)
+    g = torch.Generator("cuda").manual_seed(1)
+    c.bounds.copy_(torch.randint(-127, 128, c.bounds.shape, device="cuda", generator=g, dtype=torch.int8).sort(dim=2).values)
+    c.bscale.copy_(torch.rand(c.bscale.shape, device="cuda", generator=g))
+    for budget in (64, 1000):
+        pages, counts = c.select(budget, sink=2, recent=3)
+        want_pages, want_counts = plain_choice(c, budget, 2, 3)
+        torch.cuda.synchronize()
+        assert np.array_equal(counts.cpu().numpy(), want_counts) and np.array_equal(pages.cpu().numpy(), want_pages)
+    assert c.flags() == 0
+
+
+def test_choice_with_ties_and_odd_values(torch):
+    """Equal scores go to the lower page, zeros of both signs are equal; pages that are not
+    finite come first, pages outside the pool last; a query that is not finite says nothing."""
+    c = Case(torch, "bf16", 8, 2, 64, [PAGE * 50, PAGE * 50, PAGE * 50, PAGE * 50], seed=9)
+    c.all_bounds()
+    same = c.table[0, 5:40:3]
+    c.bounds[torch.from_numpy(same.astype(np.int64)).cuda()] = c.bounds[int(same[0])].clone()
+    c.bscale[torch.from_numpy(same.astype(np.int64)).cuda()] = c.bscale[int(same[0])].clone()
+    c.bounds[torch.from_numpy(c.table[1].astype(np.int64)).cuda()] = 0           # scores of 0 and -0
+    c.bscale[int(c.table[2, 20]), 0] = math.inf
+    c.bscale[int(c.table[2, 31]), 0] = math.nan
+    c.q[2, 0, 3], c.q[3, 5, 0] = math.nan, math.inf
+    c.block_table[3, 7] = c.npages
+    c.block_table[3, 8] = -1
+    for budget in (8, 13, 20, 49):
+        pages, counts = c.select(budget, sink=1, recent=2)
+        want_pages, want_counts = plain_choice(c, budget, 1, 2)
+        torch.cuda.synchronize()
+        assert np.array_equal(counts.cpu().numpy(), want_counts) and np.array_equal(pages.cpu().numpy(), want_pages)
+    assert {20, 31} <= set(c.select(5, sink=0, recent=1)[0][2, 0].tolist())
+    assert c.flags() == 1
+
+
+def test_choice_head_map_and_outputs(torch):
+    head_map = [2, 0, 1, 1, 0, 2, 2, 0, 1]
+    c = Case(torch, "bf16", 9, 3, 128, [900, 40], seed=10, head_map=head_map)
+    c.all_bounds()
+    out = (torch.full((2, 3, 7), 99, dtype=torch.int32, device="cuda"), torch.full((2, 3), 99, dtype=torch.int32, device="cuda"))
+    got = c.select(7, sink=1, recent=1, out=out)
+    want_pages, want_counts = plain_choice(c, 7, 1, 1)
+    assert got[0] is out[0] and got[1] is out[1]
+    assert np.array_equal(out[0].cpu().numpy(), want_pages) and np.array_equal(out[1].cpu().numpy(), want_counts)
+
+
+def test_rows_of_no_sequence(torch):
+    """Rows before the first and behind the last sequence's, and of a sequence whose offsets
+    disagree, are left as they were, by the choice and by both attentions."""
+    c = Case(torch, "bf16", 8, 2, 64, [100, 50, 80], [2, 3, 4], seed=11)
+    c.all_bounds()
+    c.q = torch.cat([c.q, c.q])[:14].contiguous()
+    for starts, live, flags in (([2, 4, 7, 11], set(range(2, 11)), 0), ([0, 2, 20, 11], {0, 1}, 2), ([-3, 2, 5, 9], set(range(2, 9)), 2)):
+        qs = torch.tensor(starts, dtype=torch.int32, device="cuda")
+        out = (torch.full((14, 2, 4), 99, dtype=torch.int32, device="cuda"), torch.full((14, 2), 99, dtype=torch.int32, device="cuda"))
+        c.q_start = qs
+        c.select(4, out=out)
+        assert c.flags() == flags
+        written = {r for r in range(14) if bool((out[1][r] != 99).all())}
+        assert written == live and all(bool((out[0][r] == 99).all()) for r in range(14) if r not in live), starts
+        lists = out[0].clamp(-1, 3), out[1].clamp(0, 4)
+        o = torch.full((14, 8, 64), 7.0, device="cuda")
+        c.attend(*lists, out=o)
+        assert {r for r in range(14) if not bool((o[r] == 7).all())} == live
+        w = torch.zeros((3, c.mp), device="cuda")
+        o.fill_(7.0)
+        ws = torch.zeros(c.layer.weighed_workspace(14, "cuda").numel(), dtype=torch.uint8, device="cuda")
+        c.weigh(w, out=o, workspace=ws)
+        assert {r for r in range(14) if not bool((o[r] == 7).all())} == live and c.flags(ws) == flags
+        c.layer._ws.clear()
+    # More rows than tokens: those before token 0 choose nothing and give zeros.
+    c = Case(torch, "bf16", 8, 2, 64, [2, 50], [5, 1], seed=12)
+    c.all_bounds()
+    pages, counts = c.select(4)
+    assert counts[:, 0].tolist() == [0, 0, 0, 1, 1, 4] and bool((pages[:3] == -1).all()) and c.flags() == 2
+    o = c.attend(pages, counts)
+    assert bool((o[:3] == 0).all()) and bool((o[3:] != 0).any(-1).all())
+
+
+# ---------------------------------------------------------------- attention over the chosen pages
+
+def random_lists(c, budget, seed, full=False):
+    rng = np.random.default_rng(seed)
+    pages = rng.integers(-5, 1000, size=(c.q.shape[0], c.hkv, budget)).astype(np.int32)   # beyond the counts: anything
+    counts = np.zeros((c.q.shape[0], c.hkv), np.int32)
+    for r, _, L in c.row_list():
+        n = max(-(-L // PAGE), 0)
+        for g in range(c.hkv):
+            m = min(n, budget) if full else int(rng.integers(0, min(n, budget) + 1))
+            pages[r, g, :m] = rng.permutation(n)[:m] if rng.random() < 0.5 else np.sort(rng.permutation(n)[:m])
+            counts[r, g] = m
+    return pages, counts
+
+
+@pytest.mark.parametrize("out", ["f32", "bf16"])
+@pytest.mark.parametrize("ranges", [0, 7, 300])
+@pytest.mark.parametrize("kv,hq,hkv,d", LAYOUTS)
+def test_selected(torch, kv, hq, hkv, d, ranges, out):
+    if kv == "f32" and out == "bf16":
+        pytest.skip("f32 layers give f32")
+    c = Case(torch, kv, hq, hkv, d, [1, 0, 16, 17, 250, 1500, 33, 640], seed=hq + d, out=out, ranges=ranges)
+    for budget, full in ((1, True), (9, False), (40, False), (120, True)):
+        pages, counts = random_lists(c, budget, budget, full)
+        got = c.attend(torch.from_numpy(pages).cuda(), torch.from_numpy(counts).cuda())
+        o, tol, _ = c.want(lambda r, g, L: pages[r, g, :counts[r, g]])
+        torch.cuda.synchronize()
+        c.check(got, o, tol, out)
+    assert c.flags() == 0
+
+
+@pytest.mark.parametrize("kv,hq,hkv,d,layout", [("bf16", 28, 4, 128, "slot"), ("fp8", 40, 8, 64, "head"), ("f32", 2, 1, 64, "slot")])
+def test_selected_of_several_rows(torch, kv, hq, hkv, d, layout):
+    rows = [3, 0, 1, 5, 17, 0, 30, 2]
+    c = Case(torch, kv, hq, hkv, d, [300, 0, 1, 5, 400, 31, 700, 33], rows, seed=7, layout=layout, max_batch=9)
+    pages, counts = random_lists(c, 11, 3)
+    got = c.attend(torch.from_numpy(pages).cuda(), torch.from_numpy(counts).cuda())
+    o, tol, _ = c.want(lambda r, g, L: pages[r, g, :counts[r, g]])
+    torch.cuda.synchronize()
+    c.check(got, o, tol)
+    assert c.flags() == 0
+
+
+def test_selected_many_rows(torch):
+    """As many rows as a call may have, of two sequences."""
+    c = Case(torch, "bf16", 4, 2, 64, [2500, 2000], [2300, 1796], seed=8)
+    pages, counts = random_lists(c, 3, 4)
+    got = c.attend(torch.from_numpy(pages).cuda(), torch.from_numpy(counts).cuda())
+    torch.cuda.synchronize()
+    full = c.attend(torch.from_numpy(pages).cuda(), torch.from_numpy(counts).cuda())
+    assert torch.equal(got, full)
+    keep = np.random.default_rng(0).permutation(4096)[:60]
+    rows = [x for x in c.row_list() if x[0] in set(keep.tolist())]
+    c.row_list = lambda: rows
+    o, tol, _ = c.want(lambda r, g, L: pages[r, g, :counts[r, g]])
+    pick = torch.tensor(sorted(keep.tolist()), device="cuda")
+    c.check(got[pick], o[pick], tol[pick])
+    assert c.flags() == 0
+
+
+def test_selected_everything_is_the_plain_attention(torch):
+    for kv, hq, hkv, d in LAYOUTS:
+        c = Case(torch, kv, hq, hkv, d, [1, 0, 100, 700, 3000], seed=5)
+        n = int(c.used.max())
+        pages = torch.arange(n, dtype=torch.int32, device="cuda").expand(5, hkv, n).contiguous()
+        counts = torch.from_numpy(np.repeat(c.used[:, None], hkv, 1).astype(np.int32)).cuda()
+        plain = c.layer(c.q, *c.cache(), **c.scales())
+        assert torch.equal(c.attend(pages, counts), plain)   # the same stream, cuts and sums
+
+
+def test_selected_twice_the_same_page_and_bad_entries(torch):
+    c = Case(torch, "bf16", 8, 2, 64, [200, 200, 200, 200], seed=6)
+    pages = torch.tensor([[3, 3, 7, 1], [0, 1, 2, 3], [5, -1, 6, 0], [2, 13, 4, 1 << 30]], dtype=torch.int32, device="cuda")
+    pages = pages[:, None].expand(4, 2, 4).contiguous()
+    counts = torch.tensor([4, -5, 4, 1 << 20], dtype=torch.int32, device="cuda")[:, None].expand(4, 2).contiguous()
+    got = c.attend(pages, counts)
+    seen = {0: [3, 3, 7, 1], 1: [], 2: [5, 6, 0], 3: [2, 4]}
+    o, tol, _ = c.want(lambda r, g, L: seen[r])
+    c.check(got, o, tol)
+    assert c.flags() == 1 and bool((got[1] == 0).all())
+
+
+def test_selected_keys_that_are_not_listed_have_no_part(torch):
+    """NaN and infinities in every other page, and behind a row's own position."""
+    for kv in ("bf16", "fp8", "f32"):
+        c = Case(torch, kv, 4, 2, 64, [330, 150], [3, 2], seed=13)
+        pages, counts = random_lists(c, 6, 1)
+        listed = {(b, int(j)) for r, b, _ in c.row_list() for g in range(2) for j in pages[r, g, :counts[r, g]]}
+        for b in range(2):
+            for j in range(c.used[b]):
+                if (b, j) not in listed:
+                    for t in (c.k, c.v):
+                        t.view(raw_type(torch, kv))[int(c.table[b, j])] = NAN[kv]
+        o, tol, _ = c.want(lambda r, g, L: pages[r, g, :counts[r, g]])
+        o, tol = torch.zeros_like(o), torch.zeros_like(tol)
+        got = c.attend(torch.from_numpy(pages).cuda(), torch.from_numpy(counts).cuda())
+        assert bool(got.isfinite().all())
+        # The last token of each sequence is seen by its last row alone.
+        for b in range(2):
+            L = int(c.lens[b])
+            for t in (c.k, c.v):
+                t.view(raw_type(torch, kv))[int(c.table[b, (L - 1) // PAGE]), :, (L - 1) % PAGE] = NAN[kv]
+        again = c.attend(torch.from_numpy(pages).cuda(), torch.from_numpy(counts).cuda())
+        for r, b, L in c.row_list():
+            if L < c.lens[b]:
+                assert torch.equal(again[r], got[r])
+
+
+# ---------------------------------------------------------------- weights
+
+def expect_weights(c, parts, w0, decay):
+    torch = c.torch
+    want, tol = w0.double().clone(), torch.zeros(w0.shape, dtype=torch.float64, device="cuda")
+    for b in range(len(c.lens)):
+        n = int(c.used[b])
+        if n == 0 or c.rows[b] == 0:
+            continue
+        got = torch.zeros(n, dtype=torch.float64, device="cuda")
+        off = torch.zeros_like(got)
+        for r, bb, L in c.row_list():
+            if bb != b or L <= 0:
+                continue
+            p, f = parts[r]
+            pad = lambda x: torch.nn.functional.pad(x.sum(0), (0, n * PAGE - L)).view(n, PAGE).sum(1)   # noqa: E731
+            got += pad(p)
+            off += pad(p * f)
+        want[b, :n] = (w0[b, :n].double() * decay if decay else 0.0) + got
+        tol[b, :n] = off + (int(c.rows[b]) * c.hq + 2) * 2.0 ** -24 * want[b, :n]
+    return want, tol
+
+
+@pytest.mark.parametrize("ranges", [0, 5, 200])
+@pytest.mark.parametrize("kv,hq,hkv,d", LAYOUTS)
+def test_weighed(torch, kv, hq, hkv, d, ranges):
+    c = Case(torch, kv, hq, hkv, d, [1, 0, 16, 17, 250, 1500, 33, 640], seed=hq, ranges=ranges, extra_pages=3)
+    o, tol, parts = c.want(lambda r, g, L: range(-(-L // PAGE)))
+    plain = c.layer(c.q, *c.cache(), **c.scales())
+    for decay in (1.0, 0.9, 0.0):
+        w0 = torch.rand((8, c.mp), device="cuda", generator=c.gen)
+        if decay == 0.0:
+            w0[:] = math.nan   # not read
+        w = w0.clone()
+        got = c.weigh(w, decay=decay)
+        torch.cuda.synchronize()
+        assert torch.equal(got, plain)
+        c.check(got, o, tol)
+        want, wtol = expect_weights(c, parts, w0, decay)
+        for b in range(8):
+            n = int(c.used[b])
+            assert torch.equal(w[b, n:].isnan(), w0[b, n:].isnan()) and torch.equal(w[b, n:].nan_to_num(), w0[b, n:].nan_to_num())
+            bad = ~((w[b, :n].double() - want[b, :n]).abs() <= wtol[b, :n] + 1e-30)
+            assert not bad.any(), (b, float(((w[b, :n] - want[b, :n]).abs() / wtol[b, :n]).max()))
+    assert c.flags(c.layer.weighed_workspace(8, "cuda")) == 0
+
+
+@pytest.mark.parametrize("kv,hq,hkv,d", [("bf16", 28, 4, 128), ("fp8", 8, 1, 64), ("f32", 4, 4, 64)])
+def test_weighed_several_rows(torch, kv, hq, hkv, d):
+    rows = [3, 0, 1, 5, 17, 0, 30, 2]
+    c = Case(torch, kv, hq, hkv, d, [300, 0, 1, 5, 400, 31, 700, 33], rows, seed=17, max_batch=9)
+    o, tol, parts = c.want(lambda r, g, L: range(-(-L // PAGE)))
+    w0 = torch.rand((8, c.mp), device="cuda", generator=c.gen)
+    w = w0.clone()
+    got = c.weigh(w, decay=0.5)
+    torch.cuda.synchronize()
+    c.check(got, o, tol)
+    want, wtol = expect_weights(c, parts, w0, 0.5)
+    assert bool(((w.double() - want).abs() <= wtol + 1e-30).all())
+    assert torch.equal(w[1], w0[1]) and torch.equal(w[5], w0[5])   # no rows, no change
+    # A sequence whose weights add up to its rows' heads.
+    w.zero_()
+    c.weigh(w)
+    total = w.double().sum(1).cpu().numpy()
+    assert np.allclose(total, np.where(c.lens > 0, c.rows * hq, 0), rtol=1e-5)
+
+
+def test_weighed_of_keys_that_are_not_finite(torch):
+    """An infinite score takes the row's whole softmax to NaN, as in plain attention; other
+    sequences' weights stay clean."""
+    c = Case(torch, "bf16", 4, 2, 64, [100, 100], seed=18)
+    c.k[int(c.table[0, 2]), 0, 3, 5] = math.nan
+    w = torch.zeros((2, c.mp), device="cuda")
+    got = c.weigh(w)
+    plain = c.layer(c.q, *c.cache())
+    assert torch.equal(got.isnan(), plain.isnan()) and bool(w[1].isfinite().all())
+    assert abs(float(w[1].sum()) - 4) < 1e-4
+
+
+def test_weighed_repeats_to_the_bit(torch):
+    c = Case(torch, "fp8", 40, 8, 128, [3000, 70, 1200, 5], seed=19)
+    runs = []
+    for _ in range(4):
+        w = torch.zeros((4, c.mp), device="cuda")
+        runs.append((c.weigh(w).clone(), w))
+    assert all(torch.equal(a, runs[0][0]) and torch.equal(b, runs[0][1]) for a, b in runs)
+
+
+# ---------------------------------------------------------------- eviction
+
+class Pool:
+    def __init__(self, torch, pages, mp=64, spare=5, seed=0, shared=0):
+        from paper_2607_09207_amd import DecodeAttention
+        rng = np.random.default_rng(seed)
+        B = len(pages)
+        self.torch = torch
+        self.lens = np.array([0 if n == 0 else (n - 1) * PAGE + rng.integers(1, PAGE + 1) for n in pages], np.int32)
+        self.np = shared + sum(max(n - shared, 0) for n in pages) + spare
+        perm = rng.permutation(self.np)
+        self.table = np.full((B, mp), -1, np.int32)
+        at = shared
+        for b, n in enumerate(pages):
+            self.table[b, :min(n, shared)] = perm[:min(n, shared)]
+            own = max(n - shared, 0)
+            self.table[b, shared:shared + own] = perm[at:at + own]
+            at += own
+        self.refs = np.zeros(self.np, np.int32)
+        for b, n in enumerate(pages):
+            np.add.at(self.refs, self.table[b, :n], 1)
+        self.w = (rng.random((B, mp)) * 10).astype(np.float32)
+        self.layer = DecodeAttention(8, 2, 64, B, mp)
+        self.dev = [torch.from_numpy(x.copy()).cuda() for x in (self.refs, self.table, self.lens, self.w)]
+
+    def evict(self, budget, **kw):
+        refs, table, lens, w = self.dev
+        return self.layer.page_evict(refs, table, lens, w, budget, **kw)
+
+    def expect(self, budget, sink=1, recent=1):
+        refs, table, lens, w = (x.copy() for x in (self.refs, self.table, self.lens, self.w))
+        dropped = np.zeros(len(lens), np.int32)
+        for b, L in enumerate(lens):
+            n = -(-int(L) // PAGE)
+            if n <= budget:
+                continue
+            key = np.where(np.isnan(w[b]), np.inf, w[b])
+            rest = sorted(range(sink, n - recent), key=lambda j: (-key[j], not np.isnan(w[b, j]), j))
+            keep = sorted(list(range(sink)) + rest[:budget - sink - recent] + list(range(n - recent, n)))
+            for j in set(range(n)) - set(keep):
+                refs[table[b, j]] -= 1
+            table[b, :budget], w[b, :budget] = table[b, keep], w[b, keep]
+            w[b, budget:n] = 0
+            lens[b] -= PAGE * (n - budget)
+            dropped[b] = n - budget
+        return refs, table, lens, w, dropped
+
+    def check(self, dropped, want):
+        self.torch.cuda.synchronize()
+        for name, a, b in zip(("refs", "table", "lens", "weights", "dropped"), self.dev + [dropped], want):
+            assert np.array_equal(a.cpu().numpy(), b, equal_nan=name == "weights"), name
+
+
+@pytest.mark.parametrize("budget,sink,recent", [(1, 0, 1), (8, 1, 2), (8, 4, 4), (20, 0, 1), (63, 2, 3)])
+def test_evict(torch, budget, sink, recent):
+    for seed, shared in ((0, 0), (1, 6), (2, 30)):
+        s = Pool(torch, [0, 1, 7, 8, 9, 20, 21, 64, 40, 33], seed=seed, shared=shared)
+        want = s.expect(budget, sink, recent)
+        s.check(s.evict(budget, sink=sink, recent=recent), want)
+        assert s.layer.page_flags(s.np, "cuda") == 0
+
+
+@pytest.mark.parametrize("n,mp", [(1500, 1500), (700, 9000), (12000, 32768)])
+def test_evict_long_rows(torch, n, mp):
+    s = Pool(torch, [n, 3, n - 1], mp=mp, seed=5)
+    s.w[0] = np.round(s.w[0])   # many equal ones
+    s.dev[3].copy_(torch.from_numpy(s.w))
+    for budget in (600, 513):
+        want = s.expect(budget, 4, 100)
+        s.check(s.evict(budget, sink=4, recent=100), want)
+        s.refs, s.table, s.lens, s.w = want[:4]
+
+
+def test_evict_odd_weights(torch):
+    """Ties to the lower page, zeros of both signs alike, NaN and infinities heaviest."""
+    s = Pool(torch, [40, 40, 40], seed=6)
+    s.w[0] = 0.0
+    s.w[0, ::2] = -0.0
+    s.w[1, 5], s.w[1, 9], s.w[1, 11], s.w[1, 30] = math.nan, math.inf, -math.inf, math.nan
+    s.w[2] = -s.w[2]
+    s.dev[3].copy_(torch.from_numpy(s.w))
+    want = s.expect(10, 1, 2)
+    s.check(s.evict(10, sink=1, recent=2), want)
+
+
+def test_evict_wrong_state(torch):
+    """A length out of range leaves its row; dropped ids outside the pool, and pages that nobody
+    holds, are flagged and change no count."""
+    s = Pool(torch, [20, 20, 20], mp=20, seed=7)
+    s.lens[0] = 20 * PAGE + 1
+    s.w[1, :10], s.w[2, :10] = 0, 0   # of these go: all but the first
+    s.table[1, 3] = s.np + 5
+    s.table[2, 4] = -1
+    s.refs[s.table[1, 2]] = 0
+    for i, x in enumerate((s.refs, s.table, s.lens, s.w)):
+        s.dev[i].copy_(torch.from_numpy(x))
+    keep = s.refs.copy()
+    dropped = s.evict(11, sink=1, recent=10)
+    torch.cuda.synchronize()
+    assert dropped.tolist() == [0, 9, 9] and s.layer.page_flags(s.np, "cuda") == 3
+    for b in (1, 2):
+        for j in range(1, 10):
+            if 0 <= s.table[b, j] < s.np and keep[s.table[b, j]] > 0:
+                keep[s.table[b, j]] -= 1
+    assert np.array_equal(s.dev[0].cpu().numpy(), keep)
+    assert np.array_equal(s.dev[1].cpu().numpy()[0], s.table[0]) and s.dev[2].tolist()[0] == 20 * PAGE + 1
+
+
+# ---------------------------------------------------------------- refusals
+
+def test_refusals(torch):
+    from paper_2607_09207_amd import RldaError
+    c = Case(torch, "fp8", 8, 2, 64, [100, 50], seed=20)
+    c.all_bounds()
+    pages, counts = c.select(4)
+    w = torch.zeros((2, c.mp), device="cuda")
+    i32 = dict(dtype=torch.int32, device="cuda")
+    L = c.layer
+    bounds = lambda **kw: L.page_bounds(**dict(dict(k_cache=c.k, block_table=c.block_table, seq_lens=c.seq_lens, bounds=c.bounds,   # noqa: E731
+                                                    bound_scale=c.bscale, k_scale=c.ks), **kw))
+    choose = lambda **kw: L.select_pages(**dict(dict(q=c.q, bounds=c.bounds, bound_scale=c.bscale, block_table=c.block_table,   # noqa: E731
+                                                     seq_lens=c.seq_lens, budget=4), **kw))
+    attend = lambda **kw: L.selected(**dict(dict(q=c.q, k_cache=c.k, v_cache=c.v, block_table=c.block_table, seq_lens=c.seq_lens,   # noqa: E731
+                                                 pages=pages, counts=counts, **c.scales()), **kw))
+    weigh = lambda **kw: L.weighed(**dict(dict(q=c.q, k_cache=c.k, v_cache=c.v, block_table=c.block_table, seq_lens=c.seq_lens,   # noqa: E731
+                                               weights=w, **c.scales()), **kw))
+    short = torch.zeros((2,), **i32)
+    for call, kws in (
+            (bounds, [dict(k_scale=None), dict(bounds=None), dict(bounds=c.bounds[:-1]), dict(bounds=c.bounds.to(torch.uint8)),
+                      dict(bounds=c.bounds[:, :, :, :32]), dict(bound_scale=c.bscale.double()), dict(bound_scale=c.bscale.t()),
+                      dict(first=torch.zeros(3, **i32)), dict(first=torch.zeros(2, device="cuda")), dict(k_cache=c.k.cpu()),
+                      dict(seq_lens=c.seq_lens.long()), dict(workspace=torch.zeros(100, dtype=torch.uint8, device="cuda"))]),
+            (choose, [dict(budget=0), dict(budget=1, sink=1, recent=1), dict(sink=-1), dict(recent=0), dict(budget=4.5), dict(budget=2 ** 31),
+                      dict(q=c.q.float()), dict(q=c.q[:1]), dict(q=c.q.detach().requires_grad_()), dict(q=c.q.cpu()), dict(bounds=None),
+                      dict(bound_scale=None), dict(out=(pages,)), dict(out=(pages[:1], counts)), dict(q_start=torch.zeros((2, 2), **i32)),
+                      dict(q_start=torch.zeros(0, **i32))]),
+            (attend, [dict(pages=None), dict(counts=None), dict(pages=pages[:1]), dict(pages=pages.long()), dict(counts=counts[:, :1]),
+                      dict(counts=short), dict(q=c.q.detach().requires_grad_()), dict(k_cache=None), dict(k_scale=None),
+                      dict(out=torch.zeros(2, 8, 64, device="cuda", dtype=torch.bfloat16)), dict(pages=pages[:, :, :0])]),
+            (weigh, [dict(weights=None), dict(weights=w[:1]), dict(weights=w.double()), dict(decay=-0.1), dict(decay=1.5),
+                     dict(decay=math.nan), dict(weights=w.clone().requires_grad_()), dict(q=c.q.detach().requires_grad_()),
+                     dict(workspace=L.workspace("cuda"))])):
+        for kw in kws:
+            with pytest.raises(RldaError):
+                call(**kw)
+                print(kw)
+    s = Pool(torch, [9, 3], mp=16)
+    refs, table, lens, weights = s.dev
+    for a, kw in (((refs, table, lens, weights, 0), {}), ((refs, table, lens, weights, 4), dict(recent=0)),
+                  ((refs, table, lens, weights[:1], 4), {}), ((refs, table, lens, None, 4), {}),
+                  ((refs, table, lens, weights, 4), dict(dropped=torch.zeros(3, **i32))), ((refs, table, lens, weights, "4"), {}),
+                  ((refs, table, lens, weights.clone().requires_grad_(), 4), {})):
+        with pytest.raises(RldaError):
+            s.layer.page_evict(*a, **kw)
+    torch.cuda.synchronize()
+    assert c.flags() == 0 and np.array_equal(table.cpu().numpy(), s.table)
+    # Empty calls.
+    e = Case(torch, "bf16", 8, 2, 64, [], max_batch=3)
+    e.make_bounds()
+    assert e.select(4)[0].shape == (0, 2, 4)
+    assert e.attend(torch.zeros((0, 2, 4), **i32), torch.zeros((0, 2), **i32)).shape == (0, 8, 64)
+    assert e.weigh(torch.zeros((0, e.mp), device="cuda")).shape == (0, 8, 64)
+
+
+# ---------------------------------------------------------------- calls as they are used
+
+@pytest.mark.parametrize("native", [True, False], ids=["native", "python"])
+def test_native_and_python_paths_agree(torch, native):
+    from paper_2607_09207_amd import _abi
+    got = []
+    for left in (True, False):
+        c = Case(torch, "fp8", 8, 2, 64, [100, 500, 33], seed=21)
+        c.layer.workspace("cuda")
+        c.layer.weighed_workspace(3, "cuda")
+        if left != native:
+            c.layer._fast = _abi.LEFT_TO_PYTHON
+        c.all_bounds()
+        pages, counts = c.select(6)
+        w = torch.zeros((3, c.mp), device="cuda")
+        v = w._version
+        got.append((c.bounds, c.bscale, pages, counts, c.attend(pages, counts), c.weigh(w), w))
+        assert w._version == v + 1
+        s = Pool(torch, [20, 9, 30], seed=1)
+        s.layer.page_workspace(s.np, "cuda")
+        if left != native:
+            s.layer._fast = _abi.LEFT_TO_PYTHON
+        got[-1] += (s.evict(8),) + tuple(s.dev)
+    for a, b in zip(*got):
+        assert torch.equal(a, b)
+
+
+def test_graph(torch):
+    """A step of all of them captured once and replayed, with eager calls of other sizes on the same
+    workspaces between, gives what eager calls give."""
+    c = Case(torch, "bf16", 28, 4, 128, [900, 2000, 64], seed=22, ranges=0)
+    L = c.layer
+    refs = torch.ones(c.npages, dtype=torch.int32, device="cuda")
+    w = torch.zeros((3, c.mp), device="cuda")
+    keep = [t.clone() for t in (c.block_table, c.seq_lens, refs)]
+
+    def step():
+        c.make_bounds()
+        pages, counts = c.select(16, recent=2)
+        o = c.attend(pages, counts)
+        o2 = c.weigh(w, decay=0.5)
+        dropped = L.page_evict(refs, c.block_table, c.seq_lens, w, 100, recent=2)
+        return pages, counts, o, o2, dropped, w, refs, c.block_table, c.seq_lens
+
+    def reset(i):
+        for t, x in zip((c.block_table, c.seq_lens, refs), keep):
+            t.copy_(x)
+        w.zero_()
+        c.q.copy_(torch.randn(c.q.shape, device="cuda", generator=torch.Generator("cuda").manual_seed(i)))
+
+    c.all_bounds()
+    L.workspace("cuda"), L.weighed_workspace(3, "cuda"), L.page_workspace(c.npages, "cuda")
+    reset(0)
+    step()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    reset(0)
+    with torch.cuda.graph(graph):
+        held = step()
+    for i in range(1, 6):
+        reset(i)
+        want = [t.clone() for t in step()]
+        reset(i)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        for a, b in zip(held, want):
+            assert torch.equal(a, b), i
+        c.weigh(torch.zeros_like(w))
+    assert c.flags() == 0
+
+
+def test_other_streams(torch):
+    c = Case(torch, "fp8", 40, 8, 128, [900, 2000, 64], seed=23)
+    c.all_bounds()
+    c.layer.weighed_workspace(3, "cuda")
+    pages, counts = c.select(16)
+    want = c.attend(pages, counts)
+    w0 = torch.zeros((3, c.mp), device="cuda")
+    c.weigh(w0)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    w = torch.zeros((3, c.mp), device="cuda")
+    torch.cuda.synchronize()
+    p, n = c.select(16, stream=side)
+    o = c.attend(p, n, stream=side)
+    c.weigh(w, stream=side.cuda_stream)
+    side.synchronize()
+    assert torch.equal(p, pages) and torch.equal(n, counts) and torch.equal(o, want) and torch.equal(w, w0)
+
+
+def test_a_rollout_that_reads_and_keeps_a_part(torch):
+    """Steps of growth, append with positions, bounds, choice, attention over it, weights and
+    eviction, each against its own plain form on the state as it then is; shared prompt pages go
+    back to the pool when their last holder drops them."""
+    from paper_2607_09207_amd import DecodeAttention, rotary_frequencies
+    torch.manual_seed(0)
+    B, hq, hkv, d, mp, npages, budget = 6, 8, 2, 64, 24, 160, 10
+    layer = DecodeAttention(hq, hkv, d, B, mp, "bf16", "bf16", "f32")
+    freqs, _ = rotary_frequencies(d)
+    k = torch.zeros((npages, hkv, PAGE, d), device="cuda", dtype=torch.bfloat16)
+    v = torch.zeros_like(k)
+    refs = torch.zeros(npages, dtype=torch.int32, device="cuda")
+    table = torch.zeros((B, mp), dtype=torch.int32, device="cuda")
+    lens = torch.zeros(B, dtype=torch.int32, device="cuda")
+    bounds = torch.zeros((npages, hkv, 2, d), dtype=torch.int8, device="cuda")
+    bscale = torch.zeros((npages, hkv), device="cuda")
+    w = torch.zeros((B, mp), device="cuda")
+    gone = torch.zeros(B, dtype=torch.int32, device="cuda")
+    i32 = dict(dtype=torch.int32, device="cuda")
+    caches = layer.caches([(k, v)])
+    # One prompt of 100 tokens, forked for the others.
+    layer.page_grow(refs, table, lens, torch.tensor([100] + [0] * (B - 1), **i32))
+    rows = lambda n, h: torch.randn((n, h, d), device="cuda", dtype=torch.bfloat16)   # noqa: E731
+    starts = torch.tensor([0, 100] + [100] * (B - 1), **i32)
+    layer.append_rotary(rows(100, hq), rows(100, hkv), rows(100, hkv), k, v, table, lens, freqs, q_start=starts)
+    layer.page_bounds(k, table, lens, bounds, bscale, first=torch.zeros(B, **i32))
+    layer.page_fork(refs, table, lens, torch.zeros(B - 1, **i32), torch.arange(1, B, **i32), caches)
+
+    def kept_values(b, L):
+        pages = table[b, :-(-L // PAGE)].long()
+        return [t[pages].transpose(1, 2).reshape(-1, hkv, d)[:L].double() for t in (k, v)]
+
+    for step in range(60):
+        layer.page_grow(refs, table, lens, torch.full((B,), 3 if step % 2 else 1, **i32))
+        n = 3 if step % 2 else 1
+        starts = torch.arange(0, B * n + 1, n, **i32)
+        pos = (lens + PAGE * gone).repeat_interleave(n) - n + torch.arange(n, **i32).repeat(B)
+        q = layer.append_rotary(rows(B * n, hq), rows(B * n, hkv), rows(B * n, hkv), k, v, table, lens, freqs, q_start=starts,
+                                positions=pos.to(torch.int32))
+        layer.page_bounds(k, table, lens, bounds, bscale, first=lens - n)
+        pages, counts = layer.select_pages(q, bounds, bscale, table, lens, 5, sink=1, recent=2, q_start=starts)
+        part = layer.selected(q, k, v, table, lens, pages, counts, q_start=starts)
+        whole = layer.weighed(q, k, v, table, lens, w, decay=0.9375, q_start=starts)
+        before = lens.clone()
+        if step % 10 == 3:
+            for r in range(B * n):
+                b, L = r // n, int(lens[r // n]) - n + r % n + 1
+                kk, vv = kept_values(b, L)
+                for h in range(hq):
+                    g = h // (hq // hkv)
+                    x = kk[:, g] @ q[r, h].double() / math.sqrt(d)
+                    p = torch.softmax(x, 0)
+                    a = float((p[:, None] * vv[:, g].abs()).sum(0).max())
+                    tol = a * (2.0 ** -8 + 2 * (d * 2.0 ** -24 * float(q[r, h].double().norm() * kk[:, g].norm(dim=-1).max()) / 8 +
+                                                2.0 ** -21 * float(x.abs().max())) + 2.0 ** -20 + 2 * L * 2.0 ** -24)
+                    assert float((whole[r, h].double() - p @ vv[:, g]).abs().max()) <= tol
+                    seen = torch.zeros(L, dtype=torch.bool, device="cuda")
+                    for j in pages[r, g, :int(counts[r, g])].tolist():
+                        seen[j * PAGE:(j + 1) * PAGE] = True
+                    p = torch.softmax(x.masked_fill(~seen, -math.inf), 0)
+                    assert float((part[r, h].double() - p @ vv[:, g]).abs().max()) <= tol * float(
+                        (p[:, None] * vv[:, g].abs()).sum(0).max()) / a + 1e-12
+        gone += layer.page_evict(refs, table, lens, w, budget, sink=1, recent=3)
+        assert int(lens.max()) <= budget * PAGE and torch.equal((before - lens) % PAGE, torch.zeros_like(lens))
+        held = torch.zeros(npages, **i32)
+        for b in range(B):
+            m = -(-int(lens[b]) // PAGE)
+            held.index_add_(0, table[b, :m], torch.ones(m, **i32))
+        assert torch.equal(held, refs), step
+    assert int(gone.min()) > 0 and layer.read_flags(device="cuda") == 0 and layer.page_flags(npages, "cuda") == 0
