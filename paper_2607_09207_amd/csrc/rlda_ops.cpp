@@ -417,7 +417,7 @@ bool budget_ok(int32_t budget, int32_t sink, int32_t recent) {
 
 // Workgroups of a choice: several to a (row, KV head) while that leaves CUs idle, none with
 // less than kPiecePages of the longest sequence there may be.
-constexpr int kWantedChoices = 512, kPiecePages = 512;
+constexpr int kWantedChoices = 256, kPiecePages = 512;
 
 }  // namespace
 
@@ -501,7 +501,7 @@ rlda_status rl_decode_attn_select_pages(rl_decode_attn_t h, int32_t batch, int32
   p.pieces = 1;
   if (segs <= (int64_t)rlda::counters_of(h) && segs * c.max_pages_per_seq * (int64_t)sizeof(uint32_t) <= (int64_t)(wl.total - wl.part_acc))
     p.pieces = (int)std::max<int64_t>(std::min<int64_t>(kWantedChoices / segs, c.max_pages_per_seq / kPiecePages), 1);
-  if (segs * p.pieces * 512 > (1ll << 32) - 1) return RLDA_ERR_UNSUPPORTED;   // threads of a launch
+  if (segs * p.pieces * 1024 > (1ll << 32) - 1) return RLDA_ERR_UNSUPPORTED;   // threads of a launch
   return rlda::launch_select_pages(c.q_dtype == RLDA_F32, c.head_dim, p, stream) == hipSuccess ? RLDA_OK : RLDA_ERR_HIP;
 }
 

@@ -21,6 +21,7 @@
 
 #include "rlda_device.h"
 #include "rlda_params.h"
+#include "rlda_split.h"
 
 namespace rlda {
 namespace {
@@ -28,9 +29,9 @@ namespace {
 typedef int i32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kSel = 512;                  // threads of a workgroup that chooses
-constexpr int kSelWaves = kSel / 64;
-constexpr int kSelSmall = 8192;            // order keys in LDS: four such workgroups to a CU
-constexpr int kDigits = 256;
+constexpr int kEvict = 512;                // ... that evicts
+constexpr int kSelSmall = 8192;            // order keys in LDS: two such workgroups to a CU
+constexpr int kDigitBits = 11, kDigits = 1 << kDigitBits;
 
 __device__ __forceinline__ bool finite(float x) { return __builtin_fabsf(x) < __builtin_huge_valf(); }
 
@@ -38,6 +39,18 @@ __device__ __forceinline__ bool finite(float x) { return __builtin_fabsf(x) < __
 __device__ __forceinline__ uint32_t order_key(float x) {
   const uint32_t b = __float_as_uint(x + 0.f);
   return x != x ? 0xFFFFFFFFu : b ^ ((uint32_t)((int32_t)b >> 31) | 0x80000000u);
+}
+
+// Maximum over a wave's lanes, by DPP (rlda_device.h: a shuffle is an LDS round trip a step).
+__device__ __forceinline__ uint32_t wave_max(uint32_t x) {
+  const auto step = [&](uint32_t y) { x = x > y ? x : y; };
+  step((uint32_t)dpp_or_zero<0x111, 0xf>((int)x));   // row_shr:1, 2, 4, 8, then across the rows
+  step((uint32_t)dpp_or_zero<0x112, 0xf>((int)x));
+  step((uint32_t)dpp_or_zero<0x114, 0xf>((int)x));
+  step((uint32_t)dpp_or_zero<0x118, 0xf>((int)x));
+  step((uint32_t)dpp_or_zero<0x142, 0xa>((int)x));
+  step((uint32_t)dpp_or_zero<0x143, 0xc>((int)x));
+  return (uint32_t)__builtin_amdgcn_readlane((int)x, 63);
 }
 
 // ---------------------------------------------------------------- bounds
@@ -197,10 +210,11 @@ struct RowAt {
 
 // The sequence and the visible tokens of query row r (the same for all lanes of a wave): the
 // last entry of q_start up to r, 64 entries a step.
-__device__ __forceinline__ RowAt row_at(const SelectParams& p, int r) {
+// `len`: seq_lens[r], where there is no q_start.
+__device__ __forceinline__ RowAt row_at(const SelectParams& p, int r, int len) {
   const int lane = threadIdx.x & 63, cap = p.max_pages * kPage;
   if (!p.q_start) {
-    const int L = uni(p.seq_lens[r]);
+    const int L = uni(len);
     if ((L < 0 || L > cap) && lane == 0) atomicOr(p.flags, kFlagBadLen);
     return {r, min(max(L, 0), cap)};
   }
@@ -222,129 +236,221 @@ __device__ __forceinline__ RowAt row_at(const SelectParams& p, int r) {
 
 // ---------------------------------------------------------------- the best of many
 
-// What a workgroup of kSel threads shares while it looks for the K largest keys.
+// What a workgroup of T threads shares while it looks for the K largest keys.
+template <int T>
 struct Search {
-  int hist[kDigits];
-  uint32_t low[kSelWaves], high[kSelWaves];
-  int sum[kSelWaves], ties[kSelWaves];
-  int digit, above, in;
+  static constexpr int kWavesOf = T / 64;
+  int hist[kDigits];                 // zero when a search begins
+  uint32_t low[kWavesOf], high[kWavesOf];
+  int sum[kWavesOf], ties[kWavesOf];
+  int digit, above, in, members;
+  uint32_t list[64];
 };
 
-// The K-th largest of keys[lo .. hi) (0 < K < hi - lo): those above *at are taken, and the
-// first *ties of those equal to it.  By digits from the highest bit in which keys differ.
-__device__ __forceinline__ void kth_largest(const uint32_t* keys, int lo, int hi, int K, Search& s, uint32_t* at, int* ties) {
+// Sum over the waves before this one of s[wave] (all lanes; `all`: over all of them).
+template <int T>
+__device__ __forceinline__ int waves_before(const int* s, int* all) {
+  const int lane = threadIdx.x & 63, wave = uni((int)(threadIdx.x >> 6));
+  constexpr int N = T / 64;
+  const int x = wave_scan(lane < N ? s[lane] : 0);
+  *all = __builtin_amdgcn_readlane(x, N - 1);
+  return wave == 0 ? 0 : __builtin_amdgcn_readlane(x, max(wave - 1, 0));
+}
+
+// The K-th largest of keys[lo .. hi) (0 < K < hi - lo), of which a thread has seen kmin to kmax: those
+// above *at are taken, and the first *ties of those equal to it.  Digits of 11 bits from the
+// highest bit in which keys differ; the first one leaves a few keys as a rule, which every
+// wave then compares with each other.  Ends with s.hist in use.
+template <int T>
+__device__ __forceinline__ void kth_largest(const uint32_t* keys, int lo, int hi, int K, uint32_t kmin, uint32_t kmax,
+                                            Search<T>& s, uint32_t* at, int* ties) {
   const int tid = threadIdx.x, lane = tid & 63, wave = uni(tid >> 6);
-  uint32_t kmin = 0xFFFFFFFFu, kmax = 0;
-  for (int j = lo + tid; j < hi; j += kSel) {
-    kmin = min(kmin, keys[j]);
-    kmax = max(kmax, keys[j]);
-  }
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    kmin = min(kmin, (uint32_t)__shfl_xor((int)kmin, o));
-    kmax = max(kmax, (uint32_t)__shfl_xor((int)kmax, o));
-  }
+  constexpr int N = T / 64, P = kDigits / T;   // digits of a thread
+  kmin = ~wave_max(~kmin);
+  kmax = wave_max(kmax);
   if (lane == 0) {
     s.low[wave] = kmin;
     s.high[wave] = kmax;
   }
+  if (tid == 0) s.members = 0;
   __syncthreads();
 #pragma unroll
-  for (int w = 0; w < kSelWaves; ++w) {
+  for (int w = 0; w < N; ++w) {
     kmin = min(kmin, s.low[w]);
     kmax = max(kmax, s.high[w]);
   }
   int bits = kmin == kmax ? 0 : 32 - __builtin_clz(kmin ^ kmax);   // still undecided
   uint32_t prefix = bits == 32 ? 0u : kmin >> bits << bits;
   *ties = K;
-  while (bits > 0) {
-    const int shift = max(bits - 8, 0);
-    if (tid < kDigits) s.hist[tid] = 0;
-    __syncthreads();
-    for (int j = lo + tid; j < hi; j += kSel) {
+  for (bool again = false; bits > 0; again = true) {
+    const int shift = max(bits - kDigitBits, 0);
+    if (again) {
+      for (int i = tid; i < kDigits; i += T) s.hist[i] = 0;
+      __syncthreads();
+    }
+    for (int j = lo + tid; j < hi; j += T) {
       const uint32_t k = keys[j];
       if (bits == 32 || ((k ^ prefix) >> bits) == 0) atomicAdd(&s.hist[(k >> shift) & ((1u << (bits - shift)) - 1u)], 1);
     }
     __syncthreads();
-    // Counts from the largest digit down, over four waves.
-    if (tid < kDigits) {
-      const int n = s.hist[kDigits - 1 - tid], x = wave_scan(n);
-      if (lane == 63) s.sum[wave] = x;
-      s.hist[kDigits - 1 - tid] = x - n;   // of its wave's larger digits
+    // Counts from the largest digit down, P a thread.
+    int n[P], sum = 0, all;
+#pragma unroll
+    for (int i = 0; i < P; ++i) {
+      n[i] = s.hist[kDigits - 1 - (tid * P + i)];
+      sum += n[i];
     }
+    const int incl = wave_scan(sum);
+    if (lane == 63) s.sum[wave] = incl;
     __syncthreads();
-    if (tid < kDigits) {
-      int before = s.hist[kDigits - 1 - tid];
-      for (int w = 0; w < wave; ++w) before += s.sum[w];
-      int after = 0;   // with this digit: the next thread's count, or its wave's total
-      after = __shfl_down(s.hist[kDigits - 1 - tid], 1);
-      if (lane == 63) after = s.sum[wave];
-      for (int w = 0; w < wave; ++w) after += s.sum[w];
-      if (before < K && K <= after) {
-        s.digit = kDigits - 1 - tid;
+    int before = waves_before<T>(s.sum, &all) + incl - sum;
+#pragma unroll
+    for (int i = 0; i < P; ++i) {
+      if (before < K && K <= before + n[i]) {
+        s.digit = kDigits - 1 - (tid * P + i);
         s.above = before;
-        s.in = after - before;
+        s.in = n[i];
       }
+      before += n[i];
     }
     __syncthreads();
     prefix |= (uint32_t)s.digit << shift;
     K -= s.above;
     bits = shift;
     *ties = K;
-    if (s.in == K) {   // all of them: whatever their lower bits are
+    const int in = s.in;
+    if (in == K) {   // all of them: whatever their lower bits are
       *ties = 0x7FFFFFFF;
+      break;
+    }
+    if (bits > 0 && in <= 64) {
+      for (int j = lo + tid; j < hi; j += T) {
+        const uint32_t k = keys[j];
+        if (((k ^ prefix) >> bits) == 0) s.list[atomicAdd(&s.members, 1)] = k;
+      }
+      __syncthreads();
+      const uint32_t mine = lane < in ? s.list[lane] : 0u;
+      int above = 0, equal = 0;
+      for (int i = 0; i < in; ++i) {
+        const uint32_t k = (uint32_t)__builtin_amdgcn_readlane((int)mine, i);
+        above += k > mine;
+        equal += k == mine;
+      }
+      const uint64_t it = __builtin_amdgcn_ballot_w64(lane < in && above < K && K <= above + equal);
+      const int l = __builtin_ctzll(it);
+      prefix = (uint32_t)__builtin_amdgcn_readlane((int)mine, l);
+      *ties = K - __builtin_amdgcn_readlane(above, l);
       break;
     }
   }
   *at = prefix;
 }
 
-// Calls take(j, rank) for the pages j of [0, n) that are chosen, in order, and leave(j) for the
-// others: those of the first `sink` and the last `recent`, and of the rest the largest keys.
-// Whatever read(j) reads is read before anything is written by take or leave of pages up to j.
-template <class Read, class Take, class Leave>
-__device__ __forceinline__ int choose(const uint32_t* keys, int n, int budget, int sink, int recent, Search& s, Read read,
-                                      Take take, Leave leave) {
-  const int tid = threadIdx.x, lane = tid & 63, wave = uni(tid >> 6);
-  const int K = budget - sink - recent;
-  uint32_t at = 0xFFFFFFFFu;
-  int ties = 0;
-  if (K > 0) kth_largest(keys, sink, n - recent, K, s, &at, &ties);
-  int taken = 0, tied = 0;   // in the pages before
-  for (int j0 = 0; j0 < n; j0 += kSel) {
-    const int j = j0 + tid;
-    const bool kept = j < n && (j < sink || j >= n - recent);
-    const bool rest = j < n && !kept && K > 0;
-    const uint32_t k = rest ? keys[j] : 0u;
-    const bool sure = kept || (rest && k > at), tie = rest && k == at;
-    const auto x = read(j);
-    const uint64_t below = (1ull << lane) - 1, ms = __builtin_amdgcn_ballot_w64(sure), mt = __builtin_amdgcn_ballot_w64(tie);
-    if (lane == 0) {
-      s.sum[wave] = __builtin_popcountll(ms);
-      s.ties[wave] = __builtin_popcountll(mt);
-    }
-    __syncthreads();
-    // Before this wave: the sure ones, and as many ties as were wanted.
-    int sures = 0, tbefore = tied, alls = 0, allt = 0;
+// The same by one wave alone, with 256 counters in `hist`: digits of 8 bits.
+__device__ __forceinline__ void kth_largest_wave(const uint32_t* keys, int lo, int hi, int K, int* hist, uint32_t* at, int* ties) {
+  const int lane = threadIdx.x & 63;
+  const auto wait = [] {   // LDS operations of a wave are done in order
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+  };
+  // Four times 64 keys at a time: f(key, whether there is one).
+  const auto each = [&](auto f) {
+    for (int j = lo + lane; j - lane < hi; j += 256) {
+      uint32_t k[4];
 #pragma unroll
-    for (int w = 0; w < kSelWaves; ++w) {
-      sures += w < wave ? s.sum[w] : 0;
-      tbefore += w < wave ? s.ties[w] : 0;
-      alls += s.sum[w];
-      allt += s.ties[w];
+      for (int i = 0; i < 4; ++i) k[i] = keys[min(j + 64 * i, hi - 1)];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) f(k[i], j + 64 * i < hi);
     }
-    const int mine = tbefore + __builtin_popcountll(mt & below);   // ties before this page
-    const bool chosen = sure || (tie && mine < ties);
-    const int rank = taken + sures + __builtin_popcountll(ms & below) + (min(mine, ties) - min(tied, ties));
-    if (chosen)
-      take(j, rank, x);
-    else if (j < n)
-      leave(j, x);
-    taken += alls + (min(tied + allt, ties) - min(tied, ties));
-    tied += allt;
-    __syncthreads();   // the counts are used again
+  };
+  uint32_t kmin = 0xFFFFFFFFu, kmax = 0;
+  each([&](uint32_t k, bool) {   // (past the end: the last one again)
+    kmin = min(kmin, k);
+    kmax = max(kmax, k);
+  });
+  kmin = ~wave_max(~kmin);
+  kmax = wave_max(kmax);
+  int bits = kmin == kmax ? 0 : 32 - __builtin_clz(kmin ^ kmax);
+  uint32_t prefix = bits == 32 ? 0u : kmin >> bits << bits;
+  *ties = K;
+  while (bits > 0) {
+    const int shift = max(bits - 8, 0);
+    const auto inside = [&](uint32_t k) { return bits == 32 || ((k ^ prefix) >> bits) == 0; };
+    *(i32x4*)&hist[4 * lane] = i32x4{0, 0, 0, 0};
+    wait();
+    each([&](uint32_t k, bool is) {
+      if (is && inside(k)) atomicAdd(&hist[255 - ((k >> shift) & ((1u << (bits - shift)) - 1u))], 1);
+    });
+    wait();
+    const i32x4 n = *(const i32x4*)&hist[4 * lane];   // from the largest digit down
+    wait();
+    const int incl = wave_scan(n[0] + n[1] + n[2] + n[3]);
+    const int l = __builtin_ctzll(__builtin_amdgcn_ballot_w64(incl >= K));   // the first lane that reaches K
+    int above = __builtin_amdgcn_readlane(incl - (n[0] + n[1] + n[2] + n[3]), l), d = 4 * l, in = __builtin_amdgcn_readlane(n[0], l);
+#pragma unroll
+    for (int i = 1; i < 4; ++i)
+      if (above + in < K) {
+        above += in;
+        in = __builtin_amdgcn_readlane(n[i], l);
+        d = 4 * l + i;
+      }
+    prefix |= (uint32_t)(255 - d) << shift;
+    K -= above;
+    bits = shift;
+    *ties = K;
+    if (in == K) {   // all of them: whatever their lower bits are
+      *ties = 0x7FFFFFFF;
+      break;
+    }
+    if (bits > 0 && in <= 64) {
+      int got = 0;
+      each([&](uint32_t k, bool is) {
+        const bool member = is && ((k ^ prefix) >> bits) == 0;
+        const uint64_t m = __builtin_amdgcn_ballot_w64(member);
+        if (member) hist[got + __builtin_popcountll(m & ((1ull << lane) - 1))] = (int)k;
+        got += __builtin_popcountll(m);
+      });
+      wait();
+      const uint32_t mine = lane < in ? (uint32_t)hist[lane] : 0u;
+      wait();
+      int greater = 0, equal = 0;
+      for (int i = 0; i < in; ++i) {
+        const uint32_t k = (uint32_t)__builtin_amdgcn_readlane((int)mine, i);
+        greater += k > mine;
+        equal += k == mine;
+      }
+      const int who = __builtin_ctzll(__builtin_amdgcn_ballot_w64(lane < in && greater < K && K <= greater + equal));
+      prefix = (uint32_t)__builtin_amdgcn_readlane((int)mine, who);
+      *ties = K - __builtin_amdgcn_readlane(greater, who);
+      break;
+    }
   }
-  return taken;
+  *at = prefix;
+}
+
+// Which pages of [0, n) are chosen: the first `sink`, the last `recent`, and of the others the
+// largest keys.
+struct Chosen {
+  uint32_t at;
+  int ties, sink, end;   // end: of the pages with a choice
+  bool any;
+  // Whether page j < n is chosen whatever its ties, and whether it is one of the ties.
+  __device__ __forceinline__ bool sure(int j, uint32_t k) const { return j < sink || j >= end || (any && k > at); }
+  __device__ __forceinline__ bool tie(int j, uint32_t k) const { return j >= sink && j < end && any && k == at; }
+};
+
+// ... found by one wave, or by the whole workgroup from keys in LDS, of which a thread has seen kmin to kmax.
+__device__ __forceinline__ Chosen choose_wave(const uint32_t* keys, int n, int budget, int sink, int recent, int* hist) {
+  Chosen c = {0xFFFFFFFFu, 0, sink, n - recent, budget > sink + recent};
+  if (c.any) kth_largest_wave(keys, sink, n - recent, budget - sink - recent, hist, &c.at, &c.ties);
+  return c;
+}
+template <int T>
+__device__ __forceinline__ Chosen choose(const uint32_t* keys, int n, int budget, int sink, int recent, uint32_t kmin,
+                                         uint32_t kmax, Search<T>& s) {
+  Chosen c = {0xFFFFFFFFu, 0, sink, n - recent, budget > sink + recent};
+  if (c.any) kth_largest<T>(keys, sink, n - recent, budget - sink - recent, kmin, kmax, s, &c.at, &c.ties);
+  return c;
 }
 
 // ---------------------------------------------------------------- choice
@@ -354,95 +460,109 @@ __device__ __forceinline__ float row_move(float x) {
   const int v = __builtin_bit_cast(int, x);
   return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(v, v, CTRL, 0xf, 0xf, true));
 }
-// Maximum over the 16 lanes of a row.
-__device__ __forceinline__ float row_max(float x) {
-  x = fmaxf(x, row_move<0x128>(x));   // row_ror:8, 4, 2, 1
-  x = fmaxf(x, row_move<0x124>(x));
-  x = fmaxf(x, row_move<0x122>(x));
-  return fmaxf(x, row_move<0x121>(x));
+// Maxima of four values over the 16 lanes of a row: lane i gets that of value i / 4.  Each
+// lane hands the values on that are not its own, so there are fewer of them every step.
+__device__ __forceinline__ float row_max4(const float* m) {
+  const int lane = threadIdx.x & 63;
+  const bool b3 = lane & 8, b2 = lane & 4;
+  const float x0 = fmaxf(b3 ? m[2] : m[0], row_move<0x128>(b3 ? m[0] : m[2]));   // row_ror:8
+  const float x1 = fmaxf(b3 ? m[3] : m[1], row_move<0x128>(b3 ? m[1] : m[3]));
+  // The lanes of the other value are 4 before or after within the eight (row_half_mirror).
+  float y = fmaxf(b2 ? x1 : x0, row_move<0x141>(b2 ? x0 : x1));
+  y = fmaxf(y, row_move<0xB1>(y));          // lane ^ 1, ^ 2
+  return fmaxf(y, row_move<0x4E>(y));
 }
 
-// The query heads of a KV head as the second operand of 16x16x64 products, in 8 bits: lane
-// 16 qg + i holds head i's elements 64 c + 16 qg .. + 15 (min(q, 0) for the lower bounds, then
-// max(q, 0) for the upper ones), and its scale.
+// The query heads of a KV head in 8 bits: min(q8, 0) for the lower bounds, then max(q8, 0) for
+// the upper ones, and their scales.  A wave a head (every wave rounding all of them for
+// itself was a third of a small call's time), rows of 16 bytes more than they hold so that
+// the reads below spread over the banks.
+template <int D>
+struct QShared {
+  int8_t bytes[kMaxGroup][2 * D + 16];
+  float scale[kMaxGroup];
+};
 template <int D, bool QF32>
-struct QBytes {
-  static constexpr int C = D / 64;
-  i32x4 v[2 * C];
-  float scale;   // -inf: no head
-
-  __device__ __forceinline__ void load(const SelectParams& p, int row, int g, int lane) {
-    const int i = lane & 15, qg = lane >> 4;
-    float x[C][16], amax = 0.f;
+__device__ __forceinline__ void round_q(const SelectParams& p, int row, int g, QShared<D>& s) {
+  constexpr int E = D / 64, N = kSel / 64, H = (kMaxGroup + N - 1) / N;   // heads of a wave: their loads in flight together
+  const int lane = threadIdx.x & 63, wave = uni((int)(threadIdx.x >> 6));
+  float x[H][E];
+#pragma unroll
+  for (int i = 0; i < H; ++i) {
+    // The head map by a scalar load: the arguments lie in host memory.
+    const int m = g * p.group + min(wave + i * N, p.group - 1);
+    const int qh = (int)(((const uint32_t*)p.q_head)[m >> 1] >> (16 * (m & 1)) & 0xFFFFu);
+    const int64_t at = ((int64_t)row * p.num_q_heads + qh) * D + lane;
+#pragma unroll
+    for (int e = 0; e < E; ++e)
+      x[i][e] = QF32 ? ((const float*)p.q)[at + 64 * e] : __uint_as_float((uint32_t)((const uint16_t*)p.q)[at + 64 * e] << 16);
+  }
+#pragma unroll
+  for (int i = 0; i < H; ++i) {
+    const int k = wave + i * N;
+    if (k >= p.group) break;
+    float amax = 0.f;
     bool odd = false;
-    const int qh = i < p.group ? p.q_head[g * p.group + i] : 0;
-    const int64_t at = ((int64_t)row * p.num_q_heads + qh) * D + 16 * qg;
 #pragma unroll
-    for (int c = 0; c < C; ++c) {
-      if constexpr (QF32) {
-#pragma unroll
-        for (int e = 0; e < 16; e += 4) *(f32x4*)&x[c][e] = *(const f32x4*)((const float*)p.q + at + 64 * c + e);
-      } else {
-#pragma unroll
-        for (int e = 0; e < 16; e += 8) {
-          const u32x4 w = *(const u32x4*)((const uint16_t*)p.q + at + 64 * c + e);
-#pragma unroll
-          for (int k = 0; k < 4; ++k) {
-            x[c][e + 2 * k] = __uint_as_float(w[k] << 16);
-            x[c][e + 2 * k + 1] = __uint_as_float(w[k] & 0xFFFF0000u);
-          }
-        }
-      }
-#pragma unroll
-      for (int e = 0; e < 16; ++e) {
-        odd |= !finite(x[c][e]);
-        amax = fmaxf(amax, __builtin_fabsf(x[c][e]));
-      }
+    for (int e = 0; e < E; ++e) {
+      odd |= !finite(x[i][e]);
+      amax = fmaxf(amax, __builtin_fabsf(x[i][e]));
     }
-    amax = fmaxf(amax, __shfl_xor(amax, 16));
-    amax = fmaxf(amax, __shfl_xor(amax, 32));
-    int any = odd;
-    any |= __shfl_xor(any, 16);
-    any |= __shfl_xor(any, 32);
-    const float s = any ? 0.f : amax / 127.f;   // (a query of infinities or NaN says nothing about pages)
+    amax = __uint_as_float(wave_max(__float_as_uint(amax)));   // (magnitudes order as integers)
+    // (A query of infinities or NaN says nothing about pages.)
+    const float sq = __builtin_amdgcn_ballot_w64(odd) != 0 ? 0.f : amax / 127.f;
 #pragma unroll
-    for (int c = 0; c < C; ++c)
+    for (int e = 0; e < E; ++e) {
+      const int q = sq > 0.f ? (int)__builtin_rintf(x[i][e] / sq) : 0;
+      s.bytes[k][64 * e + lane] = (int8_t)min(q, 0);
+      s.bytes[k][D + 64 * e + lane] = (int8_t)max(q, 0);
+    }
+    if (lane == 0) s.scale[k] = sq;
+  }
+}
+
+// ... as the second operand of 16x16x64 products: lane 16 qg + i holds head i's elements
+// 64 c + 16 qg .. + 15 (past the heads, the first one's again: the maximum is the same).
+template <int D>
+struct QBytes {
+  static constexpr int NC = 2 * D / 64;
+  i32x4 v[NC];
+  float scale;
+  __device__ __forceinline__ void load(const QShared<D>& s, int group) {
+    const int lane = threadIdx.x & 63, i = (lane & 15) < group ? lane & 15 : 0, qg = lane >> 4;
 #pragma unroll
-      for (int w = 0; w < 4; ++w) {
-        uint32_t neg = 0, pos = 0;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const int q = s > 0.f ? (int)__builtin_rintf(x[c][4 * w + e] / s) : 0;
-          neg |= (uint32_t)(min(q, 0) & 255) << (8 * e);
-          pos |= (uint32_t)(max(q, 0) & 255) << (8 * e);
-        }
-        v[c][w] = (int)neg;
-        v[C + c][w] = (int)pos;
-      }
-    scale = i < p.group ? s : neg_inf();
+    for (int c = 0; c < NC; ++c) v[c] = *(const i32x4*)&s.bytes[i][64 * c + 16 * qg];
+    scale = s.scale[i];
   }
 };
 
-// Order keys of the pages [j0, j1) of a (row, KV head), by the whole workgroup: store(j, key).
-// A wave takes 64 pages at a time, four tiles of 16 whose loads are in flight together.
-template <int D, bool QF32, class Store>
-__device__ __forceinline__ void score_pages(const SelectParams& p, const QBytes<D, QF32>& q, int seq, int g, int j0, int j1,
-                                            float (*s_val)[64], Store store) {
-  constexpr int NC = 2 * D / 64;
-  const int tid = threadIdx.x, lane = tid & 63, wave = uni(tid >> 6), i = lane & 15, qg = lane >> 4;
-  const int32_t* bt = p.block_table + (int64_t)seq * p.max_pages;
-  for (int base = j0 + 64 * wave; base < j1; base += kSel) {
-    const int j = base + lane;
-    int pid = j < j1 ? bt[j] : -1;
-    if (j < j1 && (unsigned)pid >= (unsigned)p.num_pages) {
-      atomicOr(p.flags, kFlagBadPage);
-      pid = -1;
-    }
-    const float scale = pid >= 0 ? p.bound_scale[(int64_t)pid * p.num_kv_heads + g] : 0.f;
-    i32x4 a[4][NC];
+// Tiles of 16 pages go round the waves, kTiles of a wave's at a time (a step), whose loads are in
+// flight together: the page whose id and key a lane holds.
+constexpr int kSelWaves = kSel / 64, kTiles = 2;
+__device__ __forceinline__ int page_of(int j0, int step) {
+  const int lane = threadIdx.x & 63, wave = uni((int)(threadIdx.x >> 6));
+  if (lane >= 16 * kTiles) return 0x7fffffff;
+  return j0 + 16 * ((kTiles * step + (lane >> 4)) * kSelWaves + wave) + (lane & 15);
+}
+
+// A step's bounds.
+template <int D>
+struct Tiles {
+  static constexpr int NC = 2 * D / 64;
+  i32x4 a[kTiles][NC];
+  float scale;
+  bool there;
+
+  // `id`: of the lane's page, which is one of the row's where `in`.
+  __device__ __forceinline__ void load(const SelectParams& p, int g, int id, bool in) {
+    const int lane = threadIdx.x & 63, i = lane & 15, qg = lane >> 4;
+    there = in && (unsigned)id < (unsigned)p.num_pages;
+    if (in && !there) atomicOr(p.flags, kFlagBadPage);
+    const int pid = there ? id : -1;
+    scale = there ? p.bound_scale[(int64_t)pid * p.num_kv_heads + g] : 0.f;
 #pragma unroll
-    for (int t = 0; t < 4; ++t) {
-      const int pt = __shfl(pid, 16 * t + i);
+    for (int t = 0; t < kTiles; ++t) {
+      const int pt = __shfl(pid, 16 * t + i);   // (lanes past the tiles hold none)
 #pragma unroll
       for (int c = 0; c < NC; ++c) a[t][c] = i32x4{0, 0, 0, 0};
       if (pt >= 0) {
@@ -451,39 +571,98 @@ __device__ __forceinline__ void score_pages(const SelectParams& p, const QBytes<
         for (int c = 0; c < NC; ++c) a[t][c] = *(const i32x4*)(src + 64 * c);
       }
     }
+  }
+
+  // The order key of the lane's page.  Bounds that are not finite: their page is looked at first.
+  // A page that is not there: last.
+  __device__ __forceinline__ uint32_t key(const QBytes<D>& q, float* s_val) const {
+    const int lane = threadIdx.x & 63, i = lane & 15, qg = lane >> 4;
 #pragma unroll
-    for (int t = 0; t < 4; ++t) {
+    for (int t = 0; t < kTiles; ++t) {
       i32x4 u = {0, 0, 0, 0};
 #pragma unroll
       for (int c = 0; c < NC; ++c) u = __builtin_amdgcn_mfma_i32_16x16x64_i8(a[t][c], q.v[c], u, 0, 0, 0);
       // Lane 16 qg + i: page 4 qg + r with head i.
       float m[4];
 #pragma unroll
-      for (int r = 0; r < 4; ++r) m[r] = row_max(i < p.group ? (float)u[r] * q.scale : neg_inf());
-      const float mine = i == 0 ? m[0] : i == 1 ? m[1] : i == 2 ? m[2] : m[3];
-      if (i < 4) s_val[wave][16 * t + 4 * qg + i] = mine;
+      for (int r = 0; r < 4; ++r) m[r] = (float)u[r] * q.scale;
+      const float most = row_max4(m);
+      if ((i & 3) == 0) s_val[16 * t + 4 * qg + (i >> 2)] = most;
     }
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     __builtin_amdgcn_wave_barrier();
-    const float x = s_val[wave][lane] * scale;
+    const float x = s_val[lane & (16 * kTiles - 1)] * scale;
     __builtin_amdgcn_wave_barrier();
-    // Keys that are not finite: their page is looked at first.  A page that is not there: last.
-    if (j < j1) store(j, pid < 0 ? 0u : finite(scale) ? order_key(x) : 0xFFFFFFFFu);
+    return !there ? 0u : finite(scale) ? order_key(x) : 0xFFFFFFFFu;
+  }
+};
+
+// The chosen pages of [r0, r1) in order, by one wave: `rank` chosen ones and `tied` ties lie before.
+// Four times 64 pages at a time; classes(): which of them are chosen, and which are ties.
+struct Classes {
+  uint64_t sure[4], tie[4];
+  __device__ __forceinline__ Classes(const uint32_t* keys, const Chosen& c, int at, int r1) {
+    const int lane = threadIdx.x & 63;
+    uint32_t k[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) k[i] = at + 64 * i + lane < r1 ? keys[at + 64 * i + lane] : 0u;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int j = at + 64 * i + lane;
+      sure[i] = __builtin_amdgcn_ballot_w64(j < r1 && c.sure(j, k[i]));
+      tie[i] = __builtin_amdgcn_ballot_w64(j < r1 && c.tie(j, k[i]));
+    }
+  }
+};
+__device__ __forceinline__ void write_chosen(const uint32_t* keys, const Chosen& c, int r0, int r1, int rank, int tied, int32_t* out) {
+  const int lane = threadIdx.x & 63;
+  const uint64_t below = (1ull << lane) - 1;
+  for (int j = r0; j < r1; j += 256) {
+    const Classes k(keys, c, j, r1);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const bool chosen = (k.sure[i] >> lane & 1) || ((k.tie[i] >> lane & 1) && tied + __builtin_popcountll(k.tie[i] & below) < c.ties);
+      const uint64_t m = __builtin_amdgcn_ballot_w64(chosen);
+      if (chosen) out[rank + __builtin_popcountll(m & below)] = j + 64 * i + lane;
+      rank += __builtin_popcountll(m);
+      tied += __builtin_popcountll(k.tie[i]);
+    }
   }
 }
 
-// One workgroup, or p.pieces of them, a (row, KV head).  With several, the one that finishes
-// last gathers the others' keys.
+// One workgroup, or p.pieces of them, a (row, KV head).  With several, the one that finishes last
+// gathers the others' keys.
+//   What a small call takes is its chain of dependent reads (the length, page ids, bounds) and
+// the search, so the ids and the queries are asked for before the length is known, and up to
+// kWavePages pages are searched by one wave, without barriers.  A long one is bound by the bounds
+// it reads: two buffers of tiles, one computed while the other's loads are in flight.
+constexpr int kWavePages = 256;
+
 template <int D, bool QF32, int CAP>
 __global__ __launch_bounds__(kSel) void select_pages_kernel(const SelectParams p) {
   __shared__ uint32_t s_key[CAP];
-  __shared__ float s_val[kSelWaves][64];
-  __shared__ Search s;
+  __shared__ float s_val[kSelWaves][16 * kTiles];
+  __shared__ __align__(16) QShared<D> s_q;
+  __shared__ __align__(16) Search<kSel> s;
   __shared__ int s_last;
-  const int tid = threadIdx.x, lane = tid & 63;
-  const int seg = (int)(blockIdx.x / (uint32_t)p.pieces), piece = blockIdx.x - seg * p.pieces;
-  const int row = seg / p.num_kv_heads, g = seg - row * p.num_kv_heads;
-  const RowAt at = row_at(p, row);
+  const int tid = threadIdx.x, lane = tid & 63, wave = uni(tid >> 6);
+  // A run of rows with all their KV heads to each XCD: a page's heads lie beside each other, and
+  // one head alone would use few of its L2's channels.
+  const int at_block = share_of_block(blockIdx.x, gridDim.x);
+  const int seg = p.pieces == 1 ? at_block : at_block / (uint32_t)p.pieces, piece = at_block - seg * p.pieces;
+  const int row = seg / (uint32_t)p.num_kv_heads, g = seg - row * p.num_kv_heads;
+  const bool early = !p.q_start && p.pieces == 1;   // the sequence and the first page are known
+  const int len = p.q_start ? 0 : p.seq_lens[row];
+  int ids[2] = {0, 0};
+  if (early) {
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      const int j = page_of(0, k);
+      ids[k] = j < p.max_pages ? p.block_table[(int64_t)row * p.max_pages + j] : 0;
+    }
+  }
+  round_q<D, QF32>(p, row, g, s_q);
+  const RowAt at = row_at(p, row, len);
   if (at.seq < 0) return;
   const int n = (at.tokens + kPage - 1) / kPage;
   int32_t* out = p.pages + (int64_t)seg * p.budget;
@@ -493,16 +672,54 @@ __global__ __launch_bounds__(kSel) void select_pages_kernel(const SelectParams p
     if (tid == 0) p.counts[seg] = n;
     return;
   }
-  QBytes<D, QF32> q;
-  q.load(p, row, g, lane);
-  if (p.pieces == 1) {
-    score_pages<D, QF32>(p, q, at.seq, g, 0, n, s_val, [&](int j, uint32_t k) { s_key[j] = k; });
-  } else {
-    const int per = ((n + p.pieces - 1) / p.pieces + 63) / 64 * 64;
-    uint32_t* keys = p.keys + (int64_t)seg * p.max_pages;
-    score_pages<D, QF32>(p, q, at.seq, g, min(piece * per, n), min((piece + 1) * per, n), s_val, [&](int j, uint32_t k) {
-      __hip_atomic_store(keys + j, k, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    });
+  if (tid == 0) p.counts[seg] = p.budget;
+  for (int i = tid; i < kDigits; i += kSel) s.hist[i] = 0;
+  const int per = ((n + p.pieces - 1) / p.pieces + 15) / 16 * 16, j0 = min(piece * per, n), j1 = min(j0 + per, n);
+  const int32_t* bt = p.block_table + (int64_t)at.seq * p.max_pages;
+  const auto id_of = [&](int step) {
+    const int j = page_of(j0, step);
+    return j < j1 ? bt[j] : 0;
+  };
+  if (!early) {
+    ids[0] = id_of(0);
+    ids[1] = id_of(1);
+  }
+  Tiles<D> t[2];
+  t[0].load(p, g, ids[0], page_of(j0, 0) < j1);
+  ids[0] = id_of(2);
+  __syncthreads();
+  QBytes<D> q;
+  q.load(s_q, p.group);
+  uint32_t kmin = 0xFFFFFFFFu, kmax = 0;
+  const auto keep = [&](int j, uint32_t k) {
+    s_key[j] = k;
+    if (j >= p.sink && j < n - p.recent) {
+      kmin = min(kmin, k);
+      kmax = max(kmax, k);
+    }
+  };
+  uint32_t* keys = p.keys + (int64_t)seg * p.max_pages;
+  // Step by step, a wave's own first page telling whether it has another.
+  const auto more = [&](int step) { return j0 + 16 * (kTiles * step * kSelWaves + wave) < j1; };
+  for (int step = 0; more(step); step += 2) {
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      if (!more(step + k)) break;
+      if (more(step + k + 1)) {
+        t[1 - k].load(p, g, ids[1 - k], page_of(j0, step + k + 1) < j1);
+        ids[1 - k] = id_of(step + k + 3);
+      }
+      const int j = page_of(j0, step + k);
+      const uint32_t key = t[k].key(q, s_val[wave]);
+      if (lane < 16 * kTiles && j < j1) {
+        if (p.pieces == 1)
+          keep(j, key);
+        else
+          __hip_atomic_store(keys + j, key, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      }
+    }
+  }
+  if (p.pieces > 1) {
     __builtin_amdgcn_s_waitcnt(0);   // this wave's stores have completed
     __syncthreads();
     if (tid == 0) {
@@ -513,24 +730,46 @@ __global__ __launch_bounds__(kSel) void select_pages_kernel(const SelectParams p
     }
     __syncthreads();
     if (!s_last) return;
-    for (int j = tid; j < n; j += kSel) s_key[j] = __hip_atomic_load(keys + j, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    for (int j = tid; j < n; j += kSel) keep(j, __hip_atomic_load(keys + j, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT));
   }
   __syncthreads();
-  const int count = choose(
-      s_key, n, p.budget, p.sink, p.recent, s, [](int) { return 0; }, [&](int j, int rank, int) { out[rank] = j; },
-      [](int, int) {});
-  if (tid == 0) p.counts[seg] = count;
+  if (n <= kWavePages) {
+    if (wave != 0) return;
+    const Chosen c = choose_wave(s_key, n, p.budget, p.sink, p.recent, s.hist);
+    write_chosen(s_key, c, 0, n, 0, 0, out);
+    return;
+  }
+  const Chosen c = choose<kSel>(s_key, n, p.budget, p.sink, p.recent, kmin, kmax, s);
+  // Every wave writes the chosen ones of a run of pages, behind those of the waves before.
+  const int run = ((n + kSelWaves - 1) / kSelWaves + 63) / 64 * 64, r0 = min(wave * run, n), r1 = min(r0 + run, n);
+  int sures = 0, ties = 0;
+  for (int j = r0; j < r1; j += 256) {
+    const Classes k(s_key, c, j, r1);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      sures += __builtin_popcountll(k.sure[i]);
+      ties += __builtin_popcountll(k.tie[i]);
+    }
+  }
+  if (lane == 0) {
+    s.sum[wave] = sures;
+    s.ties[wave] = ties;
+  }
+  __syncthreads();
+  int all;
+  const int rank = waves_before<kSel>(s.sum, &all), tied = waves_before<kSel>(s.ties, &all);
+  write_chosen(s_key, c, r0, r1, rank + min(tied, c.ties), tied, out);
 }
 
 // ---------------------------------------------------------------- eviction
 
-// One workgroup a row.  Entries move towards the front, kSel at a time: what a step writes lies
-// at or before what it has read.
+// One workgroup a row.  Entries move towards the front, kEvict at a time: what a step writes
+// lies at or before what it has read.
 template <int CAP>
-__global__ __launch_bounds__(kSel) void page_evict_kernel(const SelectParams p) {
+__global__ __launch_bounds__(kEvict) void page_evict_kernel(const SelectParams p) {
   __shared__ uint32_t s_key[CAP];
-  __shared__ Search s;
-  const int tid = threadIdx.x, b = blockIdx.x;
+  __shared__ Search<kEvict> s;
+  const int tid = threadIdx.x, lane = tid & 63, wave = uni(tid >> 6), b = blockIdx.x;
   const int L = p.seq_lens[b];
   const int n = (L + kPage - 1) / kPage;
   const bool bad = L < 0 || L > p.max_pages * kPage;
@@ -541,27 +780,53 @@ __global__ __launch_bounds__(kSel) void page_evict_kernel(const SelectParams p) 
   }
   int32_t* table = p.block_table + (int64_t)b * p.max_pages;
   float* w = p.weights + (int64_t)b * p.max_pages;
-  for (int j = tid; j < n; j += kSel) s_key[j] = order_key(w[j]);
+  for (int i = tid; i < kDigits; i += kEvict) s.hist[i] = 0;
+  uint32_t kmin = 0xFFFFFFFFu, kmax = 0;
+  for (int j = tid; j < n; j += kEvict) {
+    const uint32_t k = order_key(w[j]);
+    s_key[j] = k;
+    if (j >= p.sink && j < n - p.recent) {
+      kmin = min(kmin, k);
+      kmax = max(kmax, k);
+    }
+  }
   __syncthreads();
-  struct Entry {
-    int page;
-    float weight;
-  };
-  choose(
-      s_key, n, p.budget, p.sink, p.recent, s, [&](int j) { return j < n ? Entry{table[j], w[j]} : Entry{0, 0.f}; },
-      [&](int, int rank, Entry x) {
-        table[rank] = x.page;
-        w[rank] = x.weight;
-      },
-      [&](int, Entry x) {
-        if ((uint32_t)x.page >= (uint32_t)p.num_pages) {
-          atomicOr(p.flags, kFlagBadPage);
-        } else if (atomicSub(p.refs + x.page, 1) <= 0) {   // nobody held it
-          atomicAdd(p.refs + x.page, 1);
-          atomicOr(p.flags, kFlagBadPage);
-        }
-      });
-  for (int j = p.budget + tid; j < n; j += kSel) w[j] = 0.f;   // (choose ends with a barrier)
+  const Chosen c = choose<kEvict>(s_key, n, p.budget, p.sink, p.recent, kmin, kmax, s);
+  int taken = 0, tied = 0;   // in the pages before
+  const uint64_t below = (1ull << lane) - 1;
+  for (int j0 = 0; j0 < n; j0 += kEvict) {
+    const int j = j0 + tid;
+    const uint32_t k = j < n ? s_key[j] : 0u;
+    const bool sure = j < n && c.sure(j, k), tie = j < n && c.tie(j, k);
+    const int page = j < n ? table[j] : 0;
+    const float weight = j < n ? w[j] : 0.f;
+    const uint64_t ms = __builtin_amdgcn_ballot_w64(sure), mt = __builtin_amdgcn_ballot_w64(tie);
+    __syncthreads();   // the counts have been read
+    if (lane == 0) {
+      s.sum[wave] = __builtin_popcountll(ms);
+      s.ties[wave] = __builtin_popcountll(mt);
+    }
+    __syncthreads();   // ... and the step's entries, before any of them is written
+    int alls, allt;
+    const int sures = waves_before<kEvict>(s.sum, &alls) + __builtin_popcountll(ms & below);
+    const int ties = tied + waves_before<kEvict>(s.ties, &allt) + __builtin_popcountll(mt & below);
+    const int rank = taken + sures + min(ties, c.ties) - min(tied, c.ties);
+    if (sure || (tie && ties < c.ties)) {
+      table[rank] = page;
+      w[rank] = weight;
+    } else if (j < n) {
+      if ((uint32_t)page >= (uint32_t)p.num_pages) {
+        atomicOr(p.flags, kFlagBadPage);
+      } else if (atomicSub(p.refs + page, 1) <= 0) {   // nobody held it
+        atomicAdd(p.refs + page, 1);
+        atomicOr(p.flags, kFlagBadPage);
+      }
+    }
+    taken += alls + min(tied + allt, c.ties) - min(tied, c.ties);
+    tied += allt;
+  }
+  __syncthreads();
+  for (int j = p.budget + tid; j < n; j += kEvict) w[j] = 0.f;
   if (tid == 0) {
     p.dropped[b] = n - p.budget;
     p.seq_lens[b] = L - kPage * (n - p.budget);
@@ -616,9 +881,9 @@ int launch_select_pages(bool q_f32, int head_dim, const SelectParams& p, void* s
 
 int launch_page_evict(const SelectParams& p, void* stream) {
   if (p.max_pages <= kSelSmall)
-    hipLaunchKernelGGL(page_evict_kernel<kSelSmall>, dim3(p.batch), dim3(kSel), 0, (hipStream_t)stream, p);
+    hipLaunchKernelGGL(page_evict_kernel<kSelSmall>, dim3(p.batch), dim3(kEvict), 0, (hipStream_t)stream, p);
   else
-    hipLaunchKernelGGL(page_evict_kernel<kSelectMaxPages>, dim3(p.batch), dim3(kSel), 0, (hipStream_t)stream, p);
+    hipLaunchKernelGGL(page_evict_kernel<kSelectMaxPages>, dim3(p.batch), dim3(kEvict), 0, (hipStream_t)stream, p);
   return (int)hipGetLastError();
 }
 

@@ -328,10 +328,11 @@ def test_choice_of_several_rows(torch, kv, hq, hkv, d):
     assert c.flags() == 0
 
 
-@pytest.mark.parametrize("n,max_pages,rows", [(5000, 5000, 1), (700, 9000, 1), (2600, 2600, 3), (20000, 32768, 1)])
-def test_choice_of_long_rows(torch, n, max_pages, rows):
-    """Cut over several workgroups; tables beyond what the small form holds."""
-    c = Case(torch, "bf16", 4, 1, 64, [PAGE * n - 3, 900], [rows, rows], seed=n, extra_pages=max_pages - n)
+@pytest.mark.parametrize("n,max_pages,rows,hkv", [(5000, 5000, 1, 1), (700, 9000, 1, 1), (2600, 2600, 3, 1), (20000, 32768, 1, 1),
+                                                  (1500, 1500, 20, 8), (2600, 2600, 18, 8), (5000, 5000, 17, 8), (300, 9000, 17, 8)])
+def test_choice_of_long_rows(torch, n, max_pages, rows, hkv):
+    """Cut over several workgroups, or several rows to one; tables beyond what the small form holds."""
+    c = Case(torch, "bf16", 4 * hkv, hkv, 64, [PAGE * n - 3, 900], [rows, rows], seed=n, extra_pages=max_pages - n)
     g = torch.Generator("cuda").manual_seed(1)
     c.bounds.copy_(torch.randint(-127, 128, c.bounds.shape, device="cuda", generator=g, dtype=torch.int8).sort(dim=2).values)
     c.bscale.copy_(torch.rand(c.bscale.shape, device="cuda", generator=g))
