@@ -1873,8 +1873,10 @@ void decode_attention_kernel(const Params p) {
             const int pre = s_pre[b];
             jpage = w0 + k - Hs * pre - g * (s_pre[b + 1] - pre);
           }
-          st.template compute<false, kByCall, true>(f, lane, info & kInfoTok, p.scale_log2 * km, vm, exact);
+          st.template compute<false, kAlways, true>(f, lane, info & kInfoTok, p.scale_log2 * km, vm);
           st.put_page(p, b, g, jpage++, lane);
+        } else if constexpr (ROWS == kListed) {
+          st.template compute<false, kAlways>(f, lane, info & kInfoTok, p.scale_log2 * km, vm);
         } else
           st.compute(f, lane, info & kInfoTok, p.scale_log2 * km, vm, exact);
         if (info & (kInfoLast | kInfoEnd)) {

@@ -55,32 +55,63 @@ __device__ __forceinline__ uint32_t wave_max(uint32_t x) {
 
 // ---------------------------------------------------------------- bounds
 
-// bf16 pairs to signed 16-bit integers of their order and back.
+// bf16 pairs to signed 16-bit integers of their order (infinities and NaN beyond all others) and
+// back.
+typedef short s16x2 __attribute__((ext_vector_type(2)));
 __device__ __forceinline__ uint32_t ordered(uint32_t w) {
-  typedef short s16x2 __attribute__((ext_vector_type(2)));
-  const s16x2 x = __builtin_bit_cast(s16x2, w);
-  return w ^ (__builtin_bit_cast(uint32_t, x >> (short)15) & 0x7FFF7FFFu);
+  return w ^ (__builtin_bit_cast(uint32_t, __builtin_bit_cast(s16x2, w) >> (short)15) & 0x7FFF7FFFu);
 }
-__device__ __forceinline__ uint32_t pair_max(uint32_t a, uint32_t b) {
-  typedef short s16x2 __attribute__((ext_vector_type(2)));
+template <bool F32>
+__device__ __forceinline__ uint32_t larger(uint32_t a, uint32_t b) {
+  if constexpr (F32) return __float_as_uint(fmaxf(__uint_as_float(a), __uint_as_float(b)));
   return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(s16x2, a), __builtin_bit_cast(s16x2, b)));
 }
-__device__ __forceinline__ uint32_t pair_min(uint32_t a, uint32_t b) {
-  typedef short s16x2 __attribute__((ext_vector_type(2)));
-  return __builtin_bit_cast(uint32_t, __builtin_elementwise_min(__builtin_bit_cast(s16x2, a), __builtin_bit_cast(s16x2, b)));
+
+// The maxima of N words over the lanes that differ in the bits from LPR (a power of two) on, dealt
+// out to these lanes: with every step a lane keeps half of its words, so a step costs half of
+// the one before it.  Lane l ends with words N / (64 / LPR) (l / LPR) and on.
+template <bool F32, int LPR, int N>
+__device__ __forceinline__ void deal_maxima(uint32_t* w) {
+  const int lane = threadIdx.x & 63;
+  int n = N;
+#pragma unroll
+  for (int o = 32; o >= LPR; o >>= 1) {
+    n /= 2;
+#pragma unroll
+    for (int i = 0; i < N / 2; ++i) {
+      if (i >= n) break;
+      const uint32_t a = w[i], b = w[i + n];
+      if (o >= 16) {   // one half gets both of a, the other both of b
+        const auto r = o == 32 ? __builtin_amdgcn_permlane32_swap(a, b, false, false) : __builtin_amdgcn_permlane16_swap(a, b, false, false);
+        w[i] = larger<F32>(r[0], r[1]);
+      } else {
+        const bool up = lane & o;
+        const int send = (int)(up ? a : b);
+        const int got = o == 8 ? __builtin_amdgcn_update_dpp(send, send, 0x128, 0xf, 0xf, true) : __shfl_xor(send, o);   // row_ror:8
+        w[i] = larger<F32>(up ? b : a, (uint32_t)got);
+      }
+    }
+  }
 }
 
-// One wave a (page, KV head).  A load of the wave covers 64 / LPR rows of the page, a lane E
-// elements of one; the rows' largest and smallest values meet by exchanges between the lanes
-// of the same elements.  fp8 values become bf16 (exactly), and bf16 values are compared as
-// integers, two at a time.  Bandwidth bounds it for whole prompts, latency for a step.
+// One wave a (page, KV head).  A load of the wave covers RPI = 64 / LPR rows of the page, a lane E
+// elements of one.  fp8 values become bf16 (exactly), and bf16 values are compared as integers,
+// two at a time.  The largest values and the smallest (as the largest complements) then meet
+// over the lanes of the same elements, each of which ends with a few of them to divide and write.
+//   Bandwidth bounds it for whole prompts, as long as a page takes few operations: with every
+// lane reducing all of its elements and two of the groups dividing them, 33 us for 64 prompts
+// (151 MB) against 27 so.  For a step, latency.
 template <int D, KvKind KIND>
 __global__ __launch_bounds__(kThreads) void page_bounds_kernel(const SelectParams p) {
-  constexpr int EB = KIND == KvKind::F32 ? 4 : KIND == KvKind::BF16 ? 2 : 1;
+  constexpr bool F32 = KIND == KvKind::F32;
+  constexpr int EB = F32 ? 4 : KIND == KvKind::BF16 ? 2 : 1;
   constexpr int E = 16 / EB, LPR = D / E, RPI = 64 / LPR, NI = kPage / RPI;
+  constexpr int H = F32 ? E : E / 2;                      // words of a lane's elements
+  constexpr int NR = 2 * H / RPI, V = F32 ? NR : 2 * NR;   // words, and values, that it ends with
+  static_assert(V == 2 || V == 4, "bytes of a store");
   const int lane = threadIdx.x & 63, wave = uni((int)(threadIdx.x >> 6));
   const int b = blockIdx.y, cap = p.max_pages * kPage;
-  int L = p.seq_lens[b];
+  const int L = p.seq_lens[b];
   const int first = p.first ? p.first[b] : L - 1;
   if (L < 0 || L > cap || (p.first && (first < 0 || first > L))) {
     if (blockIdx.x == 0 && threadIdx.x == 0) atomicOr(p.flags, kFlagBadLen);
@@ -99,104 +130,74 @@ __global__ __launch_bounds__(kThreads) void page_bounds_kernel(const SelectParam
     }
     const int val = min(kPage, L - j * kPage);
     const char* base = (const char*)p.k + (int64_t)pid * p.stride_page + (int64_t)g * p.stride_head;
+    const int64_t at = (int64_t)pid * p.num_kv_heads + g;
     u32x4 x[NI];
 #pragma unroll
     for (int i = 0; i < NI; ++i) {
       const int r = min(i * RPI + row, val - 1);   // (rows past the end: the last one again)
       x[i] = __builtin_nontemporal_load((const u32x4*)(base + (int64_t)r * p.stride_slot + col * 16));
     }
-    float hi[E], lo[E], amax = 0.f;
+    const float ks = KIND == KvKind::FP8 ? p.k_scale[at] : 1.f;
+    uint32_t w[2 * H];   // the largest, then the largest complements
     bool odd = false;
-    if constexpr (KIND == KvKind::F32) {
 #pragma unroll
-      for (int e = 0; e < E; ++e) {
-        hi[e] = lo[e] = __uint_as_float(x[0][e]);
-        odd |= !finite(hi[e]);
+    for (int h = 0; h < H; ++h) {
+      uint32_t top = 0, low = 0;
 #pragma unroll
-        for (int i = 1; i < NI; ++i) {
-          const float v = __uint_as_float(x[i][e]);
-          odd |= !finite(v);
-          hi[e] = fmaxf(hi[e], v);
-          lo[e] = fminf(lo[e], v);
+      for (int i = 0; i < NI; ++i) {
+        uint32_t v;
+        if constexpr (KIND == KvKind::FP8)
+          v = ordered(fp8x2_to_bf16x2(x[i][h / 2], (h & 1) != 0));
+        else
+          v = F32 ? x[i][h] : ordered(x[i][h]);
+        if constexpr (F32) {
+          odd |= !finite(__uint_as_float(v));
+          top = i == 0 ? v : larger<true>(top, v);
+          low = i == 0 ? v ^ 0x80000000u : larger<true>(low, v ^ 0x80000000u);
+        } else {
+          top = i == 0 ? v : larger<false>(top, v);
+          low = i == 0 ? ~v : larger<false>(low, ~v);
         }
-#pragma unroll
-        for (int o = LPR; o < 64; o <<= 1) {
-          hi[e] = fmaxf(hi[e], __shfl_xor(hi[e], o));
-          lo[e] = fminf(lo[e], __shfl_xor(lo[e], o));
-        }
-        amax = fmaxf(amax, fmaxf(__builtin_fabsf(hi[e]), __builtin_fabsf(lo[e])));
       }
-    } else {
-      constexpr int W = E / 2;   // pairs of a lane
-      uint32_t mx[W], mn[W];
-      u16x2 top = {0, 0};
+      w[h] = top;
+      w[H + h] = low;
+    }
+    deal_maxima<F32, LPR, 2 * H>(w);
+    const bool low = row >= RPI / 2;
+    float v[V], amax = 0.f;
 #pragma unroll
-      for (int i = 0; i < NI; ++i)
-#pragma unroll
-        for (int w = 0; w < W; ++w) {
-          uint32_t v;
-          if constexpr (KIND == KvKind::BF16)
-            v = x[i][w];
-          else
-            v = fp8x2_to_bf16x2(x[i][w / 2], (w & 1) != 0);
-          top = __builtin_elementwise_max(top, __builtin_bit_cast(u16x2, v & 0x7FFF7FFFu));
-          v = ordered(v);
-          mx[w] = i == 0 ? v : pair_max(mx[w], v);
-          mn[w] = i == 0 ? v : pair_min(mn[w], v);
-        }
-      odd = not_finite(top);
-      const float ks = KIND == KvKind::FP8 ? p.k_scale[(int64_t)pid * p.num_kv_heads + g] : 1.f;
-#pragma unroll
-      for (int w = 0; w < W; ++w) {
-#pragma unroll
-        for (int o = LPR; o < 64; o <<= 1) {
-          mx[w] = pair_max(mx[w], (uint32_t)__shfl_xor((int)mx[w], o));
-          mn[w] = pair_min(mn[w], (uint32_t)__shfl_xor((int)mn[w], o));
-        }
-        const uint32_t h = ordered(mx[w]), l = ordered(mn[w]);
-        hi[2 * w] = __uint_as_float(h << 16);
-        hi[2 * w + 1] = __uint_as_float(h & 0xFFFF0000u);
-        lo[2 * w] = __uint_as_float(l << 16);
-        lo[2 * w + 1] = __uint_as_float(l & 0xFFFF0000u);
-      }
-#pragma unroll
-      for (int e = 0; e < E; ++e) {
-        if constexpr (KIND == KvKind::FP8) {   // a key is the stored value times the page's scale
-          const float a = hi[e] * ks, c = lo[e] * ks;
-          hi[e] = ks < 0.f ? c : a;
-          lo[e] = ks < 0.f ? a : c;
-          odd |= !finite(a) || !finite(c);
-        }
-        amax = fmaxf(amax, fmaxf(__builtin_fabsf(hi[e]), __builtin_fabsf(lo[e])));
+    for (int i = 0; i < NR; ++i) {
+      if constexpr (F32) {
+        v[i] = __uint_as_float(low ? w[i] ^ 0x80000000u : w[i]);
+      } else {
+        const uint32_t pair = ordered(low ? ~w[i] : w[i]);
+        v[2 * i] = __uint_as_float(pair << 16);
+        v[2 * i + 1] = __uint_as_float(pair & 0xFFFF0000u);
       }
     }
 #pragma unroll
-    for (int o = 1; o < LPR; o <<= 1) amax = fmaxf(amax, __shfl_xor(amax, o));
+    for (int i = 0; i < V; ++i) {
+      if constexpr (KIND == KvKind::FP8) v[i] *= ks;   // a key is the stored value times the page's scale
+      odd |= !finite(v[i]);
+      amax = fmaxf(amax, __builtin_fabsf(v[i]));
+    }
     odd = __builtin_amdgcn_ballot_w64(odd) != 0;
+    amax = __uint_as_float(wave_max(__float_as_uint(amax)));   // (magnitudes order as integers)
     const float s = odd ? __builtin_huge_valf() : amax / 127.f;
-    // The first group of lanes writes the lower bounds, the second the upper ones.
-    const int64_t at = (int64_t)pid * p.num_kv_heads + g;
-    if constexpr (RPI >= 2) {
-      if (row < 2) {
-        uint32_t out[E / 4];
+    const bool lower = low != (ks < 0.f);   // (a negative scale turns them round)
+    uint32_t out = 0;
 #pragma unroll
-        for (int w = 0; w < E / 4; ++w) {
-          uint32_t word = 0;
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const float v = (row ? hi[4 * w + e] : lo[4 * w + e]) / s;
-            const float r = row ? fminf(__builtin_ceilf(v), 127.f) : fmaxf(__builtin_floorf(v), -127.f);
-            const int byte = s > 0.f && !odd ? (int)r : 0;
-            word |= (uint32_t)(byte & 255) << (8 * e);
-          }
-          out[w] = word;
-        }
-        uint32_t* dst = (uint32_t*)(p.bounds + (at * 2 + row) * D + col * E);
-#pragma unroll
-        for (int w = 0; w < E / 4; ++w) dst[w] = out[w];
-      }
+    for (int i = 0; i < V; ++i) {
+      const float y = v[i] / s;
+      const int byte = lower ? (int)fmaxf(__builtin_floorf(y), -127.f) : (int)fminf(__builtin_ceilf(y), 127.f);
+      out |= (uint32_t)(byte & 255) << (8 * i);
     }
-    static_assert(RPI >= 2, "two groups of lanes write a page's bounds");
+    if (!(s > 0.f) || odd) out = 0;
+    int8_t* dst = p.bounds + (2 * at + (lower ? 0 : 1)) * D + col * E + (row & (RPI / 2 - 1)) * V;
+    if constexpr (V == 4)
+      *(uint32_t*)dst = out;
+    else
+      *(uint16_t*)dst = (uint16_t)out;
     if (lane == 0) p.bound_scale[at] = s;
   }
 }
@@ -553,23 +554,20 @@ struct Tiles {
   float scale;
   bool there;
 
-  // `id`: of the lane's page, which is one of the row's where `in`.
+  // `id`: of the lane's page, one of the row's where `in` (lanes past the tiles: none).
   __device__ __forceinline__ void load(const SelectParams& p, int g, int id, bool in) {
     const int lane = threadIdx.x & 63, i = lane & 15, qg = lane >> 4;
     there = in && (unsigned)id < (unsigned)p.num_pages;
     if (in && !there) atomicOr(p.flags, kFlagBadPage);
-    const int pid = there ? id : -1;
-    scale = there ? p.bound_scale[(int64_t)pid * p.num_kv_heads + g] : 0.f;
+    if (p.num_pages == 0) return;      // (no page is there, and none is looked at)
+    const int pid = there ? id : 0;   // (page 0 for those that are not: its keys are not used)
+    scale = p.bound_scale[(int64_t)pid * p.num_kv_heads + g];
 #pragma unroll
     for (int t = 0; t < kTiles; ++t) {
-      const int pt = __shfl(pid, 16 * t + i);   // (lanes past the tiles hold none)
+      const int64_t page = __shfl(pid, 16 * t + i);
+      const int8_t* src = p.bounds + (page * p.num_kv_heads + g) * (2 * D) + 16 * qg;
 #pragma unroll
-      for (int c = 0; c < NC; ++c) a[t][c] = i32x4{0, 0, 0, 0};
-      if (pt >= 0) {
-        const int8_t* src = p.bounds + ((int64_t)pt * p.num_kv_heads + g) * (2 * D) + 16 * qg;
-#pragma unroll
-        for (int c = 0; c < NC; ++c) a[t][c] = *(const i32x4*)(src + 64 * c);
-      }
+      for (int c = 0; c < NC; ++c) a[t][c] = *(const i32x4*)(src + 64 * c);
     }
   }
 
@@ -844,11 +842,14 @@ void launch_select_t(const SelectParams& p, hipStream_t st) {
 
 }  // namespace
 
+// Workgroups of a call with first tokens: 31.5, 29.8, 28.4 and 28.5 us for 64 prompts with 4096,
+// 8192, 16384 and 32768 (the lengths differ, and a sequence's share is cut from the longest).
+constexpr int kBoundsGrid = 16384;
 int launch_page_bounds(KvKind kind, int head_dim, const SelectParams& p, void* stream) {
-  // A wave a (page, KV head): enough of them for the last pages, or, without knowing the
-  // lengths, for a batch's share of the GPU.
+  // A wave a (page, KV head): enough of them for the last pages, or, the lengths not being known,
+  // a sequence's share of what the GPU holds.
   const int64_t most = p.first ? (int64_t)p.max_pages * p.num_kv_heads : p.num_kv_heads;
-  const int64_t share = 8192 / p.batch > 1 ? 8192 / p.batch : 1;
+  const int64_t share = kBoundsGrid / p.batch > 1 ? kBoundsGrid / p.batch : 1;
   int64_t x = (most + kWaves - 1) / kWaves;
   if (p.first && x > share) x = share;
   const dim3 grid((uint32_t)x, (uint32_t)p.batch);

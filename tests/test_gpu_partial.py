@@ -10,7 +10,7 @@ factor that has
   - the error of its score: the product of d terms accumulated in fp32, d 2^-24 of |q| |k| scale,
     and 2^-21 of the score for the log2 units; twice, for the maximum's too;
   - the exponential's 2^-21, the sum's n 2^-24 (n terms of one sign) and the product's n 2^-24;
-  - its rounding to bf16, 2^-8 (f32 caches: none).
+  - its rounding, to a bf16 value and a bf16 remainder, 2^-16 (f32 caches: none).
 A bf16 output adds half a step, 2^-8 |o|.  A page's weight has the scores' errors, the
 exponentials', twice the sums', and half a step, 2^-24, of the two logarithms (times ln 2), of
 the additions over the rows and heads (one of each, all of one sign) and of the update (two).
@@ -159,7 +159,7 @@ class Case:
             o[r] = (p[:, :, None] * v).sum(1)
             a = (p[:, :, None] * v.abs()).sum(1)
             f = 2 * err + 2.0 ** -20 + 2 * L * 2.0 ** -24
-            tol[r] = a * (f + (0.0 if self.kv == "f32" else 2.0 ** -8))
+            tol[r] = a * (f + (0.0 if self.kv == "f32" else 2.0 ** -16))
             logs = (top.abs() / math.log(2) + (L + 1.0) ** 0.5) * 2.0 ** -23      # |log2 of sums| of 1 to L terms, and of pages
             small = torch.log2(p.clamp_min(1e-38)).abs() * 2.0 ** -23
             parts[r] = (p, f + logs + small)
@@ -478,7 +478,13 @@ def test_selected_everything_is_the_plain_attention(torch):
         pages = torch.arange(n, dtype=torch.int32, device="cuda").expand(5, hkv, n).contiguous()
         counts = torch.from_numpy(np.repeat(c.used[:, None], hkv, 1).astype(np.int32)).cuda()
         plain = c.layer(c.q, *c.cache(), **c.scales())
-        assert torch.equal(c.attend(pages, counts), plain)   # the same stream, cuts and sums
+        o, tol, _ = c.want(lambda r, g, L: range(-(-L // PAGE)))
+        got = c.attend(pages, counts)
+        c.check(got, o, tol)
+        # The plain call rounds probabilities to one bf16 value where its streams are short: 2^-8
+        # of A, and |o| <= A <= max |v|.
+        assert bool(((got - plain).abs() <= 2.0 ** -8 * float(c.v.float().nan_to_num().abs().max() if c.vs is None else 4 * 448 * c.vs.max())
+                     + tol).all())
 
 
 def test_selected_twice_the_same_page_and_bad_entries(torch):
@@ -547,7 +553,6 @@ def expect_weights(c, parts, w0, decay):
 def test_weighed(torch, kv, hq, hkv, d, ranges):
     c = Case(torch, kv, hq, hkv, d, [1, 0, 16, 17, 250, 1500, 33, 640], seed=hq, ranges=ranges, extra_pages=3)
     o, tol, parts = c.want(lambda r, g, L: range(-(-L // PAGE)))
-    plain = c.layer(c.q, *c.cache(), **c.scales())
     for decay in (1.0, 0.9, 0.0):
         w0 = torch.rand((8, c.mp), device="cuda", generator=c.gen)
         if decay == 0.0:
@@ -555,7 +560,6 @@ def test_weighed(torch, kv, hq, hkv, d, ranges):
         w = w0.clone()
         got = c.weigh(w, decay=decay)
         torch.cuda.synchronize()
-        assert torch.equal(got, plain)
         c.check(got, o, tol)
         want, wtol = expect_weights(c, parts, w0, decay)
         for b in range(8):
@@ -915,7 +919,7 @@ def test_a_rollout_that_reads_and_keeps_a_part(torch):
                     x = kk[:, g] @ q[r, h].double() / math.sqrt(d)
                     p = torch.softmax(x, 0)
                     a = float((p[:, None] * vv[:, g].abs()).sum(0).max())
-                    tol = a * (2.0 ** -8 + 2 * (d * 2.0 ** -24 * float(q[r, h].double().norm() * kk[:, g].norm(dim=-1).max()) / 8 +
+                    tol = a * (2.0 ** -16 + 2 * (d * 2.0 ** -24 * float(q[r, h].double().norm() * kk[:, g].norm(dim=-1).max()) / 8 +
                                                 2.0 ** -21 * float(x.abs().max())) + 2.0 ** -20 + 2 * L * 2.0 ** -24)
                     assert float((whole[r, h].double() - p @ vv[:, g]).abs().max()) <= tol
                     seen = torch.zeros(L, dtype=torch.bool, device="cuda")
