@@ -526,8 +526,8 @@ rlda_status rl_decode_attn_page_bounds(rl_decode_attn_t handle, int32_t batch, i
  *   counts  [total_q][Hkv] int32: min(n, budget)
  * Rows that no sequence names, and those of inconsistent q_start entries (flag bit 1), are not
  * written; rows before token 0 (n_b > seq_lens[b], flag bit 1) choose nothing.
- * max_pages_per_seq up to 32768 (else RLDA_ERR_UNSUPPORTED).  workspace: as for
- * rl_decode_attn_run.  One kernel, asynchronous.
+ * max_pages_per_seq up to 32768, budget up to 2^24 (else RLDA_ERR_UNSUPPORTED).  workspace: as
+ * for rl_decode_attn_run.  One kernel, asynchronous.
  */
 rlda_status rl_decode_attn_select_pages(rl_decode_attn_t handle, int32_t batch, int32_t num_pages, int32_t total_q,
                                         int32_t budget, int32_t sink, int32_t recent, const void* q, const int8_t* bounds,

@@ -418,6 +418,7 @@ bool budget_ok(int32_t budget, int32_t sink, int32_t recent) {
 // Workgroups of a choice: several to a (row, KV head) while that leaves CUs idle, none with
 // less than kPiecePages of the longest sequence there may be.
 constexpr int kWantedChoices = 256, kPiecePages = 512;
+constexpr int32_t kMaxBudget = 1 << 24;   // entries of a choice's list
 
 }  // namespace
 
@@ -467,7 +468,7 @@ rlda_status rl_decode_attn_select_pages(rl_decode_attn_t h, int32_t batch, int32
   if (batch < 0 || batch > c.max_batch || num_pages < 0 || total_q < 0) return RLDA_ERR_INVALID_ARG;
   if (!q_start && total_q != batch) return RLDA_ERR_INVALID_ARG;
   if (!budget_ok(budget, sink, recent)) return RLDA_ERR_INVALID_ARG;
-  if (c.max_pages_per_seq > rlda::kSelectMaxPages) return RLDA_ERR_UNSUPPORTED;
+  if (c.max_pages_per_seq > rlda::kSelectMaxPages || budget > kMaxBudget) return RLDA_ERR_UNSUPPORTED;
   if (batch == 0 || total_q == 0) return RLDA_OK;
   if (!q || !block_table || !seq_lens || !pages || !counts || !aligned16(q)) return RLDA_ERR_INVALID_ARG;
   if (!aligned4(block_table) || !aligned4(seq_lens) || !aligned4(q_start) || !aligned4(pages) || !aligned4(counts))
@@ -501,7 +502,7 @@ rlda_status rl_decode_attn_select_pages(rl_decode_attn_t h, int32_t batch, int32
   p.pieces = 1;
   if (segs <= (int64_t)rlda::counters_of(h) && segs * c.max_pages_per_seq * (int64_t)sizeof(uint32_t) <= (int64_t)(wl.total - wl.part_acc))
     p.pieces = (int)std::max<int64_t>(std::min<int64_t>(kWantedChoices / segs, c.max_pages_per_seq / kPiecePages), 1);
-  if (segs * p.pieces * 1024 > (1ll << 32) - 1) return RLDA_ERR_UNSUPPORTED;   // threads of a launch
+  if (segs * p.pieces * rlda::kSelectThreads > (1ll << 32) - 1) return RLDA_ERR_UNSUPPORTED;   // threads of a launch
   return rlda::launch_select_pages(c.q_dtype == RLDA_F32, c.head_dim, p, stream) == hipSuccess ? RLDA_OK : RLDA_ERR_HIP;
 }
 

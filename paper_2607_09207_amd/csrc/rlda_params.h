@@ -253,6 +253,7 @@ constexpr int kTwoTileMaxBatch = 2048;   // two-tile multi-token rows: per-seque
 
 // Bounds of the keys of pages, the choice of pages by them, and eviction (rlda_select.hip).
 constexpr int kSelectMaxPages = 32768;   // pages of a row: a choice holds their keys in LDS
+constexpr int kSelectThreads = 512;      // threads of a workgroup that chooses
 struct SelectParams {
   const void* q;               // choice: [rows][Hq][D]
   const void* k;               // bounds: the K pool, as in Params

@@ -28,7 +28,7 @@ namespace {
 
 typedef int i32x4 __attribute__((ext_vector_type(4)));
 
-constexpr int kSel = 512;                  // threads of a workgroup that chooses
+constexpr int kSel = kSelectThreads;
 constexpr int kEvict = 512;                // ... that evicts
 constexpr int kSelSmall = 8192;            // order keys in LDS: two such workgroups to a CU
 constexpr int kDigitBits = 11, kDigits = 1 << kDigitBits;

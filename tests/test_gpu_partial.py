@@ -504,14 +504,25 @@ def test_selected_keys_that_are_not_listed_have_no_part(torch):
     for kv in ("bf16", "fp8", "f32"):
         c = Case(torch, kv, 4, 2, 64, [330, 150], [3, 2], seed=13)
         pages, counts = random_lists(c, 6, 1)
+        free = next(x for x in range(c.npages - 1, -1, -1) if x not in set(c.table.flatten().tolist()))
+        for t in (c.k, c.v, c.ks, c.vs):   # page 0 is nobody's
+            if t is not None:
+                t.view(raw_type(torch, kv) if t.dim() == 4 else t.dtype)[free] = \
+                    t.view(raw_type(torch, kv) if t.dim() == 4 else t.dtype)[0].clone()
+        c.table[c.table == 0] = free
+        c.block_table.copy_(torch.from_numpy(c.table))
+        for t in (c.ks, c.vs):
+            if t is not None:
+                t[0] = math.nan
         listed = {(b, int(j)) for r, b, _ in c.row_list() for g in range(2) for j in pages[r, g, :counts[r, g]]}
         for b in range(2):
             for j in range(c.used[b]):
                 if (b, j) not in listed:
                     for t in (c.k, c.v):
                         t.view(raw_type(torch, kv))[int(c.table[b, j])] = NAN[kv]
-        o, tol, _ = c.want(lambda r, g, L: pages[r, g, :counts[r, g]])
-        o, tol = torch.zeros_like(o), torch.zeros_like(tol)
+                    for t in (c.ks, c.vs):
+                        if t is not None:
+                            t[int(c.table[b, j])] = math.nan
         got = c.attend(torch.from_numpy(pages).cuda(), torch.from_numpy(counts).cuda())
         assert bool(got.isfinite().all())
         # The last token of each sequence is seen by its last row alone.
@@ -847,6 +858,19 @@ def test_graph(torch):
     assert c.flags() == 0
 
 
+def test_events_bracket_the_kernels(torch):
+    c = Case(torch, "bf16", 8, 2, 64, [900, 64], seed=28)
+    c.all_bounds()
+    pages, counts = c.select(6)
+    w = torch.zeros((2, c.mp), device="cuda")
+    want = c.attend(pages, counts), c.weigh(w)
+    for call, o in ((lambda e: c.attend(pages, counts, events=e), want[0]), (lambda e: c.weigh(w, events=e), want[1])):
+        ev = [torch.cuda.Event(enable_timing=True) for _ in range(2)]
+        got = call(ev)
+        torch.cuda.synchronize()
+        assert torch.equal(got, o) and 0 < ev[0].elapsed_time(ev[1]) < 1000
+
+
 def test_other_streams(torch):
     c = Case(torch, "fp8", 40, 8, 128, [900, 2000, 64], seed=23)
     c.all_bounds()
@@ -936,3 +960,112 @@ def test_a_rollout_that_reads_and_keeps_a_part(torch):
             held.index_add_(0, table[b, :m], torch.ones(m, **i32))
         assert torch.equal(held, refs), step
     assert int(gone.min()) > 0 and layer.read_flags(device="cuda") == 0 and layer.page_flags(npages, "cuda") == 0
+
+
+# ---------------------------------------------------------------- memory: streams, far offsets
+
+def stream_calls(torch):
+    """name -> call(stream), the same result every time, as test_gpu_stream_memory takes them."""
+    c = Case(torch, "bf16", 8, 2, 64, [900, 330, 700], [3, 2, 4], seed=24)
+    c.all_bounds()
+    s = Pool(torch, [9, 5, 7], seed=2)
+    pages, counts = c.select(6)
+    w = torch.zeros((3, c.mp), device="cuda")
+    c.layer.weighed_workspace(9, "cuda")
+    s.layer.page_workspace(s.np, "cuda")
+    torch.cuda.synchronize()
+    return {"select_pages": lambda st: c.select(6, stream=st)[0], "counts": lambda st: c.select(6, stream=st)[1],
+            "selected": lambda st: c.attend(pages, counts, stream=st), "weighed": lambda st: c.weigh(w, stream=st),
+            "page_evict": lambda st: s.evict(9, stream=st)}, [c.layer, s.layer]
+
+
+@pytest.mark.parametrize("raw", [False, True], ids=["stream", "handle"])
+@pytest.mark.parametrize("native", [True, False], ids=["native", "python"])
+@pytest.mark.parametrize("name", ["select_pages", "counts", "selected", "weighed", "page_evict"])
+def test_results_on_another_stream(torch, name, native, raw, monkeypatch):
+    import test_gpu_stream_memory as memory
+    monkeypatch.setattr(memory, "make_calls", stream_calls)
+    memory.test_results_on_another_stream(torch, name, native, raw, monkeypatch)
+
+
+def test_two_calls_at_once(torch):
+    """On two streams, each with workspaces of its own."""
+    c = Case(torch, "fp8", 40, 8, 128, [6000, 2000, 64, 7000], seed=25)
+    c.all_bounds()
+    pages, counts = c.select(40)
+    w = torch.zeros((4, c.mp), device="cuda")
+    want = [c.attend(pages, counts), c.weigh(w), w]
+    n = c.layer.weighed_workspace(4, "cuda").numel()
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    spaces = [torch.zeros(n, dtype=torch.uint8, device="cuda") for _ in range(2)]
+    sums = [torch.zeros((4, c.mp), device="cuda") for _ in range(2)]
+    torch.cuda.synchronize()
+    got = []
+    for _ in range(8):
+        for st, ws, sm in zip(streams, spaces, sums):
+            with torch.cuda.stream(st):
+                sm.zero_()
+                p, k = c.select(40, workspace=ws)
+                got.append((p, k, c.attend(p, k, workspace=ws), c.weigh(sm, workspace=ws), sm.clone()))
+    torch.cuda.synchronize()
+    for p, k, o, o2, sm in got:
+        assert torch.equal(p, pages) and torch.equal(k, counts) and torch.equal(o, want[0]) and torch.equal(o2, want[1]) and \
+            torch.equal(sm, want[2])
+    assert all(c.flags(ws) == 0 for ws in spaces)
+
+
+def far_copy(torch, c, ids, npages):
+    """The case's pages at other ids of a pool of `npages`: (cache tensors, table)."""
+    out = []
+    for t, s in ((c.k, c.ks), (c.v, c.vs)):
+        x = torch.empty((npages,) + t.shape[1:], dtype=t.dtype, device="cuda")
+        sc = None if s is None else torch.empty((npages,) + s.shape[1:], device="cuda")
+        x.view(raw_type(torch, c.kv))[ids] = t.view(raw_type(torch, c.kv))
+        if sc is not None:
+            sc[ids] = s
+        out.append((x, sc))
+    table = torch.where(c.block_table >= 0, ids[c.block_table.clamp_min(0).long()].to(torch.int32), -1)
+    return out, table
+
+
+@pytest.mark.parametrize("kv,hkv,d,npages", [("bf16", 8, 128, 140000), ("fp8", 1, 64, 17200000)])
+def test_pages_past_32_bits(torch, kv, hkv, d, npages):
+    """Caches of more than 4 GiB; for the fp8 one, bounds of more than 2 GiB too."""
+    c = Case(torch, kv, 2 * hkv, hkv, d, [600, 64, 1000], seed=26)
+    c.all_bounds()
+    pages, counts = c.select(12)
+    want, w0 = c.attend(pages, counts), torch.zeros((3, c.mp), device="cuda")
+    want2 = c.weigh(w0)
+    ids = torch.cat([torch.arange(npages - c.npages // 2, npages), torch.arange(npages // 2, npages // 2 + c.npages - c.npages // 2)]).cuda()
+    ids = ids[torch.randperm(c.npages, device="cuda")]
+    ((k, ks), (v, vs)), table = far_copy(torch, c, ids, npages)
+    bounds = torch.empty((npages, hkv, 2, d), dtype=torch.int8, device="cuda")
+    bscale = torch.empty((npages, hkv), device="cuda")
+    L, w = c.layer, torch.zeros((3, c.mp), device="cuda")
+    L.page_bounds(k, table, c.seq_lens, bounds, bscale, first=torch.zeros(3, dtype=torch.int32, device="cuda"), k_scale=ks)
+    p, n = L.select_pages(c.q, bounds, bscale, table, c.seq_lens, 12)
+    o = L.selected(c.q, k, v, table, c.seq_lens, p, n, k_scale=ks, v_scale=vs)
+    o2 = L.weighed(c.q, k, v, table, c.seq_lens, w, k_scale=ks, v_scale=vs)
+    torch.cuda.synchronize()
+    used = torch.unique(c.block_table[c.block_table >= 0]).long()
+    assert torch.equal(bounds[ids[used]], c.bounds[used]) and torch.equal(bscale[ids[used]], c.bscale[used])
+    assert torch.equal(p, pages) and torch.equal(n, counts) and torch.equal(o, want) and torch.equal(o2, want2) and torch.equal(w, w0)
+    assert c.flags() == 0
+
+
+def test_weights_past_32_bits(torch):
+    """Rows of 40 million pages: what is kept of every page takes more than 2^31 values."""
+    from paper_2607_09207_amd import DecodeAttention
+    c = Case(torch, "bf16", 16, 1, 64, [700, 33, 400, 900], seed=27)
+    w0 = torch.zeros((4, c.mp), device="cuda")
+    want = c.weigh(w0)
+    mp = 40_000_000
+    L = DecodeAttention(16, 1, 64, 4, mp, "bf16", "bf16", "f32")
+    table = torch.full((4, mp), -1, dtype=torch.int32, device="cuda")
+    table[:, :c.mp] = c.block_table
+    w = torch.zeros((4, mp), device="cuda")
+    got = L.weighed(c.q, c.k, c.v, table, c.seq_lens, w)
+    torch.cuda.synchronize()
+    assert torch.equal(got, want) and torch.equal(w[:, :c.mp], w0) and not bool(w[:, c.mp:].any())
+    assert L.read_flags(workspace=L.weighed_workspace(4, "cuda")) == 0
