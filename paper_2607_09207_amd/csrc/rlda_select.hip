@@ -632,8 +632,15 @@ __device__ __forceinline__ void write_chosen(const uint32_t* keys, const Chosen&
 // gathers the others' keys.
 //   What a small call takes is its chain of dependent reads (the length, page ids, bounds) and
 // the search, so the ids and the queries are asked for before the length is known, and up to
-// kWavePages pages are searched by one wave, without barriers.  A long one is bound by the bounds
-// it reads: two buffers of tiles, one computed while the other's loads are in flight.
+// kWavePages pages are searched by one wave, without barriers: 7.2 us for 8 responses of up to
+// 256 pages (2 KV heads), 9.9 before.  A long one is bound by the bounds it reads: two buffers of
+// tiles, one computed while the other's loads are in flight.  64 sequences of 512 to 2048
+// pages, 4 KV heads (92 MB): 28.7 us, of them 3.4 until the first bounds are there, 11 (mean) to
+// 17 (the longest) for the products, 4 for the search and the list.  Rows of one sequence read
+// its bounds through their XCD's L2: 4 rows each of 16 sequences (8 KV heads, 82 MB in 64 rows, 21
+// MB of them from memory) 21 us.  Tried: several rows of a sequence to a workgroup (the same to
+// 31 us: fewer, longer chains), pieces of 512 pages for all rows (43 us: their starts under load),
+// 256 and 1024 threads (32 and 29.5 against 29.9 then).
 constexpr int kWavePages = 256;
 
 template <int D, bool QF32, int CAP>
