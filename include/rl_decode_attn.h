@@ -493,7 +493,7 @@ rlda_status rl_decode_attn_page_copy(rl_decode_attn_t handle, int32_t num_pages,
  *
  * Bounds of page p for KV head g, over its tokens' keys k_t (fp8: decode(byte) * k_scale):
  *   s = max |k_t[d]| / 127,
- *   lo[d] = max(floor(min_t k_t[d] / s), -127),  hi[d] = min(ceil(max_t k_t[d] / s), 127)
+ *   lo[d] = floor(min_t k_t[d] / s),  hi[d] = ceil(max_t k_t[d] / s),  both within +-127
  * in fp32, so s lo <= k_t <= s hi up to that rounding; s = 0 has bounds of 0, and a page with an
  * infinity or NaN has s = +inf and bounds of 0.
  *   bounds       [num_pages][Hkv][2][head_dim] int8 (lo, then hi), 16-byte aligned
@@ -519,8 +519,8 @@ rlda_status rl_decode_attn_page_bounds(rl_decode_attn_t handle, int32_t batch, i
  * last `recent` (>= 1) are chosen, and of the others the best by
  *   score(p) = s_p max_i (u_i sq_i),   u_i = sum_d max(q8_i[d] lo_p[d], q8_i[d] hi_p[d])
  * over the KV head's query heads i, up to `budget` (>= sink + recent) together; equal scores
- * go to the lower page.  q8 = rint(q / sq), sq = max |q| / 127 of the (row, head), in fp32; the
- * sum is one of integers and exact.  A head whose q holds an infinity or NaN counts as 0;
+ * go to the lower page.  q8 = rint(q / sq) within +-127, sq = max |q| / 127 of the (row, head), in
+ * fp32; the sum is one of integers and exact.  A head whose q holds an infinity or NaN counts as 0;
  * a page whose s is not finite is chosen before all others, one outside the pool after them.
  *   pages   [total_q][Hkv][budget] int32: indices of the row's pages, ascending, then -1
  *   counts  [total_q][Hkv] int32: min(n, budget)

@@ -137,8 +137,8 @@ __device__ __forceinline__ void store_out(const Params& p, int b, int qh, int d0
 __device__ __forceinline__ void store_row_lse(const Params& p, int row, int qh, float m, float l) {
   p.row_lse[(int64_t)row * p.num_q_heads + qh] = m + log2_of(l);
 }
-__device__ __forceinline__ void store_page_lse(const Params& p, int row, int qh, int page, float lse) {
-  p.page_lse[((int64_t)row * p.num_q_heads + qh) * p.max_pages + page] = lse;
+__device__ __forceinline__ float* pages_lse(const Params& p, int row, int qh) {
+  return p.page_lse + ((int64_t)row * p.num_q_heads + qh) * p.max_pages;
 }
 
 // Query heads of each KV head (a copy of Params::q_head, filled at kernel start):
@@ -274,6 +274,7 @@ struct Mfma {
   int rlo, rhi, rpos;
   float slope;
   float page;   // kWeighed: the last page's part of the row's sum, log2
+  float* z;     // ... and where the row's are kept
 
   __device__ __forceinline__ static int chunk_of(int qg, int s) {
     return FP8 ? 8 * (s >> 1) + 2 * qg + (s & 1) : 4 * s + qg;
@@ -789,9 +790,12 @@ struct Mfma {
     store_row<D, 4 * DT>(p, q0 + rr / G, s_qhead[g * G + rr % G], 4 * DT * qg, o, lt > 0.f ? 1.f / lt : 0.f);
   }
 
-  // kWeighed: the page's part for every row of the tile.
-  __device__ __forceinline__ void put_page(const Params& p, int b, int g, int j, int lane) const {
-    if (lane < p.group) store_page_lse(p, b, s_qhead[g * p.group + lane], j, page);
+  // kWeighed: where the rows of a segment keep their pages' parts, and one page's.
+  __device__ __forceinline__ void aim(const Params& p, int b, int g, int lane) {
+    z = pages_lse(p, b, s_qhead[g * p.group + (lane < p.group ? lane : 0)]);
+  }
+  __device__ __forceinline__ void put_page(const Params& p, int j, int lane) const {
+    if (lane < p.group) z[j] = page;
   }
 
   // A piece this wave covered entirely: normalise and write its rows.
@@ -835,6 +839,7 @@ struct Valu {
   float qv[GM][CW];
   float m[GM], l[GM];
   float page[GM];   // kWeighed: the last page's part of each row's sum, log2
+  float* z[GM];     // ... and where the rows' are kept
   int off;
 
   __device__ __forceinline__ void setup(const Params&, int lane, int32_t ss) {
@@ -919,10 +924,14 @@ struct Valu {
     }
   }
 
-  __device__ __forceinline__ void put_page(const Params& p, int b, int g, int j, int lane) const {
+  __device__ __forceinline__ void aim(const Params& p, int b, int g, int) {
+#pragma unroll
+    for (int h = 0; h < GM; ++h) z[h] = pages_lse(p, b, s_qhead[g * p.group + (h < p.group ? h : 0)]);
+  }
+  __device__ __forceinline__ void put_page(const Params& p, int j, int lane) const {
 #pragma unroll
     for (int h = 0; h < GM; ++h)
-      if (h < p.group && lane == 0) store_page_lse(p, b, s_qhead[g * p.group + h], j, page[h]);
+      if (h < p.group && lane == 0) z[h][j] = page[h];
   }
 
   template <bool WEIGH = false>
@@ -1142,6 +1151,7 @@ __device__ __forceinline__ void whole_segment(const Params& p, int b, int g, int
   typename Pol::QOp qo;
   Pol::load_q(qo, p, b, g, lane, true);
   st.begin(qo, p, b, g, lane);
+  if constexpr (ROWS == kWeighed) st.aim(p, b, g, lane);
   if constexpr (MOD) {
     const int L = kPage * (first + nb - 1) + tail;
     st.see(lo, L, L - 1, kPage * (first + j0), slope);
@@ -1194,7 +1204,7 @@ __device__ __forceinline__ void whole_segment(const Params& p, int b, int g, int
             st.compute_mod(p, fr[k], nullptr, lane, sval[k] > 0, p.scale_log2 * skm[k], svm[k]);
           else
             st.template compute<false, kAlways, ROWS == kWeighed>(fr[k], lane, sval[k], p.scale_log2 * skm[k], svm[k]);
-          if constexpr (ROWS == kWeighed) st.put_page(p, b, g, cb + i + k, lane);
+          if constexpr (ROWS == kWeighed) st.put_page(p, cb + i + k, lane);
         }
       }
     }
@@ -1873,9 +1883,10 @@ void decode_attention_kernel(const Params p) {
           if (info & (kInfoFirst | kInfoStart)) {
             const int pre = s_pre[b];
             jpage = w0 + k - Hs * pre - g * (s_pre[b + 1] - pre);
+            st.aim(p, b, g, lane);
           }
           st.template compute<false, kAlways, true>(f, lane, info & kInfoTok, p.scale_log2 * km, vm);
-          st.put_page(p, b, g, jpage++, lane);
+          st.put_page(p, jpage++, lane);
         } else if constexpr (ROWS == kListed) {
           st.template compute<false, kAlways>(f, lane, info & kInfoTok, p.scale_log2 * km, vm);
         } else

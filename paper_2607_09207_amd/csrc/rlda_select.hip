@@ -3,7 +3,7 @@
 // that got the least weight.
 //
 // Bounds.  For the keys k_t of a page and a KV head, s = max |k| / 127 and, per element,
-//   hi = min(ceil(max_t k_t / s), 127),  lo = max(floor(min_t k_t / s), -127)      (8 bits each)
+//   hi = ceil(max_t k_t / s),  lo = floor(min_t k_t / s),   within +-127      (8 bits each)
 // so that s lo <= k_t <= s hi.  A query's score with any of these keys is then at most
 // s sum_d max(q_d lo_d, q_d hi_d) = s (min(q, 0) . lo + max(q, 0) . hi): one product of length
 // 2 d a page, over 1/32 of the bytes that its bf16 keys and values have.
@@ -189,7 +189,8 @@ __global__ __launch_bounds__(kThreads) void page_bounds_kernel(const SelectParam
 #pragma unroll
     for (int i = 0; i < V; ++i) {
       const float y = v[i] / s;
-      const int byte = lower ? (int)fmaxf(__builtin_floorf(y), -127.f) : (int)fminf(__builtin_ceilf(y), 127.f);
+      // (Beyond 127 by the rounding of s, far beyond where s is subnormal.)
+      const int byte = (int)fmaxf(fminf(lower ? __builtin_floorf(y) : __builtin_ceilf(y), 127.f), -127.f);
       out |= (uint32_t)(byte & 255) << (8 * i);
     }
     if (!(s > 0.f) || odd) out = 0;
@@ -514,7 +515,7 @@ __device__ __forceinline__ void round_q(const SelectParams& p, int row, int g, Q
     const float sq = __builtin_amdgcn_ballot_w64(odd) != 0 ? 0.f : amax / 127.f;
 #pragma unroll
     for (int e = 0; e < E; ++e) {
-      const int q = sq > 0.f ? (int)__builtin_rintf(x[i][e] / sq) : 0;
+      const int q = sq > 0.f ? (int)fmaxf(fminf(__builtin_rintf(x[i][e] / sq), 127.f), -127.f) : 0;
       s.bytes[k][64 * e + lane] = (int8_t)min(q, 0);
       s.bytes[k][D + 64 * e + lane] = (int8_t)max(q, 0);
     }

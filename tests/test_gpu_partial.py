@@ -193,8 +193,8 @@ def plain_bounds(torch, x):
     s = over_127(y.abs().amax(dim=(1, 2)))
     by = torch.where(s > 0, s, 1.0)[:, None]
     zero = (s == 0)[:, None]
-    lo = torch.where(zero, 0.0, (y.amin(1) / by).floor().clamp_min(-127))
-    hi = torch.where(zero, 0.0, (y.amax(1) / by).ceil().clamp_max(127))
+    lo = torch.where(zero, 0.0, (y.amin(1) / by).floor().clamp(-127, 127))
+    hi = torch.where(zero, 0.0, (y.amax(1) / by).ceil().clamp(-127, 127))
     return torch.stack([lo, hi], 1).to(torch.int8), torch.where(odd, math.inf, s)
 
 
@@ -248,8 +248,11 @@ def test_bounds_of_odd_keys(torch, kv, hq, hkv, d):
         c.k[t[4], 0, 2, 2] = torch.finfo(c.k.dtype).max
         c.k[t[4], 0, 2, 3] = -torch.finfo(c.k.dtype).max
         c.k[t[5], 0] = -0.0
+        c.k[t[2], 0] = c.k[t[2], 0] * 1e-38 * 1e-5   # quotients far beyond 127, one sign alone in some elements
+        c.k[t[5], 1] = -c.k[t[5], 1].abs() * 1e-38 * 1e-4
     else:
         c.ks[t[2], 0], c.ks[t[3], 0], c.ks[t[4], 1], c.ks[t[5], 0] = -0.01, 0.0, math.inf, 1e38
+        c.ks[t[2], 1], c.ks[t[5], 1] = 2e-45, -3e-45
     c.all_bounds()
     want, scale = expect_bounds(c, [0], c.bounds, c.bscale)
     torch.cuda.synchronize()
@@ -282,7 +285,7 @@ def plain_choice(c, budget, sink, recent):
     fine = q.isfinite().all(-1, keepdim=True)
     q = torch.where(fine, q, 0.0)
     sq = over_127(q.abs().amax(-1, keepdim=True))
-    q8 = torch.where(sq > 0, (q / torch.where(sq > 0, sq, 1.0)).round(), 0.0).double()
+    q8 = torch.where(sq > 0, (q / torch.where(sq > 0, sq, 1.0)).round().clamp(-127, 127), 0.0).double()
     for r, b, L in c.row_list():
         n = max(-(-L // PAGE), 0)
         page = torch.from_numpy(c.block_table[b, :n].cpu().numpy().astype(np.int64)).cuda()
@@ -365,6 +368,17 @@ def test_choice_with_ties_and_odd_values(torch):
         assert np.array_equal(counts.cpu().numpy(), want_counts) and np.array_equal(pages.cpu().numpy(), want_pages)
     assert {20, 31} <= set(c.select(5, sink=0, recent=1)[0][2, 0].tolist())
     assert c.flags() == 1
+
+
+def test_choice_by_tiny_queries(torch):
+    """Queries whose scale is subnormal: their quotients end at 127."""
+    c = Case(torch, "f32", 2, 2, 64, [PAGE * 60, PAGE * 70], seed=30)
+    c.all_bounds()
+    c.q[0] = torch.randint(-190, 191, c.q[0].shape, device="cuda").float() * 2.0 ** -149
+    c.q[1, 0] = 0.0
+    pages, counts = c.select(9)
+    want_pages, want_counts = plain_choice(c, 9, 1, 1)
+    assert np.array_equal(counts.cpu().numpy(), want_counts) and np.array_equal(pages.cpu().numpy(), want_pages)
 
 
 def test_choice_head_map_and_outputs(torch):
