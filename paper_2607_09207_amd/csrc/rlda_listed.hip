@@ -22,8 +22,26 @@ namespace {
 // with every head, eight at a time: 11.6 us for 64 long-tailed sequences of 28 heads).
 __global__ __launch_bounds__(kThreads) void page_weights_kernel(const Params p) {
   __shared__ float s_sum[kWaves][64];
+  constexpr int H = 8;   // heads of a wave whose parts are asked for together
   const int b = blockIdx.x, Hq = p.num_q_heads, cap = p.max_pages * kPage;
   const int lane = threadIdx.x & 63, wave = uni((int)(threadIdx.x >> 6));
+  const auto load = [&](float* a, int row, int h0, int j, bool seen) {
+    const float* zj = p.page_lse + (int64_t)row * Hq * p.max_pages + j;
+#pragma unroll
+    for (int k = 0; k < H; ++k) {
+      const int h = h0 + k * kWaves;
+      a[k] = seen && h < Hq ? zj[(int64_t)h * p.max_pages] : neg_inf();
+    }
+  };
+  float* const w = p.weights + (int64_t)b * p.max_pages;
+  // One row a sequence: the first pages' parts and weights, ahead of the length.
+  const bool early = !p.q_start && blockIdx.y == 0;
+  float first[H], old = 0.f;
+  if (early) {
+    const int j = min(lane, p.max_pages - 1);
+    load(first, b, wave, j, true);
+    if (wave == 0 && p.decay != 0.f) old = w[j];
+  }
   const int L = min(max(p.seq_lens[b], 0), cap), npages = (L + kPage - 1) / kPage;
   int q0 = b, n = 1;
   if (p.q_start) {
@@ -34,20 +52,22 @@ __global__ __launch_bounds__(kThreads) void page_weights_kernel(const Params p) 
   if (n == 0) return;
   for (int j0 = blockIdx.y * 64; j0 < npages; j0 += gridDim.y * 64) {
     const int j = j0 + lane, at = min(j, npages - 1);
+    const bool have = early && j0 == 0;
+    if (!have && wave == 0 && p.decay != 0.f) old = w[at];
     float got = 0.f;
     for (int i = 0; i < n; ++i) {
       const bool seen = L - n + i >= kPage * at;   // by the row
       const float* z = p.row_lse + (int64_t)(q0 + i) * Hq;
-      const float* zj = p.page_lse + (int64_t)(q0 + i) * Hq * p.max_pages + at;
-      for (int h0 = wave; h0 < Hq; h0 += 8 * kWaves) {
-        float a[8];
+      for (int h0 = wave; h0 < Hq; h0 += H * kWaves) {
+        float a[H];
+        if (have && h0 == wave) {
 #pragma unroll
-        for (int k = 0; k < 8; ++k) {
-          const int h = h0 + k * kWaves;
-          a[k] = seen && h < Hq ? zj[(int64_t)h * p.max_pages] : neg_inf();
+          for (int k = 0; k < H; ++k) a[k] = first[k];   // (past the pages: used by no lane that writes)
+        } else {
+          load(a, q0 + i, h0, at, seen);
         }
 #pragma unroll
-        for (int k = 0; k < 8; ++k)   // (no key: nothing, whatever the row's sum is)
+        for (int k = 0; k < H; ++k)   // (no key: nothing, whatever the row's sum is)
           if (a[k] != neg_inf()) got += __builtin_amdgcn_exp2f(a[k] - z[min(h0 + k * kWaves, Hq - 1)]);
       }
     }
@@ -55,8 +75,7 @@ __global__ __launch_bounds__(kThreads) void page_weights_kernel(const Params p) 
     __syncthreads();
     if (wave == 0 && j < npages) {
       got = s_sum[0][lane] + s_sum[1][lane] + s_sum[2][lane] + s_sum[3][lane];
-      float* w = p.weights + (int64_t)b * p.max_pages + j;
-      *w = p.decay == 0.f ? got : __builtin_fmaf(p.decay, *w, got);
+      w[j] = p.decay == 0.f ? got : __builtin_fmaf(p.decay, old, got);
     }
     __syncthreads();
   }
