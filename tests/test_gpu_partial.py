@@ -390,6 +390,14 @@ def test_choice_head_map_and_outputs(torch):
     want_pages, want_counts = plain_choice(c, 7, 1, 1)
     assert got[0] is out[0] and got[1] is out[1]
     assert np.array_equal(out[0].cpu().numpy(), want_pages) and np.array_equal(out[1].cpu().numpy(), want_counts)
+    o, tol, _ = c.want(lambda r, g, L: want_pages[r, g, :want_counts[r, g]])
+    c.check(c.attend(*out), o, tol)
+    o, tol, parts = c.want(lambda r, g, L: range(-(-L // PAGE)))
+    w0 = torch.zeros((2, c.mp), device="cuda")
+    w = w0.clone()
+    c.check(c.weigh(w), o, tol)
+    want, wtol = expect_weights(c, parts, w0, 1.0)
+    assert bool(((w.double() - want).abs() <= wtol + 1e-30).all())
 
 
 def test_rows_of_no_sequence(torch):
@@ -869,6 +877,41 @@ def test_graph(torch):
         for a, b in zip(held, want):
             assert torch.equal(a, b), i
         c.weigh(torch.zeros_like(w))
+    assert c.flags() == 0
+
+
+def test_two_graphs_on_one_workspace(torch):
+    """Captured one after the other, replayed in turn with eager calls between."""
+    c = Case(torch, "fp8", 8, 2, 64, [3000, 40, 700], seed=29)
+    c.all_bounds()
+    L = c.layer
+    L.workspace("cuda"), L.weighed_workspace(3, "cuda")
+    w = [torch.zeros((3, c.mp), device="cuda") for _ in range(2)]
+    qs = [c.q, (c.q.float() * -0.7 + 0.1).to(c.q.dtype)]
+
+    def step(i):
+        pages, counts = L.select_pages(qs[i], c.bounds, c.bscale, c.block_table, c.seq_lens, 10 + 30 * i)
+        return (pages, counts, L.selected(qs[i], *c.cache(), pages, counts, **c.scales()),
+                L.weighed(qs[i], *c.cache(), w[i], decay=0.0, **c.scales()), w[i])
+
+    want = [[t.clone() for t in step(i)] for i in range(2)]
+    for x in want:   # (weights past a sequence's pages stay as they are: 77, below)
+        x[4][torch.arange(c.mp, device="cuda")[None, :] * PAGE >= c.seq_lens[:, None]] = 77
+    torch.cuda.synchronize()
+    graphs, held = [torch.cuda.CUDAGraph() for _ in range(2)], []
+    for i in range(2):
+        with torch.cuda.graph(graphs[i]):
+            held.append(step(i))
+    for turn in range(6):
+        for t in held[0] + held[1]:
+            t.fill_(77)
+        torch.cuda.synchronize()
+        graphs[turn % 2].replay()
+        graphs[1 - turn % 2].replay()
+        c.attend(want[0][0], want[0][1])
+        torch.cuda.synchronize()
+        for i in range(2):
+            assert all(torch.equal(a, b) for a, b in zip(held[i], want[i])), (turn, i)
     assert c.flags() == 0
 
 
