@@ -970,18 +970,17 @@ constexpr int kActAll = 7;              // kActAll: a prompt page, every member'
 
 // The j-th page that (row, KV head) reads, of a row of sequence `seq` that sees L tokens:
 // (page id as read, tokens of it that count).  A list's entries that are none of the row's
-// pages, and places past its count, are kNoPage: nothing of any page, its scales neither.
-constexpr int kNoPage = -0x7fffffff - 1;
+// pages, and places past its count, have page -1 and no token: nothing is read for them.
 template <RowsForm ROWS>
 __device__ __forceinline__ int2 row_page(const Params& p, int row, int seq, int g, int j, int L) {
   int at = j;
   if constexpr (ROWS == kListed) {
     const int64_t list = (int64_t)row * p.num_kv_heads + g;
-    if (j >= p.list_counts[list]) return make_int2(kNoPage, 0);
+    if (j >= p.list_counts[list]) return make_int2(-1, 0);
     at = p.list[list * p.budget + j];
     if (at < 0 || at >= (L + kPage - 1) / kPage) {
       atomicOr(p.flags, kFlagBadPage);
-      return make_int2(kNoPage, 0);
+      return make_int2(-1, 0);
     }
   }
   return make_int2(p.block_table[(int64_t)seq * p.max_pages + at], min(kPage, L - kPage * at));
@@ -1172,7 +1171,7 @@ __device__ __forceinline__ void whole_segment(const Params& p, int b, int g, int
       if (k < cn) {
         pk = __builtin_amdgcn_readlane(pid, k);
         if ((unsigned)pk >= (unsigned)p.num_pages) {   // not a page of the pool: contributes nothing
-          if (lane == 0 && (ROWS != kListed || pk != kNoPage)) atomicOr(p.flags, kFlagBadPage);
+          if (lane == 0 && (ROWS != kListed || __builtin_amdgcn_readlane(row_at.y, k) != 0)) atomicOr(p.flags, kFlagBadPage);
           pk = -1;
         }
       }
@@ -1752,7 +1751,7 @@ void decode_attention_kernel(const Params p) {
           pk = __builtin_amdgcn_readlane(in_cur ? cur.pid : nxt.pid, l);
           info = __builtin_amdgcn_readlane(in_cur ? cur.info : nxt.info, l);
           if ((unsigned)pk >= (unsigned)p.num_pages) {   // not a page of the pool: contributes nothing
-            if (lane == 0 && (ROWS != kListed || pk != kNoPage)) atomicOr(p.flags, kFlagBadPage);
+            if (lane == 0 && (ROWS != kListed || (info & kInfoTok) != 0)) atomicOr(p.flags, kFlagBadPage);
             pk = -1;
             info &= ~kInfoTok;
           }

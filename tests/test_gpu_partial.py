@@ -521,6 +521,22 @@ def test_selected_twice_the_same_page_and_bad_entries(torch):
     assert c.flags() == 1 and bool((got[1] == 0).all())
 
 
+@pytest.mark.parametrize("ranges", [0, 3])
+@pytest.mark.parametrize("bad", [-1, -2 ** 31, 2 ** 31 - 1])
+def test_listed_pages_outside_the_pool(torch, bad, ranges):
+    c = Case(torch, "bf16", 8, 2, 64, [200, 330], seed=31, ranges=ranges)
+    pages = torch.tensor([[3, 7, 1], [0, 5, 2]], dtype=torch.int32, device="cuda")[:, None].expand(2, 2, 3).contiguous()
+    counts = torch.tensor([2, 3], dtype=torch.int32, device="cuda")[:, None].expand(2, 2).contiguous()
+    c.block_table[0, 1] = bad     # beyond the count
+    c.attend(pages, counts)
+    assert c.flags() == 0
+    c.block_table[1, 5] = bad
+    got = c.attend(pages, counts)
+    assert c.flags() == 1
+    o, tol, _ = c.want(lambda r, g, L: [[3, 7], [0, 2]][r])
+    c.check(got, o, tol)
+
+
 def test_selected_keys_that_are_not_listed_have_no_part(torch):
     """NaN and infinities in every other page, and behind a row's own position."""
     for kv in ("bf16", "fp8", "f32"):
