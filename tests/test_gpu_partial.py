@@ -768,6 +768,31 @@ def test_evict_wrong_state(torch):
     assert np.array_equal(s.dev[1].cpu().numpy()[0], s.table[0]) and s.dev[2].tolist()[0] == 20 * PAGE + 1
 
 
+def test_growth_and_eviction_in_a_pool_that_runs_dry(torch):
+    """A shared page that some rows drop stays taken, so a pool with room for one page a row runs
+    short: rows that get none keep what they have, and are not evicted."""
+    s = Pool(torch, [12] * 24, mp=16, spare=30, seed=12, shared=8)
+    add = torch.full((24,), PAGE, dtype=torch.int32, device="cuda")
+    rng = np.random.default_rng(13)
+    short = 0
+    for _ in range(8):
+        s.w[:, :12] = rng.random((24, 12))   # other pages go from every row
+        s.dev[3].copy_(torch.from_numpy(s.w))
+        free = list(np.flatnonzero(s.refs == 0))
+        served = np.arange(24) < len(free)   # a page of tokens more needs a page
+        for b in np.flatnonzero(served):
+            s.refs[free[b]], s.table[b, -(-int(s.lens[b]) // PAGE)] = 1, free[b]
+            s.lens[b] += PAGE
+        short += int((~served).sum())
+        s.layer.page_grow(*s.dev[:3], add)
+        want = s.expect(12, 2, 2)
+        s.check(s.evict(12, sink=2, recent=2), want)
+        assert np.array_equal(want[4], served.astype(np.int32))
+        assert s.layer.page_flags(s.np, "cuda") == (0 if served.all() else 16)   # (read and cleared)
+        s.refs, s.table, s.lens, s.w = want[:4]
+    assert short > 0
+
+
 # ---------------------------------------------------------------- refusals
 
 def test_refusals(torch):
