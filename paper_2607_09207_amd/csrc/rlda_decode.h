@@ -970,20 +970,26 @@ constexpr int kActAll = 7;              // kActAll: a prompt page, every member'
 
 // The j-th page that (row, KV head) reads, of a row of sequence `seq` that sees L tokens:
 // (page id as read, tokens of it that count).  A list's entries that are none of the row's
-// pages, and places past its count, have page -1 and no token: nothing is read for them.
-template <RowsForm ROWS>
+// pages, and places past its count, are kNoPage with no token: nothing is read for them.
+// APART: no other entry is kNoPage, so that the page alone tells them (the entry is waited for).
+// A whole segment needs it at once: 12.4 us for four stragglers' lists with the tokens asked
+// as well, 11.7 so.  The page stream has later ids in flight, and asks the tokens: 100.6 us for
+// 256 lists of 64 pages when waiting, 96.1 so.
+constexpr int kNoPage = -0x7fffffff - 1;
+template <RowsForm ROWS, bool APART = false>
 __device__ __forceinline__ int2 row_page(const Params& p, int row, int seq, int g, int j, int L) {
   int at = j;
   if constexpr (ROWS == kListed) {
     const int64_t list = (int64_t)row * p.num_kv_heads + g;
-    if (j >= p.list_counts[list]) return make_int2(-1, 0);
+    if (j >= p.list_counts[list]) return make_int2(kNoPage, 0);
     at = p.list[list * p.budget + j];
     if (at < 0 || at >= (L + kPage - 1) / kPage) {
       atomicOr(p.flags, kFlagBadPage);
-      return make_int2(-1, 0);
+      return make_int2(kNoPage, 0);
     }
   }
-  return make_int2(p.block_table[(int64_t)seq * p.max_pages + at], min(kPage, L - kPage * at));
+  const int page = p.block_table[(int64_t)seq * p.max_pages + at];
+  return make_int2(APART ? max(page, kNoPage + 1) : page, min(kPage, L - kPage * at));
 }
 
 // The page id is returned as read; it is checked where it is used, so that
@@ -1142,7 +1148,7 @@ __device__ __forceinline__ void whole_segment(const Params& p, int b, int g, int
   const int32_t* bt = p.block_table + (int64_t)b * p.max_pages + first;
   int2 row_at = make_int2(-1, 0);
   if constexpr (ROWS != kSequences) {
-    if (j0 < j1) row_at = row_page<ROWS>(p, b, lo, g, j0 + min(lane, j1 - j0 - 1), tail);
+    if (j0 < j1) row_at = row_page<ROWS, ROWS == kListed>(p, b, lo, g, j0 + min(lane, j1 - j0 - 1), tail);
   }
   int pid = ROWS != kSequences ? row_at.x : j0 < j1 ? bt[j0 + min(lane, j1 - j0 - 1)] : -1;
   Pol st;
@@ -1158,7 +1164,7 @@ __device__ __forceinline__ void whole_segment(const Params& p, int b, int g, int
   for (int cb = j0; cb < j1; cb += kChunk) {
     const int cn = min(kChunk, j1 - cb);
     if constexpr (ROWS != kSequences) {
-      if (cb > j0) row_at = row_page<ROWS>(p, b, lo, g, cb + min(lane, cn - 1), tail);
+      if (cb > j0) row_at = row_page<ROWS, ROWS == kListed>(p, b, lo, g, cb + min(lane, cn - 1), tail);
       pid = row_at.x;
     } else {
       if (cb > j0) pid = bt[cb + min(lane, cn - 1)];
@@ -1171,7 +1177,7 @@ __device__ __forceinline__ void whole_segment(const Params& p, int b, int g, int
       if (k < cn) {
         pk = __builtin_amdgcn_readlane(pid, k);
         if ((unsigned)pk >= (unsigned)p.num_pages) {   // not a page of the pool: contributes nothing
-          if (lane == 0 && (ROWS != kListed || __builtin_amdgcn_readlane(row_at.y, k) != 0)) atomicOr(p.flags, kFlagBadPage);
+          if (lane == 0 && (ROWS != kListed || pk != kNoPage)) atomicOr(p.flags, kFlagBadPage);
           pk = -1;
         }
       }
