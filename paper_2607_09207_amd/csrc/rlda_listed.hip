@@ -5,7 +5,7 @@
 // stored beside the attention (kWeighed), 4 bytes a page and query head.
 //   Reading the pages bounds both: 128 listed pages of each of 64 sequences (28/4 heads, bf16, 267
 // MB) 46 us, 5.8 TB/s; 64 of each of 256 (40/8, fp8, 532 MB) 96.5, 5.5 TB/s; weights of a long-tailed
-// batch of 64 (28/4, bf16, 462 MB) 81 and 4.8 for the second launch, the plain call 79.6.  The
+// batch of 64 (28/4, bf16, 462 MB) 86.9 of which 4.8 are the second launch, the plain call 79.6.  The
 // probabilities' bf16 remainders enter every product here: the calls take the same time with
 // and without, and a bf16 result's error falls from 2.4e-3 to the 1.7e-3 of its own rounding.
 //   With z = log2 of the sum of exp2(score) over a row's keys and z_j over page j's of them,
