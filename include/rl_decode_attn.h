@@ -525,7 +525,9 @@ rlda_status rl_decode_attn_page_bounds(rl_decode_attn_t handle, int32_t batch, i
  *   pages   [total_q][Hkv][budget] int32: indices of the row's pages, ascending, then -1
  *   counts  [total_q][Hkv] int32: min(n, budget)
  * Rows that no sequence names, and those of inconsistent q_start entries (flag bit 1), are not
- * written; rows before token 0 (n_b > seq_lens[b], flag bit 1) choose nothing.
+ * written; rows before token 0 (n_b > seq_lens[b], flag bit 1) choose nothing.  Where entries run
+ * backwards, a row that several sequences claim is one's of them or nobody's: the same here, in
+ * rl_decode_attn_run_selected and in rl_decode_attn_run_weighed.
  * max_pages_per_seq up to 32768, budget up to 2^24 (else RLDA_ERR_UNSUPPORTED).  workspace: as
  * for rl_decode_attn_run.  One kernel, asynchronous.
  */

@@ -1092,20 +1092,30 @@ __device__ __forceinline__ int2 seen_keys(const Params& p, int b, int row, int p
 
 // Query rows as units, with q_start: marks in s_seq every row that begins a sequence's rows
 // with 1 + that sequence, and returns the largest mark before row `lo`, the first of the
-// thread's rows [lo, hi).  (All threads; marks of inconsistent offsets are found out where
-// they are used.)
-__device__ __forceinline__ int rows_before(const Params& p, int32_t* s_seq, int32_t* s_scan, int rows, int cap, int lo, int hi,
-                                           int* bad) {
+// thread's rows [lo, hi).  (All threads.)  Where offsets disagree, every row is searched for
+// itself, as the choice of pages does (rows_of), and marked with its own sequence: -1 then.
+__device__ __forceinline__ int rows_before(const Params& p, int32_t* s_seq, int32_t* s_scan, int32_t* s_odd, int rows, int cap,
+                                           int lo, int hi, int* bad) {
   const int tid = threadIdx.x, lane = tid & 63, wave = uni(tid >> 6);
   for (int i = tid; i < rows; i += kThreads) s_seq[i] = 0;
+  if (tid == 0) *s_odd = 0;
   __syncthreads();
   for (int b = tid; b < p.batch; b += kThreads) {
     const int q0 = p.q_start[b], q1 = p.q_start[b + 1], L = p.seq_lens[b];
     const bool ok = q0 >= 0 && q0 <= q1 && q1 <= p.total_q;
     if (!ok || L < 0 || L > cap || q1 - q0 > L) *bad = 1;
+    if (!ok) *s_odd = 1;
     if (ok && q0 < q1) atomicMax(&s_seq[q0], b + 1);
   }
   __syncthreads();
+  if (*s_odd) {
+    for (int r = wave; r < rows; r += kWaves) {
+      const RowsOf at = rows_of(p.q_start, p.seq_lens, p.batch, p.total_q, r);
+      if (lane == 0) s_seq[r] = at.seq + 1;
+    }
+    __syncthreads();
+    return -1;
+  }
   int most = 0;
   for (int i = lo; i < hi; ++i) most = max(most, s_seq[i]);
   const int incl = wave_scan_max(most);
@@ -1448,14 +1458,14 @@ void decode_attention_kernel(const Params p) {
       int sum = 0, cnt = 0, most = 0, bad = 0;   // pages, non-empty units, the largest unit
       int seq_at = 0;   // query rows as units: 1 + the sequence of the last row before b
       if constexpr (ROWS != kSequences) {
-        if (p.q_start) seq_at = rows_before(p, s_ppre, s_scan, nunits, cap, lo, hi, &bad);
+        if (p.q_start) seq_at = rows_before(p, s_ppre, s_scan, s_scan_max, nunits, cap, lo, hi, &bad);
       }
       for (int b = lo; b < hi; ++b) {
         if constexpr (ROWS != kSequences) {
           int seq = b, L;
           if (p.q_start) {
-            seq_at = max(seq_at, s_ppre[b]);
-            seq = seq_at - 1;
+            if (seq_at >= 0) seq_at = max(seq_at, s_ppre[b]);
+            seq = (seq_at >= 0 ? seq_at : s_ppre[b]) - 1;
             const int q0 = seq >= 0 ? p.q_start[seq] : 0, q1 = seq >= 0 ? p.q_start[seq + 1] : 0;
             if (b < q0 || b >= q1 || q1 > p.total_q) seq = -1;
             L = seq >= 0 ? min(max(p.seq_lens[seq], 0), cap) - (q1 - 1 - b) : 0;

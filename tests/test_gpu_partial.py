@@ -433,6 +433,63 @@ def test_rows_of_no_sequence(torch):
     assert bool((o[:3] == 0).all()) and bool((o[3:] != 0).any(-1).all())
 
 
+def owners(starts, n):
+    """The sequence of every row (-1: none): the one that a search of 64 entries a step ends at, if its
+    offsets agree and the row lies between them."""
+    got = []
+    for r in range(n):
+        lo, hi = 0, len(starts)
+        while lo < hi:
+            step = -(-(hi - lo) // 64)
+            lo += step * sum(starts[at] <= r for at in range(lo + step - 1, min(hi, lo + 64 * step), step))
+            hi = min(hi, lo + step - 1)
+        got.append(lo - 1 if 0 < lo < len(starts) and 0 <= starts[lo - 1] <= r < starts[lo] <= n else -1)
+    return got
+
+
+CLAIMED = [[0, 5, 3, 9], [0, 5, 0, 9], [0, 9, 2, 4, 9], [0, 8, 3, 7], [70, 40, 5], [600, 520, 300]]
+
+
+def claimed_case(torch, starts, kv):
+    """Offsets that run backwards, so that two sequences claim the same rows; the rows as they are
+    taken (owners), and those of no sequence."""
+    n = 12
+    if starts[0] > 0:   # one row a sequence, but the entry of one goes back
+        n, (batch, b, to) = starts[0], starts
+        starts = list(range(batch + 1))
+        starts[b] = to
+    B = len(starts) - 1
+    rng = np.random.default_rng(B)
+    lens = [400, 50, 90, 130] if B < 5 else list(rng.integers(40, 100, size=B))
+    c = Case(torch, kv, 4, 2, 64, lens[:B], [n] + [0] * (B - 1), seed=33, extra_pages=1)
+    own = owners(starts, n)
+    c.q_start = torch.tensor(starts, dtype=torch.int32, device="cuda")
+    c.rows = np.bincount([b for b in own if b >= 0], minlength=B)
+    rows = [(r, b, int(c.lens[b]) - (starts[b + 1] - 1 - r)) for r, b in enumerate(own) if b >= 0]
+    c.row_list = lambda: rows
+    c.all_bounds()
+    return c, [r for r, b in enumerate(own) if b >= 0], [r for r, b in enumerate(own) if b < 0]
+
+
+@pytest.mark.parametrize("kv", ["bf16", "fp8", "f32"])
+@pytest.mark.parametrize("starts", CLAIMED, ids=["overlap", "whole", "inside", "hole", "70", "600"])
+def test_choice_of_rows_that_two_sequences_claim(torch, starts, kv):
+    """The choice and the attention over it take a row as the same sequence's, and say so."""
+    c, mine, free = claimed_case(torch, starts, kv)
+    n = len(c.q)
+    out = (torch.full((n, 2, 3), 99, dtype=torch.int32, device="cuda"), torch.full((n, 2), 99, dtype=torch.int32, device="cuda"))
+    c.select(3, out=out)
+    assert c.flags() == 2
+    pages, counts = plain_choice(c, 3, 1, 1)
+    assert np.array_equal(out[0].cpu().numpy()[mine], pages[mine]) and np.array_equal(out[1].cpu().numpy()[mine], counts[mine])
+    assert bool((out[0][free] == 99).all()) and bool((out[1][free] == 99).all())
+    o, tol, _ = c.want(lambda r, g, L: pages[r, g, :counts[r, g]])
+    got = torch.full((n, 4, 64), 7.0, device="cuda")
+    c.attend(torch.from_numpy(pages).cuda(), torch.from_numpy(counts).cuda(), out=got)
+    assert c.flags() == 2 and bool((got[free] == 7).all())
+    c.check(got[mine], o[mine], tol[mine])
+
+
 # ---------------------------------------------------------------- attention over the chosen pages
 
 def random_lists(c, budget, seed, full=False):
