@@ -567,6 +567,8 @@ rlda_status rl_decode_attn_run_selected(rl_decode_attn_t handle, int32_t batch, 
  *   weights  [batch][max_pages_per_seq] fp32; entries at or past a sequence's pages stay as they
  *            were.  A row of the table that is given to another sequence starts with zeros
  *            (the caller's).
+ * Rows are whose they are for rl_decode_attn_select_pages, where entries of q_start run backwards
+ * too; a sequence that then has none keeps its weights.
  * Every kv_dtype; total_q <= 4096 (RLDA_ERR_UNSUPPORTED).  A row whose scores are NaN makes its
  * sequence's weights NaN.  workspace: >= rl_decode_attn_weighed_workspace_size(total_q) bytes, with
  * the rules of rl_decode_attn_run (whose calls it serves too).  Two kernels, asynchronous;

@@ -1586,6 +1586,12 @@ void decode_attention_kernel(const Params p) {
   const int64_t C = uni64((int64_t)Hs * (s_pre[nunits] + S * s_ne[nunits]));
   auto cost_of = [&](int64_t pos, int b, int gv) { return pos + (int64_t)S * (Hs * s_ne[b] + gv + 1); };
 
+  if constexpr (ROWS == kWeighed) {   // as whose the rows are taken, for the second launch
+    if (p.q_start) {
+      for (int b = blockIdx.x * kThreads + tid; b < nunits; b += W * kThreads) p.row_seq[b] = s_ppre[b];
+    }
+  }
+
   // 2. Sequences with no pages left to stream: zero rows, or (grouped runs) the
   //    normalised prompt-pass result when the prompt is the whole sequence.
   for (int b = blockIdx.x; b < nunits; b += W) {

@@ -55,16 +55,17 @@ inline WsLayout layout_of(const rlda_handle* h) {
 }
 
 // Calls that keep the pages' weights: the plain workspace, then the parts of every row's
-// softmax, [rows][Hq][max_pages] and [rows][Hq].
+// softmax, [rows][Hq][max_pages] and [rows][Hq], and the sequence that every row was taken as.
 struct WeighedLayout {
-  size_t page_lse, row_lse, total;
+  size_t page_lse, row_lse, row_seq, total;
 };
 inline WeighedLayout weighed_layout(const rlda_handle* h, int32_t rows) {
   const size_t heads = (size_t)rows * h->cfg.num_q_heads;
   WeighedLayout w;
   w.page_lse = layout_of(h).total;
   w.row_lse = align_up(w.page_lse + sizeof(float) * heads * (size_t)h->cfg.max_pages_per_seq);
-  w.total = align_up(w.row_lse + sizeof(float) * heads);
+  w.row_seq = align_up(w.row_lse + sizeof(float) * heads);
+  w.total = align_up(w.row_seq + sizeof(int32_t) * (size_t)rows);
   return w;
 }
 

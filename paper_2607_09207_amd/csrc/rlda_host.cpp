@@ -532,6 +532,7 @@ rlda_status rows_impl(rl_decode_attn_t h, bool weigh, int32_t batch, int32_t num
   p.decay = decay;
   p.page_lse = (float*)(ws + ww.page_lse);
   p.row_lse = (float*)(ws + ww.row_lse);
+  p.row_seq = (int32_t*)(ws + ww.row_seq);
   auto* const launch = weigh ? rlda::launch_weighed : rlda::launch_selected;
   return launch(h->kind, c.head_dim, h->group, two, p, stream, event_begin, event_end) == hipSuccess ? RLDA_OK : RLDA_ERR_HIP;
 }

@@ -20,6 +20,8 @@ namespace {
 // A lane a page of a sequence, the rows' heads dealt out to the waves: wave w adds those of w, w +
 // 4, ... in order, wave 0 the four sums.  All of a lane's loads are in flight at once (one wave
 // with every head, eight at a time: 11.6 us for 64 long-tailed sequences of 28 heads).
+// STARTS: with q_start.
+template <bool STARTS>
 __global__ __launch_bounds__(kThreads) void page_weights_kernel(const Params p) {
   __shared__ float s_sum[kWaves][64];
   constexpr int H = 8;   // heads of a wave whose parts are asked for together
@@ -35,7 +37,7 @@ __global__ __launch_bounds__(kThreads) void page_weights_kernel(const Params p) 
   };
   float* const w = p.weights + (int64_t)b * p.max_pages;
   // One row a sequence: the first pages' parts and weights, ahead of the length.
-  const bool early = !p.q_start && blockIdx.y == 0;
+  const bool early = !STARTS && blockIdx.y == 0;
   float first[H], old = 0.f;
   if (early) {
     const int j = min(lane, p.max_pages - 1);
@@ -44,7 +46,7 @@ __global__ __launch_bounds__(kThreads) void page_weights_kernel(const Params p) 
   }
   const int L = min(max(p.seq_lens[b], 0), cap), npages = (L + kPage - 1) / kPage;
   int q0 = b, n = 1;
-  if (p.q_start) {
+  if constexpr (STARTS) {
     q0 = p.q_start[b];
     const int q1 = p.q_start[b + 1];
     n = q0 >= 0 && q0 <= q1 && q1 <= p.total_q ? q1 - q0 : 0;
@@ -55,7 +57,11 @@ __global__ __launch_bounds__(kThreads) void page_weights_kernel(const Params p) 
     const bool have = early && j0 == 0;
     if (!have && wave == 0 && p.decay != 0.f) old = w[at];
     float got = 0.f;
+    bool any = !STARTS;
     for (int i = 0; i < n; ++i) {
+      // (Where offsets run backwards, the attention may have taken the row as another's.)
+      const bool own = !STARTS || p.row_seq[q0 + i] == b;
+      any |= own;
       const bool seen = L - n + i >= kPage * at;   // by the row
       const float* z = p.row_lse + (int64_t)(q0 + i) * Hq;
       for (int h0 = wave; h0 < Hq; h0 += H * kWaves) {
@@ -68,12 +74,12 @@ __global__ __launch_bounds__(kThreads) void page_weights_kernel(const Params p) 
         }
 #pragma unroll
         for (int k = 0; k < H; ++k)   // (no key: nothing, whatever the row's sum is)
-          if (a[k] != neg_inf()) got += __builtin_amdgcn_exp2f(a[k] - z[min(h0 + k * kWaves, Hq - 1)]);
+          if (own && a[k] != neg_inf()) got += __builtin_amdgcn_exp2f(a[k] - z[min(h0 + k * kWaves, Hq - 1)]);
       }
     }
     s_sum[wave][lane] = got;
     __syncthreads();
-    if (wave == 0 && j < npages) {
+    if (wave == 0 && j < npages && any) {
       got = s_sum[0][lane] + s_sum[1][lane] + s_sum[2][lane] + s_sum[3][lane];
       w[j] = p.decay == 0.f ? got : __builtin_fmaf(p.decay, old, got);
     }
@@ -118,7 +124,10 @@ int launch_weighed(KvKind kind, int head_dim, int group, bool two, const Params&
   const int e = launch_rows_form<kWeighed>(kind, head_dim, group, two, p, stream, ev_begin, nullptr);
   if (e != hipSuccess) return e;
   const int y = min((p.max_pages + 63) / 64, 256);
-  hipLaunchKernelGGL(page_weights_kernel, dim3(p.batch, y), dim3(kThreads), 0, (hipStream_t)stream, p);
+  if (p.q_start)
+    hipLaunchKernelGGL(page_weights_kernel<true>, dim3(p.batch, y), dim3(kThreads), 0, (hipStream_t)stream, p);
+  else
+    hipLaunchKernelGGL(page_weights_kernel<false>, dim3(p.batch, y), dim3(kThreads), 0, (hipStream_t)stream, p);
   if (const hipError_t l = hipGetLastError(); l != hipSuccess) return (int)l;
   if (ev_end && hipEventRecord((hipEvent_t)ev_end, (hipStream_t)stream) != hipSuccess) return -1;
   return 0;

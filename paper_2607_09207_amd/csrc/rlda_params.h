@@ -106,6 +106,7 @@ struct Params {
   const int32_t* list_counts;  // [rows][Hkv]
   float* page_lse;             // [rows][Hq][max_pages] log2 of a page's sum of exp2(score)
   float* row_lse;              // [rows][Hq] ... and of the row's
+  int32_t* row_seq;            // [rows] with q_start: the row's sequence, -1: none
   float* weights;              // [batch][max_pages]
   float decay;
   int32_t budget;

@@ -676,6 +676,28 @@ def test_weighed(torch, kv, hq, hkv, d, ranges):
     assert c.flags(c.layer.weighed_workspace(8, "cuda")) == 0
 
 
+@pytest.mark.parametrize("kv", ["bf16", "fp8", "f32"])
+@pytest.mark.parametrize("starts", CLAIMED, ids=["overlap", "whole", "inside", "hole", "70", "600"])
+def test_weights_of_rows_that_two_sequences_claim(torch, starts, kv):
+    """Weights of the rows as the attention takes them: a sequence without rows of its own keeps its
+    weights, and nothing that an earlier call left in the workspace gets into any."""
+    c, mine, free = claimed_case(torch, starts, kv)
+    n = len(c.q)
+    o, tol, parts = c.want(lambda r, g, L: range(-(-L // PAGE)))
+    ws = c.layer.weighed_workspace(n, "cuda")
+    at = -ws.data_ptr() % 256 + c.layer.workspace_bytes
+    ws[at:at + (ws.numel() - at) // 4 * 4].view(torch.float32).fill_(100.0)   # what an earlier call may leave
+    w0 = torch.rand((len(c.lens), c.mp), device="cuda", generator=c.gen)
+    w = w0.clone()
+    got = torch.full((n, 4, 64), 7.0, device="cuda")
+    c.weigh(w, decay=0.5, out=got)
+    assert c.flags(ws) == 2 and bool((got[free] == 7).all())
+    c.check(got[mine], o[mine], tol[mine])
+    want, wtol = expect_weights(c, parts, w0, 0.5)
+    for b in range(len(c.lens)):
+        assert bool(((w[b].double() - want[b]).abs() <= wtol[b] + 1e-30).all()), (b, w[b].tolist(), want[b].tolist())
+
+
 @pytest.mark.parametrize("kv,hq,hkv,d", [("bf16", 28, 4, 128), ("fp8", 8, 1, 64), ("f32", 4, 4, 64)])
 def test_weighed_several_rows(torch, kv, hq, hkv, d):
     rows = [3, 0, 1, 5, 17, 0, 30, 2]
