@@ -119,10 +119,11 @@ __global__ __launch_bounds__(kThreads) void page_bounds_kernel(const SelectParam
   }
   if (L == 0) return;
   const int j0 = min(max(first, 0), L) / kPage, npages = (L + kPage - 1) / kPage;
-  const int units = (npages - j0) * p.num_kv_heads;
+  const uint32_t units = (uint32_t)(npages - j0) * (uint32_t)p.num_kv_heads;
   const int row = lane / LPR, col = lane % LPR;
-  for (int u = blockIdx.x * kWaves + wave; u < units; u += gridDim.x * kWaves) {
-    const int j = j0 + (int)((uint32_t)u / (uint32_t)p.num_kv_heads), g = u - (j - j0) * p.num_kv_heads;
+  for (uint32_t u = blockIdx.x * kWaves + wave; u < units; u = unit_after(u, gridDim.x * kWaves, units)) {
+    const PageHead at_u = page_head_of(u, p.num_kv_heads);
+    const int j = j0 + at_u.page, g = at_u.head;
     const int pid = uni(p.block_table[(int64_t)b * p.max_pages + j]);
     if ((unsigned)pid >= (unsigned)p.num_pages) {
       if (lane == 0) atomicOr(p.flags, kFlagBadPage);

@@ -27,6 +27,18 @@ RLDA_HD float split_sqrt(float x) {
 #endif
 }
 
+// The (page, KV head) pairs of a sequence, taken `step` apart: unit u of `units` (up to 2^31 - 1) is head
+// u % Hkv of page u / Hkv.  Without a sign, and never past `units`: the step after the last one
+// would be negative as an int, and a page behind the table's row.
+RLDA_HD uint32_t unit_after(uint32_t u, uint32_t step, uint32_t units) { return units - u > step ? u + step : units; }
+struct PageHead {
+  int page, head;
+};
+RLDA_HD PageHead page_head_of(uint32_t u, int num_kv_heads) {
+  const uint32_t page = u / (uint32_t)num_kv_heads;
+  return {(int)page, (int)(u - page * (uint32_t)num_kv_heads)};
+}
+
 // The calls that the lines below tell apart: plain ones by the size of their pages (half:
 // at most 4 KiB of K and V per page and KV head, two workgroups per CU), and the ones
 // that stream whole segments through the general loop (several query tokens, packed

@@ -29,11 +29,22 @@ extern "C" rlda::Split forced(int W, int nseg, int cost, int nb) {
   return rlda::split_of(rlda::kSplitFullPages, W, 0.f, nseg, cost, nb);
 }
 extern "C" int share(int b, int n) { return rlda::share_of_block(b, n); }
+extern "C" long long visit(unsigned first, unsigned step, unsigned units, int hkv, long long* last, int* page) {
+  long long n = 0;
+  for (unsigned u = first; u < units; u = rlda::unit_after(u, step, units), ++n) {
+    const rlda::PageHead at = rlda::page_head_of(u, hkv);
+    if (at.head < 0 || at.head >= hkv || (unsigned)at.page * (unsigned long long)hkv + at.head != u) return -1;
+    *last = u;
+    *page = at.page;
+  }
+  return n;
+}
 ''')
     so = str(d / "rule.so")
     subprocess.check_call(["g++", "-O1", "-std=c++17", "-shared", "-fPIC", "-I", CSRC, str(d / "rule.cpp"), "-o", so])
     lib = ctypes.CDLL(so)
     lib.split.restype = lib.forced.restype = Split
+    lib.visit.restype = ctypes.c_longlong
     return lib
 
 
@@ -134,3 +145,21 @@ def test_pieces_of_the_chosen_cut():
     assert C.features_ext([500] * 4, 4, 256, 128, "bf16")[3] == 1           # whole segments
     assert C.features_ext([3000], 1, 256, 128, "bf16")[3] == 16             # one segment alone
     assert C.features_ext([3000], 1, 256)[3] == C.max_pieces([3000], 1, 256) > 100   # 256 shares
+
+
+@pytest.mark.parametrize("hkv,pages", [(16, 2 ** 27 - 1 - START), (1, 2 ** 27 - 1 - START), (15, 2 ** 27 - 1 - START),
+                                       (3, 21846), (1, 1), (8, 1)])
+def test_the_units_of_the_longest_sequences_end(rule, hkv, pages):
+    """(page, KV head) pairs up to the most that a layer may have, near 2^31: every unit once, none
+    behind the last page, and an end."""
+    step, units = 65536, hkv * pages   # of a call with first tokens
+    assert units <= 2 ** 31 - 1
+    last, page = ctypes.c_longlong(-1), ctypes.c_int(-1)
+    most, visited = -1, 0
+    for first in (0, 1, 5, 32768, 65534, 65535):
+        n = rule.visit(first, step, units, hkv, ctypes.byref(last), ctypes.byref(page))
+        assert n == max(-(-(units - first) // step), 0)
+        if n:
+            assert units - step <= last.value < units and page.value < pages
+            most, visited = max(most, page.value), visited + 1
+    assert visited and most <= pages - 1
