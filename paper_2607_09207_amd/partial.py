@@ -11,6 +11,7 @@ from . import _abi
 from .rotary import derived, device_of, empty_on, mark_written, on_device, raw_stream
 
 _ptr = lambda t: None if t is None else t.data_ptr()   # noqa: E731
+_MAX_ROWS = 4096   # query rows of a call
 
 
 class PartialCache:
@@ -177,19 +178,29 @@ class PartialCache:
 
     def weighed_workspace(self, rows: int, device):
         """Workspace of weighed() for up to `rows` query rows, allocated (and zeroed) once and grown
-        where a call has more.  Calls that may overlap need separate ones (`workspace=`); a
-        call to be captured into a graph finds it made before."""
+        where a call has more, to twice the rows at least: those it outgrew are kept, and
+        together have less than twice its rows.  Calls that may overlap need separate ones
+        (`workspace=`); a call to be captured into a graph finds it made before."""
         device = device_of(device)
         key = str(device)
+        need = self._weighed_bytes(rows)
+        ws = self._weighed_ws.get(key)
+        if ws is None or ws.numel() < need:
+            grown = int(rows)
+            if ws is not None:
+                grown = max(grown, min(2 * self._weighed_rows[key], _MAX_ROWS))
+            new = self._zeroed(self._weighed_bytes(grown), device)
+            if ws is not None:
+                self._outgrown.append(ws)   # a graph, or a call that still runs, may use it
+            ws = self._weighed_ws[key] = new
+            self._weighed_rows[key] = grown
+        return ws
+
+    def _weighed_bytes(self, rows):
         n = ctypes.c_size_t()
         _abi.check(self._lib.rl_decode_attn_weighed_workspace_size(self._h, int(rows), ctypes.byref(n)),
                    "rl_decode_attn_weighed_workspace_size")
-        ws = self._weighed_ws.get(key)
-        if ws is None or ws.numel() < n.value + 256:
-            if ws is not None:
-                self._outgrown.append(ws)   # a graph, or a call that still runs, may use it
-            ws = self._weighed_ws[key] = self._zeroed(n.value + 256, device)
-        return ws
+        return n.value + 256
 
     def weighed(self, q, k_cache, v_cache, block_table, seq_lens, weights, *, decay: float = 1.0, q_start=None, k_scale=None,
                 v_scale=None, out=None, workspace=None, stream=None, num_pages: Optional[int] = None, events=None):

@@ -128,3 +128,32 @@ def test_page_evict_refuses(lib, handles):  # noqa: F811
            dict(budget=2), dict(sink=-1), dict(recent=0), dict(sink=2 ** 31 - 1, recent=2 ** 31 - 1)]
     check(lib.rl_decode_attn_page_evict, base, bad, [dict(h=handles["long"], bytes=page_bytes(lib, handles["long"], 10))],
           [dict(batch=0), dict(batch=0, weights=None, dropped=None, table=None, lens=None)])
+
+
+def test_rising_rows_make_few_workspaces(monkeypatch):
+    """What a layer keeps of the weights' workspaces, live and outgrown, is a small multiple of the
+    largest call's, however the calls' rows rise; the first one is made to measure."""
+    import torch
+
+    from paper_2607_09207_amd import DecodeAttention
+    layer = DecodeAttention(8, 2, 128, 16, 64, "bf16", "bf16", "f32")
+    made = []
+
+    def zeroed(nbytes, device):
+        made.append(nbytes)
+        return torch.empty(nbytes, dtype=torch.uint8)
+
+    monkeypatch.setattr(layer, "_zeroed", zeroed)
+    size = lambda rows: weighed_bytes(layer._lib, layer._h, rows) + 256   # noqa: E731
+    for rows in range(30, 700):
+        ws = layer.weighed_workspace(rows, "cuda:0")
+        assert ws.numel() >= size(rows) and layer.weighed_workspace(rows - 7, "cuda:0") is ws
+    plain = size(0)   # of which a call without rows has one
+    assert made[0] == size(30) and len(made) <= 6 and sum(n - plain for n in made) <= 4 * (size(699) - plain)
+    assert layer.weighed_workspace(4096, "cuda:0").numel() == size(4096)
+    layer.weighed_workspace(3, "cuda:1")   # another device's: to measure again
+    assert made[-1] == size(3)
+    made.clear()
+    for rows in (2100, 2200, 4096):   # never beyond what a call may have
+        layer.weighed_workspace(rows, "cuda:2")
+    assert made == [size(2100), size(4096)]
