@@ -82,7 +82,7 @@ class DecodeAttention(CacheOps, PartialCache):
                    "rl_decode_attn_grouped_workspace_size")
         self.grouped_workspace_bytes = int(n.value)
         self._ws, self._outgrown = {}, []
-        self._page_ws, self._weighed_ws, self._weighed_rows = {}, {}, {}
+        self._page_ws, self._weighed_ws, self._weighed_rows, self._weighed_old = {}, {}, {}, {}
         # The native call path (csrc/fastcall.cpp); it shares the workspaces by device.
         native = _abi.fastcall()
         self._fast = _abi.LEFT_TO_PYTHON if native is None else native.Layer(

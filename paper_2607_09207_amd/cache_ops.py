@@ -97,7 +97,7 @@ class CacheOps:
         import torch
         if torch.cuda.is_current_stream_capturing():
             self._fail("workspace", "none is made during a graph's capture, which would clear it, with its flags, in "
-                                    "every replay: call workspace() or page_workspace() before")
+                                    "every replay: call workspace(), page_workspace() or weighed_workspace() before")
         ws = torch.zeros(nbytes, dtype=torch.uint8, device=device)
         torch.cuda.current_stream(ws.device).synchronize()
         return ws

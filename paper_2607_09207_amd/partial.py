@@ -191,10 +191,23 @@ class PartialCache:
                 grown = max(grown, min(2 * self._weighed_rows[key], _MAX_ROWS))
             new = self._zeroed(self._weighed_bytes(grown), device)
             if ws is not None:
-                self._outgrown.append(ws)   # a graph, or a call that still runs, may use it
+                self._weighed_old.setdefault(key, []).append(ws)   # a graph, or a call that still runs, may use it
             ws = self._weighed_ws[key] = new
             self._weighed_rows[key] = grown
         return ws
+
+    def weighed_flags(self, device, workspace=None, stream=None) -> int:
+        """The flags that calls of weighed() raised on the device, in workspaces that later calls
+        outgrew as well (waits for the stream)."""
+        if workspace is not None:
+            return self.read_flags(workspace=workspace, stream=stream)
+        key = str(device_of(device))
+        if key not in self._weighed_ws:
+            self._fail("weighed_flags", f"no call with weights had a workspace on {key}")
+        flags = 0
+        for ws in [self._weighed_ws[key], *self._weighed_old.get(key, ())]:
+            flags |= self.read_flags(workspace=ws, stream=stream)
+        return flags
 
     def _weighed_bytes(self, rows):
         n = ctypes.c_size_t()

@@ -1246,3 +1246,30 @@ def test_weights_past_32_bits(torch):
     torch.cuda.synchronize()
     assert torch.equal(got, want) and torch.equal(w[:, :c.mp], w0) and not bool(w[:, c.mp:].any())
     assert L.read_flags(workspace=L.weighed_workspace(4, "cuda")) == 0
+
+
+def test_flags_of_weights_survive_growth(torch):
+    """What calls with weights raised is found where the layer keeps it, also in a workspace that they
+    outgrew: what it held before the growth, and what comes after, as from a graph captured before."""
+    from paper_2607_09207_amd import RldaError
+    c = Case(torch, "bf16", 8, 2, 64, [100, 50, 80], [2, 3, 4], seed=34)
+    L, w = c.layer, torch.zeros((3, c.mp), device="cuda")
+    with pytest.raises(RldaError, match="weighed_flags"):
+        L.weighed_flags("cuda")
+    first = L.weighed_workspace(9, "cuda")
+    c.weigh(w)
+    assert L.weighed_flags("cuda") == 0
+    c.block_table[1, 1] = c.npages
+    c.weigh(w)
+    assert L.weighed_flags("cuda") == 1
+    c.block_table[1, 1] = int(c.table[1, 1])
+    second = L.weighed_workspace(40, "cuda")
+    c.weigh(w)
+    assert second is not first and L.weighed_flags(None, workspace=second) == 0
+    assert L.weighed_flags("cuda:0") == 1
+    c.seq_lens[2] = 2   # fewer tokens than rows
+    c.weigh(w, workspace=first)
+    assert L.weighed_flags("cuda", stream=torch.cuda.current_stream().cuda_stream) == 3
+    assert L.weighed_flags(None, workspace=second) == 0 and L.read_flags(device="cuda") == 0
+    c.weigh(w)
+    assert L.weighed_flags("cuda", workspace=second) == 2

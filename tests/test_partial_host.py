@@ -157,3 +157,10 @@ def test_rising_rows_make_few_workspaces(monkeypatch):
     for rows in (2100, 2200, 4096):   # never beyond what a call may have
         layer.weighed_workspace(rows, "cuda:2")
     assert made == [size(2100), size(4096)]
+
+
+def test_flags_of_weights_need_a_workspace():
+    from paper_2607_09207_amd import DecodeAttention, RldaError
+    layer = DecodeAttention(8, 2, 128, 16, 64, "bf16", "bf16", "f32")
+    with pytest.raises(RldaError, match="weighed_flags"):
+        layer.weighed_flags("cuda:0")
