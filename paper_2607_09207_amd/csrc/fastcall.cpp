@@ -740,6 +740,8 @@ PyObject* layer_page_bounds(PyObject* self, PyObject* const* a, Py_ssize_t n) {
     if (!common(L, c, args, dev, B) || !bounds_ok(L, bounds, bscale, dev, c.npages) || !vector_or_none(a[9], dev, at::kInt, B, &first) ||
         !workspace(L, c, a[6], false) || !current(dev))
       return nullptr;
+    mark_written(*bounds);
+    mark_written(*bscale);
     void *kp = ptr(c.k), *ksp = ptr(c.ks), *bp = ptr(c.bt), *lp = ptr(c.lens), *fp = ptr(first), *op = ptr(bounds), *sp = ptr(bscale);
     WITHOUT_GIL(g_page_bounds(L->handle, (int32_t)B, (int32_t)c.npages, kp, (const float*)ksp, (const int32_t*)bp, (const int32_t*)lp,
                               (const int32_t*)fp, (int8_t*)op, (float*)sp, c.ws_ptr, c.ws_room, c.stream));
@@ -779,6 +781,8 @@ PyObject* layer_select_pages(PyObject* self, PyObject* const* a, Py_ssize_t n) {
         return nullptr;
       }
     }
+    for (int i = 0; i < 2; ++i)
+      if (a[7 + i] != Py_None) mark_written(*out[i]);
     void *qp = ptr(q), *op = ptr(bounds), *sp = ptr(bscale), *bp = ptr(c.bt), *lp = ptr(c.lens), *qsp = ptr(qs), *pp = ptr(out[0]),
          *cp = ptr(out[1]);
     WITHOUT_GIL(g_select_pages(L->handle, (int32_t)B, (int32_t)c.npages, (int32_t)total, budget, sink, recent, qp, (const int8_t*)op,
@@ -810,6 +814,7 @@ PyObject* layer_selected(PyObject* self, PyObject* const* a, Py_ssize_t n) {
     Tensor fresh;
     const Tensor* o = output(L, a[9], *q, total, a[7], c, fresh);
     if (!o) return nullptr;
+    if (a[9] != Py_None) mark_written(*o);
     const int32_t budget = (int32_t)pages->size(2);
     void *qp = ptr(q), *kp = ptr(c.k), *vp = ptr(c.v), *ksp = ptr(c.ks), *vsp = ptr(c.vs), *bp = ptr(c.bt), *lp = ptr(c.lens),
          *op = ptr(o), *qsp = ptr(qs), *pp = ptr(pages), *cp = ptr(counts);
@@ -847,6 +852,7 @@ PyObject* layer_weighed(PyObject* self, PyObject* const* a, Py_ssize_t n) {
     Tensor fresh;
     const Tensor* o = output(L, a[9], *q, total, a[7], c, fresh);
     if (!o) return nullptr;
+    if (a[9] != Py_None) mark_written(*o);
     mark_written(*weights);
     void *qp = ptr(q), *kp = ptr(c.k), *vp = ptr(c.v), *ksp = ptr(c.ks), *vsp = ptr(c.vs), *bp = ptr(c.bt), *lp = ptr(c.lens),
          *op = ptr(o), *qsp = ptr(qs), *wp = ptr(weights);
@@ -874,6 +880,7 @@ PyObject* layer_page_evict(PyObject* self, PyObject* const* a, Py_ssize_t n) {
     if (a[7] == Py_None) fresh = empty_on({B}, refs->options(), c.dev, a[9], c.stream);
     const Tensor* dropped = a[7] == Py_None ? &fresh : tensor(a[7]);
     if (!shaped(dropped, c.dev, at::kInt, {B})) return nullptr;
+    if (a[7] != Py_None) mark_written(*dropped);
     mark_written(*weights);
     void *rp = ptr(refs), *bp = ptr(c.bt), *lp = ptr(c.lens), *wp = ptr(weights), *dp = ptr(dropped);
     WITHOUT_GIL(g_page_evict(L->handle, (int32_t)B, (int32_t)c.npages, (int32_t*)rp, (int32_t*)bp, (int32_t*)lp, (float*)wp, budget,

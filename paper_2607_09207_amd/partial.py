@@ -89,6 +89,8 @@ class PartialCache:
             _abi.check(self._lib.rl_decode_attn_page_bounds(
                 self._h, batch, npages, k_cache.data_ptr(), _ptr(k_scale), block_table.data_ptr(), seq_lens.data_ptr(),
                 _ptr(first), bounds.data_ptr(), bound_scale.data_ptr(), *args), what)
+        mark_written(bounds)
+        mark_written(bound_scale)
 
     def select_pages(self, q, bounds, bound_scale, block_table, seq_lens, budget: int, *, sink: int = 1, recent: int = 1,
                      q_start=None, out=None, workspace=None, stream=None, num_pages: Optional[int] = None):
@@ -128,6 +130,9 @@ class PartialCache:
             _abi.check(self._lib.rl_decode_attn_select_pages(
                 self._h, batch, npages, total, budget, sink, recent, q.data_ptr(), bounds.data_ptr(), bound_scale.data_ptr(),
                 block_table.data_ptr(), seq_lens.data_ptr(), _ptr(q_start), pages.data_ptr(), counts.data_ptr(), *args), what)
+        for t in given:
+            if t is not None:
+                mark_written(t)
         return pages, counts
 
     def selected(self, q, k_cache, v_cache, block_table, seq_lens, pages, counts, *, q_start=None, k_scale=None, v_scale=None,
@@ -167,6 +172,8 @@ class PartialCache:
         with on_device(dev):
             if out is None:
                 out = empty_on(shape, dtype, dev, stream)
+            else:
+                mark_written(out)
             wp, room, raw = self._ws_args(what, ws, dev, stream)
             e0, e1 = (None, None) if events is None else tuple(self._event_handle(e) for e in events)
             _abi.check(call(self._h, batch, npages, total, *own_args, q.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(),
@@ -260,12 +267,15 @@ class PartialCache:
         if derived(weights):
             self._fail(what, "weights get no gradient here: detach them")
         with on_device(dev):
-            if dropped is None:
+            made = dropped is None
+            if made:
                 dropped = empty_on((batch,), torch.int32, dev, stream)
             self._tensor(what, "dropped", dropped, torch.int32, (batch,), dev)
             args = self._page_ws_args(what, npages, dev, workspace, stream)
             _abi.check(self._lib.rl_decode_attn_page_evict(
                 self._h, batch, npages, refs.data_ptr(), block_table.data_ptr(), seq_lens.data_ptr(), weights.data_ptr(), budget,
                 sink, recent, dropped.data_ptr(), *args), what)
+        if not made:
+            mark_written(dropped)
         mark_written(weights)
         return dropped

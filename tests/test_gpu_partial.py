@@ -1273,3 +1273,34 @@ def test_flags_of_weights_survive_growth(torch):
     assert L.weighed_flags(None, workspace=second) == 0 and L.read_flags(device="cuda") == 0
     c.weigh(w)
     assert L.weighed_flags("cuda", workspace=second) == 2
+
+
+@pytest.mark.parametrize("native", [True, False], ids=["native", "python"])
+def test_what_is_written_is_marked(torch, native):
+    """A backward pass that saved a tensor before a call wrote to it is to notice: every tensor that the
+    caller gives to be written has another version afterwards."""
+    from paper_2607_09207_amd import _abi
+    c = Case(torch, "bf16", 8, 2, 64, [100, 50, 80], seed=35)
+    L, w = c.layer, torch.zeros((3, c.mp), device="cuda")
+    s = Pool(torch, [20, 9, 30], seed=1)
+    L.workspace("cuda"), L.weighed_workspace(3, "cuda"), s.layer.page_workspace(s.np, "cuda")
+    if not native:
+        L._fast = s.layer._fast = _abi.LEFT_TO_PYTHON
+    i32 = dict(dtype=torch.int32, device="cuda")
+    pages, counts, dropped = torch.zeros((3, 2, 4), **i32), torch.zeros((3, 2), **i32), torch.zeros(3, **i32)
+    out = torch.zeros((3, 8, 64), device="cuda")
+    for call, written in ((c.make_bounds, [c.bounds, c.bscale]), (lambda: c.select(4, out=(pages, counts)), [pages, counts]),
+                          (lambda: c.select(4, out=(None, counts)), [counts]), (lambda: c.attend(pages, counts, out=out), [out]),
+                          (lambda: c.weigh(w, out=out), [out, w]), (lambda: s.evict(8, dropped=dropped), [s.dev[3], dropped])):
+        before = [t._version for t in written]
+        call()
+        assert [t._version for t in written] == [v + 1 for v in before]
+    x = torch.ones(c.bscale.shape, device="cuda", requires_grad=True)
+    y = (x * c.bscale).sum()
+    c.make_bounds()
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        y.backward()
+    with torch.inference_mode():   # tensors without versions
+        c.bounds, c.bscale, out = torch.zeros_like(c.bounds), torch.zeros_like(c.bscale), torch.zeros_like(out)
+        c.make_bounds()
+        c.attend(pages, counts, out=out)
