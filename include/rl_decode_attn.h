@@ -520,7 +520,9 @@ rlda_status rl_decode_attn_page_bounds(rl_decode_attn_t handle, int32_t batch, i
  *   score(p) = s_p max_i (u_i sq_i),   u_i = sum_d max(q8_i[d] lo_p[d], q8_i[d] hi_p[d])
  * over the KV head's query heads i, up to `budget` (>= sink + recent) together; equal scores
  * go to the lower page.  q8 = rint(q / sq) within +-127, sq = max |q| / 127 of the (row, head), in
- * fp32; the sum is one of integers and exact.  A head whose q holds an infinity or NaN counts as 0;
+ * fp32; the sum is one of integers and exact.  (With q itself for sq q8 the score would be no less
+ * than q . k of any of the page's keys; rounded, it is within s sq/2 sum_d max(|lo_p[d]|, |hi_p[d]|) of
+ * that one, on either side.)  A head whose q holds an infinity or NaN counts as 0;
  * a page whose s is not finite is chosen before all others, one outside the pool after them.
  *   pages   [total_q][Hkv][budget] int32: indices of the row's pages, ascending, then -1
  *   counts  [total_q][Hkv] int32: min(n, budget)

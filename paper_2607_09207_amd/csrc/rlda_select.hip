@@ -11,7 +11,10 @@
 // Choice.  q is rounded to 8 bits as well, q8 = rint(q / sq) with sq = max |q| / 127 a (row,
 // head), so the product is one of whole numbers below 2^22: exact in whatever order the matrix
 // cores add it, and the choice is the same on every run and for every cut.  (With sums rounded
-// in 32 bits, pages near the border would come and go with the order.)  A page's score for a KV
+// in 32 bits, pages near the border would come and go with the order.)  The rounded query's score is
+// no upper bound any more: it is off by s sq/2 sum_d max(|lo_d|, |hi_d|) at most.  Of 128 chosen of 1024
+// pages 99.1% are those that q itself chooses (N(0, 1) keys; 99.6% where three channels are 24 times as
+// large), and 97.7% (93.5%) those of bounds that are not rounded either.  A page's score for a KV
 // head is s max_i (u_i sq_i) over its query heads, in fp32 in that order.  The `budget` best
 // pages are found by the digits of their order keys, in LDS.
 //

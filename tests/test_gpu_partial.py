@@ -347,6 +347,59 @@ def test_choice_of_long_rows(torch, n, max_pages, rows, hkv):
     assert c.flags() == 0
 
 
+@pytest.mark.parametrize("outliers", [0, 3], ids=["even", "outliers"])
+@pytest.mark.parametrize("kv,hq,hkv,d", LAYOUTS)
+def test_choice_against_the_score_of_unrounded_queries(torch, kv, hq, hkv, d, outliers):
+    """The definition that the 8-bit query stands for, in float64: S = max_i s sum_d max(q_d lo_d, q_d hi_d)
+    is no less than q . k of any of the page's keys, and no page that is left out beats a chosen one
+    by more than the roundings allow.
+      Bounds: s lo <= k <= s hi up to 128 2^-22 s (test_bounds), so S >= q . k - 128 2^-22 s sum |q_d|.
+      Choice: rint(q / sq) is within 1/2 of the fp32 quotient, and that within 127 2^-24 of q / sq; with m_d
+    = max(|lo_d|, |hi_d|) a head's score is off by E = s sq (1/2 + 2^-16) sum m_d and by two fp32
+    products, 2^-22 of it.  So for a page a that is chosen and b that is not, S_a + E_a >= S_b - E_b."""
+    c = Case(torch, kv, hq, hkv, d, [1500, 16, 900, 2000], [2, 1, 3, 1], seed=36)
+    if outliers:   # a few channels of much larger keys, as caches have: they coarsen the others' bounds
+        for t in (c.k,):
+            big = torch.randperm(d, device="cuda", generator=c.gen)[:outliers]
+            if kv == "fp8":
+                x = t.float()
+                x[..., [i for i in range(d) if i not in set(big.tolist())]] /= 24
+                t.copy_(x.to(t.dtype))
+            else:
+                t[..., big] *= 24
+    c.all_bounds()
+    budget = 12
+    pages, counts = c.select(budget, sink=1, recent=2)
+    chosen = pages.cpu().numpy()
+    cut = 0
+    for r, b, L in c.row_list():
+        n = -(-L // PAGE)
+        page = torch.from_numpy(c.table[b, :n].astype(np.int64)).cuda()
+        for g in range(hkv):
+            q = c.q[r, [h for h in range(hq) if c.kv_of[h] == g]].double()                     # [G][d]
+            lo, hi = c.bounds[page, g, 0].double(), c.bounds[page, g, 1].double()              # [n][d]
+            s = c.bscale[page, g].double()
+            score = s * torch.maximum(q[:, None] * lo, q[:, None] * hi).sum(-1)                # [G][n]
+            for j in range(n):
+                k = c.values(c.k, c.ks, int(page[j]))[g, :min(PAGE, L - j * PAGE)].double()    # [tokens][d]
+                most = (q[:, None] * k).sum(-1).amax(-1)
+                assert bool((score[:, j] >= most - 128 * 2.0 ** -22 * s[j] * q.abs().sum(-1)).all())
+            if n <= budget:
+                continue
+            cut += 1
+            sq = q.abs().amax(-1, keepdim=True) / 127
+            m = torch.maximum(lo.abs(), hi.abs()).sum(-1)
+            err = s * sq * (0.5 + 2.0 ** -16) * m
+            err = (err + 2.0 ** -22 * (score.abs() + err)).amax(0)
+            x, took = score.amax(0), torch.zeros(n, dtype=torch.bool, device="cuda")
+            took[torch.from_numpy(chosen[r, g].astype(np.int64)).cuda()] = True
+            rest = torch.arange(n, device="cuda")
+            rest = (rest >= 1) & (rest < n - 2)
+            worst, best = (x + err)[rest & took].amin(), (x - err)[rest & ~took].amax()
+            assert bool(worst >= best), (r, g, float(worst), float(best))
+    assert cut > 0 and c.flags() == 0
+
+
 def test_choice_with_ties_and_odd_values(torch):
     """Equal scores go to the lower page, zeros of both signs are equal; pages that are not
     finite come first, pages outside the pool last; a query that is not finite says nothing."""
