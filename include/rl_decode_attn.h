@@ -501,8 +501,10 @@ rlda_status rl_decode_attn_page_copy(rl_decode_attn_t handle, int32_t num_pages,
  *   first        [batch] int32 device: the pages from that of token first[b] (0 <= first[b] <=
  *                seq_lens[b]) on are computed; NULL: the page of the last token alone
  * Whatever writes a page calls for its bounds again: an append (NULL, or the first token
- * appended), and page ids whose contents rl_decode_attn_page_compact or _copy moved.  The pages
- * that one call computes belong to one sequence each, or are full.
+ * appended), and page ids whose contents rl_decode_attn_page_compact or _copy moved.  A partly
+ * filled page that rl_decode_attn_page_fork copied has no bounds under its new id before the
+ * child's first append asks for them; no choice needs them (a row's last page is always chosen).
+ * The pages that one call computes belong to one sequence each, or are full.
  * Every kv_dtype.  A length out of range, or first[b]: flag bit 1; a page id outside the
  * pool: skipped, flag bit 0.  workspace: as for rl_decode_attn_run (only its flag word is
  * used).  One kernel, asynchronous.
@@ -546,6 +548,7 @@ rlda_status rl_decode_attn_select_pages(rl_decode_attn_t handle, int32_t batch, 
  * zeros.  Entries that are none of the row's pages are skipped (flag bit 0), counts beyond
  * min(the row's pages, budget) are cut back to it.  Rows and rows without a sequence as
  * for rl_decode_attn_select_pages; rows before token 0 give zeros.
+ * Every row reads its list for itself, also pages that rows of the same sequence have in common.
  * Every kv_dtype; total_q <= 4096 (RLDA_ERR_UNSUPPORTED).  Other arguments, checks and the
  * workspace as for rl_decode_attn_run.  One kernel, asynchronous; events: both NULL, or both
  * recorded around it.
@@ -565,7 +568,9 @@ rlda_status rl_decode_attn_run_selected(rl_decode_attn_t handle, int32_t batch, 
  * attending up to its own position), and for every page j of a sequence that has rows
  *   weights[b][j] <- decay weights[b][j] + sum over its rows, query heads and the page's keys of
  *                    the softmax's probabilities
- * in fp32, in one order.  decay in [0, 1]; with 0 the old weights are not read.
+ * in fp32, in one order.  decay in [0, 1]; with 0 the old weights are not read.  Every row reads the
+ * cache for itself: n rows of a sequence cost n times one row's reading (rl_decode_attn_run_multi
+ * reads it once, without weights).
  *   weights  [batch][max_pages_per_seq] fp32; entries at or past a sequence's pages stay as they
  *            were.  A row of the table that is given to another sequence starts with zeros
  *            (the caller's).

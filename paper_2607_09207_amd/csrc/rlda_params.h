@@ -55,7 +55,7 @@ struct Params {
   float* part_acc;             // [2 * nranges][part_rows][D]  unnormalised partial outputs
   float* part_ml;              // [2 * nranges][part_rows][4]  (running max in log2 units, sum, call tag, 0)
   int32_t part_rows;           // query rows per (sequence, KV head) segment: G, or n_max * G for multi-token rows
-  uint32_t* counters;          // [max_batch * Hkv * 4] finished pieces per split segment; zero between runs
+  uint32_t* counters;          // [max(4 max_batch, kRowsMax) * Hkv] finished pieces per split segment; zero between runs
   uint32_t call_tag;           // this call's tag, published with each partial (never 0 or all-ones)
   uint32_t* flags;             // contract-violation bits
   int64_t stride_page;         // bytes

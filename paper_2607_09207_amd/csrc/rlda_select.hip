@@ -103,7 +103,9 @@ __device__ __forceinline__ void deal_maxima(uint32_t* w) {
 // over the lanes of the same elements, each of which ends with a few of them to divide and write.
 //   Bandwidth bounds it for whole prompts, as long as a page takes few operations: with every
 // lane reducing all of its elements and two of the groups dividing them, 33 us for 64 prompts
-// (151 MB) against 27 so.  For a step, latency.
+// (151 MB) against 28.5 so (5.3 TB/s).  fp8 pages have half the bytes and no fewer operations (262 VALU
+// instructions a page and KV head, bf16 242): the same prompts on 8 KV heads (160 MB) take 43.4 us, 3.7
+// TB/s, 30 of it the VALU's issue.  For a step, latency.
 template <int D, KvKind KIND>
 __global__ __launch_bounds__(kThreads) void page_bounds_kernel(const SelectParams p) {
   constexpr bool F32 = KIND == KvKind::F32;
